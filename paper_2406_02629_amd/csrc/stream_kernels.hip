@@ -7,6 +7,7 @@
 #include "kernels.hpp"
 #include "eval.hpp"
 #include "digits.hpp"
+#include "truncation.hpp"
 #include "pool_plan.hpp"
 
 namespace SS_NS {
@@ -80,16 +81,6 @@ struct pack_t<2> {
     template <bool STREAM>
     __device__ __forceinline__ void send(u64 *p) const { STREAM ? store_streaming(p) : store(p); }
 };
-
-// A message that nothing in the launch reads again.  STREAM: past the caches, see streams_messages.
-template <bool STREAM>
-__device__ __forceinline__ void send(u64 *p, u64 v)
-{
-    if constexpr (STREAM)
-        __builtin_nontemporal_store(v, p);
-    else
-        *p = v;
-}
 
 // First party whose share of element e has more than one plane of the incoming product: the tiles of the last parties are
 // the ones dealt in parts (ss_part_src).
@@ -250,38 +241,6 @@ __global__ __launch_bounds__(BLOCK) void reconstruct_kernel(const u64 *__restric
     out.template send<STREAM>(secret + e0);
 }
 
-// e of the truncation mask alpha = e * 2^f: uniform in [1, 2^(32-f)]
-__device__ __forceinline__ u64 mask_e(u64 key, u64 e, int f)
-{
-    return 1 + ((ss_draw(key, e) >> 3) & ((1ULL << (32 - f)) - 1));
-}
-
-// the same before a division by kh*kw: the sample space of e shrinks to [1, floor(2^(32-f) / kdiv)], which keeps
-// alpha = e * 2^f * kdiv within (0, 2^32] (Sec. VII-B); range = 2^(32-f) gives mask_e
-__device__ __forceinline__ u64 mask_e_below(u64 key, u64 e, unsigned range)
-{
-    return 1 + (ss_draw(key, e) >> 3) % range;
-}
-
-// what the elite party does with the reconstructed x + alpha: floor division of the signed value by 2^f
-__device__ __forceinline__ u64 shift_signed(u64 v, int f)
-{
-    const int64_t sv = (v <= (SS_P - 1) / 2) ? (int64_t)v : (int64_t)v - (int64_t)SS_P;
-    const int64_t qv = sv >> f;
-    return qv >= 0 ? (u64)qv : SS_P - (u64)(-qv);
-}
-
-// The same followed by the rounding division that average pooling moves into the truncation (Sec. VI-C):
-// [q / kdiv] = floor((q + floor(kdiv/2)) / kdiv) on the signed quotient q, so that a remainder of
-// ceil(kdiv/2) or more goes up (the worst case of App. C) and [(q + e*kdiv) / kdiv] = [q / kdiv] + e.
-__device__ __forceinline__ u64 shift_round_div(u64 v, int f, int kdiv)
-{
-    const int64_t sv = (v <= (SS_P - 1) / 2) ? (int64_t)v : (int64_t)v - (int64_t)SS_P;
-    const int64_t a = (sv >> f) + kdiv / 2;
-    const u64 d = (u64)kdiv;
-    return a >= 0 ? (u64)a / d : SS_P - ((u64)(-a) + d - 1) / d;
-}
-
 // ------------------------------------------------------------------ RED + RERAND, truncation
 // The protocol steps for the element a thread owns.  All parties are simulated by that one thread, so a message is
 // written to the workspace (the "send") and what follows from it is computed in registers (the "receive"); messages and
@@ -310,64 +269,6 @@ __device__ __forceinline__ u64 shift_round_div(u64 v, int f, int kdiv)
 // without any arithmetic takes 13.9 us.
 // n = 7, t = 3: 50.4 -> 27.1 us; n = 4, t = 1: 18.9 -> 10.1 us (against values at every ID and loops over n and t).
 // N: parties fixed at compile time, or 0 for the run-time value n; T: degree.
-
-// sum of v * c over at most 8 terms, v canonical given as v = w0 + w1 2^31 (w0 < 2^31), |c| < 2^26
-struct ss_sacc2 {
-    long long lo, hi;
-    __device__ __forceinline__ void clear() { lo = 0; hi = 0; }
-    __device__ __forceinline__ void mac(u32 w0, u32 w1, int c)
-    {
-        lo += (long long)(int)w0 * c;   // |sum| < 8 * 2^31 * 2^26 = 2^60
-        hi += (long long)(int)w1 * c;
-    }
-    // the sum, below 2^61 + 2^3 (2^45 + 2^25)
-    __device__ __forceinline__ u64 lazy() const
-    {
-#if defined(SS_FIELD_P45)
-        // here |hi| < 2^43 (w1 < 2^14).  Offsets that are multiples of p make both words positive;
-        // h 2^31 with h = a 2^14 + b: a 2^45 + b 2^31 = 55 a + b 2^31
-        const u64 l = (u64)(lo + (long long)(SS_P << 16)), h = (u64)(hi + (long long)SS_P);   // < 2^62, < 2^46
-        return ss_fold(l + SS_PC * (h >> 14) + ((h & 0x3FFFull) << 31));
-#else
-        const u64 l = (u64)(lo + (long long)SS_P), h = (u64)(hi + (long long)SS_P);   // in (2^60, 2^62)
-        // h 2^31 with 2^61 = 1: low 30 bits of h shifted, the rest wraps to weight 1
-        return ss_fold(l + ((h & 0x3FFFFFFFull) << 31) + (h >> 30));
-#endif
-    }
-    __device__ __forceinline__ u64 value() const { return ss_canon(lazy()); }
-};
-#define SS_SPLIT31(v, w0, w1) const u32 w0 = (u32)(v)&0x7FFFFFFFu, w1 = (u32)((v) >> 31)
-
-
-template <int N>
-constexpr int MAXP = N ? N : SS_MAXN;
-
-template <int T>
-__device__ __forceinline__ u64 mask_of(const ss_tr_params &tp, size_t e, u64 &alpha)
-{
-    const u64 ev = tp.kdiv > 1 ? mask_e_below(tp.e_key, e, tp.e_range) : mask_e(tp.e_key, e, tp.f);
-    alpha = tp.kdiv > 1 ? (ev * (u64)tp.kdiv) << tp.f : ev << tp.f;   // <= 2^32
-    return ev;
-}
-
-// truncation steps 2 and 3 from the opened x + alpha (canonical): the new shares in o[], their secret in `secret`; the
-// messages of step 2 go to wsh unless it is nullptr
-template <int N, int T, bool STREAM>
-__device__ __forceinline__ void shift_and_unmask(u64 opened, u64 ev, u64 counter, size_t em, size_t mcount,
-                                                 u64 *__restrict__ wsh, const ss_tr_params &tp, int n, u64 (&o)[MAXP<N>],
-                                                 u64 &secret)
-{
-    const u64 w = tp.kdiv > 1 ? shift_round_div(opened, tp.f, tp.kdiv) : shift_signed(opened, tp.f);
-    u64 cw[T], co[T];
-#pragma unroll
-    for (int j = 0; j < T; j++) {
-        cw[j] = ss_draw_lazy_at(tp.gen_key[j], counter);
-        co[j] = ss_fold(cw[j] + ss_draw_lazy_at(tp.alphat_key[j], counter));
-    }
-    if (wsh) eval_points<T, MAXP<N>>(w, cw, [&](int m, u64 v) { send<STREAM>(wsh + (size_t)m * mcount + em, v); }, n);
-    secret = ss_canon(w + SS_P - ev);
-    eval_points<T, MAXP<N>>(secret, co, [&](int m, u64 v) { o[m] = v; }, n);
-}
 
 // RED + RERAND and, with TRUNC, truncation of element e: the new shares come back in o[], their secret (what any k of
 // them reconstruct to) in `secret`
@@ -1072,18 +973,6 @@ hipError_t ss_launch_reconstruct(const u64 *shares, u64 *secret, size_t count, c
 #undef SS_REC
     return hipGetLastError();
 }
-
-// (3,1) and (5,2), and the two counts of t = 3, have their party count fixed at compile time; the other counts of t = 1 and
-// 2 take theirs at run time.  SS_SCHEME(n, t, LAUNCH) runs LAUNCH(N, T).
-#define SS_SCHEME(n_, t_, LAUNCH)               \
-    do {                                        \
-        if ((n_) == 5 && (t_) == 2) LAUNCH(5, 2); \
-        else if ((n_) == 3 && (t_) == 1) LAUNCH(3, 1); \
-        else if ((t_) == 1) LAUNCH(0, 1);       \
-        else if ((t_) == 2) LAUNCH(0, 2);       \
-        else if ((n_) == 7) LAUNCH(7, 3);       \
-        else LAUNCH(8, 3);                      \
-    } while (0)
 
 // Reductions with an instance without the code for cut tiles, which costs registers (n = 6: seven waves per SIMD instead of eight): what
 // tensors and products of at most two planes per tile take where it is the faster one.  Reduce + truncate + open, us, with -> without:
