@@ -402,6 +402,118 @@ int ssnet_reduce_truncate_relu(ssnet_ctx *ctx, const uint64_t *d_c, int B, int C
 int ssnet_reduce_truncate_relu_direct(ssnet_ctx *ctx, const uint64_t *d_c, int B, int C, int HW, const uint64_t *d_beta,
                                       const uint64_t *d_betainv, uint64_t *d_out, void *d_planes);
 
+/* ---- transformer blocks: rotary positions, a paged cache, attention ----
+ *
+ * The dense layers of a block are those above; what follows is what lies between
+ * them.  Everything stays on shares: degree-t shares at scale 2^f come in (of
+ * queries, keys and values, as ssnet_degree_reduce_truncate leaves them), and
+ * the attention's result is a degree-2t sharing like that of a dense layer.
+ * d_x of the calls below is [n][tokens][ld]: the heads of a token, heads *
+ * head_dim consecutive elements, start every `ld` >= heads * head_dim elements,
+ * so that queries, keys and values may be parts of one product.
+ *
+ * Rotary positions.  Pair j < rot/2 of the first `rot` elements of every head
+ * is turned by the angle of its token: with (c, s) = table[pos[token]][j],
+ *   (x_a, x_b) -> (x_a c - x_b s, x_b c + x_a s),
+ * (a, b) = (2j, 2j+1) if interleaved, else (j, j + rot/2); elements from `rot`
+ * on pass through.  d_table [positions][rot/2][2] holds round(2^f cos),
+ * round(2^f sin), whatever the angles are (scaled for a longer context, say);
+ * entries are public and may be any int32.  d_pos [tokens]: rows of the table
+ * (a row outside of it counts as the nearest one).  2 <= rot <= head_dim, even.
+ * The turned elements have 2f fraction bits and are truncated in the same
+ * launch: results, messages and draws are those of ssnet_truncate(stream_id) on
+ * the tensor [tokens][heads][rot] of turned elements.  Requires |x_a c| + |x_b s|
+ * + 2^32 <= (p-1)/2.  Workspace: ssnet_workspace_bytes_stream(tokens * heads *
+ * rot).
+ *   ssnet_rotary_truncate: d_out [n][tokens][heads][head_dim]; it may be d_x
+ *     itself if ld = heads * head_dim, and must not overlap it otherwise. */
+typedef struct ssnet_rotary {
+    const int32_t *d_table;
+    const int32_t *d_pos;
+    int positions, rot, interleaved;
+} ssnet_rotary;
+int ssnet_rotary_truncate(ssnet_ctx *ctx, const uint64_t *d_x, size_t ld, int tokens, int heads, int head_dim,
+                          const ssnet_rotary *rotary, uint64_t stream_id, uint64_t *d_out);
+
+/* A paged cache of keys and values.  A page has `page_size` places for one token
+ * each (a multiple of 16); place number page * page_size + i is the token's
+ * slot.  The cache holds the balanced digits to the base 256 of every share (8
+ * per element, 6 over the 45-bit prime), in cells of 16 places, ready for the
+ * int8 products:
+ *   d_keys   [pages][n][heads][page_size/16][digit][head_dim/16][16 places][16 elements] int8
+ *   d_values [pages][n][heads][page_size/16][digit][head_dim][16 places] int8
+ * (ssnet_cache_page_bytes bytes per page each, 16-byte aligned, memory of the
+ * caller's; what unused places hold does not matter).  head_dim is a multiple
+ * of 16 up to SSNET_MAX_HEAD_DIM; pages * page_size < 2^31.
+ *   ssnet_cache_append: keys d_k and values d_v of `tokens` new tokens (token
+ *     strides ld_k, ld_v) go to the places d_slots [tokens], all different; a
+ *     token whose slot is negative or beyond the cache is left out.  rotary, if
+ *     not NULL, turns and truncates the keys on the way as ssnet_rotary_truncate
+ *     does (same messages, draws and workspace, heads being the cache's); keys
+ *     and values are at scale 2^f. */
+#define SSNET_MAX_HEAD_DIM 256
+typedef struct ssnet_paged_cache {
+    void *d_keys, *d_values;
+    int pages, page_size, heads, head_dim;
+} ssnet_paged_cache;
+size_t ssnet_cache_page_bytes(const ssnet_ctx *ctx, int page_size, int heads, int head_dim);
+int ssnet_cache_append(ssnet_ctx *ctx, const ssnet_paged_cache *cache, const uint64_t *d_k, size_t ld_k, const uint64_t *d_v, size_t ld_v,
+                       int tokens, const int64_t *d_slots, const ssnet_rotary *rotary, uint64_t stream_id);
+
+/* Attention of new tokens over the paged cache.  `tokens` query tokens belong to
+ * `sequences` sequences: those of sequence b are d_start[b] .. d_start[b+1] - 1
+ * (d_start[0] = 0, d_start[sequences] = tokens, none or more each).  Its context
+ * is the d_length[b] <= max_length tokens whose keys and values lie in the places
+ * of the pages d_table[b][0], d_table[b][1], ... in order; the query tokens are
+ * the last of them.  causal != 0: query token i of c sees the first d_length[b]
+ * - c + i + 1 keys, otherwise all; a row that sees nothing gives zero.  heads
+ * query heads, a multiple of the cache's; query head h reads head h / (heads /
+ * cache heads).  The arrays lie on the device; entries of d_table beyond a
+ * sequence's context are not used.
+ *
+ * Per row (token, head), row index r = token * heads + head, keys j:
+ *   1. parties i = 1..2t+1: S_i[j] = q_i . k_i[j] mod p (degree 2t, 2f fraction
+ *      bits) plus their share of a mask, uniform in F_p and the same for all keys
+ *      of the row (domains ROW_MASK and, for the t coefficients of its sharing,
+ *      ROWMASK_GEN, counter r);
+ *   2. the elite party reconstructs s[j] + mask, takes the softmax of the row,
+ *      which no constant added to it changes, and shares the weights with degree
+ *      t (domain WEIGHT_GEN, counter r 2^32 + j).  Of keys that the row does not
+ *      see every party's share is 0;
+ *   3. all parties: O_i = sum_j P_i[j] v_i[j] mod p.
+ * So the elite party learns the differences of a row's scores, that is the
+ * weights, as it learns the ratios inside a pooling kernel under a mask that is
+ * equal there; no party learns a score, a query, a key or a value.
+ * The softmax is defined in whole numbers: with d the distance of a score from
+ * the largest of its row (signed, 2f fraction bits) and h = min(2f, 24),
+ *   u = (min(d >> (2f - h), 2^37) * scale) >> (h + 8)  (octaves, 16 fraction bits),
+ *   w = E(u mod 2^16) >> (u >> 16), 0 from 31 octaves on,  E(r) ~ 2^30 2^(-r/2^16):
+ *     e = 1077640, then for c = 10033292, 59494488, 257928559, 744260865, 2^30:
+ *     e = c - ((e r) >> 16)   (off by 2.2e-7 of the weight at most),
+ *   W = sum of w, z = max(0, bits of W - 32), R = floor(2^62 / (W >> z)),
+ *   P = (((w R) >> 16) + 2^(45 - weight_bits + z)) >> (46 - weight_bits + z),
+ * P being 2^weight_bits times the weight.  scale = round(2^24 log2(e) factor), the
+ * factor of the scores (1 / sqrt(head_dim)); 2^16 <= scale < 2^26; 8 <=
+ * weight_bits <= 30; max_length <= SSNET_MAX_CONTEXT.  Requires differences of
+ * scores below p/2.  d_out [n][tokens][heads][head_dim]: a degree-2t sharing with
+ * f + weight_bits fraction bits (as with every product, RED and truncation follow;
+ * with weight_bits = 2f, which long contexts need, two truncations).
+ * Workspace: ssnet_workspace_bytes_attention for `tokens` tokens has room for the
+ * messages of the whole call; a smaller one serves if it has room for one token's,
+ * and the tokens are then taken in several runs with the same result.  Messages
+ * behind the header: [2t+1][rows][max_length rounded up to 64] masked scores, then
+ * the opened ones [rows][..] (of the last run; keys that a row does not see hold
+ * anything). */
+#define SSNET_MAX_CONTEXT (1 << 20)
+typedef struct ssnet_sequences {
+    const int32_t *d_start, *d_table, *d_length;
+    int sequences, tokens, max_pages, max_length;
+} ssnet_sequences;
+size_t ssnet_workspace_bytes_attention(const ssnet_ctx *ctx, const ssnet_paged_cache *cache, int sequences, int tokens, int heads,
+                                       int max_length);
+int ssnet_paged_attention(ssnet_ctx *ctx, const ssnet_paged_cache *cache, const ssnet_sequences *seqs, const uint64_t *d_q, size_t ld_q,
+                          int heads, uint32_t scale, int weight_bits, int causal, uint64_t stream_id, uint64_t *d_out);
+
 /* Host-side generator, exposed so that its bits can be checked without a GPU.
  * key = absorb(seed, domain, stream_id, party, j) with h <- mix64((h ^ word) +
  * 0x9E3779B97F4A7C15) from h = 0, mix64 being the SplitMix64 output function;
@@ -417,6 +529,9 @@ int ssnet_reduce_truncate_relu_direct(ssnet_ctx *ctx, const uint64_t *d_c, int B
 #define SSNET_DOM_MASK_BETA 8
 #define SSNET_DOM_BETA_GEN 9
 #define SSNET_DOM_BETAINV_GEN 10
+#define SSNET_DOM_ROW_MASK 11
+#define SSNET_DOM_ROWMASK_GEN 12
+#define SSNET_DOM_WEIGHT_GEN 13
 uint64_t ssnet_rng_key(uint64_t seed, uint64_t domain, uint64_t stream_id, uint64_t party, uint64_t j);
 uint64_t ssnet_rng_draw(uint64_t key, uint64_t e);
 uint64_t ssnet_rng_field(uint64_t key, uint64_t e);

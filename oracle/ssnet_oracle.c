@@ -838,3 +838,134 @@ void orc_relu_pool(const u64 *x, const u64 *sh_b, const u64 *sh_bi, size_t plane
             out[(size_t)i * cout + e] = orc_mul(y[e], sh_bi[(size_t)i * cout + e], p);
     free(m); free(v); free(y);
 }
+
+/* ------------------------------------------------------------------ */
+/* Transformer blocks: rotary positions, attention of new tokens.      */
+/* ------------------------------------------------------------------ */
+
+#define ORC_DOM_ROW_MASK 11
+#define ORC_DOM_ROWMASK_GEN 12
+#define ORC_DOM_WEIGHT_GEN 13
+
+/* x [n][tokens][heads][dim] -> out [n][tokens][heads][rot], the turned elements before truncation; table [positions][rot/2][2] */
+void orc_rotary_turn(const u64 *x, const int32_t *table, const int32_t *pos, int n, int tokens, int heads, int dim, int rot,
+                     int interleaved, u64 p, u64 *out)
+{
+    for (int i = 0; i < n; i++)
+        for (int a = 0; a < tokens; a++)
+            for (int h = 0; h < heads; h++)
+                for (int j = 0; j < rot / 2; j++) {
+                    int d0 = interleaved ? 2 * j : j, d1 = interleaved ? 2 * j + 1 : j + rot / 2;
+                    const u64 *src = x + (((size_t)i * tokens + a) * heads + h) * dim;
+                    u64 *dst = out + (((size_t)i * tokens + a) * heads + h) * rot;
+                    const int32_t *cs = table + ((size_t)pos[a] * (rot / 2) + j) * 2;
+                    u64 c = orc_from_signed(cs[0], p), s = orc_from_signed(cs[1], p);
+                    dst[d0] = orc_sub(orc_mul(src[d0], c, p), orc_mul(src[d1], s, p), p);
+                    dst[d1] = orc_add(orc_mul(src[d1], c, p), orc_mul(src[d0], s, p), p);
+                }
+}
+
+/* balanced digits to the base 256, the lowest first */
+void orc_digits(const u64 *x, size_t count, int digits, signed char *out)
+{
+    for (size_t e = 0; e < count; e++) {
+        u128 v = x[e];
+        for (int l = 0; l < digits; l++) {
+            int d = (int)(v & 255);
+            v >>= 8;
+            if (d > 127) {
+                d -= 256;
+                v++;
+            }
+            out[e * digits + l] = (signed char)d;
+        }
+    }
+}
+
+/* floor-cut 2^30 2^-x, x = distance `below` (2 f fraction bits) times the factor, in octaves (`scale`: 24 fraction bits) */
+u64 orc_softmax_weight(u64 below, int f, u64 scale)
+{
+    static const u64 c[5] = {10033292, 59494488, 257928559, 744260865, (u64)1 << 30};
+    int h = 2 * f < 24 ? 2 * f : 24;
+    u64 d = below >> (2 * f - h);
+    if (d > (u64)1 << 37) d = (u64)1 << 37;
+    u64 u = (u64)(((u128)d * scale) >> (h + 8)), r = u & 65535, e = 1077640;
+    for (int i = 0; i < 5; i++) e = c[i] - ((e * r) >> 16);
+    return (u >> 16) < 31 ? e >> (u >> 16) : 0;
+}
+
+/* the weights of one row from its scores (canonical, all with the same mask), `bits` fraction bits */
+void orc_softmax_row(const u64 *s, int limit, int f, u64 scale, int bits, u64 p, u64 *weight)
+{
+    if (limit < 1) return;
+    int best = 0;
+    for (int j = 1; j < limit; j++)
+        if (orc_lift1(orc_sub(s[j], s[best], p), p) > 0) best = j;
+    u64 total = 0;
+    for (int j = 0; j < limit; j++) {
+        weight[j] = orc_softmax_weight((u64)orc_lift1(orc_sub(s[best], s[j], p), p), f, scale);
+        total += weight[j];
+    }
+    int z = 0;
+    while (total >> z >> 32) z++;
+    u64 recip = ((u64)1 << 62) / (total >> z);
+    for (int j = 0; j < limit; j++)
+        weight[j] = (u64)((((u128)weight[j] * recip >> 16) + ((u128)1 << (45 - bits + z))) >> (46 - bits + z));
+}
+
+/* Attention of the c last tokens of a context of len tokens.  q [n][c][heads][dim], k, v [n][len][kv][dim] degree-t shares; token0: number
+ * of the first token in the call.  out [n][c][heads][dim] (degree 2t); msg [2t+1][c][heads][len], opened, weight [c][heads][len] if not NULL */
+void orc_attention(const u64 *q, const u64 *k, const u64 *v, int n, int t, int c, int len, int heads, int kv, int dim, int f, u64 scale, int bits,
+                   int causal, u64 p, u64 seed, u64 stream_id, int token0, u64 *msg, u64 *opened, u64 *weight, u64 *out)
+{
+    int nr = 2 * t + 1, ids[ORC_MAXN];
+    u64 lambda[ORC_MAXN];
+    for (int i = 0; i < nr; i++) ids[i] = i + 1;
+    orc_lagrange(ids, nr, p, lambda);
+#pragma omp parallel for collapse(2) schedule(dynamic)
+    for (int i = 0; i < c; i++)
+        for (int h = 0; h < heads; h++) {
+            int limit = causal ? len - c + i + 1 : len;
+            if (limit < 0) limit = 0;
+            u64 row = (u64)(token0 + i) * heads + h;
+            u64 *s = (u64 *)calloc(len + 1, sizeof(u64)), *w = (u64 *)calloc(len + 1, sizeof(u64));
+            /* the mask of the row at every reducing party */
+            u64 mask[ORC_MAXN];
+            for (int m = 0; m < nr; m++) {
+                mask[m] = orc_draw_field(orc_key(seed, ORC_DOM_ROW_MASK, stream_id, 0, 0), row, p);
+                for (int j = 1; j <= t; j++)
+                    mask[m] = orc_add(mask[m], orc_mul(orc_draw_field(orc_key(seed, ORC_DOM_ROWMASK_GEN, stream_id, 0, j), row, p),
+                                                       orc_pow(m + 1, j, p), p), p);
+            }
+            for (int j = 0; j < limit; j++) {
+                for (int m = 0; m < nr; m++) {
+                    u64 dot = mask[m];
+                    for (int d = 0; d < dim; d++)
+                        dot = orc_add(dot, orc_mul(q[(((size_t)m * c + i) * heads + h) * dim + d],
+                                                   k[(((size_t)m * len + j) * kv + h / (heads / kv)) * dim + d], p), p);
+                    if (msg) msg[(((size_t)m * c + i) * heads + h) * len + j] = dot;
+                    s[j] = orc_add(s[j], orc_mul(lambda[m], dot, p), p);
+                }
+                if (opened) opened[((size_t)i * heads + h) * len + j] = s[j];
+            }
+            orc_softmax_row(s, limit, f, scale, bits, p, w);
+            if (weight) memcpy(weight + ((size_t)i * heads + h) * len, w, sizeof(u64) * len);
+            for (int m = 0; m < n; m++)
+                for (int d = 0; d < dim; d++) out[(((size_t)m * c + i) * heads + h) * dim + d] = 0;
+            for (int j = 0; j < limit; j++) {
+                u64 coef[ORC_MAXN];
+                for (int x = 1; x <= t; x++)
+                    coef[x] = orc_draw_field(orc_key(seed, ORC_DOM_WEIGHT_GEN, stream_id, 0, x), (row << 32) + j, p);
+                for (int m = 0; m < n; m++) {
+                    u64 share = w[j] % p;
+                    for (int x = 1; x <= t; x++) share = orc_add(share, orc_mul(coef[x], orc_pow(m + 1, x, p), p), p);
+                    for (int d = 0; d < dim; d++) {
+                        u64 *o = out + (((size_t)m * c + i) * heads + h) * dim + d;
+                        *o = orc_add(*o, orc_mul(share, v[(((size_t)m * len + j) * kv + h / (heads / kv)) * dim + d], p), p);
+                    }
+                }
+            }
+            free(s);
+            free(w);
+        }
+}

@@ -332,3 +332,56 @@ def relu_pool(x, sh_b, sh_bi, planes, H, W, kh, kw, sh, sw, ph, pw, mode, n, t, 
     out = np.empty((n, cout), np.uint64)
     _relu_pool(_p(x), _p(sh_b), _p(sh_bi), planes, H, W, kh, kw, sh, sw, ph, pw, mode, n, t, p, _p(msg), _p(y), _p(out))
     return (out, msg, y) if full else out
+
+
+# ---- transformer blocks ----
+_turn = _sig("orc_rotary_turn", None, P, P, P, *([C.c_int] * 6), u64, P)
+_digits_of = _sig("orc_digits", None, P, sz, C.c_int, P)
+_softmax_weight = _sig("orc_softmax_weight", u64, u64, C.c_int, u64)
+_softmax_row = _sig("orc_softmax_row", None, P, C.c_int, C.c_int, u64, C.c_int, u64, P)
+_attention = _sig("orc_attention", None, P, P, P, *([C.c_int] * 8), u64, C.c_int, C.c_int, u64, u64, u64, C.c_int, P, P, P, P)
+
+
+def rotary_truncate(x, table, pos, t, f, p, seed, stream_id, interleaved=False, full=False):
+    """x [n, tokens, heads, dim] -> the same with the first 2 * table.shape[1] elements of every head turned and truncated
+    (full: also the messages of the truncation)"""
+    x, table, pos = _a(x), np.ascontiguousarray(table, dtype=np.int32), np.ascontiguousarray(pos, dtype=np.int32)
+    n, tokens, heads, dim = x.shape
+    rot = 2 * table.shape[1]
+    turned = np.empty((n, tokens, heads, rot), np.uint64)
+    _turn(_p(x), _p(table), _p(pos), n, tokens, heads, dim, rot, int(interleaved), p, _p(turned))
+    short, u, wsh = truncate(turned, n, t, f, p, seed, stream_id, full=True)
+    out = np.concatenate([short, x[..., rot:]], axis=-1)
+    return (out, u, wsh) if full else out
+
+
+def digits(x, count):
+    """balanced digits to the base 256 on a new last axis"""
+    x = _a(x)
+    out = np.empty(x.shape + (count,), np.int8)
+    _digits_of(_p(x), x.size, count, _p(out))
+    return out
+
+
+def softmax_weight(below, f, scale):
+    return _softmax_weight(below, f, scale)
+
+
+def softmax_row(s, f, scale, bits, p):
+    s = _a(s)
+    out = np.zeros(s.size, np.uint64)
+    _softmax_row(_p(s), s.size, f, scale, bits, p, _p(out))
+    return out
+
+
+def attention(q, k, v, t, f, scale, bits, causal, p, seed, stream_id, token0=0, full=False):
+    """q [n, c, heads, dim] over k, v [n, len, kv, dim] -> [n, c, heads, dim] (full: also masked scores, opened scores, weights)"""
+    q, k, v = _a(q), _a(k), _a(v)
+    n, c, heads, dim = q.shape
+    length, kv = k.shape[1], k.shape[2]
+    msg = np.zeros((2 * t + 1, c, heads, length), np.uint64)
+    opened, weight = np.zeros((c, heads, length), np.uint64), np.zeros((c, heads, length), np.uint64)
+    out = np.zeros(q.shape, np.uint64)
+    _attention(_p(q), _p(k), _p(v), n, t, c, length, heads, kv, dim, f, scale, bits, int(causal), p, seed, stream_id, token0, _p(msg),
+               _p(opened), _p(weight), _p(out))
+    return (out, msg, opened, weight) if full else out

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import importlib.util
+import math
 import os
 from typing import Optional, Sequence
 
@@ -73,6 +74,11 @@ SIGNATURES = {
     "ssnet_pool_out_size": (_int, [_int, _int, _int, _int]),
     "ssnet_pool_masks": (_int, [_ptr, _sz] + [_int] * 8 + [_u64, _ptr, _ptr]),
     "ssnet_relu_pool": (_int, [_ptr, _ptr, _ptr, _ptr, _sz] + [_int] * 9 + [_ptr]),
+    "ssnet_rotary_truncate": (_int, [_ptr, _ptr, _sz, _int, _int, _int, _ptr, _u64, _ptr]),
+    "ssnet_cache_page_bytes": (_sz, [_ptr, _int, _int, _int]),
+    "ssnet_cache_append": (_int, [_ptr, _ptr, _ptr, _sz, _ptr, _sz, _int, _ptr, _ptr, _u64]),
+    "ssnet_workspace_bytes_attention": (_sz, [_ptr, _ptr, _int, _int, _int, _int]),
+    "ssnet_paged_attention": (_int, [_ptr, _ptr, _ptr, _ptr, _sz, _int, _int, _int, _int, _u64, _ptr]),
     "ssnet_field_prime": (_u64, []),
     "ssnet_rng_key": (_u64, [_u64] * 5),
     "ssnet_rng_draw": (_u64, [_u64, _u64]),
@@ -99,7 +105,7 @@ class _Entries:
              "conv1x1_mod_prepacked", "share_planes", "split_planes", "conv_mod_planes", "linear_product_prepacked",
              "conv1x1_product_prepacked", "conv_product_planes", "degree_reduce", "truncate", "degree_reduce_truncate",
              "degree_reduce_truncate_div", "degree_reduce_truncate_reconstruct", "reduce_truncate_direct", "reduce_truncate_relu",
-             "reduce_truncate_relu_direct", "relu", "relu_pool")
+             "reduce_truncate_relu_direct", "relu", "relu_pool", "rotary_truncate", "cache_append", "paged_attention")
 
     def __init__(self, lib: C.CDLL):
         global _calls
@@ -154,6 +160,52 @@ def _per_party(t: torch.Tensor) -> int:
     """elements of one party's share in [n][...]; t[0].numel() without making the view (1.3 us of a call's 6 to 10)"""
     total = t.numel()
     return total // t.size(0) if total else t[0].numel()
+
+
+class _Rotary(C.Structure):
+    _fields_ = [("d_table", _ptr), ("d_pos", _ptr), ("positions", _int), ("rot", _int), ("interleaved", _int)]
+
+
+class _PagedCacheStruct(C.Structure):
+    _fields_ = [("d_keys", _ptr), ("d_values", _ptr), ("pages", _int), ("page_size", _int), ("heads", _int), ("head_dim", _int)]
+
+
+class _Sequences(C.Structure):
+    _fields_ = [("d_start", _ptr), ("d_table", _ptr), ("d_length", _ptr), ("sequences", _int), ("tokens", _int), ("max_pages", _int),
+                ("max_length", _int)]
+
+
+def _device_tensor(t: torch.Tensor, dtype: torch.dtype, name: str, shape: Optional[tuple] = None) -> torch.Tensor:
+    if t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+        raise TypeError(f"{name} must be a contiguous {dtype} tensor on the GPU")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have the shape {shape}")
+    return t
+
+
+class PagedCache:
+    """Keys and values of a context as balanced digits, in pages of page_size places for one token each (include/ssnet.h has the
+    layout).  keys, values: int8 tensors to use (of any shape, `pages` pages), else new ones."""
+
+    def __init__(self, ss: "SSNet", pages: int, page_size: int, heads: int, head_dim: int, keys: Optional[torch.Tensor] = None,
+                 values: Optional[torch.Tensor] = None):
+        page_bytes = ss.lib.ssnet_cache_page_bytes(ss._ctx, page_size, heads, head_dim)
+        if page_bytes == 0 or pages < 1:
+            raise SSNetError(EINVAL, "ssnet_cache_page_bytes")
+        self.n, self.pages, self.page_size, self.heads, self.head_dim = ss.n, pages, page_size, heads, head_dim
+        digits = page_bytes // (ss.n * heads * page_size * head_dim)
+        cells, groups = page_size // 16, head_dim // 16
+        if keys is None:
+            keys = torch.empty((pages, ss.n, heads, cells, digits, groups, 16, 16), dtype=torch.int8, device=ss.device)
+        if values is None:
+            values = torch.empty((pages, ss.n, heads, cells, digits, head_dim, 16), dtype=torch.int8, device=ss.device)
+        for name, t in (("keys", keys), ("values", values)):
+            _device_tensor(t, torch.int8, name)
+            if t.numel() != pages * page_bytes:
+                raise SSNetError(EINVAL, f"PagedCache: {name} must hold {pages} pages of {page_bytes} bytes")
+        self.keys, self.values, self.digits = keys, values, digits
+        self._struct = _PagedCacheStruct(_dptr(keys), _dptr(values), pages, page_size, heads, head_dim)
+        self._address = C.addressof(self._struct)
 
 
 class SSNet:
@@ -662,6 +714,105 @@ class SSNet:
             raise SSNetError(EINVAL, "relu_pool: out has the wrong size")
         self._ok(self._call.relu_pool(self._handle, _dptr(x), _dptr(beta), _dptr(betainv), planes, H, W, kh, kw, sh, sw,
                                       ph, pw, mode, _dptr(out)), "ssnet_relu_pool")
+        return out
+
+    # ---- transformer blocks ----
+    ATTENTION_ROOM = 8 << 30     # bytes of workspace up to which paged_attention takes all tokens at once
+
+    def _heads_view(self, x: torch.Tensor, name: str) -> int:
+        """elements between the tokens of x [n][tokens][heads][head_dim], which may be part of a longer row per token"""
+        if x.dtype != torch.int64 or x.dim() != 4 or not x.is_cuda:
+            raise TypeError(f"{name} must be an int64 tensor [n][tokens][heads][head_dim] on the GPU")
+        n, tokens, heads, dim = x.shape
+        if n != self.n:
+            raise ValueError(f"{name} must have the shares of {self.n} parties")
+        s = x.stride()
+        ld = s[1] if tokens > 1 else s[0]
+        if x.numel() and (s[0] != tokens * ld or (heads > 1 and s[2] != dim) or (dim > 1 and s[3] != 1) or ld < heads * dim):
+            raise TypeError(f"{name}: the heads of a token must be contiguous, tokens and parties equally far apart")
+        return ld
+
+    def _rotary(self, table: torch.Tensor, pos: torch.Tensor, tokens: int, layout: str) -> _Rotary:
+        _device_tensor(table, torch.int32, "table"), _device_tensor(pos, torch.int32, "pos", (tokens,))
+        if table.dim() != 3 or table.shape[2] != 2:
+            raise ValueError("table must be [positions][rot / 2][2]")
+        if layout not in ("half", "interleaved"):
+            raise ValueError("layout must be 'half' or 'interleaved'")
+        return _Rotary(_dptr(table), _dptr(pos), table.shape[0], 2 * table.shape[1], layout == "interleaved")
+
+    def rotary_truncate(self, x: torch.Tensor, table: torch.Tensor, pos: torch.Tensor, stream_id: int, layout: str = "half",
+                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x [n][tokens][heads][head_dim], turned by the rows `pos` of fixedpoint.rotary_table and truncated (the first
+        2 * table.shape[1] elements of every head; the others pass through)"""
+        ld = self._heads_view(x, "x")
+        n, tokens, heads, dim = x.shape
+        rotary = self._rotary(table, pos, tokens, layout)
+        self._reserve_stream(tokens * heads * rotary.rot)
+        if out is None:
+            out = torch.empty(tuple(x.shape), dtype=torch.int64, device=x.device)
+        else:
+            _device_tensor(out, torch.int64, "out", tuple(x.shape))
+        self._ok(self._call.rotary_truncate(self._handle, _dptr(x), ld, tokens, heads, dim, C.addressof(rotary), stream_id, _dptr(out)),
+                 "ssnet_rotary_truncate")
+        return out
+
+    def cache_append(self, cache: PagedCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream_id: int,
+                     table: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None, layout: str = "half"):
+        """keys k and values v [n][tokens][heads][head_dim] into the places `slots` [tokens] of the cache; table, pos: the keys are
+        turned and truncated on the way, as rotary_truncate does"""
+        ld_k, ld_v = self._heads_view(k, "k"), self._heads_view(v, "v")
+        if k.shape != v.shape or k.shape[2] != cache.heads or k.shape[3] != cache.head_dim or cache.n != self.n:
+            raise ValueError("k and v must be [n][tokens][heads][head_dim] of the cache")
+        tokens = k.shape[1]
+        _device_tensor(slots, torch.int64, "slots", (tokens,))
+        if (table is None) != (pos is None):
+            raise ValueError("table and pos go together")
+        rotary = None if table is None else self._rotary(table, pos, tokens, layout)
+        if rotary is not None:
+            self._reserve_stream(tokens * cache.heads * rotary.rot)
+        self._ok(self._call.cache_append(self._handle, cache._address, _dptr(k), ld_k, _dptr(v), ld_v, tokens, _dptr(slots),
+                                         None if rotary is None else C.addressof(rotary), stream_id), "ssnet_cache_append")
+
+    def workspace_bytes_attention(self, cache: PagedCache, sequences: int, tokens: int, heads: int, max_length: int) -> int:
+        return self.lib.ssnet_workspace_bytes_attention(self._ctx, cache._address, sequences, tokens, heads, max_length)
+
+    def paged_attention(self, cache: PagedCache, q: torch.Tensor, seq_start: torch.Tensor, block_table: torch.Tensor,
+                        ctx_len: torch.Tensor, max_ctx: int, stream_id: int, scale: Optional[float] = None,
+                        weight_bits: Optional[int] = None, causal: bool = True, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of the tokens q [n][tokens][heads][head_dim], those of sequence b from seq_start[b] to seq_start[b+1], over the
+        ctx_len[b] <= max_ctx tokens in the pages block_table[b] -> [n][tokens][heads][head_dim], degree 2t, f + weight_bits
+        fraction bits.  scale: factor of the scores (default 1 / sqrt(head_dim)); weight_bits: default f."""
+        ld = self._heads_view(q, "q")
+        n, tokens, heads, dim = q.shape
+        sequences = ctx_len.shape[0]
+        _device_tensor(ctx_len, torch.int32, "ctx_len", (sequences,)), _device_tensor(seq_start, torch.int32, "seq_start", (sequences + 1,))
+        _device_tensor(block_table, torch.int32, "block_table")
+        if block_table.dim() != 2 or block_table.shape[0] != sequences or dim != cache.head_dim or cache.n != self.n:
+            raise ValueError("block_table must be [sequences][pages], q [n][tokens][heads][head_dim of the cache]")
+        factor = dim ** -0.5 if scale is None else scale
+        if not 0 < factor < 4:
+            raise ValueError("scale must be positive and below 4")
+        fixed = round(factor * math.log2(math.e) * (1 << 24))
+        bits = self.f if weight_bits is None else weight_bits
+        key = ("attention", cache.heads, dim, sequences, tokens, heads, max_ctx)
+        need = self._sizes.get(key)
+        if need is None:
+            need = self.workspace_bytes_attention(cache, sequences, tokens, heads, max_ctx)
+            if need == 0:
+                raise SSNetError(EINVAL, "ssnet_workspace_bytes_attention")
+            if need > self.ATTENTION_ROOM:   # the tokens go in several runs
+                need = max(self.ATTENTION_ROOM, self.workspace_bytes_attention(cache, sequences, 1, heads, max_ctx))
+            if len(self._sizes) >= 4096:
+                self._sizes.clear()
+            self._sizes[key] = need
+        self.reserve(need)
+        if out is None:
+            out = torch.empty((n, tokens, heads, dim), dtype=torch.int64, device=q.device)
+        else:
+            _device_tensor(out, torch.int64, "out", (n, tokens, heads, dim))
+        seqs = _Sequences(_dptr(seq_start), _dptr(block_table), _dptr(ctx_len), sequences, tokens, block_table.shape[1], max_ctx)
+        self._ok(self._call.paged_attention(self._handle, cache._address, C.addressof(seqs), _dptr(q), ld, heads, fixed, bits, int(causal),
+                                            stream_id, _dptr(out)), "ssnet_paged_attention")
         return out
 
     PROF_CLASSES = ("share", "reconstruct", "pack_w", "pack_x", "gemm", "degree_reduce", "truncate", "nonlinear",

@@ -1,0 +1,709 @@
+// What a transformer block needs beside its dense layers, on shares: rotary positions, a paged cache of keys and values, and the
+// attention of new tokens over it.
+//
+// Attention of a row (token, head) over the keys j < limit, all parties holding degree-t shares:
+//   1. party i = 1..2t+1: score S_i[j] = q_i . k_i[j] mod p (degree 2t, 2 f fraction bits), plus its share of a mask that is the same for
+//      all keys of the row                                                                        -> msg[i][row][j]
+//   2. the elite party reconstructs s[j] + mask, takes the softmax of the row, which no constant added to it changes, as whole
+//      numbers (softmax_weight below), and shares the weights (degree t); every party's share of a key beyond the limit is 0
+//   3. every party i = 1..n: O_i = sum_j P_i[j] v_i[j] mod p (degree 2t)
+// Products run on int8 MFMA over balanced 8-bit digits, as in a dense layer.
+#include "kernels.hpp"
+#include "eval.hpp"
+#include "digits.hpp"
+#include "diagonals.hpp"
+#include "truncation.hpp"
+
+namespace SS_NS {
+
+namespace {
+
+constexpr int BLOCK = 256;
+constexpr int KEY_BLOCK = 256;      // keys of a workgroup of the scores
+constexpr size_t MAX_ROWS = (size_t)1 << 22;   // of a slab: a workgroup each, less than 2^32 threads in a launch
+constexpr int MAX_RUN = 16320;      // keys that the 32-bit sums of the values can take, in blocks of 64: 8 * 16383 * 2^14 < 2^31
+
+inline unsigned ceil_div(size_t a, size_t b) { return (unsigned)((a + b - 1) / b); }
+
+// ------------------------------------------------------------------ rotary positions
+
+// a c - b s as any word of the right residue below 2^63; a, b canonical, |c|, |s| <= 2^31
+__device__ __forceinline__ u64 turn(u64 a, int c, u64 b, long long s)
+{
+    const long long lo = (long long)(a & 0x7FFFFFFF) * c - (long long)(b & 0x7FFFFFFF) * s;   // two terms below 2^62 each
+    const long long hi = (long long)(a >> 31) * c - (long long)(b >> 31) * s;
+#if defined(SS_FIELD_P45)
+    const u64 l = ((u64)lo & SS_PMASK) + (u64)(lo >> 45) * SS_PC + SS_P;   // > 0, < 2^47
+    const u64 h = (u64)(hi + (long long)(SS_P << 2));                      // |hi| < 2^46
+    return l + SS_PC * (h >> 14) + ((h & 0x3FFFull) << 31);                // h 2^31, h = a 2^14 + b: 55 a + b 2^31
+#else
+    const u64 l = ((u64)lo & SS_P) + (u64)(lo >> 61) + SS_P;               // > 0, < 2^62 + 4
+    const u64 h = ((u64)hi & SS_P) + (u64)(hi >> 61) + SS_P;
+    return l + ((h & 0x3FFFFFFFull) << 31) + (h >> 30);
+#endif
+}
+
+// SSS-Truncation of the element e whose shares of the parties 1..k are xq (any residue below 2^63): the new shares in o[]
+template <int N, int T>
+__device__ __forceinline__ void truncate_element(const u64 (&xq)[T + 1], size_t e, size_t count, u64 *__restrict__ u, u64 *__restrict__ wsh,
+                                                 const ss_tr_params &tp, u64 (&o)[MAXP<N>])
+{
+    constexpr int K = T + 1;
+    const u64 counter = ss_counter(e);
+    u64 alpha, ca[T];
+    const u64 ev = mask_of<T>(tp, e, alpha);
+#pragma unroll
+    for (int j = 0; j < T; j++) ca[j] = ss_draw_lazy_at(tp.alpha_key[j], counter);
+    ss_sacc2 acc;
+    acc.clear();
+    eval_points<T, K>(alpha, ca, [&](int q, u64 v) {
+        const u64 um = ss_reduce(xq[q] + v);
+        u[(size_t)q * count + e] = um;
+        SS_SPLIT31(um, w0, w1);
+        acc.mac(w0, w1, tp.ilambda[q]);
+    });
+    u64 secret;
+    shift_and_unmask<N, T, false>(acc.value(), ev, counter, e, count, wsh, tp, N ? N : tp.n, o, secret);
+}
+
+// where the pairs and the elements that pass through of a token's heads lie: `width` threads for each head
+struct rotary_shape {
+    int tokens, heads, dim, width;
+    fdiv dWidth, dHeads;
+};
+
+__device__ __forceinline__ void pair_of(const ss_rope &rope, int j, int &a, int &b)
+{
+    const int half = rope.rot >> 1;
+    a = rope.interleaved ? 2 * j : j;
+    b = rope.interleaved ? 2 * j + 1 : j + half;
+}
+
+// the rotated and truncated pair j of (token, head): shares of both elements
+template <int N, int T>
+__device__ __forceinline__ void rotate_pair(const u64 *x, size_t ld, const rotary_shape &g, int token, int head, int j, u64 *__restrict__ u,
+                                            u64 *__restrict__ wsh, const ss_rope &rope, const ss_tr_params &tp, int &a, int &b,
+                                            u64 (&oa)[MAXP<N>], u64 (&ob)[MAXP<N>])
+{
+    constexpr int K = T + 1;
+    pair_of(rope, j, a, b);
+    const u64 *row = x + (size_t)token * ld + (size_t)head * g.dim;
+    const size_t party = (size_t)g.tokens * ld, count = (size_t)g.tokens * g.heads * rope.rot;
+    const int2 cs = rope.table[(size_t)min(max(rope.pos[token], 0), rope.positions - 1) * (rope.rot >> 1) + j];
+    u64 ra[K], rb[K];
+#pragma unroll
+    for (int q = 0; q < K; q++) {
+        const u64 xa = row[q * party + a], xb = row[q * party + b];
+        ra[q] = turn(xa, cs.x, xb, cs.y);
+        rb[q] = turn(xb, cs.x, xa, -(long long)cs.y);
+    }
+    const size_t e = ((size_t)token * g.heads + head) * rope.rot;
+    truncate_element<N, T>(ra, e + a, count, u, wsh, tp, oa);
+    truncate_element<N, T>(rb, e + b, count, u, wsh, tp, ob);
+}
+
+template <int N, int T>
+__global__ __launch_bounds__(BLOCK) void rotary_kernel(const u64 *x, size_t ld, u64 *__restrict__ u, u64 *__restrict__ wsh, u64 *out,
+                                                       rotary_shape g, ss_rope rope, ss_tr_params tp)
+{
+    const u32 i = blockIdx.x * BLOCK + threadIdx.x;
+    if (i >= (u32)(g.tokens * g.heads * g.width)) return;
+    const u32 th = fd_div(i, g.dWidth), token = fd_div(th, g.dHeads), head = th - token * g.heads;
+    const int j = (int)(i - th * g.width), half = rope.rot >> 1, n = N ? N : tp.n;
+    const size_t count = (size_t)g.tokens * g.heads * g.dim;
+    u64 *dst = out + (size_t)th * g.dim;
+    if (j >= half) {
+        const int d = j + half;      // rot + (j - half)
+#pragma unroll
+        for (int m = 0; m < MAXP<N>; m++)
+            if (N != 0 || m < n) dst[m * count + d] = x[(size_t)m * g.tokens * ld + (size_t)token * ld + (size_t)head * g.dim + d];
+        return;
+    }
+    int a, b;
+    u64 oa[MAXP<N>], ob[MAXP<N>];
+    rotate_pair<N, T>(x, ld, g, (int)token, (int)head, j, u, wsh, rope, tp, a, b, oa, ob);
+#pragma unroll
+    for (int m = 0; m < MAXP<N>; m++)
+        if (N != 0 || m < n) {
+            dst[m * count + a] = oa[m];
+            dst[m * count + b] = ob[m];
+        }
+}
+
+// ------------------------------------------------------------------ appending to the cache
+
+struct append_shape {
+    rotary_shape r;
+    const long long *slots;
+    signed char *keys, *values;
+    size_t party, head, page;          // strides in bytes
+    unsigned capacity, page_size;      // keys of the cache, of a page
+    fdiv dPage;
+};
+
+// of the token's place in the cache: its cell in head 0 of party 0, and the key inside the cell
+__device__ __forceinline__ bool place_of(const append_shape &s, int token, size_t &cell, int &key)
+{
+    const long long slot = s.slots[token];
+    if (slot < 0 || slot >= (long long)s.capacity) return false;
+    const u32 page = fd_div((u32)slot, s.dPage), in = (u32)slot - page * s.page_size;
+    key = (int)(in & 15);
+    cell = page * s.page + (size_t)(in >> 4) * (SS_NLIMB * 16) * s.r.dim;
+    return true;
+}
+
+template <int N>
+__device__ __forceinline__ void put_key(const append_shape &s, size_t cell, int key, int head, int d, const u64 (&v)[MAXP<N>], int n)
+{
+#pragma unroll
+    for (int m = 0; m < MAXP<N>; m++)
+        if (N != 0 || m < n) {
+            const u64 dig = balanced_digits(v[m]);
+            signed char *c = s.keys + cell + m * s.party + head * s.head + (d >> 4) * 256 + key * 16 + (d & 15);
+#pragma unroll
+            for (int l = 0; l < SS_NLIMB; l++) c[(size_t)l * s.r.dim * 16] = (signed char)(dig >> (8 * l));
+        }
+}
+
+// One thread per pair (or element that passes through) of a key, then one per element of a value.
+template <int N, int T>
+__global__ __launch_bounds__(BLOCK) void append_kernel(const u64 *k, size_t ld_k, const u64 *v, size_t ld_v, u64 *__restrict__ u,
+                                                       u64 *__restrict__ wsh, append_shape s, ss_rope rope, ss_tr_params tp, u32 key_blocks)
+{
+    const int n = N ? N : tp.n;
+    const rotary_shape &g = s.r;
+    u64 o[MAXP<N>];
+    size_t cell;
+    int key;
+    if (blockIdx.x >= key_blocks) {
+        const u32 i = (blockIdx.x - key_blocks) * BLOCK + threadIdx.x;
+        if (i >= (u32)(g.tokens * g.heads * g.dim)) return;
+        const u32 per = (u32)(g.heads * g.dim), token = i / per, rest = i - token * per, head = rest / g.dim, d = rest - head * g.dim;
+        if (!place_of(s, (int)token, cell, key)) return;
+#pragma unroll
+        for (int m = 0; m < MAXP<N>; m++)
+            if (N != 0 || m < n) {
+                const u64 dig = balanced_digits(v[((size_t)m * g.tokens + token) * ld_v + rest]);
+                signed char *c = s.values + cell + m * s.party + head * s.head + d * 16 + key;
+#pragma unroll
+                for (int l = 0; l < SS_NLIMB; l++) c[(size_t)l * g.dim * 16] = (signed char)(dig >> (8 * l));
+            }
+        return;
+    }
+    const u32 i = blockIdx.x * BLOCK + threadIdx.x;
+    if (i >= (u32)(g.tokens * g.heads * g.width)) return;
+    const u32 th = fd_div(i, g.dWidth), token = fd_div(th, g.dHeads), head = th - token * g.heads;
+    const int j = (int)(i - th * g.width), half = rope.rot >> 1;
+    const bool placed = place_of(s, (int)token, cell, key);
+    if (j >= half) {
+        if (!placed) return;
+        const int d = j + half;
+#pragma unroll
+        for (int m = 0; m < MAXP<N>; m++)
+            if (N != 0 || m < n) o[m] = k[((size_t)m * g.tokens + token) * ld_k + (size_t)head * g.dim + d];
+        put_key<N>(s, cell, key, (int)head, d, o, n);
+        return;
+    }
+    int a, b;
+    u64 ob[MAXP<N>];
+    rotate_pair<N, T>(k, ld_k, g, (int)token, (int)head, j, u, wsh, rope, tp, a, b, o, ob);
+    if (!placed) return;
+    put_key<N>(s, cell, key, (int)head, a, o, n);
+    put_key<N>(s, cell, key, (int)head, b, ob, n);
+}
+
+// ------------------------------------------------------------------ attention
+
+struct row_stat {
+    u64 top;        // opened score (with the row's mask) of the largest
+    u64 recip;      // reciprocal of the sum of the weights, 0 for a row that sees nothing
+    int drop;       // bits that the sum is shifted by
+    int limit;      // keys that the row sees
+};
+
+struct attn_args {
+    ss_paged c;
+    ss_sequences s;
+    size_t cell, head_bytes, party_bytes, page_bytes;
+    int heads, group, causal;
+    int tok0, tok1;                 // the slab
+    fdiv dGroup, dCells;
+    const u64 *q;
+    size_t ld_q;
+    u64 *msg, *opened;              // [2t+1][rows][keys], [rows][keys]
+    row_stat *stats;                // [rows]
+    signed char *weights;           // [n][rows][keys / 64][limb][64]
+    u64 *out, *parts;               // parts [splits][n][rows][dim]
+    size_t rows, keys;
+    int splits, run, tile_rows;
+};
+
+// a sequence's share of the slab: first token, tokens, and the limit of its first token there
+struct seq_span {
+    int first, count, limit, step;  // limit of token first + i: limit + i * step, at least 0
+};
+
+__device__ __forceinline__ seq_span span_of(const attn_args &g, int b)
+{
+    const int s0 = g.s.start[b], s1 = g.s.start[b + 1];
+    const int first = max(s0, g.tok0), last = min(s1, g.tok1);
+    int len = min(g.s.length[b], g.s.max_length);
+    len = max(0, min(len, g.s.max_pages * g.c.page_cells * 16));
+    return {first, max(0, last - first), g.causal ? len - (s1 - first) + 1 : len, g.causal ? 1 : 0};
+}
+__device__ __forceinline__ int limit_at(const seq_span &s, int i) { return max(0, s.limit + i * s.step); }
+
+// tile number -> sequence and first row of the tile (rows of a sequence and kv head: token-major, then the heads of the group);
+// every lane of the wave calls.  -1: no such tile.
+__device__ __forceinline__ int find_tile(const attn_args &g, int tile, int &row0)
+{
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int b0 = 0; b0 < g.s.seqs; b0 += 64) {
+        const int b = b0 + lane;
+        int mine = 0;
+        if (b < g.s.seqs) {
+            const int first = max(g.s.start[b], g.tok0), last = min(g.s.start[b + 1], g.tok1);
+            mine = (max(0, last - first) * g.group + g.tile_rows - 1) / g.tile_rows;
+        }
+        int upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int v = __shfl_up(upto, d);
+            if (lane >= d) upto += v;
+        }
+        const unsigned long long past = __ballot(base + upto > tile);
+        if (past) {
+            const int l = __ffsll((long long)past) - 1;
+            row0 = (tile - base - __shfl(upto - mine, l)) * g.tile_rows;
+            return b0 + l;
+        }
+        base += __shfl(upto, 63);
+    }
+    return -1;
+}
+
+// byte offset of a cell of the context of sequence b in head 0 of party 0 (cells past the table's end and pages outside the cache: some
+// cell of the cache, whose products have weight 0)
+__device__ __forceinline__ size_t cell_at(const attn_args &g, int b, int cell)
+{
+    const int slot = (int)fd_div((u32)cell, g.dCells), in = cell - slot * g.c.page_cells;
+    const int page = g.s.table[(size_t)b * g.s.max_pages + min(slot, g.s.max_pages - 1)];
+    return (size_t)min(max(page, 0), g.c.pages - 1) * g.page_bytes + (size_t)in * g.cell;
+}
+
+template <int NLn>
+__device__ __forceinline__ void clear(v4i (&acc)[NLn])
+{
+#pragma unroll
+    for (int s = 0; s < NLn; s++) acc[s] = (v4i){0, 0, 0, 0};
+}
+
+// Step 1: one workgroup per (tile of 16 MT rows, block of 256 keys, kv head and party).  The digits of the queries lie in LDS in MFMA
+// order, a wave takes a cell of 16 keys at a time straight from the cache.
+template <int MT>
+__global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_params sp)
+{
+    extern __shared__ v4i qd[];                  // [MT][dim / 64][limb][64 lanes]
+    __shared__ u64 mask[16 * MT];
+    __shared__ int rowid[16 * MT];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int head = blockIdx.z / (2 * sp.t + 1), party = blockIdx.z - head * (2 * sp.t + 1);
+    int row0 = 0;
+    const int b = find_tile(g, blockIdx.x, row0);
+    if (b < 0) return;
+    const seq_span s = span_of(g, b);
+    const int nrows = min(16 * MT, s.count * g.group - row0);
+    const int last = (int)fd_div((u32)(row0 + nrows - 1), g.dGroup), lim = limit_at(s, last);
+    const int key0 = blockIdx.y * KEY_BLOCK;
+    if (key0 >= lim) return;
+    const int kb_n = (g.c.dim + 63) / 64;
+    if (tid < 16 * MT) {
+        int id = -1;
+        if (tid < nrows) {
+            const int i = (int)fd_div((u32)(row0 + tid), g.dGroup), h = head * g.group + row0 + tid - i * g.group;
+            id = (s.first + i - g.tok0) * g.heads + h;
+            const u64 row = (u64)(s.first + i) * g.heads + h, counter = ss_counter(row);
+            u64 m = 0;
+            for (int j = sp.t - 1; j >= 0; j--) m = ss_mul_small(ss_add(m, ss_draw_field_at(sp.maskgen_key[j], counter)), party + 1);
+            mask[tid] = ss_add(m, ss_draw_field_at(sp.mask_key, counter));
+        }
+        rowid[tid] = id;
+    }
+    __syncthreads();
+    for (int it = tid; it < MT * 16 * kb_n * 16; it += 256) {
+        const int r = it / (kb_n * 16), d = (it - r * kb_n * 16) * 4, id = rowid[r];
+        u64 y[4] = {0, 0, 0, 0};
+        if (id >= 0 && d < g.c.dim) {
+            const int i = id / g.heads, h = id - i * g.heads;
+            const u64 *src = g.q + ((size_t)party * g.s.tokens + g.tok0 + i) * g.ld_q + (size_t)h * g.c.dim + d;
+#pragma unroll
+            for (int c = 0; c < 4; c++) y[c] = balanced_digits(src[c]);
+        }
+        u32 *dst = reinterpret_cast<u32 *>(qd + (size_t)((r >> 4) * kb_n + (d >> 6)) * TILE + (r & 15) + 16 * ((d & 63) >> 4)) + ((d & 15) >> 2);
+#pragma unroll
+        for (int l = 0; l < NL; l++) dst[l * 256] = limb_dword(y, l);
+    }
+    __syncthreads();
+    const signed char *base = g.c.keys + party * g.party_bytes + head * g.head_bytes;
+    const int groups = g.c.dim >> 4;
+    for (int c = wave; c < KEY_BLOCK / 16; c += 4) {
+        const int cell = key0 / 16 + c;
+        if (cell * 16 >= lim) break;
+        const signed char *src = base + cell_at(g, b, cell) + (lane & 15) * 16;
+        v4i acc[MT][ND];
+#pragma unroll
+        for (int m = 0; m < MT; m++) clear(acc[m]);
+        for (int kb = 0; kb < kb_n; kb++) {
+            v4i k[NL];
+            const int grp = min(kb * 4 + (lane >> 4), groups - 1);   // (past the head the queries' digits are 0)
+#pragma unroll
+            for (int l = 0; l < NL; l++) k[l] = *reinterpret_cast<const v4i *>(src + (size_t)(l * groups + grp) * 256);
+#pragma unroll
+            for (int i = 0; i < NL; i++)
+#pragma unroll
+                for (int m = 0; m < MT; m++) {
+                    const v4i a = qd[(m * kb_n + kb) * TILE + i * 64 + lane];
+#pragma unroll
+                    for (int j = 0; j < NL; j++) acc[m][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, k[j], acc[m][i + j], 0, 0, 0);
+                }
+        }
+#pragma unroll
+        for (int m = 0; m < MT; m++)
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                const int row = m * 16 + 4 * (lane >> 4) + r, id = rowid[row];
+                if (id >= 0)
+                    g.msg[((size_t)party * g.rows + id) * g.keys + cell * 16 + (lane & 15)] = ss_add(fold_diagonals(acc[m], r), mask[row]);
+            }
+    }
+}
+
+__device__ __forceinline__ long long lift(u64 v) { return v <= (SS_P - 1) / 2 ? (long long)v : (long long)v - (long long)SS_P; }
+
+// floor(2^30 2^-x) for the distance `below` >= 0 of a score (2 f fraction bits) from the row's maximum, x in octaves with 16 fraction
+// bits: 2^-x for x in [0, 1) by a polynomial of degree 5 that takes the value 1 at 0 and is off by 2.2e-7 at most, Horner's scheme
+// in 30 fraction bits, each product cut to them
+__device__ __forceinline__ u32 softmax_weight(long long below, const ss_softmax_params &sp)
+{
+    const int h = min(2 * sp.f, 24);
+    const u64 d = min((u64)below >> (2 * sp.f - h), 1ull << 37), u = (d * sp.scale) >> (h + 8);
+    const u32 r = (u32)u << 16;                  // the fraction, 32 bits
+    u32 w = 1077640u;
+    w = 10033292u - __umulhi(w, r);
+    w = 59494488u - __umulhi(w, r);
+    w = 257928559u - __umulhi(w, r);
+    w = 744260865u - __umulhi(w, r);
+    w = 1073741824u - __umulhi(w, r);
+    const u64 octaves = u >> 16;
+    return octaves < 31 ? w >> octaves : 0;
+}
+
+template <typename T, typename F>
+__device__ __forceinline__ T block_reduce(T v, T *lds, F &&op)   // 256 threads; lds [4]
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v = op(v, __shfl_xor(v, d));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return op(op(lds[0], lds[1]), op(lds[2], lds[3]));
+}
+
+__device__ __forceinline__ int sequence_of(const attn_args &g, int token)
+{
+    int lo = 0, hi = g.s.seqs;       // the last b with start[b] <= token
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (g.s.start[mid] <= token) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// Step 2, first half: one workgroup per row opens its scores and finds the maximum and the sum of the weights.
+__global__ __launch_bounds__(BLOCK) void row_kernel(attn_args g, ss_softmax_params sp)
+{
+    __shared__ long long red[4];
+    const int id = blockIdx.x, token = g.tok0 + id / g.heads, b = sequence_of(g, token);
+    const seq_span s = span_of(g, b);
+    const bool member = token >= s.first && token < s.first + s.count;
+    const int limit = member ? limit_at(s, token - s.first) : 0;
+    if (limit == 0) {
+        if (threadIdx.x == 0) g.stats[id] = {0, 0, 0, 0};
+        return;
+    }
+    const int nr = 2 * sp.t + 1;
+    const u64 *msg = g.msg + (size_t)id * g.keys;
+    auto open = [&](int j) {
+        ss_sacc acc;
+        acc.clear();
+        for (int i = 0; i < nr; i++) acc.mac(msg[(size_t)i * g.rows * g.keys + j], sp.ilambda[i]);
+        return acc.value();
+    };
+    u64 *opened = g.opened + (size_t)id * g.keys;
+    const u64 ref = open(0);                     // differences of a row are small, whatever its mask is
+    long long top = -(1ll << 62);
+    for (int j = threadIdx.x; j < limit; j += BLOCK) {
+        const u64 v = open(j);
+        opened[j] = v;
+        top = max(top, lift(ss_sub(v, ref)));
+    }
+    top = block_reduce(top, red, [](long long x, long long y) { return max(x, y); });
+    long long sum = 0;
+    for (int j = threadIdx.x; j < limit; j += BLOCK) sum += softmax_weight(top - lift(ss_sub(opened[j], ref)), sp);
+    sum = block_reduce(sum, red, [](long long x, long long y) { return x + y; });
+    if (threadIdx.x == 0) {
+        const int drop = max(0, 32 - __clzll(sum));
+        g.stats[id] = {ss_add(ref, top < 0 ? SS_P - (u64)(-top) : (u64)top), (1ull << 62) / ((u64)sum >> drop), drop, limit};
+    }
+}
+
+// Step 2, second half: the weights of a row, shared, as digits.  A thread takes four keys.
+template <int N, int T>
+__global__ __launch_bounds__(BLOCK) void weights_kernel(attn_args g, ss_softmax_params sp)
+{
+    const int id = blockIdx.x, i = id / g.heads, h = id - i * g.heads, token = g.tok0 + i, b = sequence_of(g, token);
+    const seq_span s = span_of(g, b);
+    if (token < s.first || token >= s.first + s.count) return;
+    // the products read whole blocks of 64 keys up to the limit of the last row of the tile
+    const int row = (token - s.first) * g.group + h % g.group, end = min((row / g.tile_rows + 1) * g.tile_rows, s.count * g.group);
+    const int lim = limit_at(s, (int)fd_div((u32)(end - 1), g.dGroup)), j0 = (blockIdx.y * BLOCK + threadIdx.x) * 4;
+    if (j0 >= ((lim + 63) & ~63)) return;
+    const row_stat st = g.stats[id];
+    const int n = N ? N : sp.n;
+    u64 y[MAXP<N>][4];
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        const int j = j0 + c;
+        if (j < st.limit) {
+            const u32 w = softmax_weight(lift(ss_sub(st.top, g.opened[(size_t)id * g.keys + j])), sp);
+            const u64 p = ((((u64)w * st.recip) >> 16) + (1ull << (45 - sp.bits + st.drop))) >> (46 - sp.bits + st.drop);
+            const u64 counter = ss_counter(((u64)token * g.heads + h) << 32 | (u32)j);
+            u64 a[T];
+#pragma unroll
+            for (int x = 0; x < T; x++) a[x] = ss_draw_lazy_at(sp.gen_key[x], counter);
+            eval_points<T, MAXP<N>>(p, a, [&](int m, u64 v) { y[m][c] = balanced_digits(v); }, n);
+        } else {
+#pragma unroll
+            for (int m = 0; m < MAXP<N>; m++) y[m][c] = 0;
+        }
+    }
+    signed char *dst = g.weights + (size_t)id * g.keys * NL + (size_t)(j0 >> 6) * (64 * NL) + (j0 & 63);
+#pragma unroll
+    for (int m = 0; m < MAXP<N>; m++)
+        if (N != 0 || m < n) {
+#pragma unroll
+            for (int l = 0; l < NL; l++) *reinterpret_cast<u32 *>(dst + m * g.rows * g.keys * NL + l * 64) = limb_dword(y[m], l);
+        }
+}
+
+// Step 3: one workgroup per (tile of 16 MT rows, run of keys and 64 elements of the head, kv head and party); a wave takes 16 elements.
+template <int MT>
+__global__ __launch_bounds__(256, 2) void values_kernel(attn_args g, int n)
+{
+    __shared__ size_t cells[MAX_RUN / 16];
+    __shared__ int rowid[16 * MT];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int head = blockIdx.z / n, party = blockIdx.z - head * n;
+    const int dblocks = (g.c.dim + 63) / 64, split = blockIdx.y / dblocks, dt = (blockIdx.y - split * dblocks) * 4 + wave;
+    int row0 = 0;
+    const int b = find_tile(g, blockIdx.x, row0);
+    if (b < 0) return;
+    const seq_span s = span_of(g, b);
+    const int nrows = min(16 * MT, s.count * g.group - row0);
+    const int lim = limit_at(s, (int)fd_div((u32)(row0 + nrows - 1), g.dGroup));
+    const int k0 = split * g.run, k1 = min(k0 + g.run, lim);
+    if (split && k0 >= lim) return;              // (the first run writes the zeros of rows that see nothing)
+    for (int c = tid; c < (k1 - k0 + 63) / 64 * 4; c += 256) cells[c] = cell_at(g, b, k0 / 16 + c);
+    if (tid < 16 * MT) {
+        const int r = min(tid, nrows - 1), i = (int)fd_div((u32)(row0 + r), g.dGroup);
+        rowid[tid] = (s.first + i - g.tok0) * g.heads + head * g.group + row0 + r - i * g.group;
+    }
+    __syncthreads();
+    if (dt * 16 >= g.c.dim) return;
+    const signed char *base = g.c.values + party * g.party_bytes + head * g.head_bytes + (dt * 16 + (lane & 15)) * 16;
+    const signed char *wrow[MT];
+    v4i acc[MT][ND];
+#pragma unroll
+    for (int m = 0; m < MT; m++) {
+        clear(acc[m]);
+        wrow[m] = g.weights + ((size_t)party * g.rows + rowid[m * 16 + (lane & 15)]) * g.keys * NL + (lane >> 4) * 16;
+    }
+    const size_t limb = (size_t)g.c.dim * 16;
+    for (int kb = k0 / 64; kb * 64 < k1; kb++) {
+        const signed char *src = base + cells[kb * 4 - k0 / 16 + (lane >> 4)];
+        v4i v[NL];
+#pragma unroll
+        for (int l = 0; l < NL; l++) v[l] = *reinterpret_cast<const v4i *>(src + l * limb);
+#pragma unroll
+        for (int i = 0; i < NL; i++)
+#pragma unroll
+            for (int m = 0; m < MT; m++) {
+                const v4i a = *reinterpret_cast<const v4i *>(wrow[m] + (size_t)kb * (64 * NL) + i * 64);
+#pragma unroll
+                for (int j = 0; j < NL; j++) acc[m][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, v[j], acc[m][i + j], 0, 0, 0);
+            }
+    }
+#pragma unroll
+    for (int m = 0; m < MT; m++)
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            const int row = m * 16 + 4 * (lane >> 4) + r;
+            if (row >= nrows) continue;
+            const size_t id = rowid[row], d = dt * 16 + (lane & 15);
+            const u64 o = fold_diagonals(acc[m], r);
+            if (g.splits == 1)
+                g.out[((size_t)party * g.s.tokens * g.heads + (size_t)g.tok0 * g.heads + id) * g.c.dim + d] = o;
+            else
+                g.parts[(((size_t)split * n + party) * g.rows + id) * g.c.dim + d] = o;
+        }
+}
+
+// the runs of a row added up
+__global__ __launch_bounds__(BLOCK) void join_kernel(attn_args g, int n)
+{
+    const int id = blockIdx.x, party = blockIdx.y, limit = g.stats[id].limit;
+    const int token = g.tok0 + id / g.heads;
+    if (token < g.s.start[0] || token >= g.s.start[g.s.seqs]) return;
+    for (int d = threadIdx.x; d < g.c.dim; d += BLOCK) {
+        u64 o = 0;
+        for (int s = 0; s * g.run < limit; s++) o = ss_add(o, g.parts[(((size_t)s * n + party) * g.rows + id) * g.c.dim + d]);
+        g.out[((size_t)party * g.s.tokens * g.heads + (size_t)g.tok0 * g.heads + id) * g.c.dim + d] = o;
+    }
+}
+
+rotary_shape make_shape(int tokens, int heads, int dim, int rot)
+{
+    const int width = dim - rot / 2;
+    return {tokens, heads, dim, width, make_fdiv((u32)width), make_fdiv((u32)heads)};
+}
+
+size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
+
+}  // namespace
+
+hipError_t ss_launch_rotary(const u64 *x, size_t ld, u64 *u, u64 *wsh, u64 *out, int tokens, int heads, int dim, const ss_rope &rope,
+                            const ss_tr_params &tp, hipStream_t stream)
+{
+    const rotary_shape g = make_shape(tokens, heads, dim, rope.rot);
+    const dim3 grid(ceil_div((size_t)tokens * heads * g.width, BLOCK));
+#define SS_LAUNCH(NC, TC) hipLaunchKernelGGL((rotary_kernel<NC, TC>), grid, dim3(BLOCK), 0, stream, x, ld, u, wsh, out, g, rope, tp)
+    SS_SCHEME(tp.n, tp.t, SS_LAUNCH);
+#undef SS_LAUNCH
+    return hipGetLastError();
+}
+
+hipError_t ss_launch_append(const ss_paged &c, const u64 *k, size_t ld_k, const u64 *v, size_t ld_v, int tokens, const long long *slots,
+                            u64 *u, u64 *wsh, const ss_rope &rope, const ss_tr_params &tp, hipStream_t stream)
+{
+    append_shape s = {};
+    s.r = make_shape(tokens, c.kv, c.dim, rope.rot);
+    s.slots = slots;
+    s.keys = c.keys;
+    s.values = c.values;
+    s.head = (size_t)c.page_cells * (SS_NLIMB * 16) * c.dim;
+    s.party = s.head * c.kv;
+    s.page = s.party * tp.n;
+    s.page_size = (unsigned)c.page_cells * 16;
+    s.capacity = s.page_size * (unsigned)c.pages;
+    s.dPage = make_fdiv(s.page_size);
+    const unsigned key_blocks = ceil_div((size_t)tokens * c.kv * s.r.width, BLOCK);
+    const dim3 grid(key_blocks + ceil_div((size_t)tokens * c.kv * c.dim, BLOCK));
+#define SS_LAUNCH(NC, TC) \
+    hipLaunchKernelGGL((append_kernel<NC, TC>), grid, dim3(BLOCK), 0, stream, k, ld_k, v, ld_v, u, wsh, s, rope, tp, key_blocks)
+    SS_SCHEME(tp.n, tp.t, SS_LAUNCH);
+#undef SS_LAUNCH
+    return hipGetLastError();
+}
+
+attention_plan plan_attention(int n, int t, int tokens, int seqs, int heads, int kv, int dim, int max_length, size_t room)
+{
+    attention_plan p = {};
+    const size_t group = heads / kv, nr = 2 * t + 1;
+    p.row_tiles = ceil_div(tokens, seqs) * group > 16 ? 2 : 1;
+    p.keys = ((size_t)max_length + 63) & ~(size_t)63;
+    p.slab = tokens;
+    for (;;) {
+        const size_t tile = 16 * p.row_tiles, tiles = p.slab * group / tile + seqs;
+        const size_t base = tiles * ceil_div(dim, 64) * kv * n;
+        const size_t wanted = base >= 1024 ? 1 : ceil_div(1024, base);
+        p.run = (int)((ceil_div(p.keys, wanted) + 63) & ~63u);
+        if (p.run > MAX_RUN) p.run = MAX_RUN;
+        if (p.run < KEY_BLOCK) p.run = KEY_BLOCK;
+        p.splits = (int)ceil_div(p.keys, p.run);
+        p.rows = (size_t)p.slab * heads;
+        p.bytes = align256((nr + 1) * p.rows * p.keys * 8) + align256(p.rows * sizeof(row_stat)) + align256((size_t)n * p.rows * p.keys * NL) +
+                  (p.splits > 1 ? align256((size_t)p.splits * n * p.rows * dim * 8) : 0);
+        if (p.bytes <= room && p.rows <= MAX_ROWS) return p;
+        if (p.slab == 1) break;
+        p.slab = (p.slab + 1) / 2;
+    }
+    p.slab = 0;
+    return p;
+}
+
+hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache, const ss_sequences &seqs, const u64 *q, size_t ld_q, int heads,
+                               int causal, const ss_softmax_params &sp, void *room, u64 *out, hipStream_t stream)
+{
+    attn_args g = {};
+    g.c = cache;
+    g.s = seqs;
+    g.cell = (size_t)NL * 16 * cache.dim;
+    g.head_bytes = g.cell * cache.page_cells;
+    g.party_bytes = g.head_bytes * cache.kv;
+    g.page_bytes = g.party_bytes * sp.n;
+    g.heads = heads;
+    g.group = heads / cache.kv;
+    g.causal = causal;
+    g.dGroup = make_fdiv((u32)g.group);
+    g.dCells = make_fdiv((u32)cache.page_cells);
+    g.q = q;
+    g.ld_q = ld_q;
+    g.rows = plan.rows;
+    g.keys = plan.keys;
+    g.splits = plan.splits;
+    g.run = plan.run;
+    g.tile_rows = 16 * plan.row_tiles;
+    const int nr = 2 * sp.t + 1, n = sp.n;
+    char *at = (char *)room;
+    g.msg = (u64 *)at;
+    g.opened = g.msg + (size_t)nr * g.rows * g.keys;
+    at += align256((size_t)(nr + 1) * g.rows * g.keys * 8);
+    g.stats = (row_stat *)at;
+    at += align256(g.rows * sizeof(row_stat));
+    g.weights = (signed char *)at;
+    at += align256((size_t)n * g.rows * g.keys * NL);
+    g.parts = (u64 *)at;
+    g.out = out;
+    const int dblocks = (cache.dim + 63) / 64;
+    const size_t lds = (size_t)plan.row_tiles * dblocks * TILE * 16;
+    if (lds > 48 * 1024) {
+        const void *scores = plan.row_tiles == 1 ? (const void *)scores_kernel<1> : (const void *)scores_kernel<2>;
+        if (hipError_t e = hipFuncSetAttribute(scores, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); e != hipSuccess) return e;
+    }
+    for (int tok = 0; tok < seqs.tokens; tok += plan.slab) {
+        g.tok0 = tok;
+        g.tok1 = min(seqs.tokens, tok + plan.slab);
+        const int rows = (g.tok1 - tok) * heads;
+        const unsigned tiles = (unsigned)((size_t)(g.tok1 - tok) * g.group / g.tile_rows + seqs.seqs);
+        const dim3 sgrid(tiles, ceil_div(plan.keys, KEY_BLOCK), cache.kv * nr), vgrid(tiles, plan.splits * dblocks, cache.kv * n);
+        const dim3 wgrid(rows, ceil_div(plan.keys, BLOCK * 4));
+        if (plan.row_tiles == 1)
+            hipLaunchKernelGGL((scores_kernel<1>), sgrid, dim3(256), lds, stream, g, sp);
+        else
+            hipLaunchKernelGGL((scores_kernel<2>), sgrid, dim3(256), lds, stream, g, sp);
+        hipLaunchKernelGGL(row_kernel, dim3(rows), dim3(BLOCK), 0, stream, g, sp);
+#define SS_LAUNCH(NC, TC) hipLaunchKernelGGL((weights_kernel<NC, TC>), wgrid, dim3(BLOCK), 0, stream, g, sp)
+        SS_SCHEME(sp.n, sp.t, SS_LAUNCH);
+#undef SS_LAUNCH
+        if (plan.row_tiles == 1)
+            hipLaunchKernelGGL((values_kernel<1>), vgrid, dim3(256), 0, stream, g, n);
+        else
+            hipLaunchKernelGGL((values_kernel<2>), vgrid, dim3(256), 0, stream, g, n);
+        if (plan.splits > 1) hipLaunchKernelGGL(join_kernel, dim3(rows, n), dim3(BLOCK), 0, stream, g, n);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace SS_NS

@@ -221,4 +221,57 @@ hipError_t ss_launch_gemm_images(const product_plan &plan, const void *packedW, 
                                  int W, int Co, int kh, int kw, int stride, int pad, int Ho, int Wo, hipStream_t stream,
                                  hipEvent_t started = nullptr, hipEvent_t stopped = nullptr);
 
+// ---- attention over a paged cache (attention_kernels.hip) ----
+// rotary positions: cosines and sines [positions][rot / 2][2], the row of every token
+struct ss_rope {
+    const int2 *table;
+    const int *pos;
+    int positions, rot, interleaved;
+};
+
+// A paged cache: pages of `page_cells` cells of 16 keys, a cell the balanced digits of one head of one party:
+//   keys   [page][party][head][cell][limb][dim / 16][16 keys][16 elements] int8
+//   values [page][party][head][cell][limb][dim][16 keys] int8
+struct ss_paged {
+    signed char *keys, *values;
+    int pages, page_cells, kv, dim;
+};
+
+// new tokens of several sequences (start [seqs + 1]), the pages of their contexts [seqs][max_pages] and how long these are
+struct ss_sequences {
+    const int *start, *table, *length;
+    int seqs, tokens, max_pages, max_length;
+};
+
+struct ss_softmax_params {        // masked opening of the scores and sharing of the weights
+    int n, t;
+    int f;                        // a score has 2 f fraction bits
+    u32 scale;                    // its factor times log2 e, 24 fraction bits
+    int bits;                     // fraction bits of the weights
+    u64 mask_key, maskgen_key[SS_MAXT], gen_key[SS_MAXT];
+    int ilambda[2 * SS_MAXT + 1]; // REC from the IDs 1..2t+1
+};
+
+// how a call over `tokens` tokens is cut up: into slabs of tokens whose messages fit the room it has; the contraction of the values
+// into `splits` runs of `run` keys, with a plane of their own each where there are several
+struct attention_plan {
+    int row_tiles;                // of 16 rows to a workgroup
+    int slab;                     // tokens, 0: the room is too small
+    int splits, run;
+    size_t keys;                  // of a row in the messages: the longest context in whole blocks of 64
+    size_t rows, bytes;           // of a slab
+};
+attention_plan plan_attention(int n, int t, int tokens, int seqs, int heads, int kv, int dim, int max_length, size_t room);
+
+// x [n][tokens][ld] (heads x dim of every token) rotated and truncated -> out [n][tokens][heads][dim]; messages u [k][count],
+// wsh [n][count], count = tokens * heads * rot
+hipError_t ss_launch_rotary(const u64 *x, size_t ld, u64 *u, u64 *wsh, u64 *out, int tokens, int heads, int dim, const ss_rope &rope,
+                            const ss_tr_params &tp, hipStream_t stream);
+// rope.rot = 0: keys as they are (no messages)
+hipError_t ss_launch_append(const ss_paged &cache, const u64 *k, size_t ld_k, const u64 *v, size_t ld_v, int tokens, const long long *slots,
+                            u64 *u, u64 *wsh, const ss_rope &rope, const ss_tr_params &tp, hipStream_t stream);
+// room: plan.bytes bytes for what the launches hand on
+hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache, const ss_sequences &seqs, const u64 *q, size_t ld_q, int heads,
+                               int causal, const ss_softmax_params &sp, void *room, u64 *out, hipStream_t stream);
+
 }  // namespace SS_NS

@@ -1224,6 +1224,142 @@ uint64_t ssnet_rng_draw(uint64_t key, uint64_t e) { return ss_draw(key, e); }
 
 uint64_t ssnet_rng_field(uint64_t key, uint64_t e) { return ss_draw_field(key, e); }
 
+namespace {
+
+static bool rotary_ok(const ssnet_rotary *r, int head_dim)
+{
+    return r->d_table && r->d_pos && !((uintptr_t)r->d_table & 7) && !((uintptr_t)r->d_pos & 3) && r->positions >= 1 && r->rot >= 2 &&
+           r->rot <= head_dim && r->rot % 2 == 0;
+}
+
+static ss_rope make_rope(const ssnet_rotary *r)
+{
+    return r ? ss_rope{(const int2 *)r->d_table, r->d_pos, r->positions, r->rot, r->interleaved ? 1 : 0} : ss_rope{};
+}
+
+// elements of a tensor of heads: the kernels count them in 31 bits
+static bool heads_ok(int tokens, int heads, int dim, size_t ld)
+{
+    return tokens >= 1 && heads >= 1 && dim >= 1 && (double)tokens * heads * dim < 2147483648.0 && ld >= (size_t)heads * dim &&
+           ld <= MAX_COUNT / tokens;
+}
+
+// bytes from the first element of a tensor of heads to the end of its last
+static size_t heads_bytes(const ssnet_ctx *ctx, int tokens, int heads, int dim, size_t ld)
+{
+    return (((size_t)ctx->n * tokens - 1) * ld + (size_t)heads * dim) * 8;
+}
+
+// bytes of the workspace behind the header and in front of a pending product, which the calls below leave as it is
+static size_t scratch_room(const ssnet_ctx *ctx)
+{
+    if (!ws_fits(ctx, 0)) return 0;
+    return ctx->pending.on ? (size_t)((char *)ctx->pending.base - ws_scratch(ctx)) : ctx->ws_bytes - WS_HEADER_BYTES;
+}
+
+// the messages of a truncation of the turned elements: [k][count], [n][count]
+static int rotary_messages(const ssnet_ctx *ctx, int tokens, int heads, const ssnet_rotary *r, u64 **u, u64 **wsh)
+{
+    const size_t count = r ? (size_t)tokens * heads * r->rot : 0;
+    if (r && scratch_room(ctx) < ((size_t)ctx->t + 1 + ctx->n) * count * 8) return SSNET_EWORKSPACE;
+    *u = r ? (u64 *)ws_scratch(ctx) : nullptr;
+    *wsh = r ? *u + (size_t)(ctx->t + 1) * count : nullptr;
+    return SSNET_OK;
+}
+
+static bool cache_ok(const ssnet_paged_cache *c, bool pointers)
+{
+    if (!c || c->page_size < 16 || c->page_size % 16 || c->page_size > (1 << 20) || c->heads < 1 || c->heads > 4096 || c->head_dim < 16 ||
+        c->head_dim % 16 || c->head_dim > SSNET_MAX_HEAD_DIM)
+        return false;
+    if (!pointers) return true;
+    return c->pages >= 1 && (long)c->pages * c->page_size < (1L << 31) && c->d_keys && c->d_values && !((uintptr_t)c->d_keys & 15) &&
+           !((uintptr_t)c->d_values & 15);
+}
+
+static ss_paged make_paged(const ssnet_paged_cache *c)
+{
+    return {(signed char *)c->d_keys, (signed char *)c->d_values, c->pages, c->page_size / 16, c->heads, c->head_dim};
+}
+
+static bool attention_ok(const ssnet_paged_cache *c, int sequences, int tokens, int heads, int max_length)
+{
+    return sequences >= 1 && sequences <= (1 << 20) && tokens >= 1 && heads >= 1 && heads % c->heads == 0 &&
+           (double)tokens * heads * c->head_dim < 2147483648.0 && max_length >= 1 && max_length <= SSNET_MAX_CONTEXT;
+}
+
+}  // namespace
+
+int ssnet_rotary_truncate(ssnet_ctx *ctx, const uint64_t *d_x, size_t ld, int tokens, int heads, int head_dim, const ssnet_rotary *rotary,
+                          uint64_t stream_id, uint64_t *d_out)
+{
+    if (!ctx || !d_x || !rotary || !d_out || !heads_ok(tokens, heads, head_dim, ld) || !rotary_ok(rotary, head_dim)) return SSNET_EINVAL;
+    const size_t in = heads_bytes(ctx, tokens, heads, head_dim, ld), size = (size_t)ctx->n * tokens * heads * head_dim * 8;
+    if (overlap(d_x, in, d_out, size) && !(d_x == d_out && ld == (size_t)heads * head_dim)) return SSNET_EINVAL;
+    u64 *u, *wsh;
+    if (int rc = rotary_messages(ctx, tokens, heads, rotary, &u, &wsh)) return rc;
+    timed tm(ctx, SSNET_PROF_TRUNCATE);
+    hipError_t e = ss_launch_rotary(d_x, ld, u, wsh, d_out, tokens, heads, head_dim, make_rope(rotary), make_tr_params(ctx, stream_id), ctx->stream);
+    return e == hipSuccess ? SSNET_OK : fail_hip(ctx, e);
+}
+
+size_t ssnet_cache_page_bytes(const ssnet_ctx *ctx, int page_size, int heads, int head_dim)
+{
+    const ssnet_paged_cache c = {nullptr, nullptr, 1, page_size, heads, head_dim};
+    return ctx && cache_ok(&c, false) ? (size_t)ctx->n * heads * page_size * head_dim * SS_NLIMB : 0;
+}
+
+int ssnet_cache_append(ssnet_ctx *ctx, const ssnet_paged_cache *cache, const uint64_t *d_k, size_t ld_k, const uint64_t *d_v, size_t ld_v,
+                       int tokens, const int64_t *d_slots, const ssnet_rotary *rotary, uint64_t stream_id)
+{
+    if (!ctx || !cache_ok(cache, true) || !d_k || !d_v || !d_slots) return SSNET_EINVAL;
+    if (!heads_ok(tokens, cache->heads, cache->head_dim, ld_k) || !heads_ok(tokens, cache->heads, cache->head_dim, ld_v)) return SSNET_EINVAL;
+    if (rotary && !rotary_ok(rotary, cache->head_dim)) return SSNET_EINVAL;
+    u64 *u, *wsh;
+    if (int rc = rotary_messages(ctx, tokens, cache->heads, rotary, &u, &wsh)) return rc;
+    timed tm(ctx, SSNET_PROF_PACK_X);
+    hipError_t e = ss_launch_append(make_paged(cache), d_k, ld_k, d_v, ld_v, tokens, (const long long *)d_slots, u, wsh, make_rope(rotary),
+                                    make_tr_params(ctx, stream_id), ctx->stream);
+    return e == hipSuccess ? SSNET_OK : fail_hip(ctx, e);
+}
+
+size_t ssnet_workspace_bytes_attention(const ssnet_ctx *ctx, const ssnet_paged_cache *cache, int sequences, int tokens, int heads, int max_length)
+{
+    if (!ctx || !cache_ok(cache, false) || !attention_ok(cache, sequences, tokens, heads, max_length)) return 0;
+    return WS_HEADER_BYTES + plan_attention(ctx->n, ctx->t, tokens, sequences, heads, cache->heads, cache->head_dim, max_length, SIZE_MAX).bytes;
+}
+
+int ssnet_paged_attention(ssnet_ctx *ctx, const ssnet_paged_cache *cache, const ssnet_sequences *seqs, const uint64_t *d_q, size_t ld_q, int heads,
+                          uint32_t scale, int weight_bits, int causal, uint64_t stream_id, uint64_t *d_out)
+{
+    if (!ctx || !cache_ok(cache, true) || !seqs || !d_q || !d_out) return SSNET_EINVAL;
+    if (!attention_ok(cache, seqs->sequences, seqs->tokens, heads, seqs->max_length)) return SSNET_EINVAL;
+    if (!heads_ok(seqs->tokens, heads, cache->head_dim, ld_q)) return SSNET_EINVAL;
+    if (!seqs->d_start || !seqs->d_table || !seqs->d_length || seqs->max_pages < 1) return SSNET_EINVAL;
+    if (scale < (1u << 16) || scale >= (1u << 26) || weight_bits < 8 || weight_bits > 30) return SSNET_EINVAL;
+    const size_t out = (size_t)ctx->n * seqs->tokens * heads * cache->head_dim * 8;
+    if (overlap(d_q, heads_bytes(ctx, seqs->tokens, heads, cache->head_dim, ld_q), d_out, out)) return SSNET_EINVAL;
+    const attention_plan plan = plan_attention(ctx->n, ctx->t, seqs->tokens, seqs->sequences, heads, cache->heads, cache->head_dim, seqs->max_length,
+                                               scratch_room(ctx));
+    if (!plan.slab) return SSNET_EWORKSPACE;
+    ss_softmax_params sp = {};
+    sp.n = ctx->n;
+    sp.t = ctx->t;
+    sp.f = ctx->f;
+    sp.scale = scale;
+    sp.bits = weight_bits;
+    sp.mask_key = ss_key(ctx->seed, SSNET_DOM_ROW_MASK, stream_id, 0, 0);
+    for (int j = 1; j <= ctx->t; j++) {
+        sp.maskgen_key[j - 1] = ss_key(ctx->seed, SSNET_DOM_ROWMASK_GEN, stream_id, 0, (u64)j);
+        sp.gen_key[j - 1] = ss_key(ctx->seed, SSNET_DOM_WEIGHT_GEN, stream_id, 0, (u64)j);
+    }
+    for (int i = 0; i < 2 * ctx->t + 1; i++) sp.ilambda[i] = ctx->ilambda_r[i];
+    const ss_sequences s = {seqs->d_start, seqs->d_table, seqs->d_length, seqs->sequences, seqs->tokens, seqs->max_pages, seqs->max_length};
+    timed tm(ctx, SSNET_PROF_GEMM);
+    hipError_t e = ss_launch_attention(plan, make_paged(cache), s, d_q, ld_q, heads, causal, sp, ws_scratch(ctx), d_out, ctx->stream);
+    return e == hipSuccess ? SSNET_OK : fail_hip(ctx, e);
+}
+
 int ssnet_host_lagrange(const ssnet_ctx *ctx, const int *party_ids, int m, uint64_t *out)
 {
     if (!ctx || !party_ids || !out || m < 1 || m > ctx->n) return SSNET_EINVAL;
