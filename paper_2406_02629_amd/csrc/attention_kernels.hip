@@ -19,8 +19,8 @@ namespace SS_NS {
 namespace {
 
 constexpr int BLOCK = 256;
-constexpr int KEY_BLOCK = 256;      // keys of a workgroup of the scores
 constexpr size_t MAX_ROWS = (size_t)1 << 22;   // of a slab: a workgroup each, less than 2^32 threads in a launch
+constexpr size_t SHORT_ROW = 4096;   // keys up to which one workgroup takes the softmax of a row
 constexpr int MAX_RUN = 16320;      // keys that the 32-bit sums of the values can take, in blocks of 64: 8 * 16383 * 2^14 < 2^31
 
 inline unsigned ceil_div(size_t a, size_t b) { return (unsigned)((a + b - 1) / b); }
@@ -214,28 +214,22 @@ __global__ __launch_bounds__(BLOCK) void append_kernel(const u64 *k, size_t ld_k
 
 // ------------------------------------------------------------------ attention
 
-struct row_stat {
-    u64 top;        // opened score (with the row's mask) of the largest
-    u64 recip;      // reciprocal of the sum of the weights, 0 for a row that sees nothing
-    int drop;       // bits that the sum is shifted by
-    int limit;      // keys that the row sees
-};
-
 struct attn_args {
     ss_paged c;
     ss_sequences s;
     size_t cell, head_bytes, party_bytes, page_bytes;
     int heads, group, causal;
     int tok0, tok1;                 // the slab
-    fdiv dGroup, dCells;
+    fdiv dGroup, dCells, dHeads;
     const u64 *q;
     size_t ld_q;
     u64 *msg, *opened;              // [2t+1][rows][keys], [rows][keys]
-    row_stat *stats;                // [rows]
+    u64 *tops, *sums;               // [rows][keys / 1024]: of long rows
     signed char *weights;           // [n][rows][keys / 64][limb][64]
     u64 *out, *parts;               // parts [splits][n][rows][dim]
     size_t rows, keys;
-    int splits, run, tile_rows;
+    int splits, run, tile_rows, key_block, dblocks;
+    u32 rows_now;                   // of this slab: the last may be smaller
 };
 
 // a sequence's share of the slab: first token, tokens, and the limit of its first token there
@@ -299,31 +293,50 @@ __device__ __forceinline__ void clear(v4i (&acc)[NLn])
     for (int s = 0; s < NLn; s++) acc[s] = (v4i){0, 0, 0, 0};
 }
 
-// Step 1: one workgroup per (tile of 16 MT rows, block of 256 keys, kv head and party).  The digits of the queries lie in LDS in MFMA
-// order, a wave takes a cell of 16 keys at a time straight from the cache.
+// Step 1: one workgroup per (tile of 16 MT rows, block of g.key_block keys, kv head and party).  The digits of the queries lie in LDS in
+// MFMA order; a wave takes a cell of 16 keys at a time straight from the cache, the next 64 elements of a cell (or the next cell's first)
+// on their way while those at hand are multiplied.
 template <int MT>
 __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_params sp)
 {
     extern __shared__ v4i qd[];                  // [MT][dim / 64][limb][64 lanes]
     __shared__ u64 mask[16 * MT];
     __shared__ int rowid[16 * MT];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ size_t rowat[16 * MT];            // of the row's query in q
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int head = blockIdx.z / (2 * sp.t + 1), party = blockIdx.z - head * (2 * sp.t + 1);
     int row0 = 0;
-    const int b = find_tile(g, blockIdx.x, row0);
+    const int b = __builtin_amdgcn_readfirstlane(find_tile(g, blockIdx.x, row0));
     if (b < 0) return;
+    row0 = __builtin_amdgcn_readfirstlane(row0);
     const seq_span s = span_of(g, b);
     const int nrows = min(16 * MT, s.count * g.group - row0);
     const int last = (int)fd_div((u32)(row0 + nrows - 1), g.dGroup), lim = limit_at(s, last);
-    const int key0 = blockIdx.y * KEY_BLOCK;
+    const int key0 = blockIdx.y * g.key_block;
     if (key0 >= lim) return;
-    const int kb_n = (g.c.dim + 63) / 64;
+    const int kb_n = (g.c.dim + 63) / 64, groups = g.c.dim >> 4;
+    const int cell_end = min(key0 + g.key_block, lim + 15) >> 4;
+    int cell = (key0 >> 4) + wave;
+    // (elements past the head's end: those of its last 16 again, the queries' digits are 0 there)
+    const signed char *base = g.c.keys + party * g.party_bytes + head * g.head_bytes + (lane & 15) * 16;
+    auto load = [&](size_t at, int kb, v4i (&k)[NL]) {
+        const signed char *src = base + at + (size_t)min(kb * 4 + (lane >> 4), groups - 1) * 256;
+#pragma unroll
+        for (int l = 0; l < NL; l++) k[l] = *reinterpret_cast<const v4i *>(src + (size_t)(l * groups) * 256);
+    };
+    v4i k[NL], next[NL];
+    size_t at = 0;
+    if (cell < cell_end) {
+        at = cell_at(g, b, cell);
+        load(at, 0, k);
+    }
     if (tid < 16 * MT) {
         int id = -1;
         if (tid < nrows) {
             const int i = (int)fd_div((u32)(row0 + tid), g.dGroup), h = head * g.group + row0 + tid - i * g.group;
             id = (s.first + i - g.tok0) * g.heads + h;
-            const u64 row = (u64)(s.first + i) * g.heads + h, counter = ss_counter(row);
+            rowat[tid] = ((size_t)party * g.s.tokens + s.first + i) * g.ld_q + (size_t)h * g.c.dim;
+            const u64 counter = ss_counter((u64)(s.first + i) * g.heads + h);
             u64 m = 0;
             for (int j = sp.t - 1; j >= 0; j--) m = ss_mul_small(ss_add(m, ss_draw_field_at(sp.maskgen_key[j], counter)), party + 1);
             mask[tid] = ss_add(m, ss_draw_field_at(sp.mask_key, counter));
@@ -332,33 +345,28 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
     }
     __syncthreads();
     for (int it = tid; it < MT * 16 * kb_n * 16; it += 256) {
-        const int r = it / (kb_n * 16), d = (it - r * kb_n * 16) * 4, id = rowid[r];
+        // four consecutive elements of row r; 16 lanes take 64 elements, so that a wave reads 512 consecutive bytes of a row
+        const int r = (it >> 4) & (16 * MT - 1), kb = it / (16 * MT * 16), d = kb * 64 + (it & 15) * 4;
         u64 y[4] = {0, 0, 0, 0};
-        if (id >= 0 && d < g.c.dim) {
-            const int i = id / g.heads, h = id - i * g.heads;
-            const u64 *src = g.q + ((size_t)party * g.s.tokens + g.tok0 + i) * g.ld_q + (size_t)h * g.c.dim + d;
+        if (r < nrows && d < g.c.dim) {
+            const u64 *src = g.q + rowat[r] + d;
 #pragma unroll
             for (int c = 0; c < 4; c++) y[c] = balanced_digits(src[c]);
         }
-        u32 *dst = reinterpret_cast<u32 *>(qd + (size_t)((r >> 4) * kb_n + (d >> 6)) * TILE + (r & 15) + 16 * ((d & 63) >> 4)) + ((d & 15) >> 2);
+        u32 *dst = reinterpret_cast<u32 *>(qd + (size_t)((r >> 4) * kb_n + kb) * TILE + (r & 15) + 16 * ((d & 63) >> 4)) + ((d & 15) >> 2);
 #pragma unroll
         for (int l = 0; l < NL; l++) dst[l * 256] = limb_dword(y, l);
     }
     __syncthreads();
-    const signed char *base = g.c.keys + party * g.party_bytes + head * g.head_bytes;
-    const int groups = g.c.dim >> 4;
-    for (int c = wave; c < KEY_BLOCK / 16; c += 4) {
-        const int cell = key0 / 16 + c;
-        if (cell * 16 >= lim) break;
-        const signed char *src = base + cell_at(g, b, cell) + (lane & 15) * 16;
+    for (; cell < cell_end; cell += 4) {
+        const bool more = cell + 4 < cell_end;
+        const size_t at_next = more ? cell_at(g, b, cell + 4) : 0;
         v4i acc[MT][ND];
 #pragma unroll
         for (int m = 0; m < MT; m++) clear(acc[m]);
         for (int kb = 0; kb < kb_n; kb++) {
-            v4i k[NL];
-            const int grp = min(kb * 4 + (lane >> 4), groups - 1);   // (past the head the queries' digits are 0)
-#pragma unroll
-            for (int l = 0; l < NL; l++) k[l] = *reinterpret_cast<const v4i *>(src + (size_t)(l * groups + grp) * 256);
+            if (kb + 1 < kb_n) load(at, kb + 1, next);
+            else if (more) load(at_next, 0, next);
 #pragma unroll
             for (int i = 0; i < NL; i++)
 #pragma unroll
@@ -367,7 +375,10 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
 #pragma unroll
                     for (int j = 0; j < NL; j++) acc[m][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, k[j], acc[m][i + j], 0, 0, 0);
                 }
+#pragma unroll
+            for (int l = 0; l < NL; l++) k[l] = next[l];
         }
+        at = at_next;
 #pragma unroll
         for (int m = 0; m < MT; m++)
 #pragma unroll
@@ -420,75 +431,79 @@ __device__ __forceinline__ int sequence_of(const attn_args &g, int token)
     return lo;
 }
 
-// Step 2, first half: one workgroup per row opens its scores and finds the maximum and the sum of the weights.
-__global__ __launch_bounds__(BLOCK) void row_kernel(attn_args g, ss_softmax_params sp)
+// where a row stands: its place in the slab, its token and head, the keys it sees, and those that the products read of its tile
+struct row_place {
+    int id, token, head, limit, covered;
+};
+
+__device__ __forceinline__ bool row_at(const attn_args &g, int id, row_place &r)
 {
-    __shared__ long long red[4];
-    const int id = blockIdx.x, token = g.tok0 + id / g.heads, b = sequence_of(g, token);
+    const int i = (int)fd_div((u32)id, g.dHeads), token = g.tok0 + i, b = sequence_of(g, token), head = id - i * g.heads;
     const seq_span s = span_of(g, b);
-    const bool member = token >= s.first && token < s.first + s.count;
-    const int limit = member ? limit_at(s, token - s.first) : 0;
-    if (limit == 0) {
-        if (threadIdx.x == 0) g.stats[id] = {0, 0, 0, 0};
-        return;
-    }
-    const int nr = 2 * sp.t + 1;
-    const u64 *msg = g.msg + (size_t)id * g.keys;
-    auto open = [&](int j) {
-        ss_sacc acc;
-        acc.clear();
-        for (int i = 0; i < nr; i++) acc.mac(msg[(size_t)i * g.rows * g.keys + j], sp.ilambda[i]);
-        return acc.value();
-    };
-    u64 *opened = g.opened + (size_t)id * g.keys;
-    const u64 ref = open(0);                     // differences of a row are small, whatever its mask is
-    long long top = -(1ll << 62);
-    for (int j = threadIdx.x; j < limit; j += BLOCK) {
-        const u64 v = open(j);
-        opened[j] = v;
-        top = max(top, lift(ss_sub(v, ref)));
-    }
-    top = block_reduce(top, red, [](long long x, long long y) { return max(x, y); });
-    long long sum = 0;
-    for (int j = threadIdx.x; j < limit; j += BLOCK) sum += softmax_weight(top - lift(ss_sub(opened[j], ref)), sp);
-    sum = block_reduce(sum, red, [](long long x, long long y) { return x + y; });
-    if (threadIdx.x == 0) {
-        const int drop = max(0, 32 - __clzll(sum));
-        g.stats[id] = {ss_add(ref, top < 0 ? SS_P - (u64)(-top) : (u64)top), (1ull << 62) / ((u64)sum >> drop), drop, limit};
-    }
+    if (token < s.first || token >= s.first + s.count) return false;
+    const int at = token - s.first, in_group = head - (int)fd_div((u32)head, g.dGroup) * g.group;
+    const int row = at * g.group + in_group, end = min((row | (g.tile_rows - 1)) + 1, s.count * g.group);
+    r = {id, token, head, limit_at(s, at), (limit_at(s, (int)fd_div((u32)(end - 1), g.dGroup)) + 63) & ~63};
+    return true;
 }
 
-// Step 2, second half: the weights of a row, shared, as digits.  A thread takes four keys.
-template <int N, int T>
-__global__ __launch_bounds__(BLOCK) void weights_kernel(attn_args g, ss_softmax_params sp)
+// Step 2, what the elite party reconstructs: four scores of a row from those of the parties 1..2t+1 (keys from j on, all loads in flight
+// together; places beyond the limit hold anything)
+template <int T>
+__device__ __forceinline__ void open_scores(const attn_args &g, const ss_softmax_params &sp, const row_place &r, int j, u64 (&v)[4])
 {
-    const int id = blockIdx.x, i = id / g.heads, h = id - i * g.heads, token = g.tok0 + i, b = sequence_of(g, token);
-    const seq_span s = span_of(g, b);
-    if (token < s.first || token >= s.first + s.count) return;
-    // the products read whole blocks of 64 keys up to the limit of the last row of the tile
-    const int row = (token - s.first) * g.group + h % g.group, end = min((row / g.tile_rows + 1) * g.tile_rows, s.count * g.group);
-    const int lim = limit_at(s, (int)fd_div((u32)(end - 1), g.dGroup)), j0 = (blockIdx.y * BLOCK + threadIdx.x) * 4;
-    if (j0 >= ((lim + 63) & ~63)) return;
-    const row_stat st = g.stats[id];
+    constexpr int NR = 2 * T + 1;
+    const size_t plane = g.rows * g.keys;
+    const u64 *msg = g.msg + (size_t)r.id * g.keys + j;
+    u64 m[NR][4];
+#pragma unroll
+    for (int i = 0; i < NR; i++)
+#pragma unroll
+        for (int c = 0; c < 4; c++) m[i][c] = msg[i * plane + c];
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        ss_sacc2 acc;
+        acc.clear();
+#pragma unroll
+        for (int i = 0; i < NR; i++) {
+            SS_SPLIT31(m[i][c], w0, w1);
+            acc.mac(w0, w1, sp.ilambda[i]);
+        }
+        v[c] = acc.value();
+    }
+    u64 *opened = g.opened + (size_t)r.id * g.keys + j;
+#pragma unroll
+    for (int c = 0; c < 4; c++) opened[c] = v[c];
+}
+
+struct row_norm {
+    u64 recip;      // reciprocal of the sum of the weights
+    int drop;       // bits that the sum is shifted by
+};
+
+__device__ __forceinline__ row_norm norm_of(u64 sum)
+{
+    const int drop = max(0, 32 - __clzll((long long)sum));
+    return {(1ull << 62) / (sum >> drop), drop};
+}
+
+// The weights of four keys (w, 30 fraction bits, 0 beyond the limit; `seen` of them are keys that the row sees), shared, as digits.
+template <int N, int T>
+__device__ __forceinline__ void share_weights(const attn_args &g, const ss_softmax_params &sp, const row_place &r, int j, const u32 (&w)[4], int seen,
+                                              const row_norm &nm)
+{
     const int n = N ? N : sp.n;
     u64 y[MAXP<N>][4];
 #pragma unroll
     for (int c = 0; c < 4; c++) {
-        const int j = j0 + c;
-        if (j < st.limit) {
-            const u32 w = softmax_weight(lift(ss_sub(st.top, g.opened[(size_t)id * g.keys + j])), sp);
-            const u64 p = ((((u64)w * st.recip) >> 16) + (1ull << (45 - sp.bits + st.drop))) >> (46 - sp.bits + st.drop);
-            const u64 counter = ss_counter(((u64)token * g.heads + h) << 32 | (u32)j);
-            u64 a[T];
+        const u64 p = ((((u64)w[c] * nm.recip) >> 16) + (1ull << (45 - sp.bits + nm.drop))) >> (46 - sp.bits + nm.drop);
+        const u64 counter = ss_counter(((u64)r.token * g.heads + r.head) << 32 | (u32)(j + c));
+        u64 a[T];
 #pragma unroll
-            for (int x = 0; x < T; x++) a[x] = ss_draw_lazy_at(sp.gen_key[x], counter);
-            eval_points<T, MAXP<N>>(p, a, [&](int m, u64 v) { y[m][c] = balanced_digits(v); }, n);
-        } else {
-#pragma unroll
-            for (int m = 0; m < MAXP<N>; m++) y[m][c] = 0;
-        }
+        for (int x = 0; x < T; x++) a[x] = ss_draw_lazy_at(sp.gen_key[x], counter);
+        eval_points<T, MAXP<N>>(p, a, [&](int m, u64 v) { y[m][c] = c < seen ? balanced_digits(v) : 0; }, n);
     }
-    signed char *dst = g.weights + (size_t)id * g.keys * NL + (size_t)(j0 >> 6) * (64 * NL) + (j0 & 63);
+    signed char *dst = g.weights + (size_t)r.id * g.keys * NL + (size_t)(j >> 6) * (64 * NL) + (j & 63);
 #pragma unroll
     for (int m = 0; m < MAXP<N>; m++)
         if (N != 0 || m < n) {
@@ -497,53 +512,205 @@ __global__ __launch_bounds__(BLOCK) void weights_kernel(attn_args g, ss_softmax_
         }
 }
 
-// Step 3: one workgroup per (tile of 16 MT rows, run of keys and 64 elements of the head, kv head and party); a wave takes 16 elements.
-template <int MT>
-__global__ __launch_bounds__(256, 2) void values_kernel(attn_args g, int n)
+// Step 2 for rows of up to 1024 RUNS keys, one workgroup each: opened once, maximum, weights and sum in registers.
+template <int N, int T, int RUNS>
+__global__ __launch_bounds__(BLOCK) void softmax_kernel(attn_args g, ss_softmax_params sp)
 {
-    __shared__ size_t cells[MAX_RUN / 16];
+    __shared__ long long red[4];
+    row_place r;
+    if (!row_at(g, blockIdx.x, r)) return;
+    const int tid = threadIdx.x;
+    long long d[RUNS][4], top = -(1ll << 62);
+    u32 w[RUNS][4];
+    u64 ref = 0;
+    if (r.limit) {                               // the first key: differences of a row are small, whatever its mask is
+        ss_sacc2 acc;
+        acc.clear();
+#pragma unroll
+        for (int i = 0; i < 2 * T + 1; i++) {
+            const u64 m = g.msg[(i * g.rows + r.id) * g.keys];
+            SS_SPLIT31(m, w0, w1);
+            acc.mac(w0, w1, sp.ilambda[i]);
+        }
+        ref = acc.value();
+    }
+#pragma unroll
+    for (int u = 0; u < RUNS; u++) {
+        const int j = (u * BLOCK + tid) * 4;
+        if (j >= r.limit) break;
+        u64 v[4];
+        open_scores<T>(g, sp, r, j, v);
+#pragma unroll
+        for (int c = 0; c < 4; c++) {
+            d[u][c] = lift(ss_sub(v[c], ref));
+            if (j + c < r.limit) top = max(top, d[u][c]);
+        }
+    }
+    top = block_reduce(top, red, [](long long x, long long y) { return max(x, y); });
+    long long sum = 0;
+#pragma unroll
+    for (int u = 0; u < RUNS; u++) {
+        const int j = (u * BLOCK + tid) * 4;
+#pragma unroll
+        for (int c = 0; c < 4; c++) {
+            w[u][c] = j + c < r.limit ? softmax_weight(top - d[u][c], sp) : 0;
+            sum += w[u][c];
+        }
+    }
+    sum = block_reduce(sum, red, [](long long x, long long y) { return x + y; });
+    const row_norm nm = sum ? norm_of((u64)sum) : row_norm{0, 0};
+#pragma unroll
+    for (int u = 0; u < RUNS; u++) {
+        const int j = (u * BLOCK + tid) * 4;
+        if (j >= r.covered) break;
+        share_weights<N, T>(g, sp, r, j, w[u], r.limit - j, nm);
+    }
+}
+
+// ... for longer rows, which several workgroups take in blocks of 1024 keys: opened, with the largest score of each block,
+template <int T>
+__global__ __launch_bounds__(BLOCK) void open_kernel(attn_args g, ss_softmax_params sp)
+{
+    __shared__ long long red[4];
+    __shared__ u64 first;
+    row_place r;
+    const int j = (blockIdx.y * BLOCK + threadIdx.x) * 4;
+    if (!row_at(g, blockIdx.x, r) || (int)blockIdx.y * 1024 >= r.limit) return;
+    u64 v[4];
+    if (j < r.limit) open_scores<T>(g, sp, r, j, v);
+    if (threadIdx.x == 0) first = v[0];
+    __syncthreads();
+    long long top = -(1ll << 62);
+    if (j < r.limit) {
+#pragma unroll
+        for (int c = 0; c < 4; c++)
+            if (j + c < r.limit) top = max(top, lift(ss_sub(v[c], first)));
+    }
+    top = block_reduce(top, red, [](long long x, long long y) { return max(x, y); });
+    if (threadIdx.x == 0) g.tops[(size_t)r.id * gridDim.y + blockIdx.y] = ss_add(first, top < 0 ? SS_P - (u64)(-top) : (u64)top);
+}
+
+// the largest score of a row
+__device__ __forceinline__ u64 top_of(const attn_args &g, const row_place &r, long long *red)
+{
+    const u64 *tops = g.tops + (size_t)r.id * gridDim.y, ref = tops[0];
+    long long top = 0;
+    for (int k = threadIdx.x; k * 1024 < r.limit; k += BLOCK) top = max(top, lift(ss_sub(tops[k], ref)));
+    top = block_reduce(top, red, [](long long x, long long y) { return max(x, y); });
+    return ss_add(ref, (u64)top);
+}
+
+// the sum of the weights of each block,
+__global__ __launch_bounds__(BLOCK) void sum_kernel(attn_args g, ss_softmax_params sp)
+{
+    __shared__ long long red[4];
+    row_place r;
+    const int j = (blockIdx.y * BLOCK + threadIdx.x) * 4;
+    if (!row_at(g, blockIdx.x, r) || (int)blockIdx.y * 1024 >= r.limit) return;
+    const u64 top = top_of(g, r, red);
+    long long sum = 0;
+#pragma unroll
+    for (int c = 0; c < 4; c++)
+        if (j + c < r.limit) sum += softmax_weight(lift(ss_sub(top, g.opened[(size_t)r.id * g.keys + j + c])), sp);
+    sum = block_reduce(sum, red, [](long long x, long long y) { return x + y; });
+    if (threadIdx.x == 0) g.sums[(size_t)r.id * gridDim.y + blockIdx.y] = (u64)sum;
+}
+
+// and the weights.
+template <int N, int T>
+__global__ __launch_bounds__(BLOCK) void weights_kernel(attn_args g, ss_softmax_params sp)
+{
+    __shared__ long long red[4];
+    row_place r;
+    const int j = (blockIdx.y * BLOCK + threadIdx.x) * 4;
+    if (!row_at(g, blockIdx.x, r) || (int)blockIdx.y * 1024 >= r.covered) return;
+    u32 w[4] = {0, 0, 0, 0};
+    row_norm nm = {0, 0};
+    if (r.limit) {
+        const u64 top = top_of(g, r, red);
+        long long sum = 0;
+        for (int k = threadIdx.x; k * 1024 < r.limit; k += BLOCK) sum += (long long)g.sums[(size_t)r.id * gridDim.y + k];
+        nm = norm_of((u64)block_reduce(sum, red, [](long long x, long long y) { return x + y; }));
+#pragma unroll
+        for (int c = 0; c < 4; c++)
+            if (j + c < r.limit) w[c] = softmax_weight(lift(ss_sub(top, g.opened[(size_t)r.id * g.keys + j + c])), sp);
+    }
+    if (j < r.covered) share_weights<N, T>(g, sp, r, j, w, r.limit - j, nm);
+}
+
+// 16 bytes of every lane to 1 KB of LDS; done when vmcnt says so
+__device__ __forceinline__ void copy_to_lds(const signed char *src, v4i *dst) { __builtin_amdgcn_global_load_lds(src, dst, 16, 0, 0); }
+
+// Step 3: one workgroup per (tile of 16 MT rows, run of keys and up to 128 elements of the head, kv head and party); a wave takes 16
+// elements.  The digits of 64 weights of every row go to LDS for all waves, those of the values to a wave's registers; the next
+// 64 keys are on their way while those at hand are multiplied.
+template <int MT>
+__global__ __launch_bounds__(512) void values_kernel(attn_args g, int n)
+{
+    __shared__ v4i wd[2][MT * TILE];
+    __shared__ size_t cells[MAX_RUN / 16 + 4];
     __shared__ int rowid[16 * MT];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
     const int head = blockIdx.z / n, party = blockIdx.z - head * n;
-    const int dblocks = (g.c.dim + 63) / 64, split = blockIdx.y / dblocks, dt = (blockIdx.y - split * dblocks) * 4 + wave;
+    const int split = blockIdx.y / g.dblocks, dt = (blockIdx.y - split * g.dblocks) * waves + wave;
     int row0 = 0;
-    const int b = find_tile(g, blockIdx.x, row0);
+    const int b = __builtin_amdgcn_readfirstlane(find_tile(g, blockIdx.x, row0));
     if (b < 0) return;
+    row0 = __builtin_amdgcn_readfirstlane(row0);
     const seq_span s = span_of(g, b);
     const int nrows = min(16 * MT, s.count * g.group - row0);
     const int lim = limit_at(s, (int)fd_div((u32)(row0 + nrows - 1), g.dGroup));
-    const int k0 = split * g.run, k1 = min(k0 + g.run, lim);
+    const int k0 = split * g.run, k1 = min(k0 + g.run, lim), units = (k1 - k0 + 63) >> 6;
     if (split && k0 >= lim) return;              // (the first run writes the zeros of rows that see nothing)
-    for (int c = tid; c < (k1 - k0 + 63) / 64 * 4; c += 256) cells[c] = cell_at(g, b, k0 / 16 + c);
+    for (int c = tid; c < units * 4; c += blockDim.x) cells[c] = cell_at(g, b, k0 / 16 + c);
     if (tid < 16 * MT) {
         const int r = min(tid, nrows - 1), i = (int)fd_div((u32)(row0 + r), g.dGroup);
         rowid[tid] = (s.first + i - g.tok0) * g.heads + head * g.group + row0 + r - i * g.group;
     }
     __syncthreads();
-    if (dt * 16 >= g.c.dim) return;
-    const signed char *base = g.c.values + party * g.party_bytes + head * g.head_bytes + (dt * 16 + (lane & 15)) * 16;
+    const bool live = dt * 16 < g.c.dim;         // (the last workgroup of a head may have a wave too many: it only copies)
+    const size_t limb = (size_t)g.c.dim * 16;
+    const signed char *base = g.c.values + party * g.party_bytes + head * g.head_bytes + (min(dt, (g.c.dim >> 4) - 1) * 16 + (lane & 15)) * 16;
     const signed char *wrow[MT];
     v4i acc[MT][ND];
 #pragma unroll
     for (int m = 0; m < MT; m++) {
         clear(acc[m]);
-        wrow[m] = g.weights + ((size_t)party * g.rows + rowid[m * 16 + (lane & 15)]) * g.keys * NL + (lane >> 4) * 16;
+        wrow[m] = g.weights + ((size_t)party * g.rows + rowid[m * 16 + (lane & 15)]) * g.keys * NL + (lane >> 4) * 16 + (size_t)k0 * NL;
     }
-    const size_t limb = (size_t)g.c.dim * 16;
-    for (int kb = k0 / 64; kb * 64 < k1; kb++) {
-        const signed char *src = base + cells[kb * 4 - k0 / 16 + (lane >> 4)];
-        v4i v[NL];
+    auto copy_weights = [&](int unit, int stage) {
+        for (int q = wave; q < MT * NL; q += waves)   // uniform
+            copy_to_lds((MT == 1 || q < NL ? wrow[0] : wrow[MT - 1]) + (size_t)unit * (64 * NL) + (q < NL ? q : q - NL) * 64, &wd[stage][q * 64]);
+    };
+    auto load_values = [&](int unit, v4i (&v)[NL]) {
+        const signed char *src = base + cells[unit * 4 + (lane >> 4)];
 #pragma unroll
         for (int l = 0; l < NL; l++) v[l] = *reinterpret_cast<const v4i *>(src + l * limb);
+    };
+    v4i v[NL], next[NL];
+    if (units) {
+        copy_weights(0, 0);
+        load_values(0, v);
+    }
+    for (int u = 0; u < units; u++) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0): this wave's part of the weights is in LDS
+        __syncthreads();                         // everyone's is, and nobody reads the other stage any more
+        if (u + 1 < units) {
+            copy_weights(u + 1, (u + 1) & 1);
+            load_values(u + 1, next);
+        }
 #pragma unroll
         for (int i = 0; i < NL; i++)
 #pragma unroll
             for (int m = 0; m < MT; m++) {
-                const v4i a = *reinterpret_cast<const v4i *>(wrow[m] + (size_t)kb * (64 * NL) + i * 64);
+                const v4i a = wd[u & 1][m * TILE + i * 64 + lane];
 #pragma unroll
                 for (int j = 0; j < NL; j++) acc[m][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, v[j], acc[m][i + j], 0, 0, 0);
             }
+#pragma unroll
+        for (int l = 0; l < NL; l++) v[l] = next[l];
     }
+    if (!live) return;
 #pragma unroll
     for (int m = 0; m < MT; m++)
 #pragma unroll
@@ -560,16 +727,16 @@ __global__ __launch_bounds__(256, 2) void values_kernel(attn_args g, int n)
 }
 
 // the runs of a row added up
-__global__ __launch_bounds__(BLOCK) void join_kernel(attn_args g, int n)
+__global__ __launch_bounds__(BLOCK) void join_kernel(attn_args g, int n, fdiv dDim)
 {
-    const int id = blockIdx.x, party = blockIdx.y, limit = g.stats[id].limit;
-    const int token = g.tok0 + id / g.heads;
-    if (token < g.s.start[0] || token >= g.s.start[g.s.seqs]) return;
-    for (int d = threadIdx.x; d < g.c.dim; d += BLOCK) {
-        u64 o = 0;
-        for (int s = 0; s * g.run < limit; s++) o = ss_add(o, g.parts[(((size_t)s * n + party) * g.rows + id) * g.c.dim + d]);
-        g.out[((size_t)party * g.s.tokens * g.heads + (size_t)g.tok0 * g.heads + id) * g.c.dim + d] = o;
-    }
+    const u32 i = blockIdx.x * BLOCK + threadIdx.x, id = fd_div(i, dDim), party = blockIdx.y;
+    row_place r;
+    if (id >= g.rows_now || !row_at(g, (int)id, r)) return;
+    const size_t plane = (size_t)n * g.rows * g.c.dim;
+    const u64 *p = g.parts + (size_t)party * g.rows * g.c.dim + i;
+    u64 o = 0;
+    for (int s = 0; s * g.run < r.limit; s++) o = ss_add(o, p[s * plane]);
+    g.out[((size_t)party * g.s.tokens + g.tok0) * g.heads * g.c.dim + i] = o;
 }
 
 rotary_shape make_shape(int tokens, int heads, int dim, int rot)
@@ -621,18 +788,22 @@ attention_plan plan_attention(int n, int t, int tokens, int seqs, int heads, int
     attention_plan p = {};
     const size_t group = heads / kv, nr = 2 * t + 1;
     p.row_tiles = ceil_div(tokens, seqs) * group > 16 ? 2 : 1;
+    p.key_block = p.row_tiles == 1 ? 256 : 512;
     p.keys = ((size_t)max_length + 63) & ~(size_t)63;
+    p.dblocks = ceil_div(dim, 128);
+    p.waves = ceil_div(dim / 16, p.dblocks);
     p.slab = tokens;
     for (;;) {
         const size_t tile = 16 * p.row_tiles, tiles = p.slab * group / tile + seqs;
-        const size_t base = tiles * ceil_div(dim, 64) * kv * n;
-        const size_t wanted = base >= 1024 ? 1 : ceil_div(1024, base);
+        const size_t base = tiles * p.dblocks * kv * n;
+        const size_t wanted = ceil_div(1024, base);
         p.run = (int)((ceil_div(p.keys, wanted) + 63) & ~63u);
         if (p.run > MAX_RUN) p.run = MAX_RUN;
-        if (p.run < KEY_BLOCK) p.run = KEY_BLOCK;
+        if (p.run < 256) p.run = 256;
         p.splits = (int)ceil_div(p.keys, p.run);
         p.rows = (size_t)p.slab * heads;
-        p.bytes = align256((nr + 1) * p.rows * p.keys * 8) + align256(p.rows * sizeof(row_stat)) + align256((size_t)n * p.rows * p.keys * NL) +
+        const size_t blocks = p.keys > SHORT_ROW ? ceil_div(p.keys, 1024) : 0;
+        p.bytes = align256((nr + 1) * p.rows * p.keys * 8) + align256(2 * p.rows * blocks * 8) + align256((size_t)n * p.rows * p.keys * NL) +
                   (p.splits > 1 ? align256((size_t)p.splits * n * p.rows * dim * 8) : 0);
         if (p.bytes <= room && p.rows <= MAX_ROWS) return p;
         if (p.slab == 1) break;
@@ -657,6 +828,7 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
     g.causal = causal;
     g.dGroup = make_fdiv((u32)g.group);
     g.dCells = make_fdiv((u32)cache.page_cells);
+    g.dHeads = make_fdiv((u32)heads);
     g.q = q;
     g.ld_q = ld_q;
     g.rows = plan.rows;
@@ -664,19 +836,25 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
     g.splits = plan.splits;
     g.run = plan.run;
     g.tile_rows = 16 * plan.row_tiles;
+    g.key_block = plan.key_block;
+    g.dblocks = plan.dblocks;
     const int nr = 2 * sp.t + 1, n = sp.n;
+    const unsigned blocks = ceil_div(plan.keys, 1024);
+    const bool split_rows = plan.keys > SHORT_ROW;
     char *at = (char *)room;
     g.msg = (u64 *)at;
     g.opened = g.msg + (size_t)nr * g.rows * g.keys;
     at += align256((size_t)(nr + 1) * g.rows * g.keys * 8);
-    g.stats = (row_stat *)at;
-    at += align256(g.rows * sizeof(row_stat));
+    if (split_rows) {
+        g.tops = (u64 *)at;
+        g.sums = g.tops + g.rows * blocks;
+        at += align256(2 * g.rows * blocks * 8);
+    }
     g.weights = (signed char *)at;
     at += align256((size_t)n * g.rows * g.keys * NL);
     g.parts = (u64 *)at;
     g.out = out;
-    const int dblocks = (cache.dim + 63) / 64;
-    const size_t lds = (size_t)plan.row_tiles * dblocks * TILE * 16;
+    const size_t lds = (size_t)plan.row_tiles * ((cache.dim + 63) / 64) * TILE * 16;
     if (lds > 48 * 1024) {
         const void *scores = plan.row_tiles == 1 ? (const void *)scores_kernel<1> : (const void *)scores_kernel<2>;
         if (hipError_t e = hipFuncSetAttribute(scores, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); e != hipSuccess) return e;
@@ -684,23 +862,23 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
     for (int tok = 0; tok < seqs.tokens; tok += plan.slab) {
         g.tok0 = tok;
         g.tok1 = min(seqs.tokens, tok + plan.slab);
-        const int rows = (g.tok1 - tok) * heads;
+        g.rows_now = (u32)(g.tok1 - tok) * heads;
         const unsigned tiles = (unsigned)((size_t)(g.tok1 - tok) * g.group / g.tile_rows + seqs.seqs);
-        const dim3 sgrid(tiles, ceil_div(plan.keys, KEY_BLOCK), cache.kv * nr), vgrid(tiles, plan.splits * dblocks, cache.kv * n);
-        const dim3 wgrid(rows, ceil_div(plan.keys, BLOCK * 4));
+        const dim3 sgrid(tiles, ceil_div(plan.keys, plan.key_block), cache.kv * nr), vgrid(tiles, plan.splits * plan.dblocks, cache.kv * n);
+        const dim3 rgrid(g.rows_now), wgrid(g.rows_now, blocks), block(BLOCK);
         if (plan.row_tiles == 1)
             hipLaunchKernelGGL((scores_kernel<1>), sgrid, dim3(256), lds, stream, g, sp);
         else
             hipLaunchKernelGGL((scores_kernel<2>), sgrid, dim3(256), lds, stream, g, sp);
-        hipLaunchKernelGGL(row_kernel, dim3(rows), dim3(BLOCK), 0, stream, g, sp);
-#define SS_LAUNCH(NC, TC) hipLaunchKernelGGL((weights_kernel<NC, TC>), wgrid, dim3(BLOCK), 0, stream, g, sp)
+#define SS_LAUNCH(NC, TC)                                                                        do {                                                                                               if (split_rows) {                                                                                  hipLaunchKernelGGL((open_kernel<TC>), wgrid, block, 0, stream, g, sp);                       hipLaunchKernelGGL(sum_kernel, wgrid, block, 0, stream, g, sp);                              hipLaunchKernelGGL((weights_kernel<NC, TC>), wgrid, block, 0, stream, g, sp);            } else if (blocks == 1)                                                                            hipLaunchKernelGGL((softmax_kernel<NC, TC, 1>), rgrid, block, 0, stream, g, sp);         else                                                                                               hipLaunchKernelGGL((softmax_kernel<NC, TC, 4>), rgrid, block, 0, stream, g, sp);     } while (0)
         SS_SCHEME(sp.n, sp.t, SS_LAUNCH);
 #undef SS_LAUNCH
         if (plan.row_tiles == 1)
-            hipLaunchKernelGGL((values_kernel<1>), vgrid, dim3(256), 0, stream, g, n);
+            hipLaunchKernelGGL((values_kernel<1>), vgrid, dim3(64 * plan.waves), 0, stream, g, n);
         else
-            hipLaunchKernelGGL((values_kernel<2>), vgrid, dim3(256), 0, stream, g, n);
-        if (plan.splits > 1) hipLaunchKernelGGL(join_kernel, dim3(rows, n), dim3(BLOCK), 0, stream, g, n);
+            hipLaunchKernelGGL((values_kernel<2>), vgrid, dim3(64 * plan.waves), 0, stream, g, n);
+        if (plan.splits > 1)
+            hipLaunchKernelGGL(join_kernel, dim3(ceil_div((size_t)g.rows_now * cache.dim, BLOCK), n), block, 0, stream, g, n, make_fdiv((u32)cache.dim));
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;
