@@ -293,6 +293,22 @@ __device__ __forceinline__ void clear(v4i (&acc)[NLn])
     for (int s = 0; s < NLn; s++) acc[s] = (v4i){0, 0, 0, 0};
 }
 
+// 64 contraction indices of MT blocks of 16 rows, whose digits lie at a in LDS, `stride` apart, times the 16 columns of k.  FIRST: the
+// sums start here.
+template <int MT, bool FIRST>
+__device__ __forceinline__ void multiply(const v4i *a, int stride, const v4i (&k)[NL], v4i (&acc)[MT][ND])
+{
+#pragma unroll
+    for (int i = 0; i < NL; i++)
+#pragma unroll
+        for (int m = 0; m < MT; m++) {
+            const v4i x = a[m * stride + i * 64];
+#pragma unroll
+            for (int j = 0; j < NL; j++)
+                acc[m][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, k[j], FIRST && (i == 0 || j == NL - 1) ? (v4i){0, 0, 0, 0} : acc[m][i + j], 0, 0, 0);
+        }
+}
+
 // Step 1: one workgroup per (tile of 16 MT rows, block of g.key_block keys, kv head and party).  The digits of the queries lie in LDS in
 // MFMA order; a wave takes a cell of 16 keys at a time straight from the cache, the next 64 elements of a cell (or the next cell's first)
 // on their way while those at hand are multiplied.
@@ -358,23 +374,20 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
         for (int l = 0; l < NL; l++) dst[l * 256] = limb_dword(y, l);
     }
     __syncthreads();
+    __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0): the first digits are there, the loop's waits are for its own loads alone
     for (; cell < cell_end; cell += 4) {
-        const bool more = cell + 4 < cell_end;
-        const size_t at_next = more ? cell_at(g, b, cell + 4) : 0;
+        const size_t at_next = cell_at(g, b, min(cell + 4, cell_end - 1));
         v4i acc[MT][ND];
-#pragma unroll
-        for (int m = 0; m < MT; m++) clear(acc[m]);
         for (int kb = 0; kb < kb_n; kb++) {
-            if (kb + 1 < kb_n) load(at, kb + 1, next);
-            else if (more) load(at_next, 0, next);
-#pragma unroll
-            for (int i = 0; i < NL; i++)
-#pragma unroll
-                for (int m = 0; m < MT; m++) {
-                    const v4i a = qd[(m * kb_n + kb) * TILE + i * 64 + lane];
-#pragma unroll
-                    for (int j = 0; j < NL; j++) acc[m][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, k[j], acc[m][i + j], 0, 0, 0);
-                }
+            // (always: a load that may not have been sent would be waited for at once.  Behind the last cell, its own first elements again)
+            const bool same = kb + 1 < kb_n;
+            load(same ? at : at_next, same ? kb + 1 : 0, next);
+            __builtin_amdgcn_sched_barrier(0);   // the loads leave before the products
+            const v4i *a = qd + kb * TILE + lane;
+            if (kb == 0)
+                multiply<MT, true>(a, kb_n * TILE, k, acc);
+            else
+                multiply<MT, false>(a, kb_n * TILE, k, acc);
 #pragma unroll
             for (int l = 0; l < NL; l++) k[l] = next[l];
         }
@@ -638,12 +651,10 @@ __global__ __launch_bounds__(BLOCK) void weights_kernel(attn_args g, ss_softmax_
     if (j < r.covered) share_weights<N, T>(g, sp, r, j, w, r.limit - j, nm);
 }
 
-// 16 bytes of every lane to 1 KB of LDS; done when vmcnt says so
-__device__ __forceinline__ void copy_to_lds(const signed char *src, v4i *dst) { __builtin_amdgcn_global_load_lds(src, dst, 16, 0, 0); }
-
 // Step 3: one workgroup per (tile of 16 MT rows, run of keys and up to 128 elements of the head, kv head and party); a wave takes 16
-// elements.  The digits of 64 weights of every row go to LDS for all waves, those of the values to a wave's registers; the next
-// 64 keys are on their way while those at hand are multiplied.
+// elements.  The digits of 64 weights of every row go through LDS to all waves, those of the values to a wave's registers; the next
+// 64 keys are on their way while those at hand are multiplied.  (The weights too by way of registers: behind copies straight into LDS the
+// compiler waits before the next read of any LDS.)
 template <int MT>
 __global__ __launch_bounds__(512) void values_kernel(attn_args g, int n)
 {
@@ -652,7 +663,7 @@ __global__ __launch_bounds__(512) void values_kernel(attn_args g, int n)
     __shared__ int rowid[16 * MT];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
     const int head = blockIdx.z / n, party = blockIdx.z - head * n;
-    const int split = blockIdx.y / g.dblocks, dt = (blockIdx.y - split * g.dblocks) * waves + wave;
+    const int split = blockIdx.y / g.dblocks, dt = (blockIdx.y - split * g.dblocks) * waves + wave;   // 16 elements each
     int row0 = 0;
     const int b = __builtin_amdgcn_readfirstlane(find_tile(g, blockIdx.x, row0));
     if (b < 0) return;
@@ -668,7 +679,7 @@ __global__ __launch_bounds__(512) void values_kernel(attn_args g, int n)
         rowid[tid] = (s.first + i - g.tok0) * g.heads + head * g.group + row0 + r - i * g.group;
     }
     __syncthreads();
-    const bool live = dt * 16 < g.c.dim;         // (the last workgroup of a head may have a wave too many: it only copies)
+    const bool live = dt * 16 < g.c.dim;         // (others only bring weights)
     const size_t limb = (size_t)g.c.dim * 16;
     const signed char *base = g.c.values + party * g.party_bytes + head * g.head_bytes + (min(dt, (g.c.dim >> 4) - 1) * 16 + (lane & 15)) * 16;
     const signed char *wrow[MT];
@@ -678,9 +689,21 @@ __global__ __launch_bounds__(512) void values_kernel(attn_args g, int n)
         clear(acc[m]);
         wrow[m] = g.weights + ((size_t)party * g.rows + rowid[m * 16 + (lane & 15)]) * g.keys * NL + (lane >> 4) * 16 + (size_t)k0 * NL;
     }
-    auto copy_weights = [&](int unit, int stage) {
-        for (int q = wave; q < MT * NL; q += waves)   // uniform
-            copy_to_lds((MT == 1 || q < NL ? wrow[0] : wrow[MT - 1]) + (size_t)unit * (64 * NL) + (q < NL ? q : q - NL) * 64, &wd[stage][q * 64]);
+    // limb slices of the weights that this wave brings to LDS: numbers wave, wave + waves, ... of MT NL; 4 waves or more
+    constexpr int SLICES = MT * NL, MOST = (SLICES + 3) / 4;
+    v4i slice[MOST];
+    auto load_weights = [&](int unit) {
+#pragma unroll
+        for (int k = 0; k < MOST; k++) {
+            const int q = wave + k * waves;      // uniform
+            if (q < SLICES)
+                slice[k] = *reinterpret_cast<const v4i *>((MT == 1 || q < NL ? wrow[0] : wrow[MT - 1]) + (size_t)unit * (64 * NL) + (q < NL ? q : q - NL) * 64);
+        }
+    };
+    auto keep_weights = [&](int stage) {
+#pragma unroll
+        for (int k = 0; k < MOST; k++)
+            if (wave + k * waves < SLICES) wd[stage][(wave + k * waves) * 64 + lane] = slice[k];
     };
     auto load_values = [&](int unit, v4i (&v)[NL]) {
         const signed char *src = base + cells[unit * 4 + (lane >> 4)];
@@ -689,24 +712,20 @@ __global__ __launch_bounds__(512) void values_kernel(attn_args g, int n)
     };
     v4i v[NL], next[NL];
     if (units) {
-        copy_weights(0, 0);
+        load_weights(0);
         load_values(0, v);
+        keep_weights(0);
     }
+    __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0): the loop's waits are for its own loads alone
     for (int u = 0; u < units; u++) {
-        __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0): this wave's part of the weights is in LDS
-        __syncthreads();                         // everyone's is, and nobody reads the other stage any more
-        if (u + 1 < units) {
-            copy_weights(u + 1, (u + 1) & 1);
-            load_values(u + 1, next);
-        }
-#pragma unroll
-        for (int i = 0; i < NL; i++)
-#pragma unroll
-            for (int m = 0; m < MT; m++) {
-                const v4i a = wd[u & 1][m * TILE + i * 64 + lane];
-#pragma unroll
-                for (int j = 0; j < NL; j++) acc[m][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, v[j], acc[m][i + j], 0, 0, 0);
-            }
+        __syncthreads();                         // everyone's weights are in LDS, and nobody reads the other stage any more
+        const int ahead = min(u + 1, units - 1); // (the last again behind the last: nobody reads it)
+        load_values(ahead, next);
+        load_weights(ahead);
+        __builtin_amdgcn_sched_barrier(0);       // the loads leave before the products
+        if (live) multiply<MT, false>(&wd[u & 1][lane], TILE, v, acc);
+        __builtin_amdgcn_sched_barrier(0);
+        keep_weights((u + 1) & 1);
 #pragma unroll
         for (int l = 0; l < NL; l++) v[l] = next[l];
     }
@@ -791,7 +810,8 @@ attention_plan plan_attention(int n, int t, int tokens, int seqs, int heads, int
     p.key_block = p.row_tiles == 1 ? 256 : 512;
     p.keys = ((size_t)max_length + 63) & ~(size_t)63;
     p.dblocks = ceil_div(dim, 128);
-    p.waves = ceil_div(dim / 16, p.dblocks);
+    p.waves = (int)ceil_div(dim / 16, p.dblocks);
+    if (p.waves < 4) p.waves = 4;
     p.slab = tokens;
     for (;;) {
         const size_t tile = 16 * p.row_tiles, tiles = p.slab * group / tile + seqs;
