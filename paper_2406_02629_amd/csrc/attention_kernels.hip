@@ -237,11 +237,15 @@ struct seq_span {
     int first, count, limit, step;  // limit of token first + i: limit + i * step, at least 0
 };
 
+// what describes the call does not change while it runs: read by way of the scalar cache wherever the index is the same for a wave
+typedef const int __attribute__((address_space(4))) *constant_ints;
+__device__ __forceinline__ int fixed_at(const int *p, size_t i) { return ((constant_ints)(uintptr_t)p)[i]; }
+
 __device__ __forceinline__ seq_span span_of(const attn_args &g, int b)
 {
-    const int s0 = g.s.start[b], s1 = g.s.start[b + 1];
+    const int s0 = fixed_at(g.s.start, b), s1 = fixed_at(g.s.start, b + 1);
     const int first = max(s0, g.tok0), last = min(s1, g.tok1);
-    int len = min(g.s.length[b], g.s.max_length);
+    int len = min(fixed_at(g.s.length, b), g.s.max_length);
     len = max(0, min(len, g.s.max_pages * g.c.page_cells * 16));
     return {first, max(0, last - first), g.causal ? len - (s1 - first) + 1 : len, g.causal ? 1 : 0};
 }
@@ -257,7 +261,7 @@ __device__ __forceinline__ int find_tile(const attn_args &g, int tile, int &row0
         const int b = b0 + lane;
         int mine = 0;
         if (b < g.s.seqs) {
-            const int first = max(g.s.start[b], g.tok0), last = min(g.s.start[b + 1], g.tok1);
+            const int first = max(fixed_at(g.s.start, b), g.tok0), last = min(fixed_at(g.s.start, b + 1), g.tok1);
             mine = (max(0, last - first) * g.group + g.tile_rows - 1) / g.tile_rows;
         }
         int upto = mine;
@@ -282,7 +286,7 @@ __device__ __forceinline__ int find_tile(const attn_args &g, int tile, int &row0
 __device__ __forceinline__ size_t cell_at(const attn_args &g, int b, int cell)
 {
     const int slot = (int)fd_div((u32)cell, g.dCells), in = cell - slot * g.c.page_cells;
-    const int page = g.s.table[(size_t)b * g.s.max_pages + min(slot, g.s.max_pages - 1)];
+    const int page = fixed_at(g.s.table, (size_t)b * g.s.max_pages + min(slot, g.s.max_pages - 1));
     return (size_t)min(max(page, 0), g.c.pages - 1) * g.page_bytes + (size_t)in * g.cell;
 }
 
@@ -307,6 +311,13 @@ __device__ __forceinline__ void multiply(const v4i *a, int stride, const v4i (&k
             for (int j = 0; j < NL; j++)
                 acc[m][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, k[j], FIRST && (i == 0 || j == NL - 1) ? (v4i){0, 0, 0, 0} : acc[m][i + j], 0, 0, 0);
         }
+    // two reads ahead of the products (left to itself the compiler waits for every read where registers are few)
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+    for (int q = 0; q < MT * NL; q++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, NL, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
 }
 
 // Step 1: one workgroup per (tile of 16 MT rows, block of g.key_block keys, kv head and party).  The digits of the queries lie in LDS in
@@ -439,7 +450,7 @@ __device__ __forceinline__ int sequence_of(const attn_args &g, int token)
     int lo = 0, hi = g.s.seqs;       // the last b with start[b] <= token
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
-        if (g.s.start[mid] <= token) lo = mid; else hi = mid;
+        if (fixed_at(g.s.start, mid) <= token) lo = mid; else hi = mid;
     }
     return lo;
 }
@@ -753,8 +764,15 @@ __global__ __launch_bounds__(BLOCK) void join_kernel(attn_args g, int n, fdiv dD
     if (id >= g.rows_now || !row_at(g, (int)id, r)) return;
     const size_t plane = (size_t)n * g.rows * g.c.dim;
     const u64 *p = g.parts + (size_t)party * g.rows * g.c.dim + i;
+    const int runs = (r.limit + g.run - 1) / g.run;
     u64 o = 0;
-    for (int s = 0; s * g.run < r.limit; s++) o = ss_add(o, p[s * plane]);
+    for (int s0 = 0; s0 < runs; s0 += 8) {       // eight loads in flight
+        u64 x[8];
+#pragma unroll
+        for (int s = 0; s < 8; s++) x[s] = p[min(s0 + s, runs - 1) * plane];
+#pragma unroll
+        for (int s = 0; s < 8; s++) o = s0 + s < runs ? ss_add(o, x[s]) : o;
+    }
     g.out[((size_t)party * g.s.tokens + g.tok0) * g.heads * g.c.dim + i] = o;
 }
 
