@@ -501,9 +501,8 @@ int ssnet_cache_append(ssnet_ctx *ctx, const ssnet_paged_cache *cache, const uin
  * Workspace: ssnet_workspace_bytes_attention for `tokens` tokens has room for the
  * messages of the whole call; a smaller one serves if it has room for one token's,
  * and the tokens are then taken in several runs with the same result.  Messages
- * behind the header: [2t+1][rows][max_length rounded up to 64] masked scores, then
- * the opened ones [rows][..] (of the last run; keys that a row does not see hold
- * anything). */
+ * behind the header: [2t+1][rows][max_length rounded up to 64] masked scores (of the
+ * last run; keys that a row does not see hold anything). */
 #define SSNET_MAX_CONTEXT (1 << 20)
 typedef struct ssnet_sequences {
     const int32_t *d_start, *d_table, *d_length;

@@ -223,8 +223,8 @@ struct attn_args {
     fdiv dGroup, dCells, dHeads;
     const u64 *q;
     size_t ld_q;
-    u64 *msg, *opened;              // [2t+1][rows][keys], [rows][keys]
-    u64 *tops, *sums;               // [rows][keys / 1024]: of long rows
+    u64 *msg;                       // [2t+1][rows][keys]
+    u64 *opened, *tops, *sums;      // of long rows: [rows][keys], [rows][keys / 1024]
     signed char *weights;           // [n][rows][keys / 64][limb][64]
     u64 *out, *parts;               // parts [splits][n][rows][dim]
     size_t rows, keys;
@@ -371,11 +371,12 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
         rowid[tid] = id;
     }
     __syncthreads();
-    for (int it = tid; it < MT * 16 * kb_n * 16; it += 256) {
-        // four consecutive elements of row r; 16 lanes take 64 elements, so that a wave reads 512 consecutive bytes of a row
-        const int r = (it >> 4) & (16 * MT - 1), kb = it / (16 * MT * 16), d = kb * 64 + (it & 15) * 4;
+    for (int it = tid; it < nrows * kb_n * 16; it += 256) {
+        // four consecutive elements of row r; 16 lanes take 64 elements, so that a wave reads 512 consecutive bytes of a row.  (What lies in
+        // the places of rows that do not exist reaches their results alone.)
+        const int rk = it >> 4, kb = kb_n > 1 ? rk % kb_n : 0, r = kb_n > 1 ? rk / kb_n : rk, d = kb * 64 + (it & 15) * 4;
         u64 y[4] = {0, 0, 0, 0};
-        if (r < nrows && d < g.c.dim) {
+        if (d < g.c.dim) {
             const u64 *src = g.q + rowat[r] + d;
 #pragma unroll
             for (int c = 0; c < 4; c++) y[c] = balanced_digits(src[c]);
@@ -434,15 +435,18 @@ __device__ __forceinline__ u32 softmax_weight(long long below, const ss_softmax_
     return octaves < 31 ? w >> octaves : 0;
 }
 
-template <typename T, typename F>
-__device__ __forceinline__ T block_reduce(T v, T *lds, F &&op)   // 256 threads; lds [4]
+template <int THREADS = BLOCK, typename T, typename F>
+__device__ __forceinline__ T block_reduce(T v, T *lds, F &&op)   // lds: one for each wave
 {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v = op(v, __shfl_xor(v, d));
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    return op(op(lds[0], lds[1]), op(lds[2], lds[3]));
+    v = lds[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; w++) v = op(v, lds[w]);
+    return v;
 }
 
 __device__ __forceinline__ int sequence_of(const attn_args &g, int token)
@@ -495,9 +499,6 @@ __device__ __forceinline__ void open_scores(const attn_args &g, const ss_softmax
         }
         v[c] = acc.value();
     }
-    u64 *opened = g.opened + (size_t)r.id * g.keys + j;
-#pragma unroll
-    for (int c = 0; c < 4; c++) opened[c] = v[c];
 }
 
 struct row_norm {
@@ -536,11 +537,11 @@ __device__ __forceinline__ void share_weights(const attn_args &g, const ss_softm
         }
 }
 
-// Step 2 for rows of up to 1024 RUNS keys, one workgroup each: opened once, maximum, weights and sum in registers.
-template <int N, int T, int RUNS>
-__global__ __launch_bounds__(BLOCK) void softmax_kernel(attn_args g, ss_softmax_params sp)
+// Step 2 for rows of up to 4 THREADS RUNS keys, one workgroup each: opened once, maximum, weights and sum in registers.
+template <int N, int T, int RUNS, int THREADS>
+__global__ __launch_bounds__(THREADS) void softmax_kernel(attn_args g, ss_softmax_params sp)
 {
-    __shared__ long long red[4];
+    __shared__ long long red[THREADS / 64];
     row_place r;
     if (!row_at(g, blockIdx.x, r)) return;
     const int tid = threadIdx.x;
@@ -560,7 +561,7 @@ __global__ __launch_bounds__(BLOCK) void softmax_kernel(attn_args g, ss_softmax_
     }
 #pragma unroll
     for (int u = 0; u < RUNS; u++) {
-        const int j = (u * BLOCK + tid) * 4;
+        const int j = (u * THREADS + tid) * 4;
         if (j >= r.limit) break;
         u64 v[4];
         open_scores<T>(g, sp, r, j, v);
@@ -570,22 +571,22 @@ __global__ __launch_bounds__(BLOCK) void softmax_kernel(attn_args g, ss_softmax_
             if (j + c < r.limit) top = max(top, d[u][c]);
         }
     }
-    top = block_reduce(top, red, [](long long x, long long y) { return max(x, y); });
+    top = block_reduce<THREADS>(top, red, [](long long x, long long y) { return max(x, y); });
     long long sum = 0;
 #pragma unroll
     for (int u = 0; u < RUNS; u++) {
-        const int j = (u * BLOCK + tid) * 4;
+        const int j = (u * THREADS + tid) * 4;
 #pragma unroll
         for (int c = 0; c < 4; c++) {
             w[u][c] = j + c < r.limit ? softmax_weight(top - d[u][c], sp) : 0;
             sum += w[u][c];
         }
     }
-    sum = block_reduce(sum, red, [](long long x, long long y) { return x + y; });
+    sum = block_reduce<THREADS>(sum, red, [](long long x, long long y) { return x + y; });
     const row_norm nm = sum ? norm_of((u64)sum) : row_norm{0, 0};
 #pragma unroll
     for (int u = 0; u < RUNS; u++) {
-        const int j = (u * BLOCK + tid) * 4;
+        const int j = (u * THREADS + tid) * 4;
         if (j >= r.covered) break;
         share_weights<N, T>(g, sp, r, j, w[u], r.limit - j, nm);
     }
@@ -601,7 +602,12 @@ __global__ __launch_bounds__(BLOCK) void open_kernel(attn_args g, ss_softmax_par
     const int j = (blockIdx.y * BLOCK + threadIdx.x) * 4;
     if (!row_at(g, blockIdx.x, r) || (int)blockIdx.y * 1024 >= r.limit) return;
     u64 v[4];
-    if (j < r.limit) open_scores<T>(g, sp, r, j, v);
+    if (j < r.limit) {
+        open_scores<T>(g, sp, r, j, v);
+        u64 *opened = g.opened + (size_t)r.id * g.keys + j;
+#pragma unroll
+        for (int c = 0; c < 4; c++) opened[c] = v[c];
+    }
     if (threadIdx.x == 0) first = v[0];
     __syncthreads();
     long long top = -(1ll << 62);
@@ -825,23 +831,23 @@ attention_plan plan_attention(int n, int t, int tokens, int seqs, int heads, int
     attention_plan p = {};
     const size_t group = heads / kv, nr = 2 * t + 1;
     p.row_tiles = ceil_div(tokens, seqs) * group > 16 ? 2 : 1;
-    p.key_block = p.row_tiles == 1 ? 256 : 512;
+    p.key_block = p.row_tiles == 1 ? 128 : 512;
     p.keys = ((size_t)max_length + 63) & ~(size_t)63;
-    p.dblocks = ceil_div(dim, 128);
+    p.dblocks = ceil_div(dim, p.row_tiles == 1 ? 64 : 128);
     p.waves = (int)ceil_div(dim / 16, p.dblocks);
     if (p.waves < 4) p.waves = 4;
     p.slab = tokens;
     for (;;) {
         const size_t tile = 16 * p.row_tiles, tiles = p.slab * group / tile + seqs;
         const size_t base = tiles * p.dblocks * kv * n;
-        const size_t wanted = ceil_div(1024, base);
+        const size_t wanted = ceil_div(p.row_tiles == 1 ? 2048 : 1024, base);
         p.run = (int)((ceil_div(p.keys, wanted) + 63) & ~63u);
         if (p.run > MAX_RUN) p.run = MAX_RUN;
         if (p.run < 256) p.run = 256;
         p.splits = (int)ceil_div(p.keys, p.run);
         p.rows = (size_t)p.slab * heads;
         const size_t blocks = p.keys > SHORT_ROW ? ceil_div(p.keys, 1024) : 0;
-        p.bytes = align256((nr + 1) * p.rows * p.keys * 8) + align256(2 * p.rows * blocks * 8) + align256((size_t)n * p.rows * p.keys * NL) +
+        p.bytes = align256(nr * p.rows * p.keys * 8) + (blocks ? align256(p.rows * (p.keys + 2 * blocks) * 8) : 0) + align256((size_t)n * p.rows * p.keys * NL) +
                   (p.splits > 1 ? align256((size_t)p.splits * n * p.rows * dim * 8) : 0);
         if (p.bytes <= room && p.rows <= MAX_ROWS) return p;
         if (p.slab == 1) break;
@@ -881,12 +887,12 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
     const bool split_rows = plan.keys > SHORT_ROW;
     char *at = (char *)room;
     g.msg = (u64 *)at;
-    g.opened = g.msg + (size_t)nr * g.rows * g.keys;
-    at += align256((size_t)(nr + 1) * g.rows * g.keys * 8);
+    at += align256((size_t)nr * g.rows * g.keys * 8);
     if (split_rows) {
-        g.tops = (u64 *)at;
+        g.opened = (u64 *)at;
+        g.tops = g.opened + g.rows * g.keys;
         g.sums = g.tops + g.rows * blocks;
-        at += align256(2 * g.rows * blocks * 8);
+        at += align256(g.rows * (g.keys + 2 * blocks) * 8);
     }
     g.weights = (signed char *)at;
     at += align256((size_t)n * g.rows * g.keys * NL);
@@ -908,7 +914,19 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
             hipLaunchKernelGGL((scores_kernel<1>), sgrid, dim3(256), lds, stream, g, sp);
         else
             hipLaunchKernelGGL((scores_kernel<2>), sgrid, dim3(256), lds, stream, g, sp);
-#define SS_LAUNCH(NC, TC)                                                                        do {                                                                                               if (split_rows) {                                                                                  hipLaunchKernelGGL((open_kernel<TC>), wgrid, block, 0, stream, g, sp);                       hipLaunchKernelGGL(sum_kernel, wgrid, block, 0, stream, g, sp);                              hipLaunchKernelGGL((weights_kernel<NC, TC>), wgrid, block, 0, stream, g, sp);            } else if (blocks == 1)                                                                            hipLaunchKernelGGL((softmax_kernel<NC, TC, 1>), rgrid, block, 0, stream, g, sp);         else                                                                                               hipLaunchKernelGGL((softmax_kernel<NC, TC, 4>), rgrid, block, 0, stream, g, sp);     } while (0)
+#define SS_LAUNCH(NC, TC)                                                                               \
+    do {                                                                                                \
+        if (split_rows) {                                                                               \
+            hipLaunchKernelGGL((open_kernel<TC>), wgrid, block, 0, stream, g, sp);                      \
+            hipLaunchKernelGGL(sum_kernel, wgrid, block, 0, stream, g, sp);                             \
+            hipLaunchKernelGGL((weights_kernel<NC, TC>), wgrid, block, 0, stream, g, sp);               \
+        } else if (blocks == 1)                                                                         \
+            hipLaunchKernelGGL((softmax_kernel<NC, TC, 1, 256>), rgrid, block, 0, stream, g, sp);       \
+        else if (g.rows_now < 1024)                                                                     \
+            hipLaunchKernelGGL((softmax_kernel<NC, TC, 1, 1024>), rgrid, dim3(1024), 0, stream, g, sp); \
+        else                                                                                            \
+            hipLaunchKernelGGL((softmax_kernel<NC, TC, 4, 256>), rgrid, block, 0, stream, g, sp);       \
+    } while (0)
         SS_SCHEME(sp.n, sp.t, SS_LAUNCH);
 #undef SS_LAUNCH
         if (plan.row_tiles == 1)

@@ -388,6 +388,20 @@ def test_many_sequences(p, f):
 
 
 @gpu
+@pytest.mark.parametrize("n,t,p,f", SCHEMES)
+@pytest.mark.parametrize("chunk,length", [(2, 3000), (300, 1100), (1, 4097), (40, 4500)])
+def test_rows_of_every_length_class(n, t, p, f, chunk, length):
+    """the softmax of a row in one workgroup, small or large, or in several"""
+    c = Context(n, t, p, f, [chunk], [length], 4 if chunk < 100 else 5, 1, 16, 64)
+    if chunk == 300:                               # more rows than the oracle need see: its last tokens
+        c.q[0] = c.q[0][:, -3:]
+        want = orc.attention(c.q[0], c.k[0], c.v[0], t, f, fixed_scale(16), f, True, p, 21, 5, chunk - 3)
+        assert np.array_equal(host(c.run(f))[:, -3:], want)
+    else:
+        assert np.array_equal(host(c.run(f)), c.want(f))
+
+
+@gpu
 @pytest.mark.parametrize("n,t", [(3, 1), (5, 2)])
 def test_a_long_context_is_joined_from_several_runs(n, t):
     """longer than the 16383 products that a 32-bit sum of digits can take"""
@@ -420,17 +434,15 @@ def test_fraction_bits(f):
 
 
 @gpu
-def test_messages_are_the_masked_and_the_opened_scores():
+def test_messages_are_the_masked_scores():
     c = Context(5, 2, P61, 13, [3], [70], 2, 1, 32, 16)
     c.run(13)
-    _, msg, opened, _ = c.want(13, full=True)[0]
-    got = host(c.ss.messages())
+    _, msg, _, _ = c.want(13, full=True)[0]
     rows, keys = 3 * 2, 128
-    m = got[:5 * rows * keys].reshape(5, 3, 2, keys)
-    o = got[5 * rows * keys:6 * rows * keys].reshape(3, 2, keys)
+    m = host(c.ss.messages())[:5 * rows * keys].reshape(5, 3, 2, keys)
     for i in range(3):
         limit = 70 - 3 + i + 1
-        assert np.array_equal(m[:, i, :, :limit], msg[:, i, :, :limit]) and np.array_equal(o[i, :, :limit], opened[i, :, :limit])
+        assert np.array_equal(m[:, i, :, :limit], msg[:, i, :, :limit])
 
 
 @gpu
