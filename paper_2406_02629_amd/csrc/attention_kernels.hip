@@ -19,11 +19,19 @@ namespace SS_NS {
 namespace {
 
 constexpr int BLOCK = 256;
+constexpr size_t STREAM_BYTES = (size_t)256 << 20;   // what a call writes, from which on past the caches
+constexpr size_t WIDE_APPEND = (size_t)1 << 17;     // elements of the new keys from which on the kernels for many tokens take them
 constexpr size_t MAX_ROWS = (size_t)1 << 22;   // of a slab: a workgroup each, less than 2^32 threads in a launch
 constexpr size_t SHORT_ROW = 4096;   // keys up to which one workgroup takes the softmax of a row
 constexpr int MAX_RUN = 16320;      // keys that the 32-bit sums of the values can take, in blocks of 64: 8 * 16383 * 2^14 < 2^31
 
 inline unsigned ceil_div(size_t a, size_t b) { return (unsigned)((a + b - 1) / b); }
+
+// what describes the call does not change while it runs: read by way of the scalar cache wherever the index is the same for a wave
+typedef const int __attribute__((address_space(4))) *constant_ints;
+__device__ __forceinline__ int fixed_at(const int *p, size_t i) { return ((constant_ints)(uintptr_t)p)[i]; }
+typedef const long long __attribute__((address_space(4))) *constant_longs;
+__device__ __forceinline__ long long fixed_at(const long long *p, size_t i) { return ((constant_longs)(uintptr_t)p)[i]; }
 
 // ------------------------------------------------------------------ rotary positions
 
@@ -43,65 +51,85 @@ __device__ __forceinline__ u64 turn(u64 a, int c, u64 b, long long s)
 #endif
 }
 
-// SSS-Truncation of the element e whose shares of the parties 1..k are xq (any residue below 2^63): the new shares in o[]
-template <int N, int T>
-__device__ __forceinline__ void truncate_element(const u64 (&xq)[T + 1], size_t e, size_t count, u64 *__restrict__ u, u64 *__restrict__ wsh,
-                                                 const ss_tr_params &tp, u64 (&o)[MAXP<N>])
+// SSS-Truncation of VEC neighbours from element e on whose shares of the parties 1..k are xq (any residue below 2^63): the new shares in o[],
+// the messages of both steps to u [k][count] and wsh [n][count]
+template <int N, int T, int VEC, bool STREAM>
+__device__ __forceinline__ void truncate_elements(const u64 (&xq)[VEC][T + 1], size_t e, size_t count, u64 *__restrict__ u, u64 *__restrict__ wsh,
+                                                  const ss_tr_params &tp, pack_t<VEC> (&o)[MAXP<N>])
 {
     constexpr int K = T + 1;
-    const u64 counter = ss_counter(e);
-    u64 alpha, ca[T];
-    const u64 ev = mask_of<T>(tp, e, alpha);
+    const int n = N ? N : tp.n;
+    pack_t<VEC> um[K], w[MAXP<N>];
 #pragma unroll
-    for (int j = 0; j < T; j++) ca[j] = ss_draw_lazy_at(tp.alpha_key[j], counter);
-    ss_sacc2 acc;
-    acc.clear();
-    eval_points<T, K>(alpha, ca, [&](int q, u64 v) {
-        const u64 um = ss_reduce(xq[q] + v);
-        u[(size_t)q * count + e] = um;
-        SS_SPLIT31(um, w0, w1);
-        acc.mac(w0, w1, tp.ilambda[q]);
-    });
-    u64 secret;
-    shift_and_unmask<N, T, false>(acc.value(), ev, counter, e, count, wsh, tp, N ? N : tp.n, o, secret);
+    for (int c = 0; c < VEC; c++) {
+        const u64 counter = ss_counter(e + c);
+        u64 alpha, a[T], b[T];
+        const u64 ev = mask_of<T>(tp, e + c, alpha);
+#pragma unroll
+        for (int j = 0; j < T; j++) a[j] = ss_draw_lazy_at(tp.alpha_key[j], counter);
+        ss_sacc2 acc;
+        acc.clear();
+        eval_points<T, K>(alpha, a, [&](int q, u64 v) {
+            const u64 m = ss_reduce(xq[c][q] + v);
+            um[q].v[c] = m;
+            SS_SPLIT31(m, w0, w1);
+            acc.mac(w0, w1, tp.ilambda[q]);
+        });
+        // the elite party's quotient, shared; the mask off
+        const u64 quotient = shift_signed(acc.value(), tp.f);
+#pragma unroll
+        for (int j = 0; j < T; j++) {
+            a[j] = ss_draw_lazy_at(tp.gen_key[j], counter);
+            b[j] = ss_fold(a[j] + ss_draw_lazy_at(tp.alphat_key[j], counter));
+        }
+        eval_points<T, MAXP<N>>(quotient, a, [&](int m, u64 v) { w[m].v[c] = v; }, n);
+        eval_points<T, MAXP<N>>(ss_canon(quotient + SS_P - ev), b, [&](int m, u64 v) { o[m].v[c] = v; }, n);
+    }
+#pragma unroll
+    for (int q = 0; q < K; q++) um[q].template send<STREAM>(u + (size_t)q * count + e);
+#pragma unroll
+    for (int m = 0; m < MAXP<N>; m++)
+        if (N != 0 || m < n) w[m].template send<STREAM>(wsh + (size_t)m * count + e);
 }
 
-// where the pairs and the elements that pass through of a token's heads lie: `width` threads for each head
+// how a tensor of heads is dealt to threads: `width` threads to each head, of which `pairs` turn pairs
 struct rotary_shape {
-    int tokens, heads, dim, width;
+    int tokens, heads, dim, width, pairs;
     fdiv dWidth, dHeads;
 };
 
-__device__ __forceinline__ void pair_of(const ss_rope &rope, int j, int &a, int &b)
+// cosine and sine of pair j of a token
+__device__ __forceinline__ int2 angle_of(const ss_rope &rope, int token, int j)
 {
-    const int half = rope.rot >> 1;
-    a = rope.interleaved ? 2 * j : j;
-    b = rope.interleaved ? 2 * j + 1 : j + half;
+    return rope.table[(size_t)min(max(rope.pos[token], 0), rope.positions - 1) * (rope.rot >> 1) + j];
 }
 
-// the rotated and truncated pair j of (token, head): shares of both elements
+// pair j of (token, head), elements a and b, rotated and truncated: shares of both
 template <int N, int T>
 __device__ __forceinline__ void rotate_pair(const u64 *x, size_t ld, const rotary_shape &g, int token, int head, int j, u64 *__restrict__ u,
                                             u64 *__restrict__ wsh, const ss_rope &rope, const ss_tr_params &tp, int &a, int &b,
-                                            u64 (&oa)[MAXP<N>], u64 (&ob)[MAXP<N>])
+                                            pack_t<1> (&oa)[MAXP<N>], pack_t<1> (&ob)[MAXP<N>])
 {
     constexpr int K = T + 1;
-    pair_of(rope, j, a, b);
+    const int half = rope.rot >> 1;
+    a = rope.interleaved ? 2 * j : j;
+    b = rope.interleaved ? 2 * j + 1 : j + half;
     const u64 *row = x + (size_t)token * ld + (size_t)head * g.dim;
     const size_t party = (size_t)g.tokens * ld, count = (size_t)g.tokens * g.heads * rope.rot;
-    const int2 cs = rope.table[(size_t)min(max(rope.pos[token], 0), rope.positions - 1) * (rope.rot >> 1) + j];
-    u64 ra[K], rb[K];
+    const int2 cs = angle_of(rope, token, j);
+    u64 ra[1][K], rb[1][K];
 #pragma unroll
     for (int q = 0; q < K; q++) {
         const u64 xa = row[q * party + a], xb = row[q * party + b];
-        ra[q] = turn(xa, cs.x, xb, cs.y);
-        rb[q] = turn(xb, cs.x, xa, -(long long)cs.y);
+        ra[0][q] = turn(xa, cs.x, xb, cs.y);
+        rb[0][q] = turn(xb, cs.x, xa, -(long long)cs.y);
     }
     const size_t e = ((size_t)token * g.heads + head) * rope.rot;
-    truncate_element<N, T>(ra, e + a, count, u, wsh, tp, oa);
-    truncate_element<N, T>(rb, e + b, count, u, wsh, tp, ob);
+    truncate_elements<N, T, 1, false>(ra, e + a, count, u, wsh, tp, oa);
+    truncate_elements<N, T, 1, false>(rb, e + b, count, u, wsh, tp, ob);
 }
 
+// One thread per pair, or element that passes through, of a head.
 template <int N, int T>
 __global__ __launch_bounds__(BLOCK) void rotary_kernel(const u64 *x, size_t ld, u64 *__restrict__ u, u64 *__restrict__ wsh, u64 *out,
                                                        rotary_shape g, ss_rope rope, ss_tr_params tp)
@@ -109,25 +137,98 @@ __global__ __launch_bounds__(BLOCK) void rotary_kernel(const u64 *x, size_t ld, 
     const u32 i = blockIdx.x * BLOCK + threadIdx.x;
     if (i >= (u32)(g.tokens * g.heads * g.width)) return;
     const u32 th = fd_div(i, g.dWidth), token = fd_div(th, g.dHeads), head = th - token * g.heads;
-    const int j = (int)(i - th * g.width), half = rope.rot >> 1, n = N ? N : tp.n;
+    const int j = (int)(i - th * g.width), n = N ? N : tp.n;
     const size_t count = (size_t)g.tokens * g.heads * g.dim;
     u64 *dst = out + (size_t)th * g.dim;
-    if (j >= half) {
-        const int d = j + half;      // rot + (j - half)
+    if (j >= g.pairs) {
+        const int d = j + g.pairs;
 #pragma unroll
         for (int m = 0; m < MAXP<N>; m++)
-            if (N != 0 || m < n) dst[m * count + d] = x[(size_t)m * g.tokens * ld + (size_t)token * ld + (size_t)head * g.dim + d];
+            if (N != 0 || m < n) dst[m * count + d] = x[((size_t)m * g.tokens + token) * ld + (size_t)head * g.dim + d];
         return;
     }
     int a, b;
-    u64 oa[MAXP<N>], ob[MAXP<N>];
+    pack_t<1> oa[MAXP<N>], ob[MAXP<N>];
     rotate_pair<N, T>(x, ld, g, (int)token, (int)head, j, u, wsh, rope, tp, a, b, oa, ob);
 #pragma unroll
     for (int m = 0; m < MAXP<N>; m++)
         if (N != 0 || m < n) {
-            dst[m * count + a] = oa[m];
-            dst[m * count + b] = ob[m];
+            oa[m].store(dst + m * count + a);
+            ob[m].store(dst + m * count + b);
         }
+}
+
+// Neighbouring elements two at a time, 16 bytes to a load and a store: interleaved pair t, or pairs 2 t and 2 t + 1 of two halves, rotated and
+// truncated; emit(element of the head, shares of it and of the next), once or twice.  src: the head in share 1, `party` elements to the next
+// share, e: its number among the turned elements.  (Everything 16-byte aligned, strides and halves even.)
+template <int N, int T, bool INTERLEAVED, bool STREAM, typename F>
+__device__ __forceinline__ void rotate_two(const u64 *src, size_t party, size_t e, size_t count, int token, int t, u64 *__restrict__ u,
+                                           u64 *__restrict__ wsh, const ss_rope &rope, const ss_tr_params &tp, F &&emit)
+{
+    constexpr int K = T + 1;
+    pack_t<2> o[MAXP<N>];
+    u64 r[2][K];
+    if constexpr (INTERLEAVED) {
+        const int2 cs = angle_of(rope, token, t);
+#pragma unroll
+        for (int q = 0; q < K; q++) {
+            pack_t<2> v;
+            v.load(src + q * party + 2 * t);
+            r[0][q] = turn(v.v[0], cs.x, v.v[1], cs.y);
+            r[1][q] = turn(v.v[1], cs.x, v.v[0], -(long long)cs.y);
+        }
+        truncate_elements<N, T, 2, STREAM>(r, e + 2 * t, count, u, wsh, tp, o);
+        emit(2 * t, o);
+    } else {
+        const int half = rope.rot >> 1, j = 2 * t;
+        const int2 c0 = angle_of(rope, token, j), c1 = angle_of(rope, token, j + 1);
+        u64 rb[2][K];
+#pragma unroll
+        for (int q = 0; q < K; q++) {
+            pack_t<2> a, b;
+            a.load(src + q * party + j);
+            b.load(src + q * party + j + half);
+            r[0][q] = turn(a.v[0], c0.x, b.v[0], c0.y);
+            r[1][q] = turn(a.v[1], c1.x, b.v[1], c1.y);
+            rb[0][q] = turn(b.v[0], c0.x, a.v[0], -(long long)c0.y);
+            rb[1][q] = turn(b.v[1], c1.x, a.v[1], -(long long)c1.y);
+        }
+        truncate_elements<N, T, 2, STREAM>(r, e + j, count, u, wsh, tp, o);
+        emit(j, o);
+        truncate_elements<N, T, 2, STREAM>(rb, e + j + half, count, u, wsh, tp, o);
+        emit(j + half, o);
+    }
+}
+
+// The rotation of a head in such steps, or two elements that pass through, to a thread.  STREAM: messages and results past the caches.
+template <int N, int T, bool INTERLEAVED, bool STREAM>
+__global__ __launch_bounds__(BLOCK) void rotary_wide_kernel(const u64 *x, size_t ld, u64 *__restrict__ u, u64 *__restrict__ wsh, u64 *out,
+                                                            rotary_shape g, ss_rope rope, ss_tr_params tp)
+{
+    const u32 i = blockIdx.x * BLOCK + threadIdx.x;
+    if (i >= (u32)(g.tokens * g.heads * g.width)) return;
+    const u32 th = fd_div(i, g.dWidth), token = fd_div(th, g.dHeads), head = th - token * g.heads;
+    const int t = (int)(i - th * g.width), n = N ? N : tp.n;
+    const size_t plane = (size_t)g.tokens * g.heads * g.dim, party = (size_t)g.tokens * ld, count = (size_t)g.tokens * g.heads * rope.rot;
+    const u64 *src = x + (size_t)token * ld + (size_t)head * g.dim;
+    u64 *dst = out + (size_t)th * g.dim;
+    if (t >= g.pairs) {
+        const int d = rope.rot + 2 * (t - g.pairs);
+#pragma unroll
+        for (int m = 0; m < MAXP<N>; m++)
+            if (N != 0 || m < n) {
+                pack_t<2> v;
+                v.load(src + m * party + d);
+                v.template send<STREAM>(dst + m * plane + d);
+            }
+        return;
+    }
+    rotate_two<N, T, INTERLEAVED, STREAM>(src, party, (size_t)th * rope.rot, count, (int)token, t, u, wsh, rope, tp,
+                                          [&](int d, const pack_t<2> (&o)[MAXP<N>]) {
+#pragma unroll
+                                              for (int m = 0; m < MAXP<N>; m++)
+                                                  if (N != 0 || m < n) o[m].template send<STREAM>(dst + m * plane + d);
+                                          });
 }
 
 // ------------------------------------------------------------------ appending to the cache
@@ -138,13 +239,15 @@ struct append_shape {
     signed char *keys, *values;
     size_t party, head, page;          // strides in bytes
     unsigned capacity, page_size;      // keys of the cache, of a page
+    int steps, step_blocks;            // many tokens: threads to a key, in blocks of 16
+    int value_blocks;                  // workgroups to 16 tokens of the values
     fdiv dPage;
 };
 
 // of the token's place in the cache: its cell in head 0 of party 0, and the key inside the cell
 __device__ __forceinline__ bool place_of(const append_shape &s, int token, size_t &cell, int &key)
 {
-    const long long slot = s.slots[token];
+    const long long slot = fixed_at(s.slots, token);
     if (slot < 0 || slot >= (long long)s.capacity) return false;
     const u32 page = fd_div((u32)slot, s.dPage), in = (u32)slot - page * s.page_size;
     key = (int)(in & 15);
@@ -153,26 +256,26 @@ __device__ __forceinline__ bool place_of(const append_shape &s, int token, size_
 }
 
 template <int N>
-__device__ __forceinline__ void put_key(const append_shape &s, size_t cell, int key, int head, int d, const u64 (&v)[MAXP<N>], int n)
+__device__ __forceinline__ void put_key(const append_shape &s, size_t cell, int key, int head, int d, const pack_t<1> (&v)[MAXP<N>], int n)
 {
 #pragma unroll
     for (int m = 0; m < MAXP<N>; m++)
         if (N != 0 || m < n) {
-            const u64 dig = balanced_digits(v[m]);
+            const u64 dig = balanced_digits(v[m].v[0]);
             signed char *c = s.keys + cell + m * s.party + head * s.head + (d >> 4) * 256 + key * 16 + (d & 15);
 #pragma unroll
             for (int l = 0; l < SS_NLIMB; l++) c[(size_t)l * s.r.dim * 16] = (signed char)(dig >> (8 * l));
         }
 }
 
-// One thread per pair (or element that passes through) of a key, then one per element of a value.
+// A few tokens: one thread per pair (or element that passes through) of a key, then one per element of a value; digits go out as bytes.
 template <int N, int T>
 __global__ __launch_bounds__(BLOCK) void append_kernel(const u64 *k, size_t ld_k, const u64 *v, size_t ld_v, u64 *__restrict__ u,
                                                        u64 *__restrict__ wsh, append_shape s, ss_rope rope, ss_tr_params tp, u32 key_blocks)
 {
     const int n = N ? N : tp.n;
     const rotary_shape &g = s.r;
-    u64 o[MAXP<N>];
+    pack_t<1> o[MAXP<N>];
     size_t cell;
     int key;
     if (blockIdx.x >= key_blocks) {
@@ -193,23 +296,145 @@ __global__ __launch_bounds__(BLOCK) void append_kernel(const u64 *k, size_t ld_k
     const u32 i = blockIdx.x * BLOCK + threadIdx.x;
     if (i >= (u32)(g.tokens * g.heads * g.width)) return;
     const u32 th = fd_div(i, g.dWidth), token = fd_div(th, g.dHeads), head = th - token * g.heads;
-    const int j = (int)(i - th * g.width), half = rope.rot >> 1;
+    const int j = (int)(i - th * g.width);
     const bool placed = place_of(s, (int)token, cell, key);
-    if (j >= half) {
+    if (j >= g.pairs) {
         if (!placed) return;
-        const int d = j + half;
+        const int d = j + g.pairs;
 #pragma unroll
         for (int m = 0; m < MAXP<N>; m++)
-            if (N != 0 || m < n) o[m] = k[((size_t)m * g.tokens + token) * ld_k + (size_t)head * g.dim + d];
+            if (N != 0 || m < n) o[m].load(k + ((size_t)m * g.tokens + token) * ld_k + (size_t)head * g.dim + d);
         put_key<N>(s, cell, key, (int)head, d, o, n);
         return;
     }
     int a, b;
-    u64 ob[MAXP<N>];
+    pack_t<1> ob[MAXP<N>];
     rotate_pair<N, T>(k, ld_k, g, (int)token, (int)head, j, u, wsh, rope, tp, a, b, o, ob);
     if (!placed) return;
     put_key<N>(s, cell, key, (int)head, a, o, n);
     put_key<N>(s, cell, key, (int)head, b, ob, n);
+}
+
+// Many tokens go in blocks of 16 that end with a cell if the tokens follow one another in the cache: the first block lacks as many as there
+// are keys in front of the first token.
+__device__ __forceinline__ int first_of_block(const append_shape &s, int block)
+{
+    const long long slot = fixed_at(s.slots, 0);
+    return block * 16 - (slot < 0 ? 0 : (int)(slot & 15));
+}
+
+// Elements d and d + 1 of a key, from each of two neighbouring lanes, which have four in a row between them: each lane stores the dwords of half
+// of the limbs.
+template <int N, typename F>
+__device__ __forceinline__ void put_key_four(const append_shape &s, size_t cell, int key, int head, int d, int n, F &&value)
+{
+    constexpr int HALF = SS_NLIMB / 2;
+    const bool odd = threadIdx.x & 1;
+    signed char *c = s.keys + cell + head * s.head + (d >> 4) * 256 + key * 16 + (d & 12) + (odd ? (size_t)HALF * s.r.dim * 16 : 0);
+#pragma unroll
+    for (int m = 0; m < MAXP<N>; m++)
+        if (N != 0 || m < n) {
+            u32 y[4];
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const u64 dig = balanced_digits(value(m, i));
+                const u32 low = (u32)dig, high = (u32)(dig >> (8 * HALF)), keep = odd ? high : low, give = odd ? low : high;
+                const u32 got = (u32)__builtin_amdgcn_update_dpp(0, (int)give, 0xB1, 0xF, 0xF, true);   // the other lane of the two
+                y[i] = odd ? got : keep;
+                y[2 + i] = odd ? keep : got;
+            }
+#pragma unroll
+            for (int l = 0; l < HALF; l++) {
+                const u32 sel = (u32)l | ((u32)(4 + l) << 8) | 0x0c0c0000u;
+                *reinterpret_cast<u32 *>(c + m * s.party + (size_t)l * s.r.dim * 16) =
+                    __builtin_amdgcn_perm(__builtin_amdgcn_perm(y[3], y[2], sel), __builtin_amdgcn_perm(y[1], y[0], sel), 0x05040100u);
+            }
+        }
+}
+
+// Many tokens, keys: eight lanes take 16 elements (or twice 16) of a token two (or two and two) at a time, a wave eight tokens, so that where
+// the tokens follow one another in the cache its dwords of a limb lie in a row, 128 bytes of a cell.  (Halves of a head in multiples of
+// four, 16-byte alignment.)
+template <int N, int T, bool INTERLEAVED>
+__device__ __forceinline__ void append_keys(const u64 *k, size_t ld, u64 *__restrict__ u, u64 *__restrict__ wsh, const append_shape &s,
+                                            const ss_rope &rope, const ss_tr_params &tp, int group, int step_block, int head)
+{
+    const int n = N ? N : tp.n, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const rotary_shape &g = s.r;
+    const int step = step_block * 16 + (wave >> 1) * 8 + (lane & 7);
+    const int token = first_of_block(s, group) + (wave & 1) * 8 + (lane >> 3);
+    if (token < 0 || token >= g.tokens || step >= s.steps) return;   // (never one of two lanes alone: steps are even)
+    size_t cell;
+    int key;
+    const bool placed = place_of(s, token, cell, key);
+    const size_t party = (size_t)g.tokens * ld;
+    const u64 *src = k + (size_t)token * ld + (size_t)head * g.dim;
+    const int turning = INTERLEAVED ? g.pairs : g.pairs >> 1;
+    if (step >= turning) {
+        if (!placed) return;
+        const int d = rope.rot + (step - turning) * 2;
+        put_key_four<N>(s, cell, key, head, d, n, [&](int m, int i) { return src[m * party + d + i]; });
+        return;
+    }
+    const size_t count = (size_t)g.tokens * g.heads * rope.rot, e = ((size_t)token * g.heads + head) * rope.rot;
+    rotate_two<N, T, INTERLEAVED, false>(src, party, e, count, token, step, u, wsh, rope, tp, [&](int d, const pack_t<2> (&o)[MAXP<N>]) {
+        if (placed) put_key_four<N>(s, cell, key, head, d, n, [&](int m, int i) { return o[m].v[i]; });
+    });
+}
+
+// Many tokens, values: a thread takes one element of 16 tokens of one party.  Where they are the 16 keys of a cell, in order, it stores 16
+// bytes of every limb and a wave 1 KB in a row; otherwise (ends of a run of tokens) bytes.
+__device__ __forceinline__ void append_values(const u64 *v, size_t ld, const append_shape &s, int group, int m, int d, int head)
+{
+    const rotary_shape &g = s.r;
+    const int t0 = first_of_block(s, group);
+    const u64 *src = v + (size_t)m * g.tokens * ld + (size_t)head * g.dim + d;
+    u64 y[4][4];
+#pragma unroll
+    for (int i = 0; i < 16; i++) y[i >> 2][i & 3] = src[(size_t)min(max(t0 + i, 0), g.tokens - 1) * ld];
+    size_t cell;
+    int key;
+    bool run = t0 >= 0 && t0 + 16 <= g.tokens && place_of(s, t0, cell, key) && key == 0;   // uniform
+    if (run) {
+        const long long slot = fixed_at(s.slots, t0);
+#pragma unroll
+        for (int i = 1; i < 16; i++) run &= fixed_at(s.slots, t0 + i) == slot + i;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; i++) y[i >> 2][i & 3] = balanced_digits(y[i >> 2][i & 3]);
+    signed char *dst = s.values + m * s.party + head * s.head + d * 16;
+    const size_t limb = (size_t)g.dim * 16;
+    if (run) {
+#pragma unroll
+        for (int l = 0; l < SS_NLIMB; l++)
+            *reinterpret_cast<v4i *>(dst + cell + l * limb) =
+                (v4i){(int)limb_dword(y[0], l), (int)limb_dword(y[1], l), (int)limb_dword(y[2], l), (int)limb_dword(y[3], l)};
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; i++)
+        if (t0 + i >= 0 && t0 + i < g.tokens && place_of(s, t0 + i, cell, key)) {
+#pragma unroll
+            for (int l = 0; l < SS_NLIMB; l++) dst[cell + l * limb + key] = (signed char)(y[i >> 2][i & 3] >> (8 * l));
+        }
+}
+
+// Both in one launch: grid.x blocks of 16 tokens by blocks of 16 steps of the keys, then by blocks of 256 elements and parties of the values;
+// grid.y heads.
+template <int N, int T, bool INTERLEAVED>
+__global__ __launch_bounds__(BLOCK) void append_many_kernel(const u64 *k, size_t ld_k, const u64 *v, size_t ld_v, u64 *__restrict__ u,
+                                                            u64 *__restrict__ wsh, append_shape s, ss_rope rope, ss_tr_params tp, int key_blocks,
+                                                            fdiv dDim)
+{
+    const int n = N ? N : tp.n, head = blockIdx.y;
+    if ((int)blockIdx.x < key_blocks) {
+        const int group = (int)blockIdx.x / s.step_blocks;
+        append_keys<N, T, INTERLEAVED>(k, ld_k, u, wsh, s, rope, tp, group, (int)blockIdx.x - group * s.step_blocks, head);
+        return;
+    }
+    const int at = (int)blockIdx.x - key_blocks, group = at / s.value_blocks;
+    const u32 i = (u32)(at - group * s.value_blocks) * BLOCK + threadIdx.x, m = fd_div(i, dDim);
+    if ((int)m < n) append_values(v, ld_v, s, group, (int)m, (int)(i - m * s.r.dim), head);
 }
 
 // ------------------------------------------------------------------ attention
@@ -236,10 +461,6 @@ struct attn_args {
 struct seq_span {
     int first, count, limit, step;  // limit of token first + i: limit + i * step, at least 0
 };
-
-// what describes the call does not change while it runs: read by way of the scalar cache wherever the index is the same for a wave
-typedef const int __attribute__((address_space(4))) *constant_ints;
-__device__ __forceinline__ int fixed_at(const int *p, size_t i) { return ((constant_ints)(uintptr_t)p)[i]; }
 
 __device__ __forceinline__ seq_span span_of(const attn_args &g, int b)
 {
@@ -782,32 +1003,50 @@ __global__ __launch_bounds__(BLOCK) void join_kernel(attn_args g, int n, fdiv dD
     g.out[((size_t)party * g.s.tokens + g.tok0) * g.heads * g.c.dim + i] = o;
 }
 
-rotary_shape make_shape(int tokens, int heads, int dim, int rot)
+rotary_shape make_shape(int tokens, int heads, int dim, int pairs, int width)
 {
-    const int width = dim - rot / 2;
-    return {tokens, heads, dim, width, make_fdiv((u32)width), make_fdiv((u32)heads)};
+    return {tokens, heads, dim, width, pairs, make_fdiv((u32)width), make_fdiv((u32)heads)};
 }
 
 size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 }  // namespace
 
 hipError_t ss_launch_rotary(const u64 *x, size_t ld, u64 *u, u64 *wsh, u64 *out, int tokens, int heads, int dim, const ss_rope &rope,
                             const ss_tr_params &tp, hipStream_t stream)
 {
-    const rotary_shape g = make_shape(tokens, heads, dim, rope.rot);
-    const dim3 grid(ceil_div((size_t)tokens * heads * g.width, BLOCK));
-#define SS_LAUNCH(NC, TC) hipLaunchKernelGGL((rotary_kernel<NC, TC>), grid, dim3(BLOCK), 0, stream, x, ld, u, wsh, out, g, rope, tp)
+    const int half = rope.rot / 2;
+    const bool wide = (rope.interleaved || half % 2 == 0) && dim % 2 == 0 && ld % 2 == 0 && aligned16(x) && aligned16(out);
+    const int pairs = !wide ? half : rope.interleaved ? half : half / 2, width = wide ? pairs + (dim - rope.rot) / 2 : dim - half;
+    const rotary_shape g = make_shape(tokens, heads, dim, pairs, width);
+    const dim3 grid(ceil_div((size_t)tokens * heads * width, BLOCK));
+    // messages and results past the caches where they are more than these hold
+    const bool streams = (size_t)tokens * heads * ((size_t)rope.rot * (tp.t + 1 + tp.n) + (size_t)dim * 2 * tp.n) * 8 > STREAM_BYTES;
+#define SS_WIDE(NC, TC, I)                                                                                                       \
+    hipLaunchKernelGGL((streams ? rotary_wide_kernel<NC, TC, I, true> : rotary_wide_kernel<NC, TC, I, false>), grid, dim3(BLOCK), 0, \
+                       stream, x, ld, u, wsh, out, g, rope, tp)
+#define SS_LAUNCH(NC, TC)                                                                                              \
+    do {                                                                                                               \
+        if (!wide)                                                                                                     \
+            hipLaunchKernelGGL((rotary_kernel<NC, TC>), grid, dim3(BLOCK), 0, stream, x, ld, u, wsh, out, g, rope, tp); \
+        else if (rope.interleaved)                                                                                     \
+            SS_WIDE(NC, TC, true);                                                                                     \
+        else                                                                                                           \
+            SS_WIDE(NC, TC, false);                                                                                    \
+    } while (0)
     SS_SCHEME(tp.n, tp.t, SS_LAUNCH);
 #undef SS_LAUNCH
+#undef SS_WIDE
     return hipGetLastError();
 }
 
 hipError_t ss_launch_append(const ss_paged &c, const u64 *k, size_t ld_k, const u64 *v, size_t ld_v, int tokens, const long long *slots,
                             u64 *u, u64 *wsh, const ss_rope &rope, const ss_tr_params &tp, hipStream_t stream)
 {
+    const int half = rope.rot / 2;
     append_shape s = {};
-    s.r = make_shape(tokens, c.kv, c.dim, rope.rot);
+    s.r = make_shape(tokens, c.kv, c.dim, half, c.dim - half);
     s.slots = slots;
     s.keys = c.keys;
     s.values = c.values;
@@ -817,6 +1056,20 @@ hipError_t ss_launch_append(const ss_paged &c, const u64 *k, size_t ld_k, const 
     s.page_size = (unsigned)c.page_cells * 16;
     s.capacity = s.page_size * (unsigned)c.pages;
     s.dPage = make_fdiv(s.page_size);
+    if ((size_t)tokens * c.kv * c.dim >= WIDE_APPEND && tokens >= 16 && half % 4 == 0 && ld_k % 2 == 0 && aligned16(k)) {
+        s.steps = (rope.interleaved ? half : half / 2) + (c.dim - rope.rot) / 2;
+        s.step_blocks = (int)ceil_div(s.steps, 16);
+        s.value_blocks = (int)ceil_div((size_t)tp.n * c.dim, BLOCK);
+        const unsigned groups = ceil_div((size_t)tokens + 15, 16);
+        const int keys = (int)groups * s.step_blocks;
+        const dim3 grid(keys + groups * s.value_blocks, c.kv);
+#define SS_LAUNCH(NC, TC)                                                                                                  \
+    hipLaunchKernelGGL((rope.interleaved ? append_many_kernel<NC, TC, true> : append_many_kernel<NC, TC, false>), grid, dim3(BLOCK), 0, \
+                       stream, k, ld_k, v, ld_v, u, wsh, s, rope, tp, keys, make_fdiv((u32)c.dim))
+        SS_SCHEME(tp.n, tp.t, SS_LAUNCH);
+#undef SS_LAUNCH
+        return hipGetLastError();
+    }
     const unsigned key_blocks = ceil_div((size_t)tokens * c.kv * s.r.width, BLOCK);
     const dim3 grid(key_blocks + ceil_div((size_t)tokens * c.kv * c.dim, BLOCK));
 #define SS_LAUNCH(NC, TC) \

@@ -6,6 +6,52 @@
 
 namespace SS_NS {
 
+template <int VEC>
+struct pack_t;
+template <>
+struct pack_t<1> {
+    u64 v[1];
+    __device__ __forceinline__ void load(const u64 *p) { v[0] = *p; }
+    __device__ __forceinline__ void load_streaming(const u64 *p) { v[0] = __builtin_nontemporal_load(p); }
+    __device__ __forceinline__ void store(u64 *p) const { *p = v[0]; }
+    __device__ __forceinline__ void store_streaming(u64 *p) const { __builtin_nontemporal_store(v[0], p); }
+    template <bool STREAM>
+    __device__ __forceinline__ void send(u64 *p) const { STREAM ? store_streaming(p) : store(p); }
+};
+template <>
+struct pack_t<2> {
+    u64 v[2];
+    __device__ __forceinline__ void load(const u64 *p)
+    {
+        const ulonglong2 q = *reinterpret_cast<const ulonglong2 *>(p);
+        v[0] = q.x;
+        v[1] = q.y;
+    }
+    __device__ __forceinline__ void load_streaming(const u64 *p)
+    {
+        typedef unsigned long long v2u __attribute__((ext_vector_type(2)));
+        const v2u q = __builtin_nontemporal_load(reinterpret_cast<const v2u *>(p));
+        v[0] = q.x;
+        v[1] = q.y;
+    }
+    __device__ __forceinline__ void store(u64 *p) const
+    {
+        ulonglong2 q;
+        q.x = v[0];
+        q.y = v[1];
+        *reinterpret_cast<ulonglong2 *>(p) = q;
+    }
+    // for output that nothing in the same launch reads again
+    __device__ __forceinline__ void store_streaming(u64 *p) const
+    {
+        typedef unsigned long long v2u __attribute__((ext_vector_type(2)));
+        v2u q = {v[0], v[1]};
+        __builtin_nontemporal_store(q, reinterpret_cast<v2u *>(p));
+    }
+    template <bool STREAM>
+    __device__ __forceinline__ void send(u64 *p) const { STREAM ? store_streaming(p) : store(p); }
+};
+
 // A message that nothing in the launch reads again.  STREAM: past the caches, see streams_messages.
 template <bool STREAM>
 __device__ __forceinline__ void send(u64 *p, u64 v)

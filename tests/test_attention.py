@@ -249,14 +249,15 @@ def cells_of(shares, digits, values):
 @gpu
 @pytest.mark.parametrize("n,t,p,f", SCHEMES)
 @pytest.mark.parametrize("tokens,heads,dim,rot,page", [(1, 1, 16, 0, 16), (5, 2, 48, 32, 32), (70, 3, 64, 64, 16), (150, 1, 128, 128, 64), (33, 2, 80, 20, 48),
-                                                       (66, 1, 96, 0, 16)])
+                                                       (66, 1, 96, 0, 16), (430, 2, 160, 160, 32), (300, 7, 64, 24, 64), (1030, 1, 128, 0, 16),
+                                                       (515, 2, 128, 20, 16)])
 def test_append_matches_the_oracle(n, t, p, f, tokens, heads, dim, rot, page):
     rng = np.random.default_rng(dim)
     digits = 6 if p == P45 else 8
     k, v = (shares_of(rng.standard_normal((tokens, heads, dim)), n, t, f, p, s) for s in (3, 4))
     pages = -(-tokens // page) + 2
-    for order in ("run", "scattered"):
-        slots = np.arange(tokens) + (page // 2 if order == "run" else 0)
+    for order in ("cells", "run", "scattered"):
+        slots = np.arange(tokens) + (page // 2 + 5 if order == "run" else 0)
         if order == "scattered":
             slots = rng.permutation(pages * page)[:tokens]
         if tokens > 4:                                      # left out
