@@ -730,7 +730,12 @@ struct row_norm {
 __device__ __forceinline__ row_norm norm_of(u64 sum)
 {
     const int drop = max(0, 32 - __clzll((long long)sum));
-    return {(1ull << 62) / (sum >> drop), drop};
+    // floor(2^62 / x), 2^30 <= x < 2^32, by way of a quotient in 53 bits that is off by one at most
+    const u64 x = sum >> drop;
+    u64 q = (u64)(4611686018427387904.0 / (double)x);
+    const long long rest = (long long)((1ull << 62) - q * x);
+    q = rest < 0 ? q - 1 : rest >= (long long)x ? q + 1 : q;
+    return {q, drop};
 }
 
 // The weights of four keys (w, 30 fraction bits, 0 beyond the limit; `seen` of them are keys that the row sees), shared, as digits.
@@ -766,31 +771,24 @@ __global__ __launch_bounds__(THREADS) void softmax_kernel(attn_args g, ss_softma
     row_place r;
     if (!row_at(g, blockIdx.x, r)) return;
     const int tid = threadIdx.x;
-    long long d[RUNS][4], top = -(1ll << 62);
+    __shared__ u64 first;
+    u64 v[RUNS][4];
+    long long top = -(1ll << 62);
     u32 w[RUNS][4];
-    u64 ref = 0;
-    if (r.limit) {                               // the first key: differences of a row are small, whatever its mask is
-        ss_sacc2 acc;
-        acc.clear();
-#pragma unroll
-        for (int i = 0; i < 2 * T + 1; i++) {
-            const u64 m = g.msg[(i * g.rows + r.id) * g.keys];
-            SS_SPLIT31(m, w0, w1);
-            acc.mac(w0, w1, sp.ilambda[i]);
-        }
-        ref = acc.value();
-    }
 #pragma unroll
     for (int u = 0; u < RUNS; u++) {
         const int j = (u * THREADS + tid) * 4;
-        if (j >= r.limit) break;
-        u64 v[4];
-        open_scores<T>(g, sp, r, j, v);
+        if (j < r.limit) open_scores<T>(g, sp, r, j, v[u]);
+    }
+    if (tid == 0) first = v[0][0];
+    __syncthreads();
+    const u64 ref = first;                       // differences of a row are small, whatever its mask is
 #pragma unroll
-        for (int c = 0; c < 4; c++) {
-            d[u][c] = lift(ss_sub(v[c], ref));
-            if (j + c < r.limit) top = max(top, d[u][c]);
-        }
+    for (int u = 0; u < RUNS; u++) {
+        const int j = (u * THREADS + tid) * 4;
+#pragma unroll
+        for (int c = 0; c < 4; c++)
+            if (j + c < r.limit) top = max(top, lift(ss_sub(v[u][c], ref)));
     }
     top = block_reduce<THREADS>(top, red, [](long long x, long long y) { return max(x, y); });
     long long sum = 0;
@@ -799,7 +797,7 @@ __global__ __launch_bounds__(THREADS) void softmax_kernel(attn_args g, ss_softma
         const int j = (u * THREADS + tid) * 4;
 #pragma unroll
         for (int c = 0; c < 4; c++) {
-            w[u][c] = j + c < r.limit ? softmax_weight(top - d[u][c], sp) : 0;
+            w[u][c] = j + c < r.limit ? softmax_weight(top - lift(ss_sub(v[u][c], ref)), sp) : 0;
             sum += w[u][c];
         }
     }
@@ -889,19 +887,19 @@ __global__ __launch_bounds__(BLOCK) void weights_kernel(attn_args g, ss_softmax_
     if (j < r.covered) share_weights<N, T>(g, sp, r, j, w, r.limit - j, nm);
 }
 
-// Step 3: one workgroup per (tile of 16 MT rows, run of keys and up to 128 elements of the head, kv head and party); a wave takes 16
+// Step 3: one workgroup per (tile of 16 MT rows, run of keys and up to 64 elements of the head, kv head and party); a wave takes 16
 // elements.  The digits of 64 weights of every row go through LDS to all waves, those of the values to a wave's registers; the next
 // 64 keys are on their way while those at hand are multiplied.  (The weights too by way of registers: behind copies straight into LDS the
 // compiler waits before the next read of any LDS.)
 template <int MT>
-__global__ __launch_bounds__(512) void values_kernel(attn_args g, int n)
+__global__ __launch_bounds__(256, 2) void values_kernel(attn_args g, int n)
 {
     __shared__ v4i wd[2][MT * TILE];
     __shared__ size_t cells[MAX_RUN / 16 + 4];
     __shared__ int rowid[16 * MT];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int head = blockIdx.z / n, party = blockIdx.z - head * n;
-    const int split = blockIdx.y / g.dblocks, dt = (blockIdx.y - split * g.dblocks) * waves + wave;   // 16 elements each
+    const int split = blockIdx.y / g.dblocks, dt = (blockIdx.y - split * g.dblocks) * 4 + wave;   // 16 elements each
     int row0 = 0;
     const int b = __builtin_amdgcn_readfirstlane(find_tile(g, blockIdx.x, row0));
     if (b < 0) return;
@@ -911,7 +909,7 @@ __global__ __launch_bounds__(512) void values_kernel(attn_args g, int n)
     const int lim = limit_at(s, (int)fd_div((u32)(row0 + nrows - 1), g.dGroup));
     const int k0 = split * g.run, k1 = min(k0 + g.run, lim), units = (k1 - k0 + 63) >> 6;
     if (split && k0 >= lim) return;              // (the first run writes the zeros of rows that see nothing)
-    for (int c = tid; c < units * 4; c += blockDim.x) cells[c] = cell_at(g, b, k0 / 16 + c);
+    for (int c = tid; c < units * 4; c += 256) cells[c] = cell_at(g, b, k0 / 16 + c);
     if (tid < 16 * MT) {
         const int r = min(tid, nrows - 1), i = (int)fd_div((u32)(row0 + r), g.dGroup);
         rowid[tid] = (s.first + i - g.tok0) * g.heads + head * g.group + row0 + r - i * g.group;
@@ -927,21 +925,19 @@ __global__ __launch_bounds__(512) void values_kernel(attn_args g, int n)
         clear(acc[m]);
         wrow[m] = g.weights + ((size_t)party * g.rows + rowid[m * 16 + (lane & 15)]) * g.keys * NL + (lane >> 4) * 16 + (size_t)k0 * NL;
     }
-    // limb slices of the weights that this wave brings to LDS: numbers wave, wave + waves, ... of MT NL; 4 waves or more
+    // limb slices of the weights that this wave brings to LDS: numbers wave, wave + 4, ... of MT NL
     constexpr int SLICES = MT * NL, MOST = (SLICES + 3) / 4;
     v4i slice[MOST];
     auto load_weights = [&](int unit) {
 #pragma unroll
         for (int k = 0; k < MOST; k++) {
-            const int q = wave + k * waves;      // uniform
-            if (q < SLICES)
-                slice[k] = *reinterpret_cast<const v4i *>((MT == 1 || q < NL ? wrow[0] : wrow[MT - 1]) + (size_t)unit * (64 * NL) + (q < NL ? q : q - NL) * 64);
+            const int q = min(wave + 4 * k, SLICES - 1);   // (twice the last where they do not come out even)
+            slice[k] = *reinterpret_cast<const v4i *>((MT == 1 || q < NL ? wrow[0] : wrow[MT - 1]) + (size_t)unit * (64 * NL) + (q < NL ? q : q - NL) * 64);
         }
     };
     auto keep_weights = [&](int stage) {
 #pragma unroll
-        for (int k = 0; k < MOST; k++)
-            if (wave + k * waves < SLICES) wd[stage][(wave + k * waves) * 64 + lane] = slice[k];
+        for (int k = 0; k < MOST; k++) wd[stage][min(wave + 4 * k, SLICES - 1) * 64 + lane] = slice[k];
     };
     auto load_values = [&](int unit, v4i (&v)[NL]) {
         const signed char *src = base + cells[unit * 4 + (lane >> 4)];
@@ -1083,17 +1079,20 @@ attention_plan plan_attention(int n, int t, int tokens, int seqs, int heads, int
 {
     attention_plan p = {};
     const size_t group = heads / kv, nr = 2 * t + 1;
-    p.row_tiles = ceil_div(tokens, seqs) * group > 16 ? 2 : 1;
-    p.key_block = p.row_tiles == 1 ? 128 : 512;
     p.keys = ((size_t)max_length + 63) & ~(size_t)63;
-    p.dblocks = ceil_div(dim, p.row_tiles == 1 ? 64 : 128);
-    p.waves = (int)ceil_div(dim / 16, p.dblocks);
-    if (p.waves < 4) p.waves = 4;
+    // workgroups of the scores with tiles of 32 rows.  Larger tiles and blocks read less, but leave fewer waves to a SIMD and fewer workgroups:
+    // scores + values, us, tiles of 32 / of 16 rows: chunk of 512 tokens over 4096, n = 5 (10400 workgroups) 1975 / 2085; chunks of 17 to 121
+    // over 121 to 777, n = 5 (1160) 155 / 129; 230 tokens over 700 to 1024, n = 3, 45-bit prime (480) 64 / 62.  Blocks of 128 keys against 256
+    // with 16 rows, scores alone: single tokens 157 / 159 and 92 / 94, the two chunks above 76 / 71 and 36.5 / 33; of 512 against 1024 with 32: 1079 / 1040.
+    const size_t sequence_rows = ceil_div(tokens, seqs) * group, tiles = tokens * group / 32 + seqs, wgs = tiles * ceil_div(p.keys, 512) * kv * nr;
+    p.row_tiles = sequence_rows > 16 && wgs >= 2048 ? 2 : 1;
+    p.key_block = p.row_tiles == 2 ? (wgs >= 8192 ? 1024 : 512) : sequence_rows > 16 ? 256 : 128;
+    p.dblocks = ceil_div(dim, 64);
     p.slab = tokens;
     for (;;) {
         const size_t tile = 16 * p.row_tiles, tiles = p.slab * group / tile + seqs;
         const size_t base = tiles * p.dblocks * kv * n;
-        const size_t wanted = ceil_div(p.row_tiles == 1 ? 2048 : 1024, base);
+        const size_t wanted = ceil_div(sequence_rows <= 16 ? 2048 : 1024, base);
         p.run = (int)((ceil_div(p.keys, wanted) + 63) & ~63u);
         if (p.run > MAX_RUN) p.run = MAX_RUN;
         if (p.run < 256) p.run = 256;
@@ -1183,9 +1182,9 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
         SS_SCHEME(sp.n, sp.t, SS_LAUNCH);
 #undef SS_LAUNCH
         if (plan.row_tiles == 1)
-            hipLaunchKernelGGL((values_kernel<1>), vgrid, dim3(64 * plan.waves), 0, stream, g, n);
+            hipLaunchKernelGGL((values_kernel<1>), vgrid, dim3(256), 0, stream, g, n);
         else
-            hipLaunchKernelGGL((values_kernel<2>), vgrid, dim3(64 * plan.waves), 0, stream, g, n);
+            hipLaunchKernelGGL((values_kernel<2>), vgrid, dim3(256), 0, stream, g, n);
         if (plan.splits > 1)
             hipLaunchKernelGGL(join_kernel, dim3(ceil_div((size_t)g.rows_now * cache.dim, BLOCK), n), block, 0, stream, g, n, make_fdiv((u32)cache.dim));
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;

@@ -259,7 +259,7 @@ struct attention_plan {
     int slab;                     // tokens, 0: the room is too small
     int splits, run;
     int key_block;                // keys of a workgroup of the scores
-    int dblocks, waves;           // workgroups to a head in the values, and their waves of 16 elements each
+    int dblocks;                  // workgroups to a head in the values, 64 elements each
     size_t keys;                  // of a row in the messages: the longest context in whole blocks of 64
     size_t rows, bytes;           // of a slab
 };
