@@ -473,9 +473,13 @@ __device__ __forceinline__ seq_span span_of(const attn_args &g, int b)
 __device__ __forceinline__ int limit_at(const seq_span &s, int i) { return max(0, s.limit + i * s.step); }
 
 // tile number -> sequence and first row of the tile (rows of a sequence and kv head: token-major, then the heads of the group);
-// every lane of the wave calls.  -1: no such tile.
+// every lane of the wave calls.  -1: no such tile (of a single sequence it may also be one without rows).
 __device__ __forceinline__ int find_tile(const attn_args &g, int tile, int &row0)
 {
+    if (g.s.seqs == 1) {
+        row0 = tile * g.tile_rows;
+        return 0;
+    }
     const int lane = threadIdx.x & 63;
     int base = 0;
     for (int b0 = 0; b0 < g.s.seqs; b0 += 64) {
@@ -559,6 +563,7 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
     row0 = __builtin_amdgcn_readfirstlane(row0);
     const seq_span s = span_of(g, b);
     const int nrows = min(16 * MT, s.count * g.group - row0);
+    if (nrows <= 0) return;
     const int last = (int)fd_div((u32)(row0 + nrows - 1), g.dGroup), lim = limit_at(s, last);
     const int key0 = blockIdx.y * g.key_block;
     if (key0 >= lim) return;
@@ -906,6 +911,7 @@ __global__ __launch_bounds__(256, 2) void values_kernel(attn_args g, int n)
     row0 = __builtin_amdgcn_readfirstlane(row0);
     const seq_span s = span_of(g, b);
     const int nrows = min(16 * MT, s.count * g.group - row0);
+    if (nrows <= 0) return;
     const int lim = limit_at(s, (int)fd_div((u32)(row0 + nrows - 1), g.dGroup));
     const int k0 = split * g.run, k1 = min(k0 + g.run, lim), units = (k1 - k0 + 63) >> 6;
     if (split && k0 >= lim) return;              // (the first run writes the zeros of rows that see nothing)
