@@ -11,6 +11,7 @@ import ctypes as C
 import importlib.util
 import math
 import os
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -175,10 +176,15 @@ class _Sequences(C.Structure):
                 ("max_length", _int)]
 
 
+# into one such structure per context, which the library reads before the call returns (making a new one takes 1 us of the host)
+_LOG2E_24 = math.log2(math.e) * (1 << 24)
+_pack_rotary, _pack_sequences = struct.Struct("PPiii").pack_into, struct.Struct("PPPiiii").pack_into
+
+
 def _device_tensor(t: torch.Tensor, dtype: torch.dtype, name: str, shape: Optional[tuple] = None) -> torch.Tensor:
-    if t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda:
         raise TypeError(f"{name} must be a contiguous {dtype} tensor on the GPU")
-    if shape is not None and tuple(t.shape) != shape:
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have the shape {shape}")
     return t
 
@@ -230,6 +236,8 @@ class SSNet:
         # the present workspace: asking again costs a foreign call (0.5 to 1.1 us), which small layers feel
         self._sizes: dict = {}
         self._fits_count = 0
+        self._rotary_arg, self._sequences_arg = _Rotary(), _Sequences()
+        self._rotary_address, self._sequences_address = C.addressof(self._rotary_arg), C.addressof(self._sequences_arg)
 
     def close(self):
         if getattr(self, "_ctx", None):
@@ -719,40 +727,44 @@ class SSNet:
     # ---- transformer blocks ----
     ATTENTION_ROOM = 8 << 30     # bytes of workspace up to which paged_attention takes all tokens at once
 
-    def _heads_view(self, x: torch.Tensor, name: str) -> int:
-        """elements between the tokens of x [n][tokens][heads][head_dim], which may be part of a longer row per token"""
-        if x.dtype != torch.int64 or x.dim() != 4 or not x.is_cuda:
+    def _heads_view(self, x: torch.Tensor, name: str):
+        """(tokens, heads, head_dim, elements between tokens) of x [n][tokens][heads][head_dim], which may be part of a longer row per token"""
+        if x.dtype is not torch.int64 or x.dim() != 4 or not x.is_cuda:
             raise TypeError(f"{name} must be an int64 tensor [n][tokens][heads][head_dim] on the GPU")
         n, tokens, heads, dim = x.shape
         if n != self.n:
             raise ValueError(f"{name} must have the shares of {self.n} parties")
+        if x.is_contiguous():
+            return tokens, heads, dim, heads * dim
         s = x.stride()
         ld = s[1] if tokens > 1 else s[0]
-        if x.numel() and (s[0] != tokens * ld or (heads > 1 and s[2] != dim) or (dim > 1 and s[3] != 1) or ld < heads * dim):
+        if s[0] != tokens * ld or (heads > 1 and s[2] != dim) or (dim > 1 and s[3] != 1) or ld < heads * dim:
             raise TypeError(f"{name}: the heads of a token must be contiguous, tokens and parties equally far apart")
-        return ld
+        return tokens, heads, dim, ld
 
-    def _rotary(self, table: torch.Tensor, pos: torch.Tensor, tokens: int, layout: str) -> _Rotary:
+    def _rotary(self, table: torch.Tensor, pos: torch.Tensor, tokens: int, layout: str) -> int:
+        """fills in the rotary argument of the next call -> elements of a head that it turns"""
         _device_tensor(table, torch.int32, "table"), _device_tensor(pos, torch.int32, "pos", (tokens,))
-        if table.dim() != 3 or table.shape[2] != 2:
+        shape = table.shape
+        if len(shape) != 3 or shape[2] != 2:
             raise ValueError("table must be [positions][rot / 2][2]")
         if layout not in ("half", "interleaved"):
             raise ValueError("layout must be 'half' or 'interleaved'")
-        return _Rotary(_dptr(table), _dptr(pos), table.shape[0], 2 * table.shape[1], layout == "interleaved")
+        rot = 2 * shape[1]
+        _pack_rotary(self._rotary_arg, 0, table.data_ptr(), pos.data_ptr(), shape[0], rot, layout == "interleaved")
+        return rot
 
     def rotary_truncate(self, x: torch.Tensor, table: torch.Tensor, pos: torch.Tensor, stream_id: int, layout: str = "half",
                         out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x [n][tokens][heads][head_dim], turned by the rows `pos` of fixedpoint.rotary_table and truncated (the first
         2 * table.shape[1] elements of every head; the others pass through)"""
-        ld = self._heads_view(x, "x")
-        n, tokens, heads, dim = x.shape
-        rotary = self._rotary(table, pos, tokens, layout)
-        self._reserve_stream(tokens * heads * rotary.rot)
+        tokens, heads, dim, ld = self._heads_view(x, "x")
+        self._reserve_stream(tokens * heads * self._rotary(table, pos, tokens, layout))
         if out is None:
-            out = torch.empty(tuple(x.shape), dtype=torch.int64, device=x.device)
+            out = torch.empty(x.shape, dtype=torch.int64, device=x.device)
         else:
             _device_tensor(out, torch.int64, "out", tuple(x.shape))
-        self._ok(self._call.rotary_truncate(self._handle, _dptr(x), ld, tokens, heads, dim, C.addressof(rotary), stream_id, _dptr(out)),
+        self._ok(self._call.rotary_truncate(self._handle, x.data_ptr(), ld, tokens, heads, dim, self._rotary_address, stream_id, out.data_ptr()),
                  "ssnet_rotary_truncate")
         return out
 
@@ -760,18 +772,19 @@ class SSNet:
                      table: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None, layout: str = "half"):
         """keys k and values v [n][tokens][heads][head_dim] into the places `slots` [tokens] of the cache; table, pos: the keys are
         turned and truncated on the way, as rotary_truncate does"""
-        ld_k, ld_v = self._heads_view(k, "k"), self._heads_view(v, "v")
-        if k.shape != v.shape or k.shape[2] != cache.heads or k.shape[3] != cache.head_dim or cache.n != self.n:
+        tokens, heads, dim, ld_k = self._heads_view(k, "k")
+        if v.shape != k.shape or heads != cache.heads or dim != cache.head_dim or cache.n != self.n:
             raise ValueError("k and v must be [n][tokens][heads][head_dim] of the cache")
-        tokens = k.shape[1]
+        ld_v = self._heads_view(v, "v")[3]
         _device_tensor(slots, torch.int64, "slots", (tokens,))
-        if (table is None) != (pos is None):
+        rotary = None
+        if table is not None and pos is not None:
+            self._reserve_stream(tokens * heads * self._rotary(table, pos, tokens, layout))
+            rotary = self._rotary_address
+        elif table is not None or pos is not None:
             raise ValueError("table and pos go together")
-        rotary = None if table is None else self._rotary(table, pos, tokens, layout)
-        if rotary is not None:
-            self._reserve_stream(tokens * cache.heads * rotary.rot)
-        self._ok(self._call.cache_append(self._handle, cache._address, _dptr(k), ld_k, _dptr(v), ld_v, tokens, _dptr(slots),
-                                         None if rotary is None else C.addressof(rotary), stream_id), "ssnet_cache_append")
+        self._ok(self._call.cache_append(self._handle, cache._address, k.data_ptr(), ld_k, v.data_ptr(), ld_v, tokens, slots.data_ptr(), rotary,
+                                         stream_id), "ssnet_cache_append")
 
     def workspace_bytes_attention(self, cache: PagedCache, sequences: int, tokens: int, heads: int, max_length: int) -> int:
         return self.lib.ssnet_workspace_bytes_attention(self._ctx, cache._address, sequences, tokens, heads, max_length)
@@ -782,8 +795,7 @@ class SSNet:
         """Attention of the tokens q [n][tokens][heads][head_dim], those of sequence b from seq_start[b] to seq_start[b+1], over the
         ctx_len[b] <= max_ctx tokens in the pages block_table[b] -> [n][tokens][heads][head_dim], degree 2t, f + weight_bits
         fraction bits.  scale: factor of the scores (default 1 / sqrt(head_dim)); weight_bits: default f."""
-        ld = self._heads_view(q, "q")
-        n, tokens, heads, dim = q.shape
+        tokens, heads, dim, ld = self._heads_view(q, "q")
         sequences = ctx_len.shape[0]
         _device_tensor(ctx_len, torch.int32, "ctx_len", (sequences,)), _device_tensor(seq_start, torch.int32, "seq_start", (sequences + 1,))
         _device_tensor(block_table, torch.int32, "block_table")
@@ -792,8 +804,6 @@ class SSNet:
         factor = dim ** -0.5 if scale is None else scale
         if not 0 < factor < 4:
             raise ValueError("scale must be positive and below 4")
-        fixed = round(factor * math.log2(math.e) * (1 << 24))
-        bits = self.f if weight_bits is None else weight_bits
         key = ("attention", cache.heads, dim, sequences, tokens, heads, max_ctx)
         need = self._sizes.get(key)
         if need is None:
@@ -807,12 +817,14 @@ class SSNet:
             self._sizes[key] = need
         self.reserve(need)
         if out is None:
-            out = torch.empty((n, tokens, heads, dim), dtype=torch.int64, device=q.device)
+            out = torch.empty(q.shape, dtype=torch.int64, device=q.device)
         else:
-            _device_tensor(out, torch.int64, "out", (n, tokens, heads, dim))
-        seqs = _Sequences(_dptr(seq_start), _dptr(block_table), _dptr(ctx_len), sequences, tokens, block_table.shape[1], max_ctx)
-        self._ok(self._call.paged_attention(self._handle, cache._address, C.addressof(seqs), _dptr(q), ld, heads, fixed, bits, int(causal),
-                                            stream_id, _dptr(out)), "ssnet_paged_attention")
+            _device_tensor(out, torch.int64, "out", tuple(q.shape))
+        _pack_sequences(self._sequences_arg, 0, seq_start.data_ptr(), block_table.data_ptr(), ctx_len.data_ptr(), sequences, tokens,
+                        block_table.shape[1], max_ctx)
+        self._ok(self._call.paged_attention(self._handle, cache._address, self._sequences_address, q.data_ptr(), ld, heads,
+                                            round(factor * _LOG2E_24), self.f if weight_bits is None else weight_bits, causal, stream_id,
+                                            out.data_ptr()), "ssnet_paged_attention")
         return out
 
     PROF_CLASSES = ("share", "reconstruct", "pack_w", "pack_x", "gemm", "degree_reduce", "truncate", "nonlinear",

@@ -545,6 +545,32 @@ __device__ __forceinline__ void multiply(const v4i *a, int stride, const v4i (&k
     }
 }
 
+// share of the mask of a row
+__device__ __forceinline__ u64 row_mask(const ss_softmax_params &sp, u64 row, int party)
+{
+    const u64 counter = ss_counter(row);
+    u64 m = 0;
+    for (int j = sp.t - 1; j >= 0; j--) m = ss_mul_small(ss_add(m, ss_draw_field_at(sp.maskgen_key[j], counter)), party + 1);
+    return ss_add(m, ss_draw_field_at(sp.mask_key, counter));
+}
+
+// Digits of the queries to LDS, qd [row / 16][dim / 64][limb][64 lanes]: item `it` is four consecutive elements of a row; 16 items take 64
+// elements, so that a wave reads 512 consecutive bytes of a row.  (What lies in the places of rows that do not exist reaches their
+// results alone.)
+__device__ __forceinline__ void stage_query(const attn_args &g, v4i *qd, const size_t *rowat, int party, int kb_n, int it)
+{
+    const int rk = it >> 4, kb = kb_n > 1 ? rk % kb_n : 0, r = kb_n > 1 ? rk / kb_n : rk, d = kb * 64 + (it & 15) * 4;
+    u64 y[4] = {0, 0, 0, 0};
+    if (d < g.c.dim) {
+        const u64 *src = g.q + (size_t)party * g.s.tokens * g.ld_q + rowat[r] + d;
+#pragma unroll
+        for (int c = 0; c < 4; c++) y[c] = balanced_digits(src[c]);
+    }
+    u32 *dst = reinterpret_cast<u32 *>(qd + (size_t)((r >> 4) * kb_n + kb) * TILE + (r & 15) + 16 * ((d & 63) >> 4)) + ((d & 15) >> 2);
+#pragma unroll
+    for (int l = 0; l < NL; l++) dst[l * 256] = limb_dword(y, l);
+}
+
 // Step 1: one workgroup per (tile of 16 MT rows, block of g.key_block keys, kv head and party).  The digits of the queries lie in LDS in
 // MFMA order; a wave takes a cell of 16 keys at a time straight from the cache, the next 64 elements of a cell (or the next cell's first)
 // on their way while those at hand are multiplied.
@@ -554,7 +580,7 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
     extern __shared__ v4i qd[];                  // [MT][dim / 64][limb][64 lanes]
     __shared__ u64 mask[16 * MT];
     __shared__ int rowid[16 * MT];
-    __shared__ size_t rowat[16 * MT];            // of the row's query in q
+    __shared__ size_t rowat[16 * MT];            // of the row's query in a share of q
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int head = blockIdx.z / (2 * sp.t + 1), party = blockIdx.z - head * (2 * sp.t + 1);
     int row0 = 0;
@@ -588,29 +614,13 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
         if (tid < nrows) {
             const int i = (int)fd_div((u32)(row0 + tid), g.dGroup), h = head * g.group + row0 + tid - i * g.group;
             id = (s.first + i - g.tok0) * g.heads + h;
-            rowat[tid] = ((size_t)party * g.s.tokens + s.first + i) * g.ld_q + (size_t)h * g.c.dim;
-            const u64 counter = ss_counter((u64)(s.first + i) * g.heads + h);
-            u64 m = 0;
-            for (int j = sp.t - 1; j >= 0; j--) m = ss_mul_small(ss_add(m, ss_draw_field_at(sp.maskgen_key[j], counter)), party + 1);
-            mask[tid] = ss_add(m, ss_draw_field_at(sp.mask_key, counter));
+            rowat[tid] = (size_t)(s.first + i) * g.ld_q + (size_t)h * g.c.dim;
+            mask[tid] = row_mask(sp, (u64)(s.first + i) * g.heads + h, party);
         }
         rowid[tid] = id;
     }
     __syncthreads();
-    for (int it = tid; it < nrows * kb_n * 16; it += 256) {
-        // four consecutive elements of row r; 16 lanes take 64 elements, so that a wave reads 512 consecutive bytes of a row.  (What lies in
-        // the places of rows that do not exist reaches their results alone.)
-        const int rk = it >> 4, kb = kb_n > 1 ? rk % kb_n : 0, r = kb_n > 1 ? rk / kb_n : rk, d = kb * 64 + (it & 15) * 4;
-        u64 y[4] = {0, 0, 0, 0};
-        if (d < g.c.dim) {
-            const u64 *src = g.q + rowat[r] + d;
-#pragma unroll
-            for (int c = 0; c < 4; c++) y[c] = balanced_digits(src[c]);
-        }
-        u32 *dst = reinterpret_cast<u32 *>(qd + (size_t)((r >> 4) * kb_n + kb) * TILE + (r & 15) + 16 * ((d & 63) >> 4)) + ((d & 15) >> 2);
-#pragma unroll
-        for (int l = 0; l < NL; l++) dst[l * 256] = limb_dword(y, l);
-    }
+    for (int it = tid; it < nrows * kb_n * 16; it += 256) stage_query(g, qd, rowat, party, kb_n, it);
     __syncthreads();
     __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0): the first digits are there, the loop's waits are for its own loads alone
     for (; cell < cell_end; cell += 4) {
@@ -985,6 +995,139 @@ __global__ __launch_bounds__(256, 2) void values_kernel(attn_args g, int n)
         }
 }
 
+// All three steps for contexts of up to 128 keys, one workgroup of eight waves per (tile of 16 rows, kv head): a launch costs the host and
+// the queue 4 to 5 us whatever it does, and the steps of such a call are hardly longer.  (party, cell), then rows, then (party, 16
+// elements of the head) go round the waves; what one step leaves for the next is the same as with a kernel for each and is read back from
+// the caches.
+constexpr int SHORT_KEYS = 128;
+constexpr size_t SHORT_LDS = 128 * 1024;      // for the digits of the queries of all parties
+template <int N, int T>
+__global__ __launch_bounds__(512) void short_kernel(attn_args g, ss_softmax_params sp)
+{
+    constexpr int NR = 2 * T + 1, WAVES = 8;
+    extern __shared__ v4i qd[];                  // [party][dim / 64][limb][64 lanes]
+    __shared__ u64 mask[NR][16];
+    __shared__ int rowid[16];
+    __shared__ size_t rowat[16], cells[SHORT_KEYS / 16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), head = blockIdx.y, n = N ? N : sp.n;
+    int row0 = 0;
+    const int b = __builtin_amdgcn_readfirstlane(find_tile(g, blockIdx.x, row0));
+    if (b < 0) return;
+    row0 = __builtin_amdgcn_readfirstlane(row0);
+    const seq_span s = span_of(g, b);
+    const int nrows = min(16, s.count * g.group - row0);
+    if (nrows <= 0) return;
+    const int lim = limit_at(s, (int)fd_div((u32)(row0 + nrows - 1), g.dGroup));
+    const int kb_n = (g.c.dim + 63) / 64, groups = g.c.dim >> 4, cell_n = (lim + 15) >> 4, blocks = (lim + 63) >> 6;
+    if (tid < blocks * 4) cells[tid] = cell_at(g, b, tid);
+    if (tid < nrows) {
+        const int i = (int)fd_div((u32)(row0 + tid), g.dGroup), h = head * g.group + row0 + tid - i * g.group;
+        rowid[tid] = (s.first + i - g.tok0) * g.heads + h;
+        rowat[tid] = (size_t)(s.first + i) * g.ld_q + (size_t)h * g.c.dim;
+    }
+    if (tid >= 64 && tid < 64 + 16 * NR) {
+        const int r = tid & 15, party = (tid >> 4) - 4;
+        if (r < nrows) {
+            const int i = (int)fd_div((u32)(row0 + r), g.dGroup), h = head * g.group + row0 + r - i * g.group;
+            mask[party][r] = row_mask(sp, (u64)(s.first + i) * g.heads + h, party);
+        }
+    }
+    __syncthreads();
+    // step 1
+    const signed char *keys = g.c.keys + head * g.head_bytes + (lane & 15) * 16;
+    auto load = [&](int unit, int kb, v4i (&k)[NL]) {
+        const int party = unit / cell_n, cell = unit - party * cell_n;
+        const signed char *src = keys + party * g.party_bytes + cells[cell] + (size_t)min(kb * 4 + (lane >> 4), groups - 1) * 256;
+#pragma unroll
+        for (int l = 0; l < NL; l++) k[l] = *reinterpret_cast<const v4i *>(src + (size_t)(l * groups) * 256);
+    };
+    const int units = NR * cell_n;
+    v4i k[NL], next[NL];
+    if (wave < units) load(wave, 0, k);
+    for (int it = tid; it < NR * nrows * kb_n * 16; it += 64 * WAVES) {
+        const int party = it / (nrows * kb_n * 16);
+        stage_query(g, qd + party * kb_n * TILE, rowat, party, kb_n, it - party * (nrows * kb_n * 16));
+    }
+    __syncthreads();
+    for (int u = wave; u < units; u += WAVES) {
+        const int party = u / cell_n, cell = u - party * cell_n;
+        v4i acc[1][ND];
+        for (int kb = 0; kb < kb_n; kb++) {
+            const bool same = kb + 1 < kb_n;
+            load(same ? u : min(u + WAVES, units - 1), same ? kb + 1 : 0, next);
+            const v4i *a = qd + (party * kb_n + kb) * TILE + lane;
+            if (kb == 0)
+                multiply<1, true>(a, 0, k, acc);
+            else
+                multiply<1, false>(a, 0, k, acc);
+#pragma unroll
+            for (int l = 0; l < NL; l++) k[l] = next[l];
+        }
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            const int row = 4 * (lane >> 4) + r;
+            if (row < nrows)
+                g.msg[((size_t)party * g.rows + rowid[row]) * g.keys + cell * 16 + (lane & 15)] = ss_add(fold_diagonals(acc[0], r), mask[party][row]);
+        }
+    }
+    __syncthreads();
+    // step 2: a wave to a row, four keys to a lane
+    for (int row = wave; row < nrows; row += WAVES) {
+        const int i = (int)fd_div((u32)(row0 + row), g.dGroup), h = head * g.group + row0 + row - i * g.group, j = lane * 4;
+        const row_place r = {rowid[row], s.first + i, h, limit_at(s, i), blocks * 64};
+        u64 v[4] = {0, 0, 0, 0};
+        u32 w[4];
+        if (j < r.limit) open_scores<T>(g, sp, r, j, v);
+        const u64 ref = __shfl(v[0], 0);
+        long long top = -(1ll << 62), sum = 0;
+#pragma unroll
+        for (int c = 0; c < 4; c++)
+            if (j + c < r.limit) top = max(top, lift(ss_sub(v[c], ref)));
+#pragma unroll
+        for (int d = 32; d; d >>= 1) top = max(top, __shfl_xor(top, d));
+#pragma unroll
+        for (int c = 0; c < 4; c++) {
+            w[c] = j + c < r.limit ? softmax_weight(top - lift(ss_sub(v[c], ref)), sp) : 0;
+            sum += w[c];
+        }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+        const row_norm nm = sum ? norm_of((u64)sum) : row_norm{0, 0};
+        if (j < r.covered) share_weights<N, T>(g, sp, r, j, w, r.limit - j, nm);
+    }
+    __syncthreads();
+    // step 3
+    const signed char *values = g.c.values + head * g.head_bytes + (lane & 15) * 16;
+    const signed char *wrow = g.weights + (size_t)rowid[min(lane & 15, nrows - 1)] * g.keys * NL + (lane >> 4) * 16;
+    const size_t limb = (size_t)g.c.dim * 16;
+    for (int u = wave; u < n * groups; u += WAVES) {
+        const int party = u / groups, dt = u - party * groups;
+        v4i acc[1][ND];
+        clear(acc[0]);
+        for (int blk = 0; blk < blocks; blk++) {
+            const signed char *src = values + party * g.party_bytes + cells[blk * 4 + (lane >> 4)] + dt * 256;
+            const signed char *wsrc = wrow + (size_t)party * g.rows * g.keys * NL + (size_t)blk * (64 * NL);
+            v4i x[NL], y[NL];
+#pragma unroll
+            for (int l = 0; l < NL; l++) {
+                x[l] = *reinterpret_cast<const v4i *>(wsrc + l * 64);
+                y[l] = *reinterpret_cast<const v4i *>(src + l * limb);
+            }
+#pragma unroll
+            for (int i = 0; i < NL; i++)
+#pragma unroll
+                for (int j = 0; j < NL; j++) acc[0][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[i], y[j], acc[0][i + j], 0, 0, 0);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            const int row = 4 * (lane >> 4) + r;
+            if (row < nrows)
+                g.out[((size_t)party * g.s.tokens * g.heads + (size_t)g.tok0 * g.heads + rowid[row]) * g.c.dim + dt * 16 + (lane & 15)] =
+                    fold_diagonals(acc[0], r);
+        }
+    }
+}
+
 // the runs of a row added up
 __global__ __launch_bounds__(BLOCK) void join_kernel(attn_args g, int n, fdiv dDim)
 {
@@ -1115,6 +1258,13 @@ attention_plan plan_attention(int n, int t, int tokens, int seqs, int heads, int
     return p;
 }
 
+namespace {
+
+// LDS of the kernel for short contexts
+size_t short_lds(int t, int dim) { return (size_t)(2 * t + 1) * ((dim + 63) / 64) * TILE * 16; }
+
+}  // namespace
+
 hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache, const ss_sequences &seqs, const u64 *q, size_t ld_q, int heads,
                                int causal, const ss_softmax_params &sp, void *room, u64 *out, hipStream_t stream)
 {
@@ -1160,6 +1310,22 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
     if (lds > 48 * 1024) {
         const void *scores = plan.row_tiles == 1 ? (const void *)scores_kernel<1> : (const void *)scores_kernel<2>;
         if (hipError_t e = hipFuncSetAttribute(scores, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); e != hipSuccess) return e;
+    }
+    if (plan.keys <= SHORT_KEYS && plan.row_tiles == 1 && plan.slab == seqs.tokens && short_lds(sp.t, cache.dim) <= SHORT_LDS) {
+        g.tok1 = seqs.tokens;
+        const size_t bytes = short_lds(sp.t, cache.dim);
+        const dim3 grid((unsigned)((size_t)seqs.tokens * g.group / 16 + seqs.seqs), cache.kv);
+#define SS_LAUNCH(NC, TC)                                                                                                            \
+    do {                                                                                                                             \
+        if (bytes > 48 * 1024)                                                                                                       \
+            if (hipError_t e = hipFuncSetAttribute((const void *)short_kernel<NC, TC>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); \
+                e != hipSuccess)                                                                                                     \
+                return e;                                                                                                            \
+        hipLaunchKernelGGL((short_kernel<NC, TC>), grid, dim3(512), bytes, stream, g, sp);                                           \
+    } while (0)
+        SS_SCHEME(sp.n, sp.t, SS_LAUNCH);
+#undef SS_LAUNCH
+        return hipGetLastError();
     }
     for (int tok = 0; tok < seqs.tokens; tok += plan.slab) {
         g.tok0 = tok;
