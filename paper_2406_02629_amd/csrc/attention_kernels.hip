@@ -20,7 +20,9 @@ namespace {
 
 constexpr int BLOCK = 256;
 constexpr size_t STREAM_BYTES = (size_t)256 << 20;   // what a call writes, from which on past the caches
-constexpr size_t WIDE_APPEND = (size_t)1 << 17;     // elements of the new keys from which on the kernels for many tokens take them
+// Elements of the new keys from which on the kernel for many tokens takes them: tokens of 8 heads of 128, us, it / one thread per pair: n = 5, 128
+// tokens 14.3 / 13.8, 256 21.8 / 25.0; n = 3 11.2 / 10.1, 12.7 / 16.0.
+constexpr size_t WIDE_APPEND = (size_t)3 << 16;
 constexpr size_t MAX_ROWS = (size_t)1 << 22;   // of a slab: a workgroup each, less than 2^32 threads in a launch
 constexpr size_t SHORT_ROW = 4096;   // keys up to which one workgroup takes the softmax of a row
 constexpr int MAX_RUN = 16320;      // keys that the 32-bit sums of the values can take, in blocks of 64: 8 * 16383 * 2^14 < 2^31
@@ -445,7 +447,7 @@ struct attn_args {
     size_t cell, head_bytes, party_bytes, page_bytes;
     int heads, group, causal;
     int tok0, tok1;                 // the slab
-    fdiv dGroup, dCells, dHeads;
+    fdiv dGroup, dCells, dHeads, dScores, dValues;   // Scores, Values: by heads x parties
     const u64 *q;
     size_t ld_q;
     u64 *msg;                       // [2t+1][rows][keys]
@@ -582,9 +584,10 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
     __shared__ int rowid[16 * MT];
     __shared__ size_t rowat[16 * MT];            // of the row's query in a share of q
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int head = blockIdx.z / (2 * sp.t + 1), party = blockIdx.z - head * (2 * sp.t + 1);
+    const int tile = (int)fd_div(blockIdx.x, g.dScores), hp = (int)blockIdx.x - tile * g.c.kv * (2 * sp.t + 1);
+    const int head = hp / (2 * sp.t + 1), party = hp - head * (2 * sp.t + 1);
     int row0 = 0;
-    const int b = __builtin_amdgcn_readfirstlane(find_tile(g, blockIdx.x, row0));
+    const int b = __builtin_amdgcn_readfirstlane(find_tile(g, tile, row0));
     if (b < 0) return;
     row0 = __builtin_amdgcn_readfirstlane(row0);
     const seq_span s = span_of(g, b);
@@ -753,6 +756,12 @@ __device__ __forceinline__ row_norm norm_of(u64 sum)
     return {q, drop};
 }
 
+// the weight of a key, w / sum, with sp.bits fraction bits
+__device__ __forceinline__ u64 weight_of(u32 w, const row_norm &nm, const ss_softmax_params &sp)
+{
+    return ((((u64)w * nm.recip) >> 16) + (1ull << (45 - sp.bits + nm.drop))) >> (46 - sp.bits + nm.drop);
+}
+
 // The weights of four keys (w, 30 fraction bits, 0 beyond the limit; `seen` of them are keys that the row sees), shared, as digits.
 template <int N, int T>
 __device__ __forceinline__ void share_weights(const attn_args &g, const ss_softmax_params &sp, const row_place &r, int j, const u32 (&w)[4], int seen,
@@ -762,7 +771,7 @@ __device__ __forceinline__ void share_weights(const attn_args &g, const ss_softm
     u64 y[MAXP<N>][4];
 #pragma unroll
     for (int c = 0; c < 4; c++) {
-        const u64 p = ((((u64)w[c] * nm.recip) >> 16) + (1ull << (45 - sp.bits + nm.drop))) >> (46 - sp.bits + nm.drop);
+        const u64 p = weight_of(w[c], nm, sp);
         const u64 counter = ss_counter(((u64)r.token * g.heads + r.head) << 32 | (u32)(j + c));
         u64 a[T];
 #pragma unroll
@@ -913,10 +922,11 @@ __global__ __launch_bounds__(256, 2) void values_kernel(attn_args g, int n)
     __shared__ size_t cells[MAX_RUN / 16 + 4];
     __shared__ int rowid[16 * MT];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int head = blockIdx.z / n, party = blockIdx.z - head * n;
+    const int tile = (int)fd_div(blockIdx.x, g.dValues), hp = (int)blockIdx.x - tile * g.c.kv * n;
+    const int head = hp / n, party = hp - head * n;
     const int split = blockIdx.y / g.dblocks, dt = (blockIdx.y - split * g.dblocks) * 4 + wave;   // 16 elements each
     int row0 = 0;
-    const int b = __builtin_amdgcn_readfirstlane(find_tile(g, blockIdx.x, row0));
+    const int b = __builtin_amdgcn_readfirstlane(find_tile(g, tile, row0));
     if (b < 0) return;
     row0 = __builtin_amdgcn_readfirstlane(row0);
     const seq_span s = span_of(g, b);
@@ -995,21 +1005,18 @@ __global__ __launch_bounds__(256, 2) void values_kernel(attn_args g, int n)
         }
 }
 
-// All three steps for contexts of up to 128 keys, one workgroup of eight waves per (tile of 16 rows, kv head): a launch costs the host and
-// the queue 4 to 5 us whatever it does, and the steps of such a call are hardly longer.  (party, cell), then rows, then (party, 16
-// elements of the head) go round the waves; what one step leaves for the next is the same as with a kernel for each and is read back from
-// the caches.
-constexpr int SHORT_KEYS = 128;
-constexpr size_t SHORT_LDS = 128 * 1024;      // for the digits of the queries of all parties
-template <int N, int T>
-__global__ __launch_bounds__(512) void short_kernel(attn_args g, ss_softmax_params sp)
+// Steps 2 and 3 in one launch for contexts of up to 256 keys: one workgroup of eight waves per (tile of 16 rows, kv head and party) takes the
+// softmax of the rows, a wave to a row and four keys to a lane, keeps its own party's shares of the weights in LDS and multiplies, a
+// wave to 16 elements of the head.  All parties' workgroups take the same softmax, which costs less than a launch.
+constexpr int SHORT_KEYS = 256;
+template <int T>
+__global__ __launch_bounds__(512) void finish_kernel(attn_args g, ss_softmax_params sp)
 {
-    constexpr int NR = 2 * T + 1, WAVES = 8;
-    extern __shared__ v4i qd[];                  // [party][dim / 64][limb][64 lanes]
-    __shared__ u64 mask[NR][16];
+    constexpr int WAVES = 8;
+    __shared__ v4i wd[SHORT_KEYS / 64 * TILE];   // [key / 64][limb][64 lanes]
     __shared__ int rowid[16];
-    __shared__ size_t rowat[16], cells[SHORT_KEYS / 16];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), head = blockIdx.y, n = N ? N : sp.n;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int head = blockIdx.y / sp.n, party = blockIdx.y - head * sp.n;
     int row0 = 0;
     const int b = __builtin_amdgcn_readfirstlane(find_tile(g, blockIdx.x, row0));
     if (b < 0) return;
@@ -1017,106 +1024,64 @@ __global__ __launch_bounds__(512) void short_kernel(attn_args g, ss_softmax_para
     const seq_span s = span_of(g, b);
     const int nrows = min(16, s.count * g.group - row0);
     if (nrows <= 0) return;
-    const int lim = limit_at(s, (int)fd_div((u32)(row0 + nrows - 1), g.dGroup));
-    const int kb_n = (g.c.dim + 63) / 64, groups = g.c.dim >> 4, cell_n = (lim + 15) >> 4, blocks = (lim + 63) >> 6;
-    if (tid < blocks * 4) cells[tid] = cell_at(g, b, tid);
-    if (tid < nrows) {
-        const int i = (int)fd_div((u32)(row0 + tid), g.dGroup), h = head * g.group + row0 + tid - i * g.group;
-        rowid[tid] = (s.first + i - g.tok0) * g.heads + h;
-        rowat[tid] = (size_t)(s.first + i) * g.ld_q + (size_t)h * g.c.dim;
-    }
-    if (tid >= 64 && tid < 64 + 16 * NR) {
-        const int r = tid & 15, party = (tid >> 4) - 4;
-        if (r < nrows) {
-            const int i = (int)fd_div((u32)(row0 + r), g.dGroup), h = head * g.group + row0 + r - i * g.group;
-            mask[party][r] = row_mask(sp, (u64)(s.first + i) * g.heads + h, party);
-        }
-    }
-    __syncthreads();
-    // step 1
-    const signed char *keys = g.c.keys + head * g.head_bytes + (lane & 15) * 16;
-    auto load = [&](int unit, int kb, v4i (&k)[NL]) {
-        const int party = unit / cell_n, cell = unit - party * cell_n;
-        const signed char *src = keys + party * g.party_bytes + cells[cell] + (size_t)min(kb * 4 + (lane >> 4), groups - 1) * 256;
+    const int lim = limit_at(s, (int)fd_div((u32)(row0 + nrows - 1), g.dGroup)), blocks = (lim + 63) >> 6, groups = g.c.dim >> 4;
+    const signed char *values = g.c.values + party * g.party_bytes + head * g.head_bytes + (lane & 15) * 16;
+    const size_t limb = (size_t)g.c.dim * 16;
+    auto load = [&](int dt, int blk, v4i (&v)[NL]) {
+        const signed char *src = values + cell_at(g, b, blk * 4 + (lane >> 4)) + dt * 256;
 #pragma unroll
-        for (int l = 0; l < NL; l++) k[l] = *reinterpret_cast<const v4i *>(src + (size_t)(l * groups) * 256);
+        for (int l = 0; l < NL; l++) v[l] = *reinterpret_cast<const v4i *>(src + l * limb);
     };
-    const int units = NR * cell_n;
-    v4i k[NL], next[NL];
-    if (wave < units) load(wave, 0, k);
-    for (int it = tid; it < NR * nrows * kb_n * 16; it += 64 * WAVES) {
-        const int party = it / (nrows * kb_n * 16);
-        stage_query(g, qd + party * kb_n * TILE, rowat, party, kb_n, it - party * (nrows * kb_n * 16));
-    }
-    __syncthreads();
-    for (int u = wave; u < units; u += WAVES) {
-        const int party = u / cell_n, cell = u - party * cell_n;
-        v4i acc[1][ND];
-        for (int kb = 0; kb < kb_n; kb++) {
-            const bool same = kb + 1 < kb_n;
-            load(same ? u : min(u + WAVES, units - 1), same ? kb + 1 : 0, next);
-            const v4i *a = qd + (party * kb_n + kb) * TILE + lane;
-            if (kb == 0)
-                multiply<1, true>(a, 0, k, acc);
-            else
-                multiply<1, false>(a, 0, k, acc);
-#pragma unroll
-            for (int l = 0; l < NL; l++) k[l] = next[l];
-        }
-#pragma unroll
-        for (int r = 0; r < 4; r++) {
-            const int row = 4 * (lane >> 4) + r;
-            if (row < nrows)
-                g.msg[((size_t)party * g.rows + rowid[row]) * g.keys + cell * 16 + (lane & 15)] = ss_add(fold_diagonals(acc[0], r), mask[party][row]);
-        }
-    }
-    __syncthreads();
-    // step 2: a wave to a row, four keys to a lane
+    v4i v[NL], next[NL];
+    if (blocks && wave < groups) load(wave, 0, v);
     for (int row = wave; row < nrows; row += WAVES) {
         const int i = (int)fd_div((u32)(row0 + row), g.dGroup), h = head * g.group + row0 + row - i * g.group, j = lane * 4;
-        const row_place r = {rowid[row], s.first + i, h, limit_at(s, i), blocks * 64};
-        u64 v[4] = {0, 0, 0, 0};
+        const row_place r = {(s.first + i - g.tok0) * g.heads + h, s.first + i, h, limit_at(s, i), blocks * 64};
+        if (lane == 0) rowid[row] = r.id;
+        u64 o[4] = {0, 0, 0, 0}, y[4];
         u32 w[4];
-        if (j < r.limit) open_scores<T>(g, sp, r, j, v);
-        const u64 ref = __shfl(v[0], 0);
+        if (j < r.limit) open_scores<T>(g, sp, r, j, o);
+        const u64 ref = __shfl(o[0], 0);
         long long top = -(1ll << 62), sum = 0;
 #pragma unroll
         for (int c = 0; c < 4; c++)
-            if (j + c < r.limit) top = max(top, lift(ss_sub(v[c], ref)));
+            if (j + c < r.limit) top = max(top, lift(ss_sub(o[c], ref)));
 #pragma unroll
         for (int d = 32; d; d >>= 1) top = max(top, __shfl_xor(top, d));
 #pragma unroll
         for (int c = 0; c < 4; c++) {
-            w[c] = j + c < r.limit ? softmax_weight(top - lift(ss_sub(v[c], ref)), sp) : 0;
+            w[c] = j + c < r.limit ? softmax_weight(top - lift(ss_sub(o[c], ref)), sp) : 0;
             sum += w[c];
         }
 #pragma unroll
         for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
         const row_norm nm = sum ? norm_of((u64)sum) : row_norm{0, 0};
-        if (j < r.covered) share_weights<N, T>(g, sp, r, j, w, r.limit - j, nm);
+#pragma unroll
+        for (int c = 0; c < 4; c++) {
+            const u64 counter = ss_counter(((u64)r.token * g.heads + h) << 32 | (u32)(j + c));
+            u64 a[T];
+#pragma unroll
+            for (int x = 0; x < T; x++) a[x] = ss_draw_field_at(sp.gen_key[x], counter);
+            const u64 share = ss_poly_eval<T>(weight_of(w[c], nm, sp), a, T, party + 1);
+            y[c] = j + c < r.limit ? balanced_digits(share) : 0;
+        }
+        if (j < r.covered) {
+            u32 *dst = reinterpret_cast<u32 *>(wd + (j >> 6) * TILE + row + (j & 48)) + ((j & 15) >> 2);
+#pragma unroll
+            for (int l = 0; l < NL; l++) dst[l * 256] = limb_dword(y, l);
+        }
     }
     __syncthreads();
-    // step 3
-    const signed char *values = g.c.values + head * g.head_bytes + (lane & 15) * 16;
-    const signed char *wrow = g.weights + (size_t)rowid[min(lane & 15, nrows - 1)] * g.keys * NL + (lane >> 4) * 16;
-    const size_t limb = (size_t)g.c.dim * 16;
-    for (int u = wave; u < n * groups; u += WAVES) {
-        const int party = u / groups, dt = u - party * groups;
+    for (int dt = wave; dt < groups; dt += WAVES) {
         v4i acc[1][ND];
         clear(acc[0]);
         for (int blk = 0; blk < blocks; blk++) {
-            const signed char *src = values + party * g.party_bytes + cells[blk * 4 + (lane >> 4)] + dt * 256;
-            const signed char *wsrc = wrow + (size_t)party * g.rows * g.keys * NL + (size_t)blk * (64 * NL);
-            v4i x[NL], y[NL];
+            // (behind the last, its own again)
+            const bool same = blk + 1 < blocks, more = dt + WAVES < groups;
+            load(same || !more ? dt : dt + WAVES, same ? blk + 1 : 0, next);
+            multiply<1, false>(wd + blk * TILE + lane, 0, v, acc);
 #pragma unroll
-            for (int l = 0; l < NL; l++) {
-                x[l] = *reinterpret_cast<const v4i *>(wsrc + l * 64);
-                y[l] = *reinterpret_cast<const v4i *>(src + l * limb);
-            }
-#pragma unroll
-            for (int i = 0; i < NL; i++)
-#pragma unroll
-                for (int j = 0; j < NL; j++) acc[0][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[i], y[j], acc[0][i + j], 0, 0, 0);
+            for (int l = 0; l < NL; l++) v[l] = next[l];
         }
 #pragma unroll
         for (int r = 0; r < 4; r++) {
@@ -1224,6 +1189,17 @@ hipError_t ss_launch_append(const ss_paged &c, const u64 *k, size_t ld_k, const 
     return hipGetLastError();
 }
 
+namespace {
+
+// most tiles of `rows` rows that the sequences of a call can have
+size_t tile_bound(size_t tokens, size_t seqs, size_t group, size_t rows)
+{
+    const size_t one = tokens * ceil_div(group, rows), all = tokens * group / rows + seqs;
+    return one < all ? one : all;
+}
+
+}  // namespace
+
 attention_plan plan_attention(int n, int t, int tokens, int seqs, int heads, int kv, int dim, int max_length, size_t room)
 {
     attention_plan p = {};
@@ -1233,22 +1209,24 @@ attention_plan plan_attention(int n, int t, int tokens, int seqs, int heads, int
     // scores + values, us, tiles of 32 / of 16 rows: chunk of 512 tokens over 4096, n = 5 (10400 workgroups) 1975 / 2085; chunks of 17 to 121
     // over 121 to 777, n = 5 (1160) 155 / 129; 230 tokens over 700 to 1024, n = 3, 45-bit prime (480) 64 / 62.  Blocks of 128 keys against 256
     // with 16 rows, scores alone: single tokens 157 / 159 and 92 / 94, the two chunks above 76 / 71 and 36.5 / 33; of 512 against 1024 with 32: 1079 / 1040.
-    const size_t sequence_rows = ceil_div(tokens, seqs) * group, tiles = tokens * group / 32 + seqs, wgs = tiles * ceil_div(p.keys, 512) * kv * nr;
+    const size_t sequence_rows = ceil_div(tokens, seqs) * group, wgs = tile_bound(tokens, seqs, group, 32) * ceil_div(p.keys, 512) * kv * nr;
     p.row_tiles = sequence_rows > 16 && wgs >= 2048 ? 2 : 1;
     p.key_block = p.row_tiles == 2 ? (wgs >= 8192 ? 1024 : 512) : sequence_rows > 16 ? 256 : 128;
     p.dblocks = ceil_div(dim, 64);
+    // one launch for softmax and values while each of its workgroups has a CU to itself (us, one launch / two): single tokens of 32 heads of
+    // 128 over 64 keys, n = 5, one sequence 15.1 / 18.2, 4 17.3 / 20.9, 16 (800 workgroups) 38.4 / 37.9, 64 109 / 104; over 256 keys, one 21.2 / 22.4
+    p.finish = p.row_tiles == 1 && p.keys <= SHORT_KEYS && tile_bound(tokens, seqs, group, 16) * kv * n <= 256;
     p.slab = tokens;
     for (;;) {
-        const size_t tile = 16 * p.row_tiles, tiles = p.slab * group / tile + seqs;
-        const size_t base = tiles * p.dblocks * kv * n;
+        const size_t base = tile_bound(p.slab, seqs, group, 16 * p.row_tiles) * p.dblocks * kv * n;
         const size_t wanted = ceil_div(sequence_rows <= 16 ? 2048 : 1024, base);
         p.run = (int)((ceil_div(p.keys, wanted) + 63) & ~63u);
         if (p.run > MAX_RUN) p.run = MAX_RUN;
         if (p.run < 256) p.run = 256;
-        p.splits = (int)ceil_div(p.keys, p.run);
+        p.splits = p.finish ? 1 : (int)ceil_div(p.keys, p.run);
         p.rows = (size_t)p.slab * heads;
         const size_t blocks = p.keys > SHORT_ROW ? ceil_div(p.keys, 1024) : 0;
-        p.bytes = align256(nr * p.rows * p.keys * 8) + (blocks ? align256(p.rows * (p.keys + 2 * blocks) * 8) : 0) + align256((size_t)n * p.rows * p.keys * NL) +
+        p.bytes = align256(nr * p.rows * p.keys * 8) + (blocks ? align256(p.rows * (p.keys + 2 * blocks) * 8) : 0) + (p.finish ? 0 : align256((size_t)n * p.rows * p.keys * NL)) +
                   (p.splits > 1 ? align256((size_t)p.splits * n * p.rows * dim * 8) : 0);
         if (p.bytes <= room && p.rows <= MAX_ROWS) return p;
         if (p.slab == 1) break;
@@ -1257,13 +1235,6 @@ attention_plan plan_attention(int n, int t, int tokens, int seqs, int heads, int
     p.slab = 0;
     return p;
 }
-
-namespace {
-
-// LDS of the kernel for short contexts
-size_t short_lds(int t, int dim) { return (size_t)(2 * t + 1) * ((dim + 63) / 64) * TILE * 16; }
-
-}  // namespace
 
 hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache, const ss_sequences &seqs, const u64 *q, size_t ld_q, int heads,
                                int causal, const ss_softmax_params &sp, void *room, u64 *out, hipStream_t stream)
@@ -1281,6 +1252,8 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
     g.dGroup = make_fdiv((u32)g.group);
     g.dCells = make_fdiv((u32)cache.page_cells);
     g.dHeads = make_fdiv((u32)heads);
+    g.dScores = make_fdiv((u32)cache.kv * (2 * sp.t + 1));
+    g.dValues = make_fdiv((u32)cache.kv * sp.n);
     g.q = q;
     g.ld_q = ld_q;
     g.rows = plan.rows;
@@ -1303,7 +1276,7 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
         at += align256(g.rows * (g.keys + 2 * blocks) * 8);
     }
     g.weights = (signed char *)at;
-    at += align256((size_t)n * g.rows * g.keys * NL);
+    at += plan.finish ? 0 : align256((size_t)n * g.rows * g.keys * NL);
     g.parts = (u64 *)at;
     g.out = out;
     const size_t lds = (size_t)plan.row_tiles * ((cache.dim + 63) / 64) * TILE * 16;
@@ -1311,33 +1284,30 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
         const void *scores = plan.row_tiles == 1 ? (const void *)scores_kernel<1> : (const void *)scores_kernel<2>;
         if (hipError_t e = hipFuncSetAttribute(scores, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); e != hipSuccess) return e;
     }
-    if (plan.keys <= SHORT_KEYS && plan.row_tiles == 1 && plan.slab == seqs.tokens && short_lds(sp.t, cache.dim) <= SHORT_LDS) {
-        g.tok1 = seqs.tokens;
-        const size_t bytes = short_lds(sp.t, cache.dim);
-        const dim3 grid((unsigned)((size_t)seqs.tokens * g.group / 16 + seqs.seqs), cache.kv);
-#define SS_LAUNCH(NC, TC)                                                                                                            \
-    do {                                                                                                                             \
-        if (bytes > 48 * 1024)                                                                                                       \
-            if (hipError_t e = hipFuncSetAttribute((const void *)short_kernel<NC, TC>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); \
-                e != hipSuccess)                                                                                                     \
-                return e;                                                                                                            \
-        hipLaunchKernelGGL((short_kernel<NC, TC>), grid, dim3(512), bytes, stream, g, sp);                                           \
-    } while (0)
-        SS_SCHEME(sp.n, sp.t, SS_LAUNCH);
-#undef SS_LAUNCH
-        return hipGetLastError();
-    }
     for (int tok = 0; tok < seqs.tokens; tok += plan.slab) {
         g.tok0 = tok;
         g.tok1 = min(seqs.tokens, tok + plan.slab);
         g.rows_now = (u32)(g.tok1 - tok) * heads;
-        const unsigned tiles = (unsigned)((size_t)(g.tok1 - tok) * g.group / g.tile_rows + seqs.seqs);
-        const dim3 sgrid(tiles, ceil_div(plan.keys, plan.key_block), cache.kv * nr), vgrid(tiles, plan.splits * plan.dblocks, cache.kv * n);
+        // heads and parties run fastest over the workgroups, which are dealt to the XCDs in turn: every head and party has the same work,
+        // whatever the lengths of the sequences, and the tiles of one read the same keys and values
+        const unsigned tiles = (unsigned)tile_bound(g.tok1 - tok, seqs.seqs, g.group, g.tile_rows);
+        const dim3 sgrid(tiles * cache.kv * nr, ceil_div(plan.keys, plan.key_block)), vgrid(tiles * cache.kv * n, plan.splits * plan.dblocks);
         const dim3 rgrid(g.rows_now), wgrid(g.rows_now, blocks), block(BLOCK);
         if (plan.row_tiles == 1)
             hipLaunchKernelGGL((scores_kernel<1>), sgrid, dim3(256), lds, stream, g, sp);
         else
             hipLaunchKernelGGL((scores_kernel<2>), sgrid, dim3(256), lds, stream, g, sp);
+        if (plan.finish) {
+            const dim3 fgrid(tiles, cache.kv * n);
+            if (sp.t == 1)
+                hipLaunchKernelGGL(finish_kernel<1>, fgrid, dim3(512), 0, stream, g, sp);
+            else if (sp.t == 2)
+                hipLaunchKernelGGL(finish_kernel<2>, fgrid, dim3(512), 0, stream, g, sp);
+            else
+                hipLaunchKernelGGL(finish_kernel<3>, fgrid, dim3(512), 0, stream, g, sp);
+            if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+            continue;
+        }
 #define SS_LAUNCH(NC, TC)                                                                               \
     do {                                                                                                \
         if (split_rows) {                                                                               \

@@ -260,6 +260,7 @@ struct attention_plan {
     int splits, run;
     int key_block;                // keys of a workgroup of the scores
     int dblocks;                  // workgroups to a head in the values, 64 elements each
+    bool finish;                  // softmax and values in one launch
     size_t keys;                  // of a row in the messages: the longest context in whole blocks of 64
     size_t rows, bytes;           // of a slab
 };
