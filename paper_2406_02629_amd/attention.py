@@ -1,0 +1,107 @@
+"""The attention of a transformer block on Shamir shares, from the block's input to the projection of its heads, with its keys and values
+in a paged cache:
+
+    share the input (GEN) -> queries, keys and values in one dense layer -> degree reduction, truncation -> rotary positions of the
+    queries, keys (turned on the way) and values into the cache -> attention over the cache -> degree reduction, truncation -> dense
+    layer of the heads -> degree reduction, truncation
+
+Everything runs on the shares; the result is a degree-t sharing at scale 2^f.  `Sequences` is the caller's side of the paged cache: which
+pages belong to which sequence.
+"""
+from __future__ import annotations
+
+from typing import Dict, List, Optional
+
+import torch
+
+from . import fixedpoint as fx
+from .binding import PagedCache, SSNet
+
+
+class Sequences:
+    """Pages of a cache, given to sequences as they grow."""
+
+    def __init__(self, cache: PagedCache):
+        self.cache = cache
+        self.free: List[int] = list(range(cache.pages - 1, -1, -1))
+        self.pages: Dict[int, List[int]] = {}
+        self.length: Dict[int, int] = {}
+
+    def release(self, name: int):
+        """the sequence is over: its pages are free again"""
+        self.free += reversed(self.pages.pop(name, []))
+        self.length.pop(name, None)
+
+    def extend(self, counts: Dict[int, int], device=None):
+        """counts: new tokens of each sequence, in the order in which they stand in the batch.  Takes the pages that they need and
+        returns what the calls ask for: dict(pos, slots, seq_start, block_table, ctx_len, max_ctx)."""
+        size = self.cache.page_size
+        need = sum(-(-(self.length.get(s, 0) + c) // size) - len(self.pages.get(s, ())) for s, c in counts.items())
+        if need > len(self.free):
+            raise MemoryError(f"{need} pages needed, {len(self.free)} free")
+        pos, slots, start = [], [], [0]
+        for s, c in counts.items():
+            pages, old = self.pages.setdefault(s, []), self.length.get(s, 0)
+            while len(pages) * size < old + c:
+                pages.append(self.free.pop())
+            self.length[s] = old + c
+            pos += range(old, old + c)
+            slots += [pages[p // size] * size + p % size for p in range(old, old + c)]
+            start.append(start[-1] + c)
+        longest = max(1, max(len(self.pages[s]) for s in counts))
+        table = [self.pages[s] + [0] * (longest - len(self.pages[s])) for s in counts]
+        lengths = [self.length[s] for s in counts]
+
+        def i32(v):
+            return torch.tensor(v, dtype=torch.int32, device=device)
+
+        return dict(pos=i32(pos), slots=torch.tensor(slots, dtype=torch.int64, device=device), seq_start=i32(start), block_table=i32(table),
+                    ctx_len=i32(lengths), max_ctx=max(1, max(lengths)))
+
+
+class Attention:
+    """One attention layer.  w_qkv [width][(heads + 2 kv_heads) head_dim], w_out [heads head_dim][width]: float64 weights of the model's
+    owner, shared and packed once.  table: fixedpoint.rotary_table.  weight_bits: f, or 2 f for long contexts (a weight of a long
+    context's key is about 2^f / length)."""
+
+    STREAMS = 8      # stream ids that a forward pass uses
+
+    def __init__(self, ss: SSNet, w_qkv: torch.Tensor, w_out: torch.Tensor, heads: int, kv_heads: int, table: torch.Tensor, pages: int,
+                 page_size: int = 64, layout: str = "half", weight_bits: Optional[int] = None, stream_base: int = 1 << 22):
+        self.ss, self.heads, self.kv, self.table, self.layout = ss, heads, kv_heads, table, layout
+        self.dim = w_out.shape[0] // heads
+        self.width = w_out.shape[1]
+        self.bits = ss.f if weight_bits is None else weight_bits
+        if self.bits not in (ss.f, 2 * ss.f):
+            raise ValueError("weight_bits must be f or 2 f: the result is brought back to scale by truncations by 2^f")
+        if w_qkv.shape != (self.width, (heads + 2 * kv_heads) * self.dim):
+            raise ValueError("w_qkv must be [width][(heads + 2 kv_heads) head_dim]")
+        self.stream = stream_base
+
+        def packed(w, stream):
+            return ss.pack_weights_linear(ss.share(fx.encode(w.to(ss.device), ss.f, ss.p).contiguous(), stream_id=stream))
+
+        self.w_qkv, self.w_out = packed(w_qkv, stream_base - 1), packed(w_out, stream_base - 2)
+        self.cache = PagedCache(ss, pages, page_size, kv_heads, self.dim)
+        self.sequences = Sequences(self.cache)
+
+    def forward(self, x: torch.Tensor, counts: Dict[int, int]) -> torch.Tensor:
+        """x: shares [n][tokens][width] at scale 2^f of the new tokens, counts as in Sequences.extend -> shares [n][tokens][width]"""
+        ss, heads, kv, dim = self.ss, self.heads, self.kv, self.dim
+        n, tokens, _ = x.shape
+        batch = self.sequences.extend(counts, x.device)
+        if batch["pos"].numel() != tokens:
+            raise ValueError("counts must add up to the tokens of x")
+        stream, self.stream = self.stream, self.stream + self.STREAMS
+        qkv = ss.linear_mod_packed(x, self.w_qkv, (heads + 2 * kv) * dim)
+        qkv = ss.degree_reduce_truncate(qkv, stream_id=stream).view(n, tokens, heads + 2 * kv, dim)
+        q = ss.rotary_truncate(qkv[:, :, :heads], self.table, batch["pos"], stream + 1, layout=self.layout)
+        ss.cache_append(self.cache, qkv[:, :, heads:heads + kv], qkv[:, :, heads + kv:], batch["slots"], stream + 2, table=self.table,
+                        pos=batch["pos"], layout=self.layout)
+        o = ss.paged_attention(self.cache, q, batch["seq_start"], batch["block_table"], batch["ctx_len"], batch["max_ctx"], stream + 3,
+                               weight_bits=self.bits)
+        o = ss.degree_reduce_truncate(o, stream_id=stream + 4)
+        if self.bits == 2 * ss.f:
+            o = ss.truncate(o, stream_id=stream + 5)
+        y = ss.linear_mod_packed(o.view(n, tokens, heads * dim), self.w_out, self.width)
+        return ss.degree_reduce_truncate(y, stream_id=stream + 6)
