@@ -113,7 +113,7 @@ def test_refusals_of_the_binding():
                  lambda: ss.paged_attention(cache, x, start.long(), tab, ln, 4, 0), lambda: ss.rotary_truncate(x, table, pos, 0, out=x.cpu())):
         with pytest.raises(TypeError):
             call()
-    for call in (lambda: ss.rotary_truncate(x[:2], table, pos, 0), lambda: ss.rotary_truncate(x, table[..., 0], pos, 0),
+    for call in (lambda: ss.rotary_truncate(x[:2], table, pos, 0), lambda: ss.rotary_truncate(x, table[..., 0].contiguous(), pos, 0),
                  lambda: ss.rotary_truncate(x, table, pos, 0, layout="quarter"), lambda: ss.rotary_truncate(x, table, pos[:3].contiguous(), 0),
                  lambda: ss.cache_append(cache, x, x, slots, 0, table=table), lambda: ss.cache_append(cache, x[:, :, :1], x[:, :, :1], slots, 0),
                  lambda: ss.paged_attention(cache, x, start, tab[0], ln, 4, 0), lambda: ss.paged_attention(cache, x, start[:1], tab, ln, 4, 0),
