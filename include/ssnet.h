@@ -410,7 +410,8 @@ int ssnet_reduce_truncate_relu_direct(ssnet_ctx *ctx, const uint64_t *d_c, int B
  * the attention's result is a degree-2t sharing like that of a dense layer.
  * d_x of the calls below is [n][tokens][ld]: the heads of a token, heads *
  * head_dim consecutive elements, start every `ld` >= heads * head_dim elements,
- * so that queries, keys and values may be parts of one product.
+ * so that queries, keys and values may be parts of one product; tokens * heads *
+ * head_dim < SSNET_MAX_HEADS_COUNT.
  *
  * Rotary positions.  Pair j < rot/2 of the first `rot` elements of every head
  * is turned by the angle of its token: with (c, s) = table[pos[token]][j],
@@ -427,6 +428,7 @@ int ssnet_reduce_truncate_relu_direct(ssnet_ctx *ctx, const uint64_t *d_c, int B
  * rot).
  *   ssnet_rotary_truncate: d_out [n][tokens][heads][head_dim]; it may be d_x
  *     itself if ld = heads * head_dim, and must not overlap it otherwise. */
+#define SSNET_MAX_HEADS_COUNT (1L << 30)
 typedef struct ssnet_rotary {
     const int32_t *d_table;
     const int32_t *d_pos;

@@ -469,7 +469,7 @@ __device__ __forceinline__ seq_span span_of(const attn_args &g, int b)
     const int s0 = fixed_at(g.s.start, b), s1 = fixed_at(g.s.start, b + 1);
     const int first = max(s0, g.tok0), last = min(s1, g.tok1);
     int len = min(fixed_at(g.s.length, b), g.s.max_length);
-    len = max(0, min(len, g.s.max_pages * g.c.page_cells * 16));
+    len = max(0, (int)min((long long)len, (long long)g.s.max_pages * g.c.page_cells * 16));
     return {first, max(0, last - first), g.causal ? len - (s1 - first) + 1 : len, g.causal ? 1 : 0};
 }
 __device__ __forceinline__ int limit_at(const seq_span &s, int i) { return max(0, s.limit + i * s.step); }

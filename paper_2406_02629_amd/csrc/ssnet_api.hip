@@ -1237,10 +1237,10 @@ static ss_rope make_rope(const ssnet_rotary *r)
     return r ? ss_rope{(const int2 *)r->d_table, r->d_pos, r->positions, r->rot, r->interleaved ? 1 : 0} : ss_rope{};
 }
 
-// elements of a tensor of heads: the kernels count them in 31 bits
+// elements of a tensor of heads: the kernels count up to two threads for each in 31 bits
 static bool heads_ok(int tokens, int heads, int dim, size_t ld)
 {
-    return tokens >= 1 && heads >= 1 && dim >= 1 && (double)tokens * heads * dim < 2147483648.0 && ld >= (size_t)heads * dim &&
+    return tokens >= 1 && heads >= 1 && dim >= 1 && (double)tokens * heads * dim < SSNET_MAX_HEADS_COUNT && ld >= (size_t)heads * dim &&
            ld <= MAX_COUNT / tokens;
 }
 
@@ -1285,7 +1285,7 @@ static ss_paged make_paged(const ssnet_paged_cache *c)
 static bool attention_ok(const ssnet_paged_cache *c, int sequences, int tokens, int heads, int max_length)
 {
     return sequences >= 1 && sequences <= (1 << 20) && tokens >= 1 && heads >= 1 && heads % c->heads == 0 &&
-           (double)tokens * heads * c->head_dim < 2147483648.0 && max_length >= 1 && max_length <= SSNET_MAX_CONTEXT;
+           (double)tokens * heads * c->head_dim < SSNET_MAX_HEADS_COUNT && max_length >= 1 && max_length <= SSNET_MAX_CONTEXT;
 }
 
 }  // namespace
