@@ -745,15 +745,24 @@ struct row_norm {
     int drop;       // bits that the sum is shifted by
 };
 
-__device__ __forceinline__ row_norm norm_of(u64 sum)
+__device__ __forceinline__ u64 wave_value(u64 v)   // that all lanes have
 {
+    return (u64)(u32)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (u32)__builtin_amdgcn_readfirstlane((int)v);
+}
+
+// A row belongs to a wave or a workgroup: both words are kept in scalar registers.  The shifts by `drop` need it: a 64-bit shift whose amount
+// lies in the last vector register that the wave has can read v0 in its place here, which the compiler does not avoid.
+__device__ __forceinline__ row_norm norm_of(u64 of)
+{
+    const u64 sum = wave_value(of);
+    if (!sum) return {0, 0};
     const int drop = max(0, 32 - __clzll((long long)sum));
     // floor(2^62 / x), 2^30 <= x < 2^32, by way of a quotient in 53 bits that is off by one at most
     const u64 x = sum >> drop;
     u64 q = (u64)(4611686018427387904.0 / (double)x);
     const long long rest = (long long)((1ull << 62) - q * x);
     q = rest < 0 ? q - 1 : rest >= (long long)x ? q + 1 : q;
-    return {q, drop};
+    return {wave_value(q), drop};
 }
 
 // the weight of a key, w / sum, with sp.bits fraction bits
@@ -826,7 +835,7 @@ __global__ __launch_bounds__(THREADS) void softmax_kernel(attn_args g, ss_softma
         }
     }
     sum = block_reduce<THREADS>(sum, red, [](long long x, long long y) { return x + y; });
-    const row_norm nm = sum ? norm_of((u64)sum) : row_norm{0, 0};
+    const row_norm nm = norm_of((u64)sum);
 #pragma unroll
     for (int u = 0; u < RUNS; u++) {
         const int j = (u * THREADS + tid) * 4;
@@ -1055,7 +1064,7 @@ __global__ __launch_bounds__(512) void finish_kernel(attn_args g, ss_softmax_par
         }
 #pragma unroll
         for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-        const row_norm nm = sum ? norm_of((u64)sum) : row_norm{0, 0};
+        const row_norm nm = norm_of((u64)sum);
 #pragma unroll
         for (int c = 0; c < 4; c++) {
             const u64 counter = ss_counter(((u64)r.token * g.heads + h) << 32 | (u32)(j + c));

@@ -403,6 +403,20 @@ def test_rows_of_every_length_class(n, t, p, f, chunk, length):
 
 
 @gpu
+@pytest.mark.parametrize("n,t,p,f", SCHEMES)
+@pytest.mark.parametrize("chunk,length", [(250, 900), (300, 1100), (700, 2000)])
+def test_every_row_of_more_rows_than_the_card_holds_workgroups(n, t, p, f, chunk, length):
+    """rows of a chunk whose workgroups follow others on their CU, several calls"""
+    c = Context(n, t, p, f, [chunk], [length], 8, 1, 16, 64)
+    c.q[0] = c.q[0][:, chunk // 2:]
+    want = orc.attention(c.q[0], c.k[0], c.v[0], t, f, fixed_scale(16), f, True, p, 21, 5, chunk - chunk // 2)
+    first = c.run(f)
+    assert np.array_equal(host(first)[:, chunk // 2:], want)
+    for _ in range(3):
+        assert torch.equal(c.run(f), first)
+
+
+@gpu
 @pytest.mark.parametrize("n,t", [(3, 1), (5, 2)])
 def test_a_long_context_is_joined_from_several_runs(n, t):
     """longer than the 16383 products that a 32-bit sum of digits can take"""
