@@ -1226,37 +1226,37 @@ attention_plan plan_attention(int n, int t, int tokens, int seqs, int heads, int
     attention_plan p = {};
     const size_t group = heads / kv, nr = 2 * t + 1;
     p.keys = ((size_t)max_length + 63) & ~(size_t)63;
-    // Larger tiles and blocks read less, but leave fewer waves to a SIMD and fewer workgroups.  Scores + values, us, tiles of 32 / of 16 rows (by
-    // the workgroups of the scores with 32): chunk of 512 tokens over 4096, n = 5 (10400) 1975 / 2085; chunks of 17 to 121 over 121 to 777, n = 5
-    // (1160) 155 / 129; 230 tokens over 700 to 1024, n = 3, 45-bit prime (480) 64 / 62.  Keys to a workgroup, scores alone: single
-    // tokens over 32768 and 500 to 2001 128 / 256 / 1024 157 / 159 / 167, 92 / 94 / 105; the chunks above 256 / 512 / 1024 1157 / 1079 / 1040,
-    // 62 / 59 / 54, 29 / 30 / 32 (there 1024 leaves 384 workgroups for 768 places).
-    const size_t sequence_rows = ceil_div(tokens, seqs) * group;
-    auto workgroups = [&](size_t rows, size_t block) { return tile_bound(tokens, seqs, group, rows) * ceil_div(p.keys, block) * kv * nr; };
-    p.row_tiles = sequence_rows > 16 && workgroups(32, 512) >= 2048 ? 2 : 1;
-    p.key_block = sequence_rows > 16 ? 1024 : 128;
-    while (p.key_block > 256 && workgroups(16 * p.row_tiles, p.key_block) < (p.row_tiles == 2 ? 4096 : 768)) p.key_block /= 2;
     p.dblocks = ceil_div(dim, 64);
-    // one launch for softmax and values while each of its workgroups has a CU to itself (us, one launch / two): single tokens of 32 heads of
-    // 128 over 64 keys, n = 5, one sequence 15.1 / 18.2, 4 17.3 / 20.9, 16 (800 workgroups) 38.4 / 37.9, 64 109 / 104; over 256 keys, one 21.2 / 22.4
-    p.finish = p.row_tiles == 1 && p.keys <= SHORT_KEYS && tile_bound(tokens, seqs, group, 16) * kv * n <= 256;
-    p.slab = tokens;
-    for (;;) {
-        const size_t base = tile_bound(p.slab, seqs, group, 16 * p.row_tiles) * p.dblocks * kv * n;
+    // (a run of tokens is planned as a call of as many: a single token always fits into what a call of one needs)
+    for (p.slab = tokens;; p.slab = (p.slab + 1) / 2) {
+        // Larger tiles and blocks read less, but leave fewer waves to a SIMD and fewer workgroups.  Scores + values, us, tiles of 32 / of 16 rows
+        // (by the workgroups of the scores with 32): chunk of 512 tokens over 4096, n = 5 (10400) 1975 / 2085; chunks of 17 to 121 over 121 to
+        // 777, n = 5 (1160) 155 / 129; 230 tokens over 700 to 1024, n = 3, 45-bit prime (480) 64 / 62.  Keys to a workgroup, scores alone:
+        // single tokens over 32768 and 500 to 2001 128 / 256 / 1024 157 / 159 / 167, 92 / 94 / 105; the chunks above 256 / 512 / 1024 1157 /
+        // 1079 / 1040, 62 / 59 / 54, 29 / 30 / 32 (there 1024 leaves 384 workgroups for 768 places).
+        const size_t sequence_rows = ceil_div(p.slab, seqs) * group;
+        auto tiles = [&](size_t rows) { return tile_bound(p.slab, seqs, group, rows); };
+        auto workgroups = [&](size_t rows, size_t block) { return tiles(rows) * ceil_div(p.keys, block) * kv * nr; };
+        p.row_tiles = sequence_rows > 16 && workgroups(32, 512) >= 2048 ? 2 : 1;
+        p.key_block = sequence_rows > 16 ? 1024 : 128;
+        while (p.key_block > 256 && workgroups(16 * p.row_tiles, p.key_block) < (p.row_tiles == 2 ? 4096 : 768)) p.key_block /= 2;
+        // one launch for softmax and values while each of its workgroups has a CU to itself (us, one launch / two): single tokens of 32 heads of
+        // 128 over 64 keys, n = 5, one sequence 15.1 / 18.2, 4 17.3 / 20.9, 16 (800 workgroups) 38.4 / 37.9, 64 109 / 104; over 256 keys, one
+        // 21.2 / 22.4
+        p.finish = p.row_tiles == 1 && p.keys <= SHORT_KEYS && tiles(16) * kv * n <= 256;
         // single tokens read the values once, which several rounds of workgroups spread best over the memory (us, 2048 / 1024 workgroups wanted:
         // 87 / 98); chunks multiply, and a round of 384 that needs no sum is as good as three runs (20.4 / 19.5 + 5.2 for the sum)
-        const size_t wanted = ceil_div(sequence_rows <= 16 ? 2048 : 384, base);
+        const size_t wanted = ceil_div(sequence_rows <= 16 ? 2048 : 384, tiles(16 * p.row_tiles) * p.dblocks * kv * n);
         p.run = (int)((ceil_div(p.keys, wanted) + 63) & ~63u);
         if (p.run > MAX_RUN) p.run = MAX_RUN;
         if (p.run < 256) p.run = 256;
         p.splits = p.finish ? 1 : (int)ceil_div(p.keys, p.run);
         p.rows = (size_t)p.slab * heads;
         const size_t blocks = p.keys > SHORT_ROW ? ceil_div(p.keys, 1024) : 0;
-        p.bytes = align256(nr * p.rows * p.keys * 8) + (blocks ? align256(p.rows * (p.keys + 2 * blocks) * 8) : 0) + (p.finish ? 0 : align256((size_t)n * p.rows * p.keys * NL)) +
-                  (p.splits > 1 ? align256((size_t)p.splits * n * p.rows * dim * 8) : 0);
+        p.bytes = align256(nr * p.rows * p.keys * 8) + (blocks ? align256(p.rows * (p.keys + 2 * blocks) * 8) : 0) +
+                  (p.finish ? 0 : align256((size_t)n * p.rows * p.keys * NL)) + (p.splits > 1 ? align256((size_t)p.splits * n * p.rows * dim * 8) : 0);
         if (p.bytes <= room && p.rows <= MAX_ROWS) return p;
         if (p.slab == 1) break;
-        p.slab = (p.slab + 1) / 2;
     }
     p.slab = 0;
     return p;

@@ -481,6 +481,19 @@ def test_a_small_workspace_gives_the_same_result(n, t, p, f):
 
 
 @gpu
+@pytest.mark.parametrize("chunks,lengths,heads,kv,dim", [([5, 130], [40, 2600], 48, 1, 64), ([60], [200], 16, 16, 32), ([33], [4500], 20, 1, 96)])
+def test_room_for_one_token_serves_a_chunk(chunks, lengths, heads, kv, dim):
+    """a chunk whose tokens one by one go other ways than together: larger tiles, fewer runs, softmax and values apart"""
+    n, t, f = 5, 2, 13
+    c = Context(n, t, P61, f, chunks, lengths, heads, kv, dim, 32)
+    want = c.run(f)
+    c.ss = SSNet(n, t, f=f, seed=21, p=P61)
+    c.ss.ATTENTION_ROOM = 0
+    assert torch.equal(c.run(f), want)
+    assert c.ss._ws.numel() == c.ss.workspace_bytes_attention(c.cache, len(chunks), 1, heads, max(lengths))
+
+
+@gpu
 def test_workspace_too_small_is_refused_and_a_pending_product_survives():
     n, t = 5, 2
     c = Context(n, t, P61, 13, [2], [70], 2, 1, 32, 16)
