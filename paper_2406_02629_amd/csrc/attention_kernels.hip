@@ -8,6 +8,13 @@
 //      numbers (softmax_weight below), and shares the weights (degree t); every party's share of a key beyond the limit is 0
 //   3. every party i = 1..n: O_i = sum_j P_i[j] v_i[j] mod p (degree 2t)
 // Products run on int8 MFMA over balanced 8-bit digits, as in a dense layer.
+//
+// Every message lies in memory, as the protocol has it: a row of L keys costs 8 (2t+1) L bytes of scores and NL n L of weights, each written
+// and read once, beside the cache itself.  So three kernels, not one: a workgroup that took all steps for its rows would
+// take 2t+1 parties' keys and n parties' values one after the other (single tokens of 32 heads of 128 over 64 keys, n = 5: 24 to 46 us for one
+// sequence to four, against 16 to 19.5).  Only softmax and values go together, over short contexts.
+// Figures of the kernels below are those of MI355X, where a copy moves 6.3 TB/s, a sum reads 6.1 and int8 MFMA reaches 3.6 POP/s on random
+// digits.
 #include "kernels.hpp"
 #include "eval.hpp"
 #include "digits.hpp"
@@ -19,12 +26,16 @@ namespace SS_NS {
 namespace {
 
 constexpr int BLOCK = 256;
-constexpr size_t STREAM_BYTES = (size_t)256 << 20;   // what a call writes, from which on past the caches
+// What a rotation reads and writes, from which on it goes past the caches: heads of 128 turned whole, us, past / by way of them: 151 MB 25.7 / 22.2,
+// 185 MB 28.8 / 31.7, 302 MB 44.7 / 48.8, 369 MB 53 / 66, 738 MB 106 / 125.
+constexpr size_t STREAM_BYTES = (size_t)256 << 20;
 // Elements of the new keys from which on the kernel for many tokens takes them: tokens of 8 heads of 128, us, it / one thread per pair: n = 5, 128
 // tokens 14.3 / 13.8, 256 21.8 / 25.0; n = 3 11.2 / 10.1, 12.7 / 16.0.
 constexpr size_t WIDE_APPEND = (size_t)3 << 16;
 constexpr size_t MAX_ROWS = (size_t)1 << 22;   // of a slab: a workgroup each, less than 2^32 threads in a launch
-constexpr size_t SHORT_ROW = 4096;   // keys up to which one workgroup takes the softmax of a row
+// Keys up to which one workgroup takes the softmax of a row (the whole attention, us, so / in blocks of 1024 keys: 32 rows of 1100 keys, n = 5,
+// 36 / 41, of 4096, n = 3, 61 / 65, 512 rows of 4096 135 / 150).
+constexpr size_t SHORT_ROW = 4096;
 constexpr int MAX_RUN = 16320;      // keys that the 32-bit sums of the values can take, in blocks of 64: 8 * 16383 * 2^14 < 2^31
 
 inline unsigned ceil_div(size_t a, size_t b) { return (unsigned)((a + b - 1) / b); }
@@ -131,7 +142,7 @@ __device__ __forceinline__ void rotate_pair(const u64 *x, size_t ld, const rotar
     truncate_elements<N, T, 1, false>(rb, e + b, count, u, wsh, tp, ob);
 }
 
-// One thread per pair, or element that passes through, of a head.
+// One thread per pair, or element that passes through, of a head: for whatever the kernel below cannot load 16 bytes at a time.
 template <int N, int T>
 __global__ __launch_bounds__(BLOCK) void rotary_kernel(const u64 *x, size_t ld, u64 *__restrict__ u, u64 *__restrict__ wsh, u64 *out,
                                                        rotary_shape g, ss_rope rope, ss_tr_params tp)
@@ -202,7 +213,10 @@ __device__ __forceinline__ void rotate_two(const u64 *src, size_t party, size_t 
     }
 }
 
-// The rotation of a head in such steps, or two elements that pass through, to a thread.  STREAM: messages and results past the caches.
+// The rotation of a head in such steps, or two elements that pass through, to a thread.  The random polynomials of the truncation are drawn
+// where they are used, so that memory bounds it: shares in and out, t + 1 + n words of messages per element.  2048 tokens, 32 heads of
+// 128, half of each turned, n = 3: 93 us, 537 MB at 5.8 TB/s (one thread per pair: 118).  8 tokens, n = 5: 7 us, a launch and one element's
+// chain of draws.  STREAM: messages and results past the caches.
 template <int N, int T, bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(BLOCK) void rotary_wide_kernel(const u64 *x, size_t ld, u64 *__restrict__ u, u64 *__restrict__ wsh, u64 *out,
                                                             rotary_shape g, ss_rope rope, ss_tr_params tp)
@@ -270,7 +284,8 @@ __device__ __forceinline__ void put_key(const append_shape &s, size_t cell, int 
         }
 }
 
-// A few tokens: one thread per pair (or element that passes through) of a key, then one per element of a value; digits go out as bytes.
+// A few tokens: one thread per pair (or element that passes through) of a key, then one per element of a value; digits go out as bytes.  A
+// launch and one element's chain of draws bound it: 8 tokens of 8 heads of 128, n = 5, 6.1 us.
 template <int N, int T>
 __global__ __launch_bounds__(BLOCK) void append_kernel(const u64 *k, size_t ld_k, const u64 *v, size_t ld_v, u64 *__restrict__ u,
                                                        u64 *__restrict__ wsh, append_shape s, ss_rope rope, ss_tr_params tp, u32 key_blocks)
@@ -421,8 +436,9 @@ __device__ __forceinline__ void append_values(const u64 *v, size_t ld, const app
         }
 }
 
-// Both in one launch: grid.x blocks of 16 tokens by blocks of 16 steps of the keys, then by blocks of 256 elements and parties of the values;
-// grid.y heads.
+// Both in one launch, bound by memory: keys, values and their digits, t + 1 + n words of messages per element of a key.  2048 tokens of 8 heads of
+// 128, n = 5: 97 us, 436 MB at 4.5 TB/s (the kernel for a few tokens, whose bytes go out one by one: 269).
+// Grid.x: blocks of 16 tokens by blocks of 16 steps of the keys, then by blocks of 256 elements and parties of the values; grid.y: heads.
 template <int N, int T, bool INTERLEAVED>
 __global__ __launch_bounds__(BLOCK) void append_many_kernel(const u64 *k, size_t ld_k, const u64 *v, size_t ld_v, u64 *__restrict__ u,
                                                             u64 *__restrict__ wsh, append_shape s, ss_rope rope, ss_tr_params tp, int key_blocks,
@@ -575,7 +591,11 @@ __device__ __forceinline__ void stage_query(const attn_args &g, v4i *qd, const s
 
 // Step 1: one workgroup per (tile of 16 MT rows, block of g.key_block keys, kv head and party).  The digits of the queries lie in LDS in
 // MFMA order; a wave takes a cell of 16 keys at a time straight from the cache, the next 64 elements of a cell (or the next cell's first)
-// on their way while those at hand are multiplied.
+// on their way while those at hand are multiplied.  A cell is a wave's own (no other has a use for it) and its digits are in MFMA order as
+// they lie, so they need no LDS.
+// Single tokens are bound by reading the keys once: 32 heads over 8 of 128, n = 5, eight contexts of 500 to 2001, 410 MB in 83 to 89 us (4.6 to
+// 4.9 TB/s); n = 3, one of 32768, 805 MB in 153 to 159 (5.1 to 5.3).  Chunks by the matrix cores: 512 tokens of 16 heads over 4096 keys, n = 5,
+// 980 to 1060 us, 2.4 to 2.6 POP/s of the products, their reads from LDS (MT = 2: 16 for 128 products) and the fold of 15 sums beside them.
 template <int MT>
 __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_params sp)
 {
@@ -796,7 +816,9 @@ __device__ __forceinline__ void share_weights(const attn_args &g, const ss_softm
         }
 }
 
-// Step 2 for rows of up to 4 THREADS RUNS keys, one workgroup each: opened once, maximum, weights and sum in registers.
+// Step 2 for rows of up to 4 THREADS RUNS keys, one workgroup each: opened once, maximum, weights and sum in registers.  Bound by the messages
+// in and the weights out where there are many rows: 8192 of 3585 to 4096 keys, n = 5, 538 us for 2.5 GB, 4.7 TB/s (past the caches 626 to 672: the weights
+// are read again at once); 256 rows of 2001 keys 13 to 15 us, the chain from load to load of one row.
 template <int N, int T, int RUNS, int THREADS>
 __global__ __launch_bounds__(THREADS) void softmax_kernel(attn_args g, ss_softmax_params sp)
 {
@@ -844,7 +866,8 @@ __global__ __launch_bounds__(THREADS) void softmax_kernel(attn_args g, ss_softma
     }
 }
 
-// ... for longer rows, which several workgroups take in blocks of 1024 keys: opened, with the largest score of each block,
+// ... for longer rows, which several workgroups take in blocks of 1024 keys (32 rows of 32768, n = 3: 10 + 7.9 + 13 us; in one workgroup to a row
+// they would leave seven CUs of eight idle): opened, with the largest score of each block,
 template <int T>
 __global__ __launch_bounds__(BLOCK) void open_kernel(attn_args g, ss_softmax_params sp)
 {
@@ -923,7 +946,10 @@ __global__ __launch_bounds__(BLOCK) void weights_kernel(attn_args g, ss_softmax_
 // Step 3: one workgroup per (tile of 16 MT rows, run of keys and up to 64 elements of the head, kv head and party); a wave takes 16
 // elements.  The digits of 64 weights of every row go through LDS to all waves, those of the values to a wave's registers; the next
 // 64 keys are on their way while those at hand are multiplied.  (The weights too by way of registers: behind copies straight into LDS the
-// compiler waits before the next read of any LDS.)
+// compiler waits before the next read of any LDS.)  Long rows of few tokens are cut into runs, which join_kernel adds up.
+// Single tokens are bound by reading the values once: the sizes at scores_kernel 84 to 88 and 144 to 150 us, 4.7 to 5.6 TB/s.  Chunks by the
+// matrix cores: 890 to 940 us there, 2.7 to 2.9 POP/s.  A workgroup of eight waves that takes 128 elements saves half of the weights' reads but
+// leaves one workgroup to a CU: 1020 against 935 us; waves by the head's size (5 for 80 elements) 64 against 54.
 template <int MT>
 __global__ __launch_bounds__(256, 2) void values_kernel(attn_args g, int n)
 {
@@ -1016,7 +1042,8 @@ __global__ __launch_bounds__(256, 2) void values_kernel(attn_args g, int n)
 
 // Steps 2 and 3 in one launch for contexts of up to 256 keys: one workgroup of eight waves per (tile of 16 rows, kv head and party) takes the
 // softmax of the rows, a wave to a row and four keys to a lane, keeps its own party's shares of the weights in LDS and multiplies, a
-// wave to 16 elements of the head.  All parties' workgroups take the same softmax, which costs less than a launch.
+// wave to 16 elements of the head.  All parties' workgroups take the same softmax, which costs less than a launch.  Bound by its chain of
+// loads: 4 heads of 64 over 33 keys, n = 3, 6.4 to 6.8 us beside 4.7 to 5.0 of the scores (three launches: 19 for all).
 constexpr int SHORT_KEYS = 256;
 template <int T>
 __global__ __launch_bounds__(512) void finish_kernel(attn_args g, ss_softmax_params sp)
@@ -1334,6 +1361,8 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
             if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
             continue;
         }
+        // rows of 1024 to 4096 keys: four runs of 256 threads where they fill the card, 1024 threads otherwise (the whole attention, us, four runs /
+        // 1024 threads: 2048 rows of 2000 keys, n = 3, 201 / 211, of 1100 682 / 695; 32 rows of 1100, n = 5, 37.1 / 35.7, of 4096 89.9 / 88.7)
 #define SS_LAUNCH(NC, TC)                                                                               \
     do {                                                                                                \
         if (split_rows) {                                                                               \
