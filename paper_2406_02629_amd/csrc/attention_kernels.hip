@@ -682,7 +682,7 @@ __device__ __forceinline__ long long lift(u64 v) { return v <= (SS_P - 1) / 2 ? 
 __device__ __forceinline__ u32 softmax_weight(long long below, const ss_softmax_params &sp)
 {
     const int h = min(2 * sp.f, 24);
-    const u64 d = min((u64)below >> (2 * sp.f - h), 1ull << 37), u = (d * sp.scale) >> (h + 8);
+    const u64 d = min((u64)below >> (2 * sp.f - h), (u64)1 << 37), u = (d * sp.scale) >> (h + 8);
     const u32 r = (u32)u << 16;                  // the fraction, 32 bits
     u32 w = 1077640u;
     w = 10033292u - __umulhi(w, r);
@@ -791,28 +791,30 @@ __device__ __forceinline__ u64 weight_of(u32 w, const row_norm &nm, const ss_sof
     return ((((u64)w * nm.recip) >> 16) + (1ull << (45 - sp.bits + nm.drop))) >> (46 - sp.bits + nm.drop);
 }
 
-// The weights of four keys (w, 30 fraction bits, 0 beyond the limit; `seen` of them are keys that the row sees), shared, as digits.
+// The weights of four keys (w, 30 fraction bits, 0 beyond the limit; `seen` of them are keys that the row sees), shared, as digits.  The shares
+// need not be below p for that: any word of the residue has digits that the sums of the values hold.
 template <int N, int T>
 __device__ __forceinline__ void share_weights(const attn_args &g, const ss_softmax_params &sp, const row_place &r, int j, const u32 (&w)[4], int seen,
                                               const row_norm &nm)
 {
     const int n = N ? N : sp.n;
     u64 y[MAXP<N>][4];
+    const u64 counter = ss_counter(((u64)r.token * g.heads + r.head) << 32 | (u32)j);
 #pragma unroll
     for (int c = 0; c < 4; c++) {
-        const u64 p = weight_of(w[c], nm, sp);
-        const u64 counter = ss_counter(((u64)r.token * g.heads + r.head) << 32 | (u32)(j + c));
         u64 a[T];
 #pragma unroll
-        for (int x = 0; x < T; x++) a[x] = ss_draw_lazy_at(sp.gen_key[x], counter);
-        eval_points<T, MAXP<N>>(p, a, [&](int m, u64 v) { y[m][c] = c < seen ? balanced_digits(v) : 0; }, n);
+        for (int x = 0; x < T; x++) a[x] = c < seen ? ss_draw_lazy_at(sp.gen_key[x], counter + c * SS_GAMMA) : 0;
+        eval_points<T, MAXP<N>, LAZY>(weight_of(w[c], nm, sp), a, [&](int m, u64 v) { y[m][c] = balanced_digits(v); }, n);
     }
     signed char *dst = g.weights + (size_t)r.id * g.keys * NL + (size_t)(j >> 6) * (64 * NL) + (j & 63);
 #pragma unroll
     for (int m = 0; m < MAXP<N>; m++)
         if (N != 0 || m < n) {
+            u32 d[8];
+            limb_dwords(y[m], d);
 #pragma unroll
-            for (int l = 0; l < NL; l++) *reinterpret_cast<u32 *>(dst + m * g.rows * g.keys * NL + l * 64) = limb_dword(y[m], l);
+            for (int l = 0; l < NL; l++) *reinterpret_cast<u32 *>(dst + m * g.rows * g.keys * NL + l * 64) = d[l];
         }
 }
 
@@ -843,7 +845,11 @@ __global__ __launch_bounds__(THREADS) void softmax_kernel(attn_args g, ss_softma
         const int j = (u * THREADS + tid) * 4;
 #pragma unroll
         for (int c = 0; c < 4; c++)
-            if (j + c < r.limit) top = max(top, lift(ss_sub(v[u][c], ref)));
+            if (j + c < r.limit) {
+                const long long d = lift(ss_sub(v[u][c], ref));
+                v[u][c] = (u64)d;
+                top = max(top, d);
+            }
     }
     top = block_reduce<THREADS>(top, red, [](long long x, long long y) { return max(x, y); });
     long long sum = 0;
@@ -852,7 +858,7 @@ __global__ __launch_bounds__(THREADS) void softmax_kernel(attn_args g, ss_softma
         const int j = (u * THREADS + tid) * 4;
 #pragma unroll
         for (int c = 0; c < 4; c++) {
-            w[u][c] = j + c < r.limit ? softmax_weight(top - lift(ss_sub(v[u][c], ref)), sp) : 0;
+            w[u][c] = j + c < r.limit ? softmax_weight(top - (long long)v[u][c], sp) : 0;
             sum += w[u][c];
         }
     }

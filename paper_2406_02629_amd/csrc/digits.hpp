@@ -18,6 +18,22 @@ __device__ __forceinline__ u32 limb_dword(const u64 (&y)[4], int limb)
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, sel), __builtin_amdgcn_perm(b, a, sel), 0x05040100u);
 }
 
+// all of them, d[limb] (those of six limbs in the 45-bit field are d[0..5]): bytes of two words side by side first, two steps of v_perm_b32
+// for a dword instead of three
+__device__ __forceinline__ void limb_dwords(const u64 (&y)[4], u32 (&d)[8])
+{
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        const u32 a = (u32)(y[0] >> (32 * h)), b = (u32)(y[1] >> (32 * h)), c = (u32)(y[2] >> (32 * h)), e = (u32)(y[3] >> (32 * h));
+        const u32 ab0 = __builtin_amdgcn_perm(b, a, 0x05010400u), ce0 = __builtin_amdgcn_perm(e, c, 0x05010400u);   // digits 0 and 1
+        const u32 ab2 = __builtin_amdgcn_perm(b, a, 0x07030602u), ce2 = __builtin_amdgcn_perm(e, c, 0x07030602u);   // digits 2 and 3
+        d[4 * h] = __builtin_amdgcn_perm(ce0, ab0, 0x05040100u);
+        d[4 * h + 1] = __builtin_amdgcn_perm(ce0, ab0, 0x07060302u);
+        d[4 * h + 2] = __builtin_amdgcn_perm(ce2, ab2, 0x05040100u);
+        d[4 * h + 3] = __builtin_amdgcn_perm(ce2, ab2, 0x07060302u);
+    }
+}
+
 // the values of v in the four lanes r, r + 16, r + 32, r + 48 of the caller's r, which all four call (register swaps: a
 // shuffle by index goes through LDS)
 __device__ __forceinline__ void gather_rows(u64 v, u64 (&y)[4])

@@ -5,12 +5,14 @@
 // values a0 + a[0] x + ... at x = 1..m (m <= M <= 8), canonical, handed to emit(x - 1, value); a0, a[] may be
 // unreduced sums: a0 < 2 * 2^61 + 2^8, a[] < 2^61 + 2^8 (over the 45-bit prime: below 2^57).  Forward differences;
 // in the bounds below one unit is 2^61 + 2^8 and a word holds less than eight.  PACED: the longer form of the
-// reduction, which a kernel bound by its stores may prefer.
-template <int T, int M, bool PACED = false, typename F>
+// reduction, which a kernel bound by its stores may prefer.  LAZY: values folded once, below 2^61 + 8 (2^45 + 2^25)
+// instead of canonical.
+enum eval_form { PLAIN, PACED, LAZY };
+template <int T, int M, int FORM = PLAIN, typename F>
 __device__ __forceinline__ void eval_points(u64 a0, const u64 (&a)[T], F &&emit, int m = M)
 {
     static_assert(T >= 1 && T <= 3 && M <= 8, "degrees 1 to 3, up to 8 points");
-    auto reduce = [](u64 x) { return PACED ? ss_canon(ss_fold(x)) : ss_reduce(x); };
+    auto reduce = [](u64 x) { return FORM == LAZY ? ss_fold(x) : FORM == PACED ? ss_canon(ss_fold(x)) : ss_reduce(x); };
     u64 s = a0;
     if constexpr (T == 1) {
 #pragma unroll
