@@ -595,7 +595,8 @@ __device__ __forceinline__ void stage_query(const attn_args &g, v4i *qd, const s
 // they lie, so they need no LDS.
 // Single tokens are bound by reading the keys once: 32 heads over 8 of 128, n = 5, eight contexts of 500 to 2001, 410 MB in 83 to 89 us (4.6 to
 // 4.9 TB/s); n = 3, one of 32768, 805 MB in 153 to 159 (5.1 to 5.3).  Chunks by the matrix cores: 512 tokens of 16 heads over 4096 keys, n = 5,
-// 980 to 1060 us, 2.4 to 2.6 POP/s of the products, their reads from LDS (MT = 2: 16 for 128 products) and the fold of 15 sums beside them.
+// 1020 to 1140 us, 2.3 to 2.5 POP/s, at the 1.7 GHz that this work leaves the card (the first calls take 940 to 980): products 69 % of the
+// cycles, the folds of 15 sums (MT = 2: 8 for 256 products) beside them.
 template <int MT>
 __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_params sp)
 {
@@ -818,9 +819,10 @@ __device__ __forceinline__ void share_weights(const attn_args &g, const ss_softm
         }
 }
 
-// Step 2 for rows of up to 4 THREADS RUNS keys, one workgroup each: opened once, maximum, weights and sum in registers.  Bound by the messages
-// in and the weights out where there are many rows: 8192 of 3585 to 4096 keys, n = 5, 538 us for 2.5 GB, 4.7 TB/s (past the caches 626 to 672: the weights
-// are read again at once); 256 rows of 2001 keys 13 to 15 us, the chain from load to load of one row.
+// Step 2 for rows of up to 4 THREADS RUNS keys, one workgroup each: opened once, maximum, weights and sum in registers.  Many rows are
+// bound by their arithmetic (210 vector instructions to a key at n = 5, a seventh of them products) and, next to it, by the messages in and the weights
+// out: 8192 of 3585 to 4096 keys, n = 5, 490 us for 2.5 GB, 5.1 TB/s (past the caches 90 to 130 more: the weights are read again at once).
+// 256 rows of 2001 keys 13 us, the chain from load to load of one row.
 template <int N, int T, int RUNS, int THREADS>
 __global__ __launch_bounds__(THREADS) void softmax_kernel(attn_args g, ss_softmax_params sp)
 {
@@ -954,7 +956,7 @@ __global__ __launch_bounds__(BLOCK) void weights_kernel(attn_args g, ss_softmax_
 // 64 keys are on their way while those at hand are multiplied.  (The weights too by way of registers: behind copies straight into LDS the
 // compiler waits before the next read of any LDS.)  Long rows of few tokens are cut into runs, which join_kernel adds up.
 // Single tokens are bound by reading the values once: the sizes at scores_kernel 84 to 88 and 144 to 150 us, 4.7 to 5.6 TB/s.  Chunks by the
-// matrix cores: 890 to 940 us there, 2.7 to 2.9 POP/s.  A workgroup of eight waves that takes 128 elements saves half of the weights' reads but
+// matrix cores: 915 to 1000 us there, 2.6 to 2.8 POP/s, products 79 % of the cycles.  A workgroup of eight waves that takes 128 elements saves half of the weights' reads but
 // leaves one workgroup to a CU: 1020 against 935 us; waves by the head's size (5 for 80 elements) 64 against 54.
 template <int MT>
 __global__ __launch_bounds__(256, 2) void values_kernel(attn_args g, int n)
