@@ -32,7 +32,7 @@ constexpr size_t STREAM_BYTES = (size_t)256 << 20;
 // Elements of the new keys from which on the kernel for many tokens takes them: tokens of 8 heads of 128, us, it / one thread per pair: n = 5, 128
 // tokens 14.3 / 13.8, 256 21.8 / 25.0; n = 3 11.2 / 10.1, 12.7 / 16.0.
 constexpr size_t WIDE_APPEND = (size_t)3 << 16;
-constexpr size_t MAX_ROWS = (size_t)1 << 22;   // of a slab: a workgroup each, less than 2^32 threads in a launch
+constexpr size_t MAX_GROUPS = ((size_t)1 << 24) - 1;   // workgroups of 256 threads in a launch: less than 2^32 threads (the runtime cuts more off)
 // Keys up to which one workgroup takes the softmax of a row (the whole attention, us, so / in blocks of 1024 keys: 32 rows of 1100 keys, n = 5,
 // 36 / 41, of 4096, n = 3, 61 / 65, 512 rows of 4096 135 / 150).
 constexpr size_t SHORT_ROW = 4096;
@@ -956,8 +956,9 @@ __global__ __launch_bounds__(BLOCK) void weights_kernel(attn_args g, ss_softmax_
 // 64 keys are on their way while those at hand are multiplied.  (The weights too by way of registers: behind copies straight into LDS the
 // compiler waits before the next read of any LDS.)  Long rows of few tokens are cut into runs, which join_kernel adds up.
 // Single tokens are bound by reading the values once: the sizes at scores_kernel 84 to 88 and 144 to 150 us, 4.7 to 5.6 TB/s.  Chunks by the
-// matrix cores: 915 to 1000 us there, 2.6 to 2.8 POP/s, products 79 % of the cycles.  A workgroup of eight waves that takes 128 elements saves half of the weights' reads but
-// leaves one workgroup to a CU: 1020 against 935 us; waves by the head's size (5 for 80 elements) 64 against 54.
+// matrix cores: 915 to 1000 us there, 2.6 to 2.8 POP/s, products 79 % of the cycles.  A workgroup of eight waves that takes 128 elements
+// saves half of the weights' reads but leaves one workgroup to a CU: 1020 against 935 us; waves by the head's size (5 for 80 elements) 64
+// against 54.
 template <int MT>
 __global__ __launch_bounds__(256, 2) void values_kernel(attn_args g, int n)
 {
@@ -1290,7 +1291,9 @@ attention_plan plan_attention(int n, int t, int tokens, int seqs, int heads, int
         const size_t blocks = p.keys > SHORT_ROW ? ceil_div(p.keys, 1024) : 0;
         p.bytes = align256(nr * p.rows * p.keys * 8) + (blocks ? align256(p.rows * (p.keys + 2 * blocks) * 8) : 0) +
                   (p.finish ? 0 : align256((size_t)n * p.rows * p.keys * NL)) + (p.splits > 1 ? align256((size_t)p.splits * n * p.rows * dim * 8) : 0);
-        if (p.bytes <= room && p.rows <= MAX_ROWS) return p;
+        const size_t most = max(max(workgroups(16 * p.row_tiles, p.key_block), tiles(16 * p.row_tiles) * kv * n * p.splits * p.dblocks),
+                                max(p.rows * max(blocks, (size_t)1), (size_t)ceil_div(p.rows * dim, BLOCK / (p.splits > 8 ? 4 : 1)) * n));
+        if (p.bytes <= room && most <= MAX_GROUPS) return p;
         if (p.slab == 1) break;
     }
     p.slab = 0;

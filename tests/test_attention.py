@@ -480,6 +480,22 @@ def test_a_small_workspace_gives_the_same_result(n, t, p, f):
     assert np.array_equal(host(out), want)
 
 
+@pytest.mark.parametrize("tokens,heads,dim,keys", [(1024, 32, 64, 16384), (8192, 8, 128, 8192), (4096, 64, 32, 4000), (100, 8, 64, 1000)])
+def test_no_launch_has_2_32_threads(tokens, heads, dim, keys):
+    """single tokens of many sequences: the workspace asked for is that of a run of tokens whose workgroups of scores, one of 256 threads to a token, head
+    of the cache, party and 128 keys, are fewer (more would be cut off without an error).  It holds the messages and the weights; sums of
+    runs of keys add less than 2 % here."""
+    for n, t, f, p, digits in ((5, 2, 13, P61, 8), (3, 1, 12, P45, 6), (8, 3, 13, P61, 8)):
+        ss = SSNet(n, t, f=f, seed=1, p=p, device=None)
+        cache = binding._PagedCacheStruct(None, None, 1, 16, heads, dim)
+        need = ss.lib.ssnet_workspace_bytes_attention(ss._ctx, C.addressof(cache), tokens, tokens, heads, keys)
+        parties, padded = 2 * t + 1, (keys + 63) // 64 * 64
+        run = need / (heads * padded * (8 * parties + digits * n))
+        assert run * heads * parties * math.ceil(padded / 128) < 1.02 * 2 ** 24
+        if tokens * heads * parties * math.ceil(padded / 128) < 2 ** 24:
+            assert run >= tokens
+
+
 @gpu
 @pytest.mark.parametrize("chunks,lengths,heads,kv,dim", [([5, 130], [40, 2600], 48, 1, 64), ([60], [200], 16, 16, 32), ([33], [4500], 20, 1, 96)])
 def test_room_for_one_token_serves_a_chunk(chunks, lengths, heads, kv, dim):
