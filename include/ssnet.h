@@ -476,8 +476,11 @@ int ssnet_cache_append(ssnet_ctx *ctx, const ssnet_paged_cache *cache, const uin
  * Per row (token, head), row index r = token * heads + head, keys j:
  *   1. parties i = 1..2t+1: S_i[j] = q_i . k_i[j] mod p (degree 2t, 2f fraction
  *      bits) plus their share of a mask, uniform in F_p and the same for all keys
- *      of the row (domains ROW_MASK and, for the t coefficients of its sharing,
- *      ROWMASK_GEN, counter r);
+ *      of the row (domain ROW_MASK, counter r).  It is shared afresh with degree 2t
+ *      for every key: the shares of parties 1..2t are uniform (domain ROWMASK_GEN,
+ *      party i, counter r 2^32 + j), that of party 2t+1 is the one with which all of
+ *      them open to the mask.  So the messages of a key are uniform but for the
+ *      sum they open to;
  *   2. the elite party reconstructs s[j] + mask, takes the softmax of the row,
  *      which no constant added to it changes, and shares the weights with degree
  *      t (domain WEIGHT_GEN, counter r 2^32 + j).  Of keys that the row does not
@@ -485,7 +488,10 @@ int ssnet_cache_append(ssnet_ctx *ctx, const ssnet_paged_cache *cache, const uin
  *   3. all parties: O_i = sum_j P_i[j] v_i[j] mod p.
  * So the elite party learns the differences of a row's scores, that is the
  * weights, as it learns the ratios inside a pooling kernel under a mask that is
- * equal there; no party learns a score, a query, a key or a value.
+ * equal there.  Beyond these differences t parties learn nothing of scores,
+ * queries, keys or values.  The differences of more than head_dim rows over as
+ * many keys give the queries and the differences of keys up to a linear map that
+ * is common to them: where that is too much, weights must not be opened.
  * The softmax is defined in whole numbers: with d the distance of a score from
  * the largest of its row (signed, 2f fraction bits) and h = min(2f, 24),
  *   u = (min(d >> (2f - h), 2^37) * scale) >> (h + 8)  (octaves, 16 fraction bits),

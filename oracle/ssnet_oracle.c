@@ -929,15 +929,15 @@ void orc_attention(const u64 *q, const u64 *k, const u64 *v, int n, int t, int c
             if (limit < 0) limit = 0;
             u64 row = (u64)(token0 + i) * heads + h;
             u64 *s = (u64 *)calloc(len + 1, sizeof(u64)), *w = (u64 *)calloc(len + 1, sizeof(u64));
-            /* the mask of the row at every reducing party */
-            u64 mask[ORC_MAXN];
-            for (int m = 0; m < nr; m++) {
-                mask[m] = orc_draw_field(orc_key(seed, ORC_DOM_ROW_MASK, stream_id, 0, 0), row, p);
-                for (int j = 1; j <= t; j++)
-                    mask[m] = orc_add(mask[m], orc_mul(orc_draw_field(orc_key(seed, ORC_DOM_ROWMASK_GEN, stream_id, 0, j), row, p),
-                                                       orc_pow(m + 1, j, p), p), p);
-            }
+            /* the mask of the row, shared afresh with degree 2t for every key: the shares of all parties but the last are drawn */
+            u64 mask[ORC_MAXN], rho = orc_draw_field(orc_key(seed, ORC_DOM_ROW_MASK, stream_id, 0, 0), row, p);
             for (int j = 0; j < limit; j++) {
+                u64 rest = rho;
+                for (int m = 0; m < nr - 1; m++) {
+                    mask[m] = orc_draw_field(orc_key(seed, ORC_DOM_ROWMASK_GEN, stream_id, m + 1, 0), (row << 32) + j, p);
+                    rest = orc_sub(rest, orc_mul(lambda[m], mask[m], p), p);
+                }
+                mask[nr - 1] = orc_mul(rest, orc_inv(lambda[nr - 1], p), p);
                 for (int m = 0; m < nr; m++) {
                     u64 dot = mask[m];
                     for (int d = 0; d < dim; d++)

@@ -3,7 +3,7 @@
 //
 // Attention of a row (token, head) over the keys j < limit, all parties holding degree-t shares:
 //   1. party i = 1..2t+1: score S_i[j] = q_i . k_i[j] mod p (degree 2t, 2 f fraction bits), plus its share of a mask that is the same for
-//      all keys of the row                                                                        -> msg[i][row][j]
+//      all keys of the row, shared afresh with degree 2t for every key                            -> msg[i][row][j]
 //   2. the elite party reconstructs s[j] + mask, takes the softmax of the row, which no constant added to it changes, as whole
 //      numbers (softmax_weight below), and shares the weights (degree t); every party's share of a key beyond the limit is 0
 //   3. every party i = 1..n: O_i = sum_j P_i[j] v_i[j] mod p (degree 2t)
@@ -563,13 +563,20 @@ __device__ __forceinline__ void multiply(const v4i *a, int stride, const v4i (&k
     }
 }
 
-// share of the mask of a row
-__device__ __forceinline__ u64 row_mask(const ss_softmax_params &sp, u64 row, int party)
+// A party's share of the mask of a row for one key, below 2^62 (2^47): those of parties 1..2t are drawn, that of party 2t+1 is what makes them open to
+// the mask, of which its own multiplier is 1.  One set of shares for the whole row would leave the differences of a party's messages plain
+// products of its queries and keys.  (acc: at most six terms.)
+__device__ __forceinline__ u64 mask_share(const ss_softmax_params &sp, u64 mask, u64 counter, int party)
 {
-    const u64 counter = ss_counter(row);
-    u64 m = 0;
-    for (int j = sp.t - 1; j >= 0; j--) m = ss_mul_small(ss_add(m, ss_draw_field_at(sp.maskgen_key[j], counter)), party + 1);
-    return ss_add(m, ss_draw_field_at(sp.mask_key, counter));
+    if (party < 2 * sp.t) return ss_draw_lazy_at(sp.maskgen_key[party], counter);
+    ss_sacc2 acc;
+    acc.clear();
+    for (int i = 0; i < 2 * sp.t; i++) {
+        const u64 v = ss_draw_lazy_at(sp.maskgen_key[i], counter);
+        SS_SPLIT31(v, w0, w1);
+        acc.mac(w0, w1, -sp.ilambda[i]);
+    }
+    return mask + acc.lazy();
 }
 
 // Digits of the queries to LDS, qd [row / 16][dim / 64][limb][64 lanes]: item `it` is four consecutive elements of a row; 16 items take 64
@@ -601,7 +608,7 @@ template <int MT>
 __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_params sp)
 {
     extern __shared__ v4i qd[];                  // [MT][dim / 64][limb][64 lanes]
-    __shared__ u64 mask[16 * MT];
+    __shared__ u64 mask[16 * MT], counter[16 * MT];   // of the row, and of its draws for key 0
     __shared__ int rowid[16 * MT];
     __shared__ size_t rowat[16 * MT];            // of the row's query in a share of q
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -639,7 +646,9 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
             const int i = (int)fd_div((u32)(row0 + tid), g.dGroup), h = head * g.group + row0 + tid - i * g.group;
             id = (s.first + i - g.tok0) * g.heads + h;
             rowat[tid] = (size_t)(s.first + i) * g.ld_q + (size_t)h * g.c.dim;
-            mask[tid] = row_mask(sp, (u64)(s.first + i) * g.heads + h, party);
+            const u64 row = (u64)(s.first + i) * g.heads + h;
+            mask[tid] = ss_draw_field(sp.mask_key, row);
+            counter[tid] = ss_counter(row << 32);
         }
         rowid[tid] = id;
     }
@@ -668,9 +677,10 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
         for (int m = 0; m < MT; m++)
 #pragma unroll
             for (int r = 0; r < 4; r++) {
-                const int row = m * 16 + 4 * (lane >> 4) + r, id = rowid[row];
+                const int row = m * 16 + 4 * (lane >> 4) + r, id = rowid[row], key = cell * 16 + (lane & 15);
                 if (id >= 0)
-                    g.msg[((size_t)party * g.rows + id) * g.keys + cell * 16 + (lane & 15)] = ss_add(fold_diagonals(acc[m], r), mask[row]);
+                    g.msg[((size_t)party * g.rows + id) * g.keys + key] =
+                        fold_diagonals(acc[m], r, mask_share(sp, mask[row], counter[row] + (u64)key * SS_GAMMA, party));
             }
     }
 }

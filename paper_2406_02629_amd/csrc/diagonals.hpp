@@ -34,9 +34,9 @@ __device__ __forceinline__ long long join3(int d0, int d1, int d2)
 
 // The ND diagonal sums of one output -> canonical field element.  The sums are signed 32-bit numbers and
 // stay signed: four of them at a time go into one signed 64-bit word, the words are joined with the field's
-// reduction rule, and a multiple of p makes the total positive before it is reduced.
+// reduction rule, and a multiple of p makes the total positive before it is reduced.  `more` < 2^62 (2^47) is added on the way.
 #if defined(SS_FIELD_P45)
-__device__ __forceinline__ u64 fold_diagonals(const v4i (&acc)[ND], int r)
+__device__ __forceinline__ u64 fold_diagonals(const v4i (&acc)[ND], int r, u64 more = 0)
 {
     const long long off = (long long)(SS_P << 12);   // a multiple of p above 2^56
     const u64 g0 = (u64)(join4(acc[0][r], acc[1][r], acc[2][r], acc[3][r]) + off);
@@ -47,10 +47,10 @@ __device__ __forceinline__ u64 fold_diagonals(const v4i (&acc)[ND], int r)
     const u64 r1 = ss_reduce(g1), r2 = ss_reduce(g2);
     const u64 t1 = SS_PC * (r1 >> 13) + ((r1 & 0x1FFFull) << 32);   // < 2^38 + 2^45
     const u64 t2 = ss_mul(r2, SS_PC << 19);
-    return ss_reduce(ss_fold(g0) + t1 + t2);
+    return ss_reduce(ss_fold(g0) + t1 + t2 + more);
 }
 #else
-__device__ __forceinline__ u64 fold_diagonals(const v4i (&acc)[15], int r)
+__device__ __forceinline__ u64 fold_diagonals(const v4i (&acc)[15], int r, u64 more = 0)
 {
     const long long g0 = join4(acc[0][r], acc[1][r], acc[2][r], acc[3][r]);
     const long long g1 = join4(acc[4][r], acc[5][r], acc[6][r], acc[7][r]);
@@ -60,7 +60,7 @@ __device__ __forceinline__ u64 fold_diagonals(const v4i (&acc)[15], int r)
     const long long lo = g0 + (g2 << 3), hi = g1 + (g3 << 3);   // |.| < 2^60
     // hi 2^32 = (hi >> 29) 2^61 + (hi mod 2^29) 2^32 = (hi >> 29) + (hi mod 2^29) 2^32
     const long long tot = lo + (hi >> 29) + (long long)(((u64)hi & ((1ULL << 29) - 1)) << 32) + (long long)(2 * SS_P);
-    return ss_reduce((u64)tot);   // 2^61 < tot < 2^63
+    return ss_reduce((u64)tot + more);   // 2^61 < tot < 2^63
 }
 #endif
 

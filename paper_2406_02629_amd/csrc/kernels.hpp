@@ -248,7 +248,7 @@ struct ss_softmax_params {        // masked opening of the scores and sharing of
     int f;                        // a score has 2 f fraction bits
     u32 scale;                    // its factor times log2 e, 24 fraction bits
     int bits;                     // fraction bits of the weights
-    u64 mask_key, maskgen_key[SS_MAXT], gen_key[SS_MAXT];
+    u64 mask_key, maskgen_key[2 * SS_MAXT], gen_key[SS_MAXT];   // maskgen_key: of the parties 1..2t
     int ilambda[2 * SS_MAXT + 1]; // REC from the IDs 1..2t+1
 };
 

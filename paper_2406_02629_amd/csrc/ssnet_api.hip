@@ -1349,10 +1349,8 @@ int ssnet_paged_attention(ssnet_ctx *ctx, const ssnet_paged_cache *cache, const 
     sp.scale = scale;
     sp.bits = weight_bits;
     sp.mask_key = ss_key(ctx->seed, SSNET_DOM_ROW_MASK, stream_id, 0, 0);
-    for (int j = 1; j <= ctx->t; j++) {
-        sp.maskgen_key[j - 1] = ss_key(ctx->seed, SSNET_DOM_ROWMASK_GEN, stream_id, 0, (u64)j);
-        sp.gen_key[j - 1] = ss_key(ctx->seed, SSNET_DOM_WEIGHT_GEN, stream_id, 0, (u64)j);
-    }
+    for (int i = 1; i <= 2 * ctx->t; i++) sp.maskgen_key[i - 1] = ss_key(ctx->seed, SSNET_DOM_ROWMASK_GEN, stream_id, (u64)i, 0);
+    for (int j = 1; j <= ctx->t; j++) sp.gen_key[j - 1] = ss_key(ctx->seed, SSNET_DOM_WEIGHT_GEN, stream_id, 0, (u64)j);
     for (int i = 0; i < 2 * ctx->t + 1; i++) sp.ilambda[i] = ctx->ilambda_r[i];
     const ss_sequences s = {seqs->d_start, seqs->d_table, seqs->d_length, seqs->sequences, seqs->tokens, seqs->max_pages, seqs->max_length};
     timed tm(ctx, SSNET_PROF_GEMM);
