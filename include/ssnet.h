@@ -480,7 +480,7 @@ int ssnet_cache_append(ssnet_ctx *ctx, const ssnet_paged_cache *cache, const uin
  *      for every key: the shares of parties 1..2t are uniform (domain ROWMASK_GEN,
  *      party i, counter r 2^32 + j), that of party 2t+1 is the one with which all of
  *      them open to the mask.  So the messages of a key are uniform but for the
- *      sum they open to;
+ *      sum they open to.  Of keys that the row does not see none are sent;
  *   2. the elite party reconstructs s[j] + mask, takes the softmax of the row,
  *      which no constant added to it changes, and shares the weights with degree
  *      t (domain WEIGHT_GEN, counter r 2^32 + j).  Of keys that the row does not
@@ -510,7 +510,7 @@ int ssnet_cache_append(ssnet_ctx *ctx, const ssnet_paged_cache *cache, const uin
  * messages of the whole call; a smaller one serves if it has room for one token's,
  * and the tokens are then taken in several runs with the same result.  Messages
  * behind the header: [2t+1][rows][max_length rounded up to 64] masked scores (of the
- * last run; keys that a row does not see hold anything). */
+ * last run; the places of keys that a row does not see are left as they were). */
 #define SSNET_MAX_CONTEXT (1 << 20)
 typedef struct ssnet_sequences {
     const int32_t *d_start, *d_table, *d_length;

@@ -4,6 +4,7 @@
 // Attention of a row (token, head) over the keys j < limit, all parties holding degree-t shares:
 //   1. party i = 1..2t+1: score S_i[j] = q_i . k_i[j] mod p (degree 2t, 2 f fraction bits), plus its share of a mask that is the same for
 //      all keys of the row, shared afresh with degree 2t for every key                            -> msg[i][row][j]
+//      (of keys that the row does not see nothing is sent: the mask would not hide their differences from the others)
 //   2. the elite party reconstructs s[j] + mask, takes the softmax of the row, which no constant added to it changes, as whole
 //      numbers (softmax_weight below), and shares the weights (degree t); every party's share of a key beyond the limit is 0
 //   3. every party i = 1..n: O_i = sum_j P_i[j] v_i[j] mod p (degree 2t)
@@ -609,7 +610,7 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
 {
     extern __shared__ v4i qd[];                  // [MT][dim / 64][limb][64 lanes]
     __shared__ u64 mask[16 * MT], counter[16 * MT];   // of the row, and of its draws for key 0
-    __shared__ int rowid[16 * MT];
+    __shared__ int rowid[16 * MT], seen[16 * MT];     // keys that the row sees: none where there is no row
     __shared__ size_t rowat[16 * MT];            // of the row's query in a share of q
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tile = (int)fd_div(blockIdx.x, g.dScores), hp = (int)blockIdx.x - tile * g.c.kv * (2 * sp.t + 1);
@@ -641,16 +642,16 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
         load(at, 0, k);
     }
     if (tid < 16 * MT) {
-        int id = -1;
+        seen[tid] = 0;
         if (tid < nrows) {
             const int i = (int)fd_div((u32)(row0 + tid), g.dGroup), h = head * g.group + row0 + tid - i * g.group;
-            id = (s.first + i - g.tok0) * g.heads + h;
+            rowid[tid] = (s.first + i - g.tok0) * g.heads + h;
+            seen[tid] = limit_at(s, i);
             rowat[tid] = (size_t)(s.first + i) * g.ld_q + (size_t)h * g.c.dim;
             const u64 row = (u64)(s.first + i) * g.heads + h;
             mask[tid] = ss_draw_field(sp.mask_key, row);
             counter[tid] = ss_counter(row << 32);
         }
-        rowid[tid] = id;
     }
     __syncthreads();
     for (int it = tid; it < nrows * kb_n * 16; it += 256) stage_query(g, qd, rowat, party, kb_n, it);
@@ -677,9 +678,9 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
         for (int m = 0; m < MT; m++)
 #pragma unroll
             for (int r = 0; r < 4; r++) {
-                const int row = m * 16 + 4 * (lane >> 4) + r, id = rowid[row], key = cell * 16 + (lane & 15);
-                if (id >= 0)
-                    g.msg[((size_t)party * g.rows + id) * g.keys + key] =
+                const int row = m * 16 + 4 * (lane >> 4) + r, key = cell * 16 + (lane & 15);
+                if (key < seen[row])
+                    g.msg[((size_t)party * g.rows + rowid[row]) * g.keys + key] =
                         fold_diagonals(acc[m], r, mask_share(sp, mask[row], counter[row] + (u64)key * SS_GAMMA, party));
             }
     }

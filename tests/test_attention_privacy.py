@@ -87,3 +87,24 @@ def test_messages_of_every_kernel_are_the_oracles(n, t, p, f, chunk, length, hea
     for i in range(last):
         seen = length - last + i + 1
         assert np.array_equal(msg[:, i, :, :seen], want[:, i, :, :seen])
+
+
+@gpu
+@pytest.mark.parametrize("n,t,p,f,chunks,lengths,heads", [(3, 1, P61, 13, [5], [40], 2), (5, 2, P61, 13, [30, 1, 0, 50], [90, 17, 5, 30], 3),
+                                                          (3, 1, P45, 12, [3], [4500], 1), (5, 2, P61, 13, [600], [2000], 8)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_scores_of_keys_that_a_row_does_not_see_are_not_sent(n, t, p, f, chunks, lengths, heads, causal):
+    """under the row's mask, the opening party would learn them: of later tokens, and of what unused places held"""
+    c = Context(n, t, p, f, chunks, lengths, heads, 1, 16, 16)
+    ss, tokens = c.ss, sum(chunks)
+    ss.reserve(ss.workspace_bytes_attention(c.cache, len(chunks), tokens, heads, max(lengths)))
+    ss.messages().fill_(-1)                            # no field element
+    c.run(f, causal)
+    keys = (max(lengths) + 63) // 64 * 64
+    sent = (ss.messages()[:(2 * t + 1) * tokens * heads * keys].view(2 * t + 1, tokens, heads, keys) != -1).cpu().numpy()
+    at = 0
+    for count, length in zip(chunks, lengths):
+        for i in range(count):
+            seen = max(0, length - count + i + 1) if causal else length
+            assert sent[:, at, :, :seen].all() and not sent[:, at, :, seen:].any(), (at, seen)
+            at += 1
