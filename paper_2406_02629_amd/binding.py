@@ -198,7 +198,7 @@ class PagedCache:
         page_bytes = ss.lib.ssnet_cache_page_bytes(ss._ctx, page_size, heads, head_dim)
         if page_bytes == 0 or pages < 1:
             raise SSNetError(EINVAL, "ssnet_cache_page_bytes")
-        self.n, self.pages, self.page_size, self.heads, self.head_dim = ss.n, pages, page_size, heads, head_dim
+        self.n, self.p, self.pages, self.page_size, self.heads, self.head_dim = ss.n, ss.p, pages, page_size, heads, head_dim
         digits = page_bytes // (ss.n * heads * page_size * head_dim)
         cells, groups = page_size // 16, head_dim // 16
         if keys is None:
@@ -742,6 +742,11 @@ class SSNet:
             raise TypeError(f"{name}: the heads of a token must be contiguous, tokens and parties equally far apart")
         return tokens, heads, dim, ld
 
+    def _check_cache(self, cache: PagedCache):
+        """the library takes the sizes of a page from its own field and parties"""
+        if cache.n != self.n or cache.p != self.p:
+            raise ValueError(f"the cache is one of {cache.n} parties over the prime {cache.p}, not of {self.n} over {self.p}")
+
     def _rotary(self, table: torch.Tensor, pos: torch.Tensor, tokens: int, layout: str) -> int:
         """fills in the rotary argument of the next call -> elements of a head that it turns"""
         _device_tensor(table, torch.int32, "table"), _device_tensor(pos, torch.int32, "pos", (tokens,))
@@ -772,8 +777,9 @@ class SSNet:
                      table: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None, layout: str = "half"):
         """keys k and values v [n][tokens][heads][head_dim] into the places `slots` [tokens] of the cache; table, pos: the keys are
         turned and truncated on the way, as rotary_truncate does"""
+        self._check_cache(cache)
         tokens, heads, dim, ld_k = self._heads_view(k, "k")
-        if v.shape != k.shape or heads != cache.heads or dim != cache.head_dim or cache.n != self.n:
+        if v.shape != k.shape or heads != cache.heads or dim != cache.head_dim:
             raise ValueError("k and v must be [n][tokens][heads][head_dim] of the cache")
         ld_v = self._heads_view(v, "v")[3]
         _device_tensor(slots, torch.int64, "slots", (tokens,))
@@ -795,11 +801,12 @@ class SSNet:
         """Attention of the tokens q [n][tokens][heads][head_dim], those of sequence b from seq_start[b] to seq_start[b+1], over the
         ctx_len[b] <= max_ctx tokens in the pages block_table[b] -> [n][tokens][heads][head_dim], degree 2t, f + weight_bits
         fraction bits.  scale: factor of the scores (default 1 / sqrt(head_dim)); weight_bits: default f."""
+        self._check_cache(cache)
         tokens, heads, dim, ld = self._heads_view(q, "q")
         sequences = ctx_len.shape[0]
         _device_tensor(ctx_len, torch.int32, "ctx_len", (sequences,)), _device_tensor(seq_start, torch.int32, "seq_start", (sequences + 1,))
         _device_tensor(block_table, torch.int32, "block_table")
-        if block_table.dim() != 2 or block_table.shape[0] != sequences or dim != cache.head_dim or cache.n != self.n:
+        if block_table.dim() != 2 or block_table.shape[0] != sequences or dim != cache.head_dim:
             raise ValueError("block_table must be [sequences][pages], q [n][tokens][heads][head_dim of the cache]")
         factor = dim ** -0.5 if scale is None else scale
         if not 0 < factor < 4:
