@@ -505,7 +505,10 @@ int ssnet_cache_append(ssnet_ctx *ctx, const ssnet_paged_cache *cache, const uin
  * weight_bits <= 30; max_length <= SSNET_MAX_CONTEXT.  Requires differences of
  * scores below p/2.  d_out [n][tokens][heads][head_dim]: a degree-2t sharing with
  * f + weight_bits fraction bits (as with every product, RED and truncation follow;
- * with weight_bits = 2f, which long contexts need, two truncations).
+ * with weight_bits = 2f two truncations).  A weight below 2^-(weight_bits+1) is 0
+ * and nothing makes up for it: weight_bits has to grow with the context.  Weights of
+ * scores of unit variance sum to 1 within 0.3 % over up to 2^(weight_bits-2) keys, to
+ * 0.994 over twice and 0.94 over four times as many.
  * Workspace: ssnet_workspace_bytes_attention for `tokens` tokens has room for the
  * messages of the whole call; a smaller one serves if it has room for one token's,
  * and the tokens are then taken in several runs with the same result.  Messages

@@ -61,8 +61,8 @@ class Sequences:
 
 class Attention:
     """One attention layer.  w_qkv [width][(heads + 2 kv_heads) head_dim], w_out [heads head_dim][width]: float64 weights of the model's
-    owner, shared and packed once.  table: fixedpoint.rotary_table.  weight_bits: f, or 2 f for long contexts (a weight of a long
-    context's key is about 2^f / length)."""
+    owner, shared and packed once.  table: fixedpoint.rotary_table.  weight_bits: f, or 2 f for long contexts (the weights of `length`
+    keys are about 1 / length); default: what the longest context that table and cache have room for needs."""
 
     STREAMS = 8      # stream ids that a forward pass uses
 
@@ -71,7 +71,9 @@ class Attention:
         self.ss, self.heads, self.kv, self.table, self.layout = ss, heads, kv_heads, table, layout
         self.dim = w_out.shape[0] // heads
         self.width = w_out.shape[1]
-        self.bits = ss.f if weight_bits is None else weight_bits
+        if weight_bits is None:
+            weight_bits = ss.f if ss.short_weights_serve(min(table.shape[0], pages * page_size)) else 2 * ss.f
+        self.bits = weight_bits
         if self.bits not in (ss.f, 2 * ss.f):
             raise ValueError("weight_bits must be f or 2 f: the result is brought back to scale by truncations by 2^f")
         if w_qkv.shape != (self.width, (heads + 2 * kv_heads) * self.dim):

@@ -792,6 +792,11 @@ class SSNet:
         self._ok(self._call.cache_append(self._handle, cache._address, k.data_ptr(), ld_k, v.data_ptr(), ld_v, tokens, slots.data_ptr(), rotary,
                                          stream_id), "ssnet_cache_append")
 
+    def short_weights_serve(self, max_ctx: int) -> bool:
+        """Whether weights of f bits do for a context of max_ctx keys.  A weight below 2^-(f+1) rounds to 0 and nothing makes up for it: of scores with unit
+        variance the weights sum to 1 within 0.3 % up to 2^(f-2) keys, to 0.994 at 2^(f-1), 0.94 at 2^f, 0.8 at 2^(f+1)."""
+        return 4 * max_ctx <= 1 << self.f
+
     def workspace_bytes_attention(self, cache: PagedCache, sequences: int, tokens: int, heads: int, max_length: int) -> int:
         return self.lib.ssnet_workspace_bytes_attention(self._ctx, cache._address, sequences, tokens, heads, max_length)
 
@@ -800,8 +805,13 @@ class SSNet:
                         weight_bits: Optional[int] = None, causal: bool = True, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of the tokens q [n][tokens][heads][head_dim], those of sequence b from seq_start[b] to seq_start[b+1], over the
         ctx_len[b] <= max_ctx tokens in the pages block_table[b] -> [n][tokens][heads][head_dim], degree 2t, f + weight_bits
-        fraction bits.  scale: factor of the scores (default 1 / sqrt(head_dim)); weight_bits: default f."""
+        fraction bits.  scale: factor of the scores (default 1 / sqrt(head_dim)); weight_bits: default f, which serves up to
+        2^(f-2) keys; for a longer max_ctx it has to be given (2 f, say)."""
         self._check_cache(cache)
+        if weight_bits is None:
+            if not self.short_weights_serve(max_ctx):
+                raise ValueError(f"give weight_bits: weights of f = {self.f} bits do not add up over {max_ctx} keys")
+            weight_bits = self.f
         tokens, heads, dim, ld = self._heads_view(q, "q")
         sequences = ctx_len.shape[0]
         _device_tensor(ctx_len, torch.int32, "ctx_len", (sequences,)), _device_tensor(seq_start, torch.int32, "seq_start", (sequences + 1,))
@@ -830,7 +840,7 @@ class SSNet:
         _pack_sequences(self._sequences_arg, 0, seq_start.data_ptr(), block_table.data_ptr(), ctx_len.data_ptr(), sequences, tokens,
                         block_table.shape[1], max_ctx)
         self._ok(self._call.paged_attention(self._handle, cache._address, self._sequences_address, q.data_ptr(), ld, heads,
-                                            round(factor * _LOG2E_24), self.f if weight_bits is None else weight_bits, causal, stream_id,
+                                            round(factor * _LOG2E_24), weight_bits, causal, stream_id,
                                             out.data_ptr()), "ssnet_paged_attention")
         return out
 
