@@ -35,28 +35,43 @@ class Sequences:
     def extend(self, counts: Dict[int, int], device=None):
         """counts: new tokens of each sequence, in the order in which they stand in the batch.  Takes the pages that they need and
         returns what the calls ask for: dict(pos, slots, seq_start, block_table, ctx_len, max_ctx)."""
+        batch, after = self.place(counts, device)
+        self.keep(after)
+        return batch
+
+    def keep(self, after):
+        """the second part of what place() returned: its tokens are in the cache"""
+        sequences, taken = after
+        del self.free[len(self.free) - taken:]
+        for s, (pages, length) in sequences.items():
+            self.pages[s], self.length[s] = pages, length
+
+    def place(self, counts: Dict[int, int], device=None):
+        """What extend() returns, and what keep() makes of the sequences once the calls have been made: until then they stay as they are, also
+        if a call fails."""
         size = self.cache.page_size
         need = sum(-(-(self.length.get(s, 0) + c) // size) - len(self.pages.get(s, ())) for s, c in counts.items())
         if need > len(self.free):
             raise MemoryError(f"{need} pages needed, {len(self.free)} free")
-        pos, slots, start = [], [], [0]
+        pos, slots, start, after, taken = [], [], [0], {}, 0
         for s, c in counts.items():
-            pages, old = self.pages.setdefault(s, []), self.length.get(s, 0)
+            pages, old = list(self.pages.get(s, ())), self.length.get(s, 0)
             while len(pages) * size < old + c:
-                pages.append(self.free.pop())
-            self.length[s] = old + c
+                taken += 1
+                pages.append(self.free[-taken])
+            after[s] = pages, old + c
             pos += range(old, old + c)
             slots += [pages[p // size] * size + p % size for p in range(old, old + c)]
             start.append(start[-1] + c)
-        longest = max(1, max(len(self.pages[s]) for s in counts))
-        table = [self.pages[s] + [0] * (longest - len(self.pages[s])) for s in counts]
-        lengths = [self.length[s] for s in counts]
+        longest = max(1, max(len(pages) for pages, _ in after.values()))
+        table = [pages + [0] * (longest - len(pages)) for pages, _ in after.values()]
+        lengths = [length for _, length in after.values()]
 
         def i32(v):
             return torch.tensor(v, dtype=torch.int32, device=device)
 
         return dict(pos=i32(pos), slots=torch.tensor(slots, dtype=torch.int64, device=device), seq_start=i32(start), block_table=i32(table),
-                    ctx_len=i32(lengths), max_ctx=max(1, max(lengths)))
+                    ctx_len=i32(lengths), max_ctx=max(1, max(lengths))), (after, taken)
 
 
 class Attention:
@@ -88,12 +103,13 @@ class Attention:
         self.sequences = Sequences(self.cache)
 
     def forward(self, x: torch.Tensor, counts: Dict[int, int]) -> torch.Tensor:
-        """x: shares [n][tokens][width] at scale 2^f of the new tokens, counts as in Sequences.extend -> shares [n][tokens][width]"""
+        """x: shares [n][tokens][width] at scale 2^f of the new tokens, counts as in Sequences.extend -> shares [n][tokens][width].  A call
+        that is refused or fails leaves the sequences as they were."""
         ss, heads, kv, dim = self.ss, self.heads, self.kv, self.dim
         n, tokens, _ = x.shape
-        batch = self.sequences.extend(counts, x.device)
-        if batch["pos"].numel() != tokens:
+        if sum(counts.values()) != tokens:
             raise ValueError("counts must add up to the tokens of x")
+        batch, after = self.sequences.place(counts, x.device)
         stream, self.stream = self.stream, self.stream + self.STREAMS
         qkv = ss.linear_mod_packed(x, self.w_qkv, (heads + 2 * kv) * dim)
         qkv = ss.degree_reduce_truncate(qkv, stream_id=stream).view(n, tokens, heads + 2 * kv, dim)
@@ -106,4 +122,6 @@ class Attention:
         if self.bits == 2 * ss.f:
             o = ss.truncate(o, stream_id=stream + 5)
         y = ss.linear_mod_packed(o.view(n, tokens, heads * dim), self.w_out, self.width)
-        return ss.degree_reduce_truncate(y, stream_id=stream + 6)
+        y = ss.degree_reduce_truncate(y, stream_id=stream + 6)
+        self.sequences.keep(after)
+        return y
