@@ -49,6 +49,8 @@ class Sequences:
     def place(self, counts: Dict[int, int], device=None):
         """What extend() returns, and what keep() makes of the sequences once the calls have been made: until then they stay as they are, also
         if a call fails."""
+        if any(c < 0 for c in counts.values()):
+            raise ValueError("a sequence grows by no tokens or more")
         size = self.cache.page_size
         need = sum(-(-(self.length.get(s, 0) + c) // size) - len(self.pages.get(s, ())) for s, c in counts.items())
         if need > len(self.free):

@@ -93,3 +93,16 @@ def test_a_call_that_fails_leaves_the_sequences_as_they_were(ss, kind):
     ss.fail = None
     at.forward(x(16), {0: 14, 1: 2})               # the same places again
     assert ss.appended[-1] == list(range(20, 34)) + [48, 49]
+
+
+def test_a_negative_number_of_tokens_is_refused(ss):
+    """it would shorten a sequence and leave its pages taken"""
+    at = layer(ss)
+    at.forward(x(20), {0: 20})
+    before = state(at)
+    with pytest.raises(ValueError):
+        at.sequences.extend({0: -3})
+    with pytest.raises(ValueError):
+        at.forward(x(2), {0: -3, 1: 5})
+    assert state(at) == before
+    assert at.sequences.extend({0: 0})["ctx_len"].tolist() == [20]
