@@ -112,6 +112,8 @@ class Attention:
         if sum(counts.values()) != tokens:
             raise ValueError("counts must add up to the tokens of x")
         batch, after = self.sequences.place(counts, x.device)
+        if batch["max_ctx"] > self.table.shape[0]:
+            raise ValueError(f"the table has {self.table.shape[0]} positions, a sequence would have {batch['max_ctx']}")
         stream, self.stream = self.stream, self.stream + self.STREAMS
         qkv = ss.linear_mod_packed(x, self.w_qkv, (heads + 2 * kv) * dim)
         qkv = ss.degree_reduce_truncate(qkv, stream_id=stream).view(n, tokens, heads + 2 * kv, dim)

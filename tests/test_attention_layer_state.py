@@ -106,3 +106,16 @@ def test_a_negative_number_of_tokens_is_refused(ss):
         at.forward(x(2), {0: -3, 1: 5})
     assert state(at) == before
     assert at.sequences.extend({0: 0})["ctx_len"].tolist() == [20]
+
+
+def test_a_sequence_does_not_outgrow_its_table(ss):
+    """the kernels take the last row of the table for every position behind it"""
+    at = layer(ss, positions=21)
+    at.forward(x(20), {0: 20})
+    before = state(at)
+    for counts in ({0: 2}, {1: 1, 0: 2}, {1: 22}):
+        with pytest.raises(ValueError, match="table"):
+            at.forward(x(sum(counts.values())), counts)
+        assert state(at) == before
+    at.forward(x(22), {0: 1, 1: 21})               # up to its last row
+    assert at.sequences.length == {0: 21, 1: 21}
