@@ -79,12 +79,14 @@ class Sequences:
 class Attention:
     """One attention layer.  w_qkv [width][(heads + 2 kv_heads) head_dim], w_out [heads head_dim][width]: float64 weights of the model's
     owner, shared and packed once.  table: fixedpoint.rotary_table.  weight_bits: f, or 2 f for long contexts (the weights of `length`
-    keys are about 1 / length); default: what the longest context that table and cache have room for needs."""
+    keys are about 1 / length); default: what the longest context that table and cache have room for needs.  stream_base: the first
+    stream id of its calls, each of which takes STREAMS of them; the two in front of it share the weights.  Default: whatever ids the context has free
+    (SSNet.take_streams); ids that another layer has are refused."""
 
     STREAMS = 8      # stream ids that a forward pass uses
 
     def __init__(self, ss: SSNet, w_qkv: torch.Tensor, w_out: torch.Tensor, heads: int, kv_heads: int, table: torch.Tensor, pages: int,
-                 page_size: int = 64, layout: str = "half", weight_bits: Optional[int] = None, stream_base: int = 1 << 22):
+                 page_size: int = 64, layout: str = "half", weight_bits: Optional[int] = None, stream_base: Optional[int] = None):
         self.ss, self.heads, self.kv, self.table, self.layout = ss, heads, kv_heads, table, layout
         self.dim = w_out.shape[0] // heads
         self.width = w_out.shape[1]
@@ -95,12 +97,13 @@ class Attention:
             raise ValueError("weight_bits must be f or 2 f: the result is brought back to scale by truncations by 2^f")
         if w_qkv.shape != (self.width, (heads + 2 * kv_heads) * self.dim):
             raise ValueError("w_qkv must be [width][(heads + 2 kv_heads) head_dim]")
-        self.stream = stream_base
+        self.stream = stream_base        # of the next call, where the caller has a say
+        weights = ss.take_streams(2, None if stream_base is None else stream_base - 2)
 
         def packed(w, stream):
             return ss.pack_weights_linear(ss.share(fx.encode(w.to(ss.device), ss.f, ss.p).contiguous(), stream_id=stream))
 
-        self.w_qkv, self.w_out = packed(w_qkv, stream_base - 1), packed(w_out, stream_base - 2)
+        self.w_qkv, self.w_out = packed(w_qkv, weights + 1), packed(w_out, weights)
         self.cache = PagedCache(ss, pages, page_size, kv_heads, self.dim)
         self.sequences = Sequences(self.cache)
 
@@ -114,7 +117,9 @@ class Attention:
         batch, after = self.sequences.place(counts, x.device)
         if batch["max_ctx"] > self.table.shape[0]:
             raise ValueError(f"the table has {self.table.shape[0]} positions, a sequence would have {batch['max_ctx']}")
-        stream, self.stream = self.stream, self.stream + self.STREAMS
+        stream = ss.take_streams(self.STREAMS, self.stream)
+        if self.stream is not None:
+            self.stream += self.STREAMS
         qkv = ss.linear_mod_packed(x, self.w_qkv, (heads + 2 * kv) * dim)
         qkv = ss.degree_reduce_truncate(qkv, stream_id=stream).view(n, tokens, heads + 2 * kv, dim)
         q = ss.rotary_truncate(qkv[:, :, :heads], self.table, batch["pos"], stream + 1, layout=self.layout)

@@ -218,6 +218,8 @@ class SSNet:
     """One (k = t+1, n) scheme over F_p, p = 2^61-1 (or P45, served by the second library), fixed-point
     fraction bits f."""
 
+    FIRST_TAKEN = 1 << 22        # what take_streams gives out by itself: apart from the ids of chain.py
+
     def __init__(self, n: int, t: int, f: int = 13, seed: int = 0, p: int = P61,
                  device: Optional[str] = "cuda:0", stream: Optional[int] = None):
         self.lib = load_library(p)
@@ -236,6 +238,7 @@ class SSNet:
         # the present workspace: asking again costs a foreign call (0.5 to 1.1 us), which small layers feel
         self._sizes: dict = {}
         self._fits_count = 0
+        self._taken: list = []       # stream ids that take_streams gave out: (first, behind the last), in order, apart
         self._rotary_arg, self._sequences_arg = _Rotary(), _Sequences()
         self._rotary_address, self._sequences_address = C.addressof(self._rotary_arg), C.addressof(self._sequences_arg)
 
@@ -264,6 +267,27 @@ class SSNet:
     def _ok(self, rc: int, where: str):
         if rc:
             raise SSNetError(rc, where, self.lib.ssnet_last_hip_error(self._ctx))
+
+    # ---- stream ids ----
+    def take_streams(self, count: int, first: Optional[int] = None) -> int:
+        """The first of `count` stream ids in a row that no other call of this method on this context gets, for whoever needs a fresh one per call (two calls
+        with one id draw the same masks): from `first` on, or the next that are free from FIRST_TAKEN on.  Ids that a program chooses by itself are
+        not known here, and contexts of one seed do not know of each other."""
+        if first is None:
+            first = self.FIRST_TAKEN
+            for begin, end in self._taken:
+                if begin < first + count and first < end:
+                    first = end
+        elif first < 0 or first + count > 1 << 64 or any(begin < first + count and first < end for begin, end in self._taken):
+            raise ValueError(f"stream ids {first} to {first + count - 1} are taken or out of range")
+        runs = []
+        for begin, end in sorted(self._taken + [(first, first + count)]):
+            if runs and runs[-1][1] == begin:
+                runs[-1] = runs[-1][0], end
+            else:
+                runs.append((begin, end))
+        self._taken = runs
+        return first
 
     # ---- workspace ----
     def reserve(self, nbytes: int):

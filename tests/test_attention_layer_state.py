@@ -119,3 +119,42 @@ def test_a_sequence_does_not_outgrow_its_table(ss):
         assert state(at) == before
     at.forward(x(22), {0: 1, 1: 21})               # up to its last row
     assert at.sequences.length == {0: 21, 1: 21}
+
+
+def test_layers_of_a_context_never_use_a_stream_id_twice(ss):
+    """the same id would share two layers' weights with the same polynomials, and mask their scores and truncations alike"""
+    first, other = layer(ss), layer(ss, weight_bits=2 * ss.f)
+    for at in (first, other, first, other, other):
+        at.forward(x(3), {0: 3})
+    ids = [i for _, i in ss.streams]
+    assert len(ids) == 2 * 2 + 2 * 6 + 3 * 7 and len(set(ids)) == len(ids)
+
+
+def test_ids_that_are_asked_for_are_kept_apart_from_the_others(ss):
+    at = layer(ss, stream_base=1000)
+    at.forward(x(1), {0: 1})
+    at.forward(x(1), {0: 1})
+    assert sorted({i for _, i in ss.streams}) == [998, 999] + [1000 + i for i in (0, 1, 2, 3, 4, 6)] + [1008 + i for i in (0, 1, 2, 3, 4, 6)]
+    for base in (1, 993, 1000, 1017):              # weights or the first call would meet them
+        with pytest.raises(ValueError):
+            b = layer(ss, stream_base=base)
+            b.forward(x(1), {0: 1})
+    ahead = layer(ss, stream_base=1026)
+    before = state(at)
+    at.forward(x(1), {0: 1})                       # 1016 to 1023
+    with pytest.raises(ValueError):                # 1024 and 1025 are the other's weights
+        at.forward(x(1), {0: 1})
+    assert state(at) != before and at.sequences.length == {0: 3}
+    ahead.forward(x(1), {0: 1})
+
+
+def test_ids_of_a_context():
+    ss = SSNet(3, 1, device=None)
+    a, b = ss.take_streams(2), ss.take_streams(8)
+    assert b == a + 2 and ss.take_streams(1, first=b + 8 + 4) == b + 12
+    assert ss.take_streams(5) == b + 13 and ss.take_streams(4) == b + 8 and ss.take_streams(1) == b + 18
+    for first, count in ((b + 7, 1), (b + 18, 3), (a - 1, 2), (-1, 1), (1 << 64, 1), ((1 << 64) - 1, 2)):
+        with pytest.raises(ValueError):
+            ss.take_streams(count, first=first)
+    assert ss.take_streams(2, first=a - 2) == a - 2 and ss.take_streams(1, first=0) == 0
+    assert SSNet(3, 1, device=None).take_streams(1) == a
