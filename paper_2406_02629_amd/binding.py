@@ -829,22 +829,23 @@ class SSNet:
                         weight_bits: Optional[int] = None, causal: bool = True, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of the tokens q [n][tokens][heads][head_dim], those of sequence b from seq_start[b] to seq_start[b+1], over the
         ctx_len[b] <= max_ctx tokens in the pages block_table[b] -> [n][tokens][heads][head_dim], degree 2t, f + weight_bits
-        fraction bits.  scale: factor of the scores (default 1 / sqrt(head_dim)); weight_bits: default f, which serves up to
+        fraction bits.  scale: factor of the scores (default 1 / sqrt(head_dim)), 0.00271 to 2.7725; weight_bits: default f, which serves up to
         2^(f-2) keys; for a longer max_ctx it has to be given (2 f, say)."""
         self._check_cache(cache)
         if weight_bits is None:
             if not self.short_weights_serve(max_ctx):
                 raise ValueError(f"give weight_bits: weights of f = {self.f} bits do not add up over {max_ctx} keys")
             weight_bits = self.f
+        factor = cache.head_dim ** -0.5 if scale is None else scale
+        factor = round(factor * _LOG2E_24) if 0 < factor < 4 else 0
+        if not 1 << 16 <= factor < 1 << 26:
+            raise ValueError("scale must lie between 0.00271 and 2.7725")
         tokens, heads, dim, ld = self._heads_view(q, "q")
         sequences = ctx_len.shape[0]
         _device_tensor(ctx_len, torch.int32, "ctx_len", (sequences,)), _device_tensor(seq_start, torch.int32, "seq_start", (sequences + 1,))
         _device_tensor(block_table, torch.int32, "block_table")
         if block_table.dim() != 2 or block_table.shape[0] != sequences or dim != cache.head_dim:
             raise ValueError("block_table must be [sequences][pages], q [n][tokens][heads][head_dim of the cache]")
-        factor = dim ** -0.5 if scale is None else scale
-        if not 0 < factor < 4:
-            raise ValueError("scale must be positive and below 4")
         key = ("attention", cache.heads, dim, sequences, tokens, heads, max_ctx)
         need = self._sizes.get(key)
         if need is None:
@@ -864,7 +865,7 @@ class SSNet:
         _pack_sequences(self._sequences_arg, 0, seq_start.data_ptr(), block_table.data_ptr(), ctx_len.data_ptr(), sequences, tokens,
                         block_table.shape[1], max_ctx)
         self._ok(self._call.paged_attention(self._handle, cache._address, self._sequences_address, q.data_ptr(), ld, heads,
-                                            round(factor * _LOG2E_24), weight_bits, causal, stream_id,
+                                            factor, weight_bits, causal, stream_id,
                                             out.data_ptr()), "ssnet_paged_attention")
         return out
 

@@ -85,3 +85,14 @@ def test_default_weight_bits():
         table = fx.rotary_table(positions, fx.rotary_frequencies(16), 13).cuda()
         assert Attention(ss, w_qkv, w_out, 2, 1, table, pages, page_size=16).bits == bits
     assert Attention(ss, w_qkv, w_out, 2, 1, table, 200, page_size=16, weight_bits=13).bits == 13
+
+
+@pytest.mark.parametrize("scale,taken", [(0.0, False), (-1.0, False), (0.0027, False), (0.0028, True), (2.77, True), (2.78, False), (3.0, False), (4.0, False),
+                                         (math.inf, False), (math.nan, False)])
+def test_factors_of_the_scores_are_those_that_the_library_takes(scale, taken):
+    """2^16 <= round(2^24 log2(e) scale) < 2^26"""
+    ss = SSNet(3, 1, device=None)
+    x, start = torch.zeros((3, 1, 2, 32), dtype=torch.int64), torch.zeros(2, dtype=torch.int32)
+    assert taken == (math.isfinite(scale) and 1 << 16 <= round(scale * math.log2(math.e) * 2 ** 24) < 1 << 26)
+    with pytest.raises(TypeError if taken else ValueError):      # (goes on, to the tensors that are not on a GPU)
+        ss.paged_attention(cache_like(ss), x, start, torch.zeros((1, 1), dtype=torch.int32), start[:1], 1, 0, scale=scale)
