@@ -27,17 +27,6 @@ namespace SS_NS {
 namespace {
 
 constexpr int BLOCK = 256;
-// What a rotation reads and writes, from which on it goes past the caches: heads of 128 turned whole, us, past / by way of them: 151 MB 25.7 / 22.2,
-// 185 MB 28.8 / 31.7, 302 MB 44.7 / 48.8, 369 MB 53 / 66, 738 MB 106 / 125.
-constexpr size_t STREAM_BYTES = (size_t)256 << 20;
-// Elements of the new keys from which on the kernel for many tokens takes them: tokens of 8 heads of 128, us, it / one thread per pair: n = 5, 128
-// tokens 14.3 / 13.8, 256 21.8 / 25.0; n = 3 11.2 / 10.1, 12.7 / 16.0.
-constexpr size_t WIDE_APPEND = (size_t)3 << 16;
-constexpr size_t MAX_GROUPS = ((size_t)1 << 24) - 1;   // workgroups of 256 threads in a launch: less than 2^32 threads (the runtime cuts more off)
-// Keys up to which one workgroup takes the softmax of a row (the whole attention, us, so / in blocks of 1024 keys: 32 rows of 1100 keys, n = 5,
-// 36 / 41, of 4096, n = 3, 61 / 65, 512 rows of 4096 135 / 150).
-constexpr size_t SHORT_ROW = 4096;
-constexpr int MAX_RUN = 16320;      // keys that the 32-bit sums of the values can take, in blocks of 64: 8 * 16383 * 2^14 < 2^31
 
 inline unsigned ceil_div(size_t a, size_t b) { return (unsigned)((a + b - 1) / b); }
 
@@ -1064,7 +1053,6 @@ __global__ __launch_bounds__(256, 2) void values_kernel(attn_args g, int n)
 // softmax of the rows, a wave to a row and four keys to a lane, keeps its own party's shares of the weights in LDS and multiplies, a
 // wave to 16 elements of the head.  All parties' workgroups take the same softmax, which costs less than a launch.  Bound by its chain of
 // loads: 4 heads of 64 over 33 keys, n = 3, 6.4 to 6.8 us beside 4.7 to 5.0 of the scores (three launches: 19 for all).
-constexpr int SHORT_KEYS = 256;
 template <int T>
 __global__ __launch_bounds__(512) void finish_kernel(attn_args g, ss_softmax_params sp)
 {
@@ -1195,12 +1183,11 @@ hipError_t ss_launch_rotary(const u64 *x, size_t ld, u64 *u, u64 *wsh, u64 *out,
                             const ss_tr_params &tp, hipStream_t stream)
 {
     const int half = rope.rot / 2;
-    const bool wide = (rope.interleaved || half % 2 == 0) && dim % 2 == 0 && ld % 2 == 0 && aligned16(x) && aligned16(out);
+    const bool wide = wide_rotary(dim, rope.rot, rope.interleaved, ld, aligned16(x) && aligned16(out));
     const int pairs = !wide ? half : rope.interleaved ? half : half / 2, width = wide ? pairs + (dim - rope.rot) / 2 : dim - half;
     const rotary_shape g = make_shape(tokens, heads, dim, pairs, width);
     const dim3 grid(ceil_div((size_t)tokens * heads * width, BLOCK));
-    // messages and results past the caches where they are more than these hold
-    const bool streams = (size_t)tokens * heads * ((size_t)rope.rot * (tp.t + 1 + tp.n) + (size_t)dim * 2 * tp.n) * 8 > STREAM_BYTES;
+    const bool streams = rotary_streams(tp.n, tp.t, tokens, heads, dim, rope.rot);
 #define SS_WIDE(NC, TC, I)                                                                                                       \
     hipLaunchKernelGGL((streams ? rotary_wide_kernel<NC, TC, I, true> : rotary_wide_kernel<NC, TC, I, false>), grid, dim3(BLOCK), 0, \
                        stream, x, ld, u, wsh, out, g, rope, tp)
@@ -1234,7 +1221,7 @@ hipError_t ss_launch_append(const ss_paged &c, const u64 *k, size_t ld_k, const 
     s.page_size = (unsigned)c.page_cells * 16;
     s.capacity = s.page_size * (unsigned)c.pages;
     s.dPage = make_fdiv(s.page_size);
-    if ((size_t)tokens * c.kv * c.dim >= WIDE_APPEND && tokens >= 16 && half % 4 == 0 && ld_k % 2 == 0 && aligned16(k)) {
+    if (wide_append(tokens, c.kv, c.dim, rope.rot, ld_k, aligned16(k))) {
         s.steps = (rope.interleaved ? half : half / 2) + (c.dim - rope.rot) / 2;
         s.step_blocks = (int)ceil_div(s.steps, 16);
         s.value_blocks = (int)ceil_div((size_t)tp.n * c.dim, BLOCK);
@@ -1255,60 +1242,6 @@ hipError_t ss_launch_append(const ss_paged &c, const u64 *k, size_t ld_k, const 
     SS_SCHEME(tp.n, tp.t, SS_LAUNCH);
 #undef SS_LAUNCH
     return hipGetLastError();
-}
-
-namespace {
-
-// most tiles of `rows` rows that the sequences of a call can have
-size_t tile_bound(size_t tokens, size_t seqs, size_t group, size_t rows)
-{
-    const size_t one = tokens * ceil_div(group, rows), all = tokens * group / rows + seqs;
-    return one < all ? one : all;
-}
-
-}  // namespace
-
-attention_plan plan_attention(int n, int t, int tokens, int seqs, int heads, int kv, int dim, int max_length, size_t room)
-{
-    attention_plan p = {};
-    const size_t group = heads / kv, nr = 2 * t + 1;
-    p.keys = ((size_t)max_length + 63) & ~(size_t)63;
-    p.dblocks = ceil_div(dim, 64);
-    // (a run of tokens is planned as a call of as many: a single token always fits into what a call of one needs)
-    for (p.slab = tokens;; p.slab = (p.slab + 1) / 2) {
-        // Larger tiles and blocks read less, but leave fewer waves to a SIMD and fewer workgroups.  Scores + values, us, tiles of 32 / of 16 rows
-        // (by the workgroups of the scores with 32): chunk of 512 tokens over 4096, n = 5 (10400) 1975 / 2085; chunks of 17 to 121 over 121 to
-        // 777, n = 5 (1160) 155 / 129; 230 tokens over 700 to 1024, n = 3, 45-bit prime (480) 64 / 62.  Keys to a workgroup, scores alone:
-        // single tokens over 32768 and 500 to 2001 128 / 256 / 1024 157 / 159 / 167, 92 / 94 / 105; the chunks above 256 / 512 / 1024 1157 /
-        // 1079 / 1040, 62 / 59 / 54, 29 / 30 / 32 (there 1024 leaves 384 workgroups for 768 places).
-        const size_t sequence_rows = ceil_div(p.slab, seqs) * group;
-        auto tiles = [&](size_t rows) { return tile_bound(p.slab, seqs, group, rows); };
-        auto workgroups = [&](size_t rows, size_t block) { return tiles(rows) * ceil_div(p.keys, block) * kv * nr; };
-        p.row_tiles = sequence_rows > 16 && workgroups(32, 512) >= 2048 ? 2 : 1;
-        p.key_block = sequence_rows > 16 ? 1024 : 128;
-        while (p.key_block > 256 && workgroups(16 * p.row_tiles, p.key_block) < (p.row_tiles == 2 ? 4096 : 768)) p.key_block /= 2;
-        // one launch for softmax and values while each of its workgroups has a CU to itself (us, one launch / two): single tokens of 32 heads of
-        // 128 over 64 keys, n = 5, one sequence 15.1 / 18.2, 4 17.3 / 20.9, 16 (800 workgroups) 38.4 / 37.9, 64 109 / 104; over 256 keys, one
-        // 21.2 / 22.4
-        p.finish = p.row_tiles == 1 && p.keys <= SHORT_KEYS && tiles(16) * kv * n <= 256;
-        // single tokens read the values once, which several rounds of workgroups spread best over the memory (us, 2048 / 1024 workgroups wanted:
-        // 87 / 98); chunks multiply, and a round of 384 that needs no sum is as good as three runs (20.4 / 19.5 + 5.2 for the sum)
-        const size_t wanted = ceil_div(sequence_rows <= 16 ? 2048 : 384, tiles(16 * p.row_tiles) * p.dblocks * kv * n);
-        p.run = (int)((ceil_div(p.keys, wanted) + 63) & ~63u);
-        if (p.run > MAX_RUN) p.run = MAX_RUN;
-        if (p.run < 256) p.run = 256;
-        p.splits = p.finish ? 1 : (int)ceil_div(p.keys, p.run);
-        p.rows = (size_t)p.slab * heads;
-        const size_t blocks = p.keys > SHORT_ROW ? ceil_div(p.keys, 1024) : 0;
-        p.bytes = align256(nr * p.rows * p.keys * 8) + (blocks ? align256(p.rows * (p.keys + 2 * blocks) * 8) : 0) +
-                  (p.finish ? 0 : align256((size_t)n * p.rows * p.keys * NL)) + (p.splits > 1 ? align256((size_t)p.splits * n * p.rows * dim * 8) : 0);
-        const size_t most = max(max(workgroups(16 * p.row_tiles, p.key_block), tiles(16 * p.row_tiles) * kv * n * p.splits * p.dblocks),
-                                max(p.rows * max(blocks, (size_t)1), (size_t)ceil_div(p.rows * dim, BLOCK / (p.splits > 8 ? 4 : 1)) * n));
-        if (p.bytes <= room && most <= MAX_GROUPS) return p;
-        if (p.slab == 1) break;
-    }
-    p.slab = 0;
-    return p;
 }
 
 hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache, const ss_sequences &seqs, const u64 *q, size_t ld_q, int heads,
@@ -1340,11 +1273,10 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
     g.dblocks = plan.dblocks;
     const int nr = 2 * sp.t + 1, n = sp.n;
     const unsigned blocks = ceil_div(plan.keys, 1024);
-    const bool split_rows = plan.keys > SHORT_ROW;
     char *at = (char *)room;
     g.msg = (u64 *)at;
     at += align256((size_t)nr * g.rows * g.keys * 8);
-    if (split_rows) {
+    if (plan.split_rows) {
         g.opened = (u64 *)at;
         g.tops = g.opened + g.rows * g.keys;
         g.sums = g.tops + g.rows * blocks;
@@ -1354,7 +1286,7 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
     at += plan.finish ? 0 : align256((size_t)n * g.rows * g.keys * NL);
     g.parts = (u64 *)at;
     g.out = out;
-    const size_t lds = (size_t)plan.row_tiles * ((cache.dim + 63) / 64) * TILE * 16;
+    const size_t lds = plan.query_bytes;
     if (lds > 48 * 1024) {
         const void *scores = plan.row_tiles == 1 ? (const void *)scores_kernel<1> : (const void *)scores_kernel<2>;
         if (hipError_t e = hipFuncSetAttribute(scores, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); e != hipSuccess) return e;
@@ -1387,7 +1319,7 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
         // 1024 threads: 2048 rows of 2000 keys, n = 3, 201 / 211, of 1100 682 / 695; 32 rows of 1100, n = 5, 37.1 / 35.7, of 4096 89.9 / 88.7)
 #define SS_LAUNCH(NC, TC)                                                                               \
     do {                                                                                                \
-        if (split_rows) {                                                                               \
+        if (plan.split_rows) {                                                                          \
             hipLaunchKernelGGL((open_kernel<TC>), wgrid, block, 0, stream, g, sp);                      \
             hipLaunchKernelGGL(sum_kernel, wgrid, block, 0, stream, g, sp);                             \
             hipLaunchKernelGGL((weights_kernel<NC, TC>), wgrid, block, 0, stream, g, sp);               \

@@ -3,6 +3,7 @@
 #pragma once
 #include "field.hpp"
 #include "gemm_plan.hpp"
+#include "attention_plan.hpp"
 
 // Everything below lives in a namespace named after the field (ss61 / ss45), so that the two libraries built
 // from these sources never share a C++ symbol or a kernel name.
@@ -251,20 +252,6 @@ struct ss_softmax_params {        // masked opening of the scores and sharing of
     u64 mask_key, maskgen_key[2 * SS_MAXT], gen_key[SS_MAXT];   // maskgen_key: of the parties 1..2t
     int ilambda[2 * SS_MAXT + 1]; // REC from the IDs 1..2t+1
 };
-
-// how a call over `tokens` tokens is cut up: into slabs of tokens whose messages fit the room it has; the contraction of the values
-// into `splits` runs of `run` keys, with a plane of their own each where there are several
-struct attention_plan {
-    int row_tiles;                // of 16 rows to a workgroup
-    int slab;                     // tokens, 0: the room is too small
-    int splits, run;
-    int key_block;                // keys of a workgroup of the scores
-    int dblocks;                  // workgroups to a head in the values, 64 elements each
-    bool finish;                  // softmax and values in one launch
-    size_t keys;                  // of a row in the messages: the longest context in whole blocks of 64
-    size_t rows, bytes;           // of a slab
-};
-attention_plan plan_attention(int n, int t, int tokens, int seqs, int heads, int kv, int dim, int max_length, size_t room);
 
 // x [n][tokens][ld] (heads x dim of every token) rotated and truncated -> out [n][tokens][heads][dim]; messages u [k][count],
 // wsh [n][count], count = tokens * heads * rot
