@@ -553,20 +553,32 @@ __device__ __forceinline__ void multiply(const v4i *a, int stride, const v4i (&k
     }
 }
 
-// A party's share of the mask of a row for one key, below 2^62 (2^47): those of parties 1..2t are drawn, that of party 2t+1 is what makes them open to
-// the mask, of which its own multiplier is 1.  One set of shares for the whole row would leave the differences of a party's messages plain
-// products of its queries and keys.  (acc: at most six terms.)
-__device__ __forceinline__ u64 mask_share(const ss_softmax_params &sp, u64 mask, u64 counter, int party)
+// A party's shares of the masks of four rows for one key, below 2^62 (2^47): those of parties 1..2t are drawn (own_key), those of party 2t+1 are what
+// makes them open to the mask, its own multiplier being 1.  One set of shares for the whole row would leave the differences of a party's messages
+// plain products of its queries and keys.  mask, counter: of the rows; step: the key's part of the counter.  (Four rows together, so that
+// a key of the generator is waited for once.  acc: at most six terms.)
+__device__ __forceinline__ void mask_shares(const ss_softmax_params &sp, const u64 *mask, const u64 *counter, u64 step, bool last, u64 own_key, u64 (&v)[4])
 {
-    if (party < 2 * sp.t) return ss_draw_lazy_at(sp.maskgen_key[party], counter);
-    ss_sacc2 acc;
-    acc.clear();
-    for (int i = 0; i < 2 * sp.t; i++) {
-        const u64 v = ss_draw_lazy_at(sp.maskgen_key[i], counter);
-        SS_SPLIT31(v, w0, w1);
-        acc.mac(w0, w1, -sp.ilambda[i]);
+    if (!last) {
+#pragma unroll
+        for (int r = 0; r < 4; r++) v[r] = ss_draw_lazy_at(own_key, counter[r] + step);
+        return;
     }
-    return mask + acc.lazy();
+    ss_sacc2 acc[4];
+#pragma unroll
+    for (int r = 0; r < 4; r++) acc[r].clear();
+    for (int i = 0; i < 2 * sp.t; i++) {
+        const u64 k = sp.maskgen_key[i];
+        const int c = -sp.ilambda[i];
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            const u64 x = ss_draw_lazy_at(k, counter[r] + step);
+            SS_SPLIT31(x, w0, w1);
+            acc[r].mac(w0, w1, c);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; r++) v[r] = mask[r] + acc[r].lazy();
 }
 
 // Digits of the queries to LDS, qd [row / 16][dim / 64][limb][64 lanes]: item `it` is four consecutive elements of a row; 16 items take 64
@@ -646,6 +658,8 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
     for (int it = tid; it < nrows * kb_n * 16; it += 256) stage_query(g, qd, rowat, party, kb_n, it);
     __syncthreads();
     __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0): the first digits are there, the loop's waits are for its own loads alone
+    const bool last_party = party == 2 * sp.t;
+    const u64 own_key = sp.maskgen_key[last_party ? 0 : party];
     for (; cell < cell_end; cell += 4) {
         const size_t at_next = cell_at(g, b, min(cell + 4, cell_end - 1));
         v4i acc[MT][ND];
@@ -664,14 +678,14 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
         }
         at = at_next;
 #pragma unroll
-        for (int m = 0; m < MT; m++)
+        for (int m = 0; m < MT; m++) {
+            const int row = m * 16 + 4 * (lane >> 4), key = cell * 16 + (lane & 15);
+            u64 share[4];
+            mask_shares(sp, mask + row, counter + row, (u64)key * SS_GAMMA, last_party, own_key, share);
 #pragma unroll
-            for (int r = 0; r < 4; r++) {
-                const int row = m * 16 + 4 * (lane >> 4) + r, key = cell * 16 + (lane & 15);
-                if (key < seen[row])
-                    g.msg[((size_t)party * g.rows + rowid[row]) * g.keys + key] =
-                        fold_diagonals(acc[m], r, mask_share(sp, mask[row], counter[row] + (u64)key * SS_GAMMA, party));
-            }
+            for (int r = 0; r < 4; r++)
+                if (key < seen[row + r]) g.msg[((size_t)party * g.rows + rowid[row + r]) * g.keys + key] = fold_diagonals(acc[m], r, share[r]);
+        }
     }
 }
 
