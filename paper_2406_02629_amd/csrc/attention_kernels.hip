@@ -427,7 +427,7 @@ __device__ __forceinline__ void append_values(const u64 *v, size_t ld, const app
 }
 
 // Both in one launch, bound by memory: keys, values and their digits, t + 1 + n words of messages per element of a key.  2048 tokens of 8 heads of
-// 128, n = 5: 97 us, 436 MB at 4.5 TB/s (the kernel for a few tokens, whose bytes go out one by one: 269).
+// 128, n = 5, one run of places: 98 us, 436 MB at 4.4 TB/s (the kernel for a few tokens, whose bytes go out one by one: 269).
 // Grid.x: blocks of 16 tokens by blocks of 16 steps of the keys, then by blocks of 256 elements and parties of the values; grid.y: heads.
 template <int N, int T, bool INTERLEAVED>
 __global__ __launch_bounds__(BLOCK) void append_many_kernel(const u64 *k, size_t ld_k, const u64 *v, size_t ld_v, u64 *__restrict__ u,
@@ -602,10 +602,10 @@ __device__ __forceinline__ void stage_query(const attn_args &g, v4i *qd, const s
 // MFMA order; a wave takes a cell of 16 keys at a time straight from the cache, the next 64 elements of a cell (or the next cell's first)
 // on their way while those at hand are multiplied.  A cell is a wave's own (no other has a use for it) and its digits are in MFMA order as
 // they lie, so they need no LDS.
-// Single tokens are bound by reading the keys once: 32 heads over 8 of 128, n = 5, eight contexts of 500 to 2001, 410 MB in 83 to 89 us (4.6 to
-// 4.9 TB/s); n = 3, one of 32768, 805 MB in 153 to 159 (5.1 to 5.3).  Chunks by the matrix cores: 512 tokens of 16 heads over 4096 keys, n = 5,
-// 1020 to 1140 us, 2.3 to 2.5 POP/s, at the 1.7 GHz that this work leaves the card (the first calls take 940 to 980): products 69 % of the
-// cycles, the folds of 15 sums (MT = 2: 8 for 256 products) beside them.
+// Single tokens are bound by reading the keys once: 32 heads over 8 of 128, n = 5, eight contexts of 500 to 2001, 410 MB in 86 to 92 us (4.4 to
+// 4.8 TB/s); n = 3, one of 32768, 805 MB in 155 to 163 (4.9 to 5.2).  Chunks by the matrix cores and by what stands between the products: 512 tokens
+// of 16 heads over 4096 keys, n = 5, 1150 to 1240 us, 2.1 to 2.3 POP/s, at the 1.8 GHz that this work leaves the card: products 57 % of the cycles, beside
+// them the folds of 15 sums (MT = 2: 8 for 256 products) and the masks (one draw to a score, 2t at party 2t+1: 200 of the us).
 template <int MT>
 __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_params sp)
 {
@@ -836,7 +836,7 @@ __device__ __forceinline__ void share_weights(const attn_args &g, const ss_softm
 // Step 2 for rows of up to 4 THREADS RUNS keys, one workgroup each: opened once, maximum, weights and sum in registers.  Many rows are
 // bound by their arithmetic (210 vector instructions to a key at n = 5, a seventh of them products) and, next to it, by the messages in and the weights
 // out: 8192 of 3585 to 4096 keys, n = 5, 490 us for 2.5 GB, 5.1 TB/s (past the caches 90 to 130 more: the weights are read again at once).
-// 256 rows of 2001 keys 13 us, the chain from load to load of one row.
+// 256 rows of 2001 keys 13 to 14 us, the chain from load to load of one row.
 template <int N, int T, int RUNS, int THREADS>
 __global__ __launch_bounds__(THREADS) void softmax_kernel(attn_args g, ss_softmax_params sp)
 {
@@ -888,7 +888,7 @@ __global__ __launch_bounds__(THREADS) void softmax_kernel(attn_args g, ss_softma
     }
 }
 
-// ... for longer rows, which several workgroups take in blocks of 1024 keys (32 rows of 32768, n = 3: 10 + 7.9 + 13 us; in one workgroup to a row
+// ... for longer rows, which several workgroups take in blocks of 1024 keys (32 rows of 32768, n = 3: 10 + 7.4 + 12.5 us; in one workgroup to a row
 // they would leave seven CUs of eight idle): opened, with the largest score of each block,
 template <int T>
 __global__ __launch_bounds__(BLOCK) void open_kernel(attn_args g, ss_softmax_params sp)
@@ -1066,7 +1066,7 @@ __global__ __launch_bounds__(256, 2) void values_kernel(attn_args g, int n)
 // Steps 2 and 3 in one launch for contexts of up to 256 keys: one workgroup of eight waves per (tile of 16 rows, kv head and party) takes the
 // softmax of the rows, a wave to a row and four keys to a lane, keeps its own party's shares of the weights in LDS and multiplies, a
 // wave to 16 elements of the head.  All parties' workgroups take the same softmax, which costs less than a launch.  Bound by its chain of
-// loads: 4 heads of 64 over 33 keys, n = 3, 6.4 to 6.8 us beside 4.7 to 5.0 of the scores (three launches: 19 for all).
+// loads: 4 heads of 64 over 33 keys, n = 3, 6.0 to 6.9 us beside 5.4 to 5.9 of the scores (three launches: 19 for all).
 template <int T>
 __global__ __launch_bounds__(512) void finish_kernel(attn_args g, ss_softmax_params sp)
 {
@@ -1330,7 +1330,8 @@ hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache
             continue;
         }
         // rows of 1024 to 4096 keys: four runs of 256 threads where they fill the card, 1024 threads otherwise (the whole attention, us, four runs /
-        // 1024 threads: 2048 rows of 2000 keys, n = 3, 201 / 211, of 1100 682 / 695; 32 rows of 1100, n = 5, 37.1 / 35.7, of 4096 89.9 / 88.7)
+        // 1024 threads: n = 3, 2048 rows of 2000 keys 209 / 220, 8192 of 1100 408 / 454, of 4096 1576 / 1574; n = 5, 992 rows of 4096 399 / 401, 512 228.8 / 227.5,
+        // 32 of 1100 37.1 / 36.3, of 4096 90.0 / 88.6)
 #define SS_LAUNCH(NC, TC)                                                                               \
     do {                                                                                                \
         if (plan.split_rows) {                                                                          \

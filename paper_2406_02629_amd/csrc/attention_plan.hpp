@@ -20,7 +20,10 @@ inline bool rotary_streams(int n, int t, int tokens, int heads, int dim, int rot
     return (size_t)tokens * heads * ((size_t)rot * (t + 1 + n) + (size_t)dim * 2 * n) * 8 > STREAM_BYTES;
 }
 
-// two elements at a time, 16 bytes to a load; aligned: the tensors to 16 bytes
+// two elements at a time, 16 bytes to a load; aligned: the tensors to 16 bytes.  (us, so / one pair of a head to a thread.  Interleaved, 321 tokens
+// of 12 heads of 80: n = 5 10.0 / 11.3, n = 3 7.4 / 8.3.  Halves, whose threads take two pairs: 512 tokens of 32 heads of 128, n = 3 27.3 / 27.9, n = 5
+// 45.5 / 42.8; 256 15.1 / 15.9, 22.1 / 23.9; of 12 heads of 80, 640 11.8 / 10.4, 17.0 / 14.5, 321 8.5 / 7.9, 12.1 / 10.8, 64 5.2 / 5.1, 6.8 / 5.5: below
+// about 600000 elements the pair to a thread would be the faster one there.  2048 tokens 93 / 118.)
 inline bool wide_rotary(int dim, int rot, int interleaved, size_t ld, bool aligned)
 {
     return (interleaved || rot / 2 % 2 == 0) && dim % 2 == 0 && ld % 2 == 0 && aligned;
@@ -29,7 +32,9 @@ inline bool wide_rotary(int dim, int rot, int interleaved, size_t ld, bool align
 // ------------------------------------------------------------------ appending to the cache
 
 // Elements of the new keys from which on the kernel for many tokens takes them: tokens of 8 heads of 128, us, it / one thread per pair: n = 5, 128
-// tokens 14.3 / 13.8, 256 21.8 / 25.0; n = 3 11.2 / 10.1, 12.7 / 16.0.
+// tokens 14.3 / 13.8, 256 20.9 / 25.6; n = 3 11.2 / 10.1, 13.8 / 16.3.  Those are one run of places; several runs leave whole cells only as far as the first
+// one's phase holds, but the rest costs no more than there: 16 runs of 64 n = 5 87 / 143, n = 3 57 / 58, runs of 333, 700 and 1015 189 / 277, 127 / 189.
+// Single tokens of many sequences, bytes on either side: 256 51.5 / 49.6, 31.4 / 30.4, 2048 1058 / 929, 640 / 571.
 constexpr size_t WIDE_APPEND = (size_t)3 << 16;
 inline bool wide_append(int tokens, int kv, int dim, int rot, size_t ld_k, bool aligned)
 {
@@ -39,8 +44,8 @@ inline bool wide_append(int tokens, int kv, int dim, int rot, size_t ld_k, bool 
 // ------------------------------------------------------------------ attention
 
 constexpr size_t MAX_GROUPS = ((size_t)1 << 24) - 1;   // workgroups of 256 threads in a launch: less than 2^32 threads (the runtime cuts more off)
-// Keys up to which one workgroup takes the softmax of a row (the whole attention, us, so / in blocks of 1024 keys: 32 rows of 1100 keys, n = 5,
-// 36 / 41, of 4096, n = 3, 61 / 65, 512 rows of 4096 135 / 150).
+// Keys up to which one workgroup takes the softmax of a row, as many as its registers hold (the whole attention, us, so / in blocks of 1024 keys: 32
+// rows of 1100 keys, n = 5, 36.3 / 43.3, of 4096 87.5 / 91.1, n = 3 52.2 / 56.6; 512 rows of 2048, n = 5, 115 / 127, of 4096 222 / 242; 2048 rows 734 / 790).
 constexpr size_t SHORT_ROW = 4096;
 constexpr int MAX_RUN = 16320;      // keys that the 32-bit sums of the values can take, in blocks of 64: 8 * 16383 * 2^14 < 2^31
 constexpr int SHORT_KEYS = 256;     // that softmax and values in one launch hold
@@ -75,11 +80,13 @@ inline attention_plan plan_attention(int n, int t, int tokens, int seqs, int hea
     p.dblocks = blocks_of(dim, 64);
     // (a run of tokens is planned as a call of as many: a single token always fits into what a call of one needs)
     for (p.slab = tokens;; p.slab = (p.slab + 1) / 2) {
-        // Larger tiles and blocks read less, but leave fewer waves to a SIMD and fewer workgroups.  Scores + values, us, tiles of 32 / of 16 rows
-        // (by the workgroups of the scores with 32): chunk of 512 tokens over 4096, n = 5 (10400) 1975 / 2085; chunks of 17 to 121 over 121 to
-        // 777, n = 5 (1160) 155 / 129; 230 tokens over 700 to 1024, n = 3, 45-bit prime (480) 64 / 62.  Keys to a workgroup, scores alone:
-        // single tokens over 32768 and 500 to 2001 128 / 256 / 1024 157 / 159 / 167, 92 / 94 / 105; the chunks above 256 / 512 / 1024 1157 /
-        // 1079 / 1040, 62 / 59 / 54, 29 / 30 / 32 (there 1024 leaves 384 workgroups for 768 places).
+        // Larger tiles and blocks read less, but leave fewer waves to a SIMD and fewer workgroups.  The whole attention, us, tiles of 32 / of 16 rows
+        // (by the workgroups of the scores with 32), chunks of 64 to 512 tokens of 16 heads over 4 of 128: n = 5, (320) 126 / 106, (720) 210 / 210,
+        // (1280) 368 / 368, (1920) 520 / 536, (2560) 673 / 699, (7680) 1980 / 2065, (10400) 2572 / 2693; n = 3 (432) 155 / 142, (1152) 330 / 320, (1536) 398 / 398,
+        // (4608) 1192 / 1209, over the 45-bit prime 137 / 122, 269 / 271, 336 / 333, 1000 / 1042; chunks of 17 to 121 over 121 to 777, heads of 80, n = 5
+        // (1160) 174 / 154; 230 tokens over 700 to 1024, n = 3, 45-bit prime (480) 88 / 74.  Keys to a workgroup, 128 / 256 / 512 / 1024: single tokens over 32768
+        // 333 / 335 / 342 / 343, over 500 to 2001 189 / 193 / 204 / 203; 512 tokens over 4096 2757 / 2638 / 2577 / 2577, the last two 162 / 155 / 154 / 154 and
+        // 74.5 / 72.2 / 74.5 / 76.8 (there 1024 leaves 384 workgroups for 768 places).
         const size_t sequence_rows = blocks_of(p.slab, seqs) * group;
         auto tiles = [&](size_t rows) { return tile_bound(p.slab, seqs, group, rows); };
         auto workgroups = [&](size_t rows, size_t block) { return tiles(rows) * blocks_of(p.keys, block) * kv * nr; };
@@ -87,8 +94,8 @@ inline attention_plan plan_attention(int n, int t, int tokens, int seqs, int hea
         p.key_block = sequence_rows > 16 ? 1024 : 128;
         while (p.key_block > 256 && workgroups(16 * p.row_tiles, p.key_block) < (p.row_tiles == 2 ? 4096 : 768)) p.key_block /= 2;
         // one launch for softmax and values while each of its workgroups has a CU to itself (us, one launch / two): single tokens of 32 heads of
-        // 128 over 64 keys, n = 5, one sequence 15.1 / 18.2, 4 17.3 / 20.9, 16 (800 workgroups) 38.4 / 37.9, 64 109 / 104; over 256 keys, one
-        // 21.2 / 22.4
+        // 128 over 64 keys, n = 5, one sequence 15.9 / 17.8, 4 16.9 / 19.9, 16 (800 workgroups) 33.1 / 33.5, 64 103 / 97; over 256 keys, one
+        // 21.8 / 22.4
         p.finish = p.row_tiles == 1 && p.keys <= SHORT_KEYS && tiles(16) * kv * n <= 256;
         // single tokens read the values once, which several rounds of workgroups spread best over the memory (us, 2048 / 1024 workgroups wanted:
         // 87 / 98); chunks multiply, and a round of 384 that needs no sum is as good as three runs (20.4 / 19.5 + 5.2 for the sum)
