@@ -524,6 +524,83 @@ size_t ssnet_workspace_bytes_attention(const ssnet_ctx *ctx, const ssnet_paged_c
 int ssnet_paged_attention(ssnet_ctx *ctx, const ssnet_paged_cache *cache, const ssnet_sequences *seqs, const uint64_t *d_q, size_t ld_q,
                           int heads, uint32_t scale, int weight_bits, int causal, uint64_t stream_id, uint64_t *d_out);
 
+/* Low-rank adapters of many requests beside a projection that they share.  An
+ * adapter changes a dense layer W [K][N] by A B, A [K][rank], B [rank][N] (any
+ * factor of theirs belongs into B).  A set holds `adapters` of them, all of one
+ * K, N and rank, as the digits that the products need:
+ *   d_down, d_up: ssnet_adapter_down_bytes / ssnet_adapter_up_bytes for each, one
+ *     after the other, 16-byte aligned, memory of the caller's;
+ *   ssnet_pack_adapter: shares d_a [n][K][rank], d_b [n][rank][N] (degree t, scale
+ *     2^f) go to place `index`, in place of what it held; rank may be less than
+ *     the set's.  Places that nothing was packed into hold no adapter: zeroed
+ *     memory stands for one that changes nothing.
+ * K <= SSNET_MAX_K, N <= 2^20.
+ *   ssnet_adapters_mod: `tokens` tokens belong to `requests` requests, those of
+ *     request b are d_start[b] .. d_start[b+1] - 1 (d_start[0] = 0,
+ *     d_start[requests] = tokens, none or more each) and take adapter d_adapter[b];
+ *     a number outside the set is none.  Per token:
+ *       1. parties i = 1..2t+1: Z_i = x_i A_i mod p (degree 2t, 2f fraction bits);
+ *       2. degree reduction and truncation of Z, messages and draws as in
+ *          ssnet_degree_reduce_truncate with count = tokens * rank -> z;
+ *       3. all parties: y_i = base_i + z_i B_i mod p,
+ *     a degree-2t sharing with 2f fraction bits as the shared projection's product
+ *     d_base [n][tokens][N] is, so RED and truncation of both follow once.  Of a
+ *     token without an adapter y = base.  d_base may be d_y, or NULL for 0.
+ *     d_x [n][tokens][K], d_base and d_y [n][tokens][N] may be parts of longer
+ *     rows: element j of a token is number (party * tokens + token) * ld + j.
+ *     d_y overlaps neither d_x nor, unless it is the same, d_base.  The range of z
+ *     is that of the truncation.  Who takes which adapter is known to all parties. */
+#define SSNET_MAX_RANK 128
+typedef struct ssnet_adapters {
+    void *d_down, *d_up;
+    int adapters, K, rank, N;
+} ssnet_adapters;
+typedef struct ssnet_requests {
+    const int32_t *d_start, *d_adapter;
+    int requests, tokens;
+} ssnet_requests;
+size_t ssnet_adapter_down_bytes(const ssnet_ctx *ctx, int K, int rank);
+size_t ssnet_adapter_up_bytes(const ssnet_ctx *ctx, int rank, int N);
+int ssnet_pack_adapter(ssnet_ctx *ctx, const ssnet_adapters *set, int index, const uint64_t *d_a, const uint64_t *d_b, int rank);
+size_t ssnet_workspace_bytes_adapters(const ssnet_ctx *ctx, const ssnet_adapters *set, int requests, int tokens);
+int ssnet_adapters_mod(ssnet_ctx *ctx, const ssnet_adapters *set, const ssnet_requests *requests, const uint64_t *d_x, size_t ld_x, const uint64_t *d_base,
+                       size_t ld_base, uint64_t stream_id, uint64_t *d_y, size_t ld_y);
+
+/* The next token of every row, drawn from the softmax of its logits: REC from the
+ * parties party_ids (as in ssnet_reconstruct, degree t) for whoever receives the
+ * result, and the draw in one call; nothing but the logits is opened.  d_logits
+ * [n][rows][vocab], possibly part of longer rows (element j of a row is number
+ * (party * rows + row) * ld + j), at scale 2^f.  d_params [rows][4] (16-byte
+ * aligned): scale, top_k, top_p, min_p of each row; d_random [rows]: uniform
+ * numbers below 2^62 (higher bits are ignored); d_allowed [rows][ld_allowed], if
+ * not NULL: bit j % 32 of word j / 32 is 1 for tokens that may be drawn.  In whole
+ * numbers, per row, over the allowed tokens:
+ *   h = min(f, 16); L = the logit in units of 2^-h (floor), limited to +-(2^31 - 1);
+ *   d = the largest L of the row - L;
+ *   u = (d * scale) >> (h + 8)  (octaves, 16 fraction bits), scale = round(2^24
+ *     log2(e) / temperature), taken as 2^14 where it is less;
+ *   w = floor(2^30 2^-u), as in ssnet_paged_attention (0 from 31 octaves on);
+ *   order: by d, equal ones by their number.
+ *   top_k > 0: the first top_k stay.  scale <= 0: the first alone.
+ *   top_p < 2^30: of these the fewest first ones stay whose weights sum to at least
+ *     max(1, ceil(top_p * sum of all of these / 2^30)) (a negative top_p is 0).
+ *   Of these stay those with w >= max(1, min(min_p, 2^30)): min_p is 2^30 times a part
+ *     of the largest weight.
+ * S = the sum of what stays.  d_tokens: the first token, by number, up to and
+ * with which the weights sum to more than floor(random * S / 2^62); d_shown: its
+ * probability floor((2^30 w + S / 2) / S).  A row that allows nothing: -1, 0.
+ * vocab <= SSNET_MAX_VOCAB.  Needs ssnet_workspace_bytes_sample. */
+#define SSNET_MAX_VOCAB (1 << 20)
+typedef struct ssnet_sampling {
+    const int32_t *d_params;
+    const int64_t *d_random;
+    const uint32_t *d_allowed;
+    size_t ld_allowed;
+} ssnet_sampling;
+size_t ssnet_workspace_bytes_sample(const ssnet_ctx *ctx, int rows, int vocab);
+int ssnet_sample(ssnet_ctx *ctx, const uint64_t *d_logits, size_t ld, int rows, int vocab, const int *party_ids, int m, const ssnet_sampling *how,
+                 int64_t *d_tokens, int32_t *d_shown);
+
 /* Host-side generator, exposed so that its bits can be checked without a GPU.
  * key = absorb(seed, domain, stream_id, party, j) with h <- mix64((h ^ word) +
  * 0x9E3779B97F4A7C15) from h = 0, mix64 being the SplitMix64 output function;

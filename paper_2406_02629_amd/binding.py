@@ -80,6 +80,13 @@ SIGNATURES = {
     "ssnet_cache_append": (_int, [_ptr, _ptr, _ptr, _sz, _ptr, _sz, _int, _ptr, _ptr, _u64]),
     "ssnet_workspace_bytes_attention": (_sz, [_ptr, _ptr, _int, _int, _int, _int]),
     "ssnet_paged_attention": (_int, [_ptr, _ptr, _ptr, _ptr, _sz, _int, _int, _int, _int, _u64, _ptr]),
+    "ssnet_adapter_down_bytes": (_sz, [_ptr, _int, _int]),
+    "ssnet_adapter_up_bytes": (_sz, [_ptr, _int, _int]),
+    "ssnet_pack_adapter": (_int, [_ptr, _ptr, _int, _ptr, _ptr, _int]),
+    "ssnet_workspace_bytes_adapters": (_sz, [_ptr, _ptr, _int, _int]),
+    "ssnet_adapters_mod": (_int, [_ptr, _ptr, _ptr, _ptr, _sz, _ptr, _sz, _u64, _ptr, _sz]),
+    "ssnet_workspace_bytes_sample": (_sz, [_ptr, _int, _int]),
+    "ssnet_sample": (_int, [_ptr, _ptr, _sz, _int, _int, C.POINTER(_int), _int, _ptr, _ptr, _ptr]),
     "ssnet_field_prime": (_u64, []),
     "ssnet_rng_key": (_u64, [_u64] * 5),
     "ssnet_rng_draw": (_u64, [_u64, _u64]),
@@ -106,7 +113,7 @@ class _Entries:
              "conv1x1_mod_prepacked", "share_planes", "split_planes", "conv_mod_planes", "linear_product_prepacked",
              "conv1x1_product_prepacked", "conv_product_planes", "degree_reduce", "truncate", "degree_reduce_truncate",
              "degree_reduce_truncate_div", "degree_reduce_truncate_reconstruct", "reduce_truncate_direct", "reduce_truncate_relu",
-             "reduce_truncate_relu_direct", "relu", "relu_pool", "rotary_truncate", "cache_append", "paged_attention")
+             "reduce_truncate_relu_direct", "relu", "relu_pool", "rotary_truncate", "cache_append", "paged_attention", "adapters_mod", "sample")
 
     def __init__(self, lib: C.CDLL):
         global _calls
@@ -176,9 +183,22 @@ class _Sequences(C.Structure):
                 ("max_length", _int)]
 
 
+class _AdaptersStruct(C.Structure):
+    _fields_ = [("d_down", _ptr), ("d_up", _ptr), ("adapters", _int), ("K", _int), ("rank", _int), ("N", _int)]
+
+
+class _Requests(C.Structure):
+    _fields_ = [("d_start", _ptr), ("d_adapter", _ptr), ("requests", _int), ("tokens", _int)]
+
+
+class _Sampling(C.Structure):
+    _fields_ = [("d_params", _ptr), ("d_random", _ptr), ("d_allowed", _ptr), ("ld_allowed", _sz)]
+
+
 # into one such structure per context, which the library reads before the call returns (making a new one takes 1 us of the host)
 _LOG2E_24 = math.log2(math.e) * (1 << 24)
 _pack_rotary, _pack_sequences = struct.Struct("PPiii").pack_into, struct.Struct("PPPiiii").pack_into
+_pack_requests, _pack_sampling = struct.Struct("PPii").pack_into, struct.Struct("PPPN").pack_into
 
 
 def _device_tensor(t: torch.Tensor, dtype: torch.dtype, name: str, shape: Optional[tuple] = None) -> torch.Tensor:
@@ -214,6 +234,37 @@ class PagedCache:
         self._address = C.addressof(self._struct)
 
 
+class Adapters:
+    """A set of low-rank adapters of a dense layer [K][N], as balanced digits (include/ssnet.h).  Places that nothing was loaded into change
+    nothing.  down, up: int8 tensors to use (of any shape), else new ones."""
+
+    def __init__(self, ss: "SSNet", adapters: int, K: int, rank: int, N: int, down: Optional[torch.Tensor] = None,
+                 up: Optional[torch.Tensor] = None):
+        sizes = ss.lib.ssnet_adapter_down_bytes(ss._ctx, K, rank), ss.lib.ssnet_adapter_up_bytes(ss._ctx, rank, N)
+        if 0 in sizes or not 1 <= adapters <= 1 << 20:
+            raise SSNetError(EINVAL, "ssnet_adapter_down_bytes")
+        self.ss, self.n, self.t, self.p, self.adapters, self.K, self.rank, self.N = ss, ss.n, ss.t, ss.p, adapters, K, rank, N
+        held = []
+        for name, t, size in (("down", down, sizes[0]), ("up", up, sizes[1])):
+            if t is None:
+                t = torch.zeros((adapters, size), dtype=torch.int8, device=ss.device)
+            elif _device_tensor(t, torch.int8, name).numel() != adapters * size:
+                raise SSNetError(EINVAL, f"Adapters: {name} must hold {adapters} adapters of {size} bytes")
+            held.append(t)
+        self.down, self.up = held
+        self._struct = _AdaptersStruct(_dptr(self.down), _dptr(self.up), adapters, K, rank, N)
+        self._address = C.addressof(self._struct)
+
+    def load(self, index: int, a: torch.Tensor, b: torch.Tensor):
+        """shares a [n][K][r], b [n][r][N], r up to the set's rank, into place `index`"""
+        _device_tensor(a, torch.int64, "a"), _device_tensor(b, torch.int64, "b")
+        r = a.shape[2] if a.dim() == 3 else 0
+        if a.shape != (self.n, self.K, r) or b.shape != (self.n, r, self.N) or not 1 <= r <= self.rank:
+            raise ValueError("a and b must be [n][K][r] and [n][r][N], r at most the set's rank")
+        ss = self.ss
+        ss._ok(ss.lib.ssnet_pack_adapter(ss._ctx, self._address, index, _dptr(a), _dptr(b), r), "ssnet_pack_adapter")
+
+
 class SSNet:
     """One (k = t+1, n) scheme over F_p, p = 2^61-1 (or P45, served by the second library), fixed-point
     fraction bits f."""
@@ -241,6 +292,8 @@ class SSNet:
         self._taken: list = []       # stream ids that take_streams gave out: (first, behind the last), in order, apart
         self._rotary_arg, self._sequences_arg = _Rotary(), _Sequences()
         self._rotary_address, self._sequences_address = C.addressof(self._rotary_arg), C.addressof(self._sequences_arg)
+        self._requests_arg, self._sampling_arg = _Requests(), _Sampling()
+        self._requests_address, self._sampling_address = C.addressof(self._requests_arg), C.addressof(self._sampling_arg)
 
     def close(self):
         if getattr(self, "_ctx", None):
@@ -868,6 +921,83 @@ class SSNet:
                                             factor, weight_bits, causal, stream_id,
                                             out.data_ptr()), "ssnet_paged_attention")
         return out
+
+    # ---- many requests at once ----
+    def _rows_view(self, x: torch.Tensor, name: str, shape: Optional[tuple] = None):
+        """elements between rows of x [n][rows][width], which may be part of a longer row each"""
+        if x.dtype is not torch.int64 or x.dim() != 3 or not x.is_cuda:
+            raise TypeError(f"{name} must be an int64 tensor of three dimensions on the GPU")
+        n, rows, width = x.shape
+        if n != self.n or (shape is not None and (rows, width) != shape):
+            raise ValueError(f"{name} must have the shape {(self.n,) + (shape or ('rows', 'width'))}")
+        if x.is_contiguous():
+            return width
+        s = x.stride()
+        ld = s[1] if rows > 1 else s[0]
+        if (n > 1 and s[0] != rows * ld) or (width > 1 and s[2] != 1) or ld < width:
+            raise TypeError(f"{name}: a row must be contiguous, rows and parties equally far apart")
+        return ld
+
+    def adapters_mod(self, adapters: Adapters, x: torch.Tensor, start: torch.Tensor, index: torch.Tensor, stream_id: int,
+                     base: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """base + trunc(x A) B of every token's adapter: x [n][tokens][K] at scale 2^f, base [n][tokens][N] the shared projection's product
+        (linear_mod_packed; None: 0) -> [n][tokens][N], degree 2t, 2f fraction bits.  Tokens start[b] to start[b+1] take adapter index[b], none
+        if there is no such place.  out may be base."""
+        if adapters.n != self.n or adapters.t != self.t or adapters.p != self.p:
+            raise ValueError(f"the adapters are of {adapters.n} parties, degree {adapters.t}, prime {adapters.p}")
+        ld_x = self._rows_view(x, "x")
+        tokens, requests = x.shape[1], index.shape[0]
+        if x.shape[2] != adapters.K:
+            raise ValueError(f"x must be [n][tokens][{adapters.K}]")
+        _device_tensor(start, torch.int32, "start", (requests + 1,)), _device_tensor(index, torch.int32, "index", (requests,))
+        shape = (tokens, adapters.N)
+        ld_base = 0 if base is None else self._rows_view(base, "base", shape)
+        if out is None:
+            out = torch.empty((self.n,) + shape, dtype=torch.int64, device=x.device)
+        ld_y = self._rows_view(out, "out", shape)
+        key = ("adapters", adapters.K, adapters.rank, adapters.N, requests, tokens)
+        need = self._sizes.get(key)
+        if need is None:
+            need = self.lib.ssnet_workspace_bytes_adapters(self._ctx, adapters._address, requests, tokens)
+            if need == 0:
+                raise SSNetError(EINVAL, "ssnet_workspace_bytes_adapters")
+            if len(self._sizes) >= 4096:
+                self._sizes.clear()
+            self._sizes[key] = need
+        self.reserve(need)
+        _pack_requests(self._requests_arg, 0, start.data_ptr(), index.data_ptr(), requests, tokens)
+        self._ok(self._call.adapters_mod(self._handle, adapters._address, self._requests_address, x.data_ptr(), ld_x,
+                                         None if base is None else base.data_ptr(), ld_base, stream_id, out.data_ptr(), ld_y), "ssnet_adapters_mod")
+        return out
+
+    def sample(self, logits: torch.Tensor, ids: Sequence[int], params: torch.Tensor, random: torch.Tensor,
+               allowed: Optional[torch.Tensor] = None, tokens: Optional[torch.Tensor] = None, shown: Optional[torch.Tensor] = None):
+        """The next token of every row of logits [n][rows][vocab] (degree t, scale 2^f), opened from the parties `ids` and drawn: params int32
+        [rows][4] (fixedpoint.sampling_parameters), random int64 [rows] uniform below 2^62, allowed int32 [rows][(vocab + 31) / 32 or more] with a
+        bit for every token that may be drawn -> (tokens int64 [rows], -1 where nothing is allowed, their probabilities int32 [rows] in
+        units of 2^-30)"""
+        ld = self._rows_view(logits, "logits")
+        rows, vocab = logits.shape[1:]
+        _device_tensor(params, torch.int32, "params", (rows, 4)), _device_tensor(random, torch.int64, "random", (rows,))
+        if allowed is not None:
+            _device_tensor(allowed, torch.int32, "allowed")
+            if allowed.dim() != 2 or allowed.shape[0] != rows or allowed.shape[1] * 32 < vocab:
+                raise ValueError("allowed must be [rows][(vocab + 31) / 32 or more]")
+        if tokens is None:
+            tokens = torch.empty(rows, dtype=torch.int64, device=logits.device)
+        if shown is None:
+            shown = torch.empty(rows, dtype=torch.int32, device=logits.device)
+        _device_tensor(tokens, torch.int64, "tokens", (rows,)), _device_tensor(shown, torch.int32, "shown", (rows,))
+        need = self._size("ssnet_workspace_bytes_sample", rows, vocab)
+        if need == 0:
+            raise SSNetError(EINVAL, "ssnet_workspace_bytes_sample")
+        self.reserve(need)
+        _pack_sampling(self._sampling_arg, 0, params.data_ptr(), random.data_ptr(), 0 if allowed is None else allowed.data_ptr(),
+                       0 if allowed is None else allowed.shape[1])
+        arr = (_int * len(ids))(*ids)
+        self._ok(self._call.sample(self._handle, logits.data_ptr(), ld, rows, vocab, C.addressof(arr), len(ids), self._sampling_address,
+                                   tokens.data_ptr(), shown.data_ptr()), "ssnet_sample")
+        return tokens, shown
 
     PROF_CLASSES = ("share", "reconstruct", "pack_w", "pack_x", "gemm", "degree_reduce", "truncate", "nonlinear",
                     "gemm_kernel")   # gemm_kernel: the product kernels from their own start to their own end

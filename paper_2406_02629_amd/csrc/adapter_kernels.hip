@@ -1,0 +1,381 @@
+// Low-rank adapters of many requests beside a projection that they share, on shares.  A request's tokens x take its adapter (A [K][rank],
+// B [rank][N]):
+//   1. parties i = 1..2t+1: Z_i = x_i A_i mod p (degree 2t, 2 f fraction bits), the contraction cut into runs with a plane of sums each
+//   2. degree reduction and truncation of Z (the reduction's own kernel, which adds the planes) -> z, degree t, f fraction bits
+//   3. every party: y_i = base_i + z_i B_i mod p (degree 2t), base being the shared projection's product
+// Products run on int8 MFMA over balanced 8-bit digits, as in a dense layer.
+#include "kernels.hpp"
+#include "digits.hpp"
+#include "diagonals.hpp"
+#include "truncation.hpp"
+
+namespace SS_NS {
+
+namespace {
+
+constexpr int BLOCK = 256;
+
+typedef const int __attribute__((address_space(4))) *constant_ints;
+__device__ __forceinline__ int fixed_at(const int *p, size_t i) { return ((constant_ints)(uintptr_t)p)[i]; }
+
+// ------------------------------------------------------------------ laying an adapter out
+
+// 16 elements of a column of A to a thread (down, see serving_plan.hpp).  a [.][K][given] of each party; given <= rank, the rest is zero.
+__global__ __launch_bounds__(BLOCK) void pack_down_kernel(const u64 *a, signed char *down, int K, int given, int rank, unsigned items, size_t party_bytes)
+{
+    const unsigned i = blockIdx.x * BLOCK + threadIdx.x;
+    if (i >= items) return;
+    const int party = blockIdx.y, r = (int)(i % (unsigned)rank), q = (int)(i / (unsigned)rank & 3), kb = (int)(i / (unsigned)rank >> 2);
+    u64 y[4][4];
+#pragma unroll
+    for (int b = 0; b < 16; b++) {
+        const int k = 64 * kb + 8 * (b >> 1) + 2 * q + (b & 1);
+        y[b >> 2][b & 3] = balanced_digits(k < K && r < given ? a[((size_t)party * K + k) * given + r] : 0);
+    }
+    signed char *dst = down + party * party_bytes + ((size_t)kb * SS_NLIMB * 4 + q) * rank * 16 + (size_t)r * 16;
+#pragma unroll
+    for (int l = 0; l < SS_NLIMB; l++)
+        *reinterpret_cast<v4i *>(dst + (size_t)l * 4 * rank * 16) =
+            (v4i){(int)limb_dword(y[0], l), (int)limb_dword(y[1], l), (int)limb_dword(y[2], l), (int)limb_dword(y[3], l)};
+}
+
+// 16 digits of a column of B to a thread (up).  b [n][given][N]; padded: the rank in whole eights
+__global__ __launch_bounds__(BLOCK) void pack_up_kernel(const u64 *b, signed char *up, int given, int padded, int N, unsigned items, size_t party_bytes)
+{
+    const unsigned i = blockIdx.x * BLOCK + threadIdx.x;
+    if (i >= items) return;
+    const unsigned chunks = (unsigned)(SS_NLIMB * padded / 16);
+    const int party = blockIdx.y, c = (int)(i & 15), chunk = (int)(i / 16 % chunks), half = (int)(i / 16 / chunks);
+    const int col = 32 * (half >> 1) + 2 * c + (half & 1);
+    u32 d[4] = {0, 0, 0, 0};
+    for (int e = 0; e < 16; e++) {
+        const int at = chunk * 16 + e, limb = at / padded, r = at - limb * padded;
+        const u64 x = r < given && col < N ? b[((size_t)party * given + r) * N + col] : 0;
+        d[e >> 2] |= ((u32)(balanced_digits(x) >> (8 * limb)) & 255) << (8 * (e & 3));
+    }
+    *reinterpret_cast<v4i *>(up + party * party_bytes + (size_t)i * 16) = (v4i){(int)d[0], (int)d[1], (int)d[2], (int)d[3]};
+}
+
+// ------------------------------------------------------------------ products
+
+struct adapter_args {
+    const int *start, *adapter;     // [requests + 1], [requests]
+    int requests, tokens, adapters;
+    int K, rank, padded, N;
+    const signed char *down, *up;
+    size_t down_party, up_party, down_bytes, up_bytes;   // of a party, of an adapter
+    const u64 *x, *base;
+    size_t ld_x, ld_base, ld_y;
+    u64 *planes, *y;                // planes [splits][2t+1][tokens][rank]
+    const u64 *z;                   // [n][tokens][rank]
+    int nr, n, rank_tiles, run, col_groups;
+    size_t plane;                   // 2t+1 shares
+};
+
+// the tokens of a tile, all of one request
+struct request_tile {
+    int first, count, adapter;      // adapter: -1 if the request has none
+};
+
+// tile number -> its tokens; every lane of the wave calls.  False: no such tile.
+__device__ __forceinline__ bool tile_at(const adapter_args &g, int tile, int rows, request_tile &r)
+{
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int b0 = 0; b0 < g.requests; b0 += 64) {
+        const int b = b0 + lane;
+        int first = 0, count = 0;
+        if (b < g.requests) {
+            first = min(max(g.start[b], 0), g.tokens);
+            count = max(0, min(g.start[b + 1], g.tokens) - first);
+        }
+        const int mine = (count + rows - 1) / rows;
+        int upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int v = __shfl_up(upto, d);
+            if (lane >= d) upto += v;
+        }
+        const unsigned long long past = __ballot(base + upto > tile);
+        if (past) {
+            const int l = __ffsll((long long)past) - 1, at = (tile - base - __shfl(upto - mine, l)) * rows;
+            r.first = __builtin_amdgcn_readfirstlane(__shfl(first, l) + at);
+            r.count = __builtin_amdgcn_readfirstlane(min(rows, __shfl(count, l) - at));
+            const int adapter = fixed_at(g.adapter, (size_t)__builtin_amdgcn_readfirstlane(b0 + l));
+            r.adapter = adapter < 0 || adapter >= g.adapters ? -1 : adapter;
+            return true;
+        }
+        base += __shfl(upto, 63);
+    }
+    return false;
+}
+
+// 16 elements of a row for a lane of quarter q, in the order of the laid out A; past the row's end anything (A is zero there)
+template <bool WIDE>
+__device__ __forceinline__ void load_row(const u64 *row, int k0, int K, u64 (&v)[16])
+{
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        const int k = k0 + 8 * j;
+        if constexpr (WIDE) {
+            pack_t<2> p;
+            p.load(row + (k < K ? k : 0));
+            v[2 * j] = p.v[0], v[2 * j + 1] = p.v[1];
+        } else {
+            v[2 * j] = row[k < K ? k : 0];
+            v[2 * j + 1] = row[k + 1 < K ? k + 1 : 0];
+        }
+    }
+}
+
+// Step 1: one workgroup per (tile of 16 tokens, 16 columns of A, party and run of the contraction); its four waves take every fourth block of 64
+// elements, and add their sums up in LDS as whole numbers.
+template <bool WIDE>
+__global__ __launch_bounds__(BLOCK, 2) void down_kernel(adapter_args g)
+{
+    __shared__ int sums[ND][BLOCK];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int column = blockIdx.y / g.nr, party = blockIdx.y - column * g.nr, split = blockIdx.z;
+    request_tile r;
+    if (!tile_at(g, blockIdx.x, 16, r)) return;
+    u64 *out = g.planes + split * g.plane + (size_t)party * g.tokens * g.rank;
+    const int token = tid >> 4, c = column * 16 + (tid & 15);
+    const bool live = token < r.count && c < g.rank;
+    const size_t at = (size_t)(r.first + token) * g.rank + c;
+    if (r.adapter < 0) {
+        if (live) out[at] = 0;
+        return;
+    }
+#pragma unroll
+    for (int s = 0; s < ND; s++) sums[s][tid] = 0;
+    __syncthreads();
+    const int blocks = (g.K + 63) >> 6, end = min((split + 1) * g.run, blocks);
+    const u64 *row = g.x + ((size_t)party * g.tokens + r.first + min(lane & 15, r.count - 1)) * g.ld_x;
+    const signed char *a = g.down + r.adapter * g.down_bytes + party * g.down_party + ((size_t)(lane >> 4) * g.rank + min(column * 16 + (lane & 15), g.rank - 1)) * 16;
+    const size_t limb = (size_t)g.rank * 64;
+    v4i acc[ND];
+#pragma unroll
+    for (int s = 0; s < ND; s++) acc[s] = (v4i){0, 0, 0, 0};
+    for (int kb = split * g.run + wave; kb < end; kb += 4) {
+        v4i w[NL];
+#pragma unroll
+        for (int l = 0; l < NL; l++) w[l] = *reinterpret_cast<const v4i *>(a + (size_t)kb * NL * limb + l * limb);
+        u64 v[16];
+        load_row<WIDE>(row, 64 * kb + 2 * (lane >> 4), g.K, v);
+        u32 d[4][8];
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+            const u64 y[4] = {balanced_digits(v[4 * b]), balanced_digits(v[4 * b + 1]), balanced_digits(v[4 * b + 2]), balanced_digits(v[4 * b + 3])};
+            limb_dwords(y, d[b]);
+        }
+#pragma unroll
+        for (int i = 0; i < NL; i++) {
+            const v4i x = (v4i){(int)d[0][i], (int)d[1][i], (int)d[2][i], (int)d[3][i]};
+#pragma unroll
+            for (int j = 0; j < NL; j++) acc[i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, w[j], acc[i + j], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < ND; s++)
+#pragma unroll
+        for (int q = 0; q < 4; q++) atomicAdd(&sums[s][(4 * (lane >> 4) + q) * 16 + (lane & 15)], acc[s][q]);
+    __syncthreads();
+    if (!live) return;
+    v4i total[ND];
+#pragma unroll
+    for (int s = 0; s < ND; s++) total[s][0] = sums[s][tid];
+    out[at] = fold_diagonals(total, 0);
+}
+
+// Words that four rows of 16 lanes hold of four items, one part of each: afterwards row q has the four parts of item q.
+__device__ __forceinline__ void exchange(long long (&g)[4])
+{
+    u32 h[2][4];
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        const auto a = __builtin_amdgcn_permlane32_swap((u32)((u64)g[0] >> (32 * i)), (u32)((u64)g[2] >> (32 * i)), false, false);   // parts 0 1 of items 0 and 2, 2 3
+        const auto b = __builtin_amdgcn_permlane32_swap((u32)((u64)g[1] >> (32 * i)), (u32)((u64)g[3] >> (32 * i)), false, false);
+        const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+        h[i][0] = lo[0], h[i][1] = lo[1], h[i][2] = hi[0], h[i][3] = hi[1];
+    }
+#pragma unroll
+    for (int q = 0; q < 4; q++) g[q] = (long long)((u64)h[1][q] << 32 | h[0][q]);
+}
+
+// four items' diagonal sums 4 q .. 4 q + 3 of a column in row q -> in row q item q's field element plus `more`
+__device__ __forceinline__ u64 fold_items(const v4i (&acc)[4], u64 more)
+{
+    long long g[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) g[i] = join4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+    exchange(g);
+#if defined(SS_FIELD_P45)
+    return fold_words((u64)(g[0] + WORD_OFFSET), (u64)(g[1] + WORD_OFFSET), (u64)(g[2] + WORD_OFFSET), more);
+#else
+    return fold_words(g[0], g[1], g[2], g[3], more);
+#endif
+}
+
+// Step 3.  The contraction is short, so it runs over limbs and rank together: D[s][c] = sum over (j, r) of z_{s-j}[r] B_j[r][c] is diagonal sum s
+// of column c, which makes one MFMA of 16 diagonals by 16 columns for 64 digits of a column, and one accumulator.  A's rows are the
+// digits of z, in LDS with their limbs falling and zeros around them, read from a place that moves up by the rank with every diagonal.
+// One workgroup per (tile of ROWS tokens, part of the columns and party).  Its waves take 32 columns of 16 tokens at a time, or 64 of
+// one.  WIDE: pairs of columns in 16 bytes.
+template <int ROWS, bool WIDE>
+__global__ __launch_bounds__(BLOCK, 2) void up_kernel(adapter_args g)
+{
+    extern __shared__ signed char zd[];          // [ROWS][stride]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int part = blockIdx.y / g.n, party = blockIdx.y - part * g.n;
+    request_tile r;
+    if (!tile_at(g, blockIdx.x, ROWS, r)) return;
+    const u64 *base = g.base ? g.base + ((size_t)party * g.tokens + r.first) * g.ld_base : nullptr;
+    u64 *y = g.y + ((size_t)party * g.tokens + r.first) * g.ld_y;
+    if (r.adapter < 0) {
+        if (base == y) return;
+        for (int t = 0; t < r.count; t++)
+            for (int c = part * BLOCK + tid; c < g.N; c += g.col_groups * BLOCK) y[t * g.ld_y + c] = base ? base[t * g.ld_base + c] : 0;
+        return;
+    }
+    const int R = g.padded, chunks = NL * R / 16, steps = (chunks + 3) >> 2, stride = 15 * R + 64 * steps;
+    // limb l of element i of a token's z lies at (15 - l) R + i
+    for (int i = tid * 4; i < ROWS * stride; i += BLOCK * 4) *reinterpret_cast<int *>(zd + i) = 0;
+    __syncthreads();
+    for (int i = tid; i < r.count * g.rank; i += BLOCK) {
+        const int t = i / g.rank, e = i - t * g.rank;
+        const u64 d = balanced_digits(g.z[((size_t)party * g.tokens + r.first) * g.rank + i]);
+#pragma unroll
+        for (int l = 0; l < NL; l++) zd[t * stride + (15 - l) * R + e] = (signed char)(d >> (8 * l));
+    }
+    __syncthreads();
+    const int q = lane >> 4, c16 = lane & 15;
+    const signed char *z = zd + (15 - c16) * R + q * 16;
+    auto digits = [&](int t, int m) {            // (8-byte alignment)
+        const int2 *p = reinterpret_cast<const int2 *>(z + t * stride + m * 64);
+        const int2 a = p[0], b = p[1];
+        return (v4i){a.x, a.y, b.x, b.y};
+    };
+    const size_t half = (size_t)chunks * 256;    // bytes of 16 columns
+    const signed char *b = g.up + r.adapter * g.up_bytes + party * g.up_party + c16 * 16;
+    auto columns = [&](size_t at, int m) {
+        const int chunk = 4 * m + q;
+        const v4i v = *reinterpret_cast<const v4i *>(b + at * half + (size_t)min(chunk, chunks - 1) * 256);
+        return chunk < chunks ? v : (v4i){0, 0, 0, 0};
+    };
+    if constexpr (ROWS == 1) {
+        const int halves = 2 * ((g.N + 31) >> 5);
+        for (int u = part * 4 + wave; u * 64 < g.N; u += g.col_groups * 4) {
+            v4i acc[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) acc[i] = (v4i){0, 0, 0, 0};
+            const int col = 64 * u + 32 * (q >> 1) + 2 * c16 + (q & 1);
+            const u64 more = base && col < g.N ? base[col] : 0;
+            for (int m = 0; m < steps; m++) {
+                const v4i a = digits(0, m);
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, columns((size_t)min(4 * u + i, halves - 1), m), acc[i], 0, 0, 0);
+            }
+            const u64 o = fold_items(acc, more);
+            if (col < g.N) y[col] = o;
+        }
+    } else {
+        for (int u = part * 4 + wave; u * 32 < g.N; u += g.col_groups * 4) {
+            v4i acc[2][ROWS];
+#pragma unroll
+            for (int t = 0; t < ROWS; t++) acc[0][t] = acc[1][t] = (v4i){0, 0, 0, 0};
+            for (int m = 0; m < steps; m++) {
+                const v4i b0 = columns(2 * (size_t)u, m), b1 = columns(2 * (size_t)u + 1, m);
+#pragma unroll
+                for (int t = 0; t < ROWS; t++) {
+                    const v4i a = digits(t, m);
+                    acc[0][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b0, acc[0][t], 0, 0, 0);
+                    acc[1][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b1, acc[1][t], 0, 0, 0);
+                }
+            }
+            const int col = 32 * u + 2 * c16;
+#pragma unroll
+            for (int t0 = 0; t0 < ROWS; t0 += 4) {
+                const int t = t0 + q;
+                const bool live = t < r.count;
+                pack_t<2> v = {{0, 0}};
+                if (base && live) {
+                    if (WIDE) {
+                        if (col < g.N) v.load(base + t * g.ld_base + col);
+                    } else {
+                        if (col < g.N) v.v[0] = base[t * g.ld_base + col];
+                        if (col + 1 < g.N) v.v[1] = base[t * g.ld_base + col + 1];
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const v4i four[4] = {acc[h][t0], acc[h][t0 + 1], acc[h][t0 + 2], acc[h][t0 + 3]};
+                    v.v[h] = fold_items(four, v.v[h]);
+                }
+                if (!live) continue;
+                if (WIDE) {
+                    if (col < g.N) v.store(y + t * g.ld_y + col);
+                } else {
+                    if (col < g.N) y[t * g.ld_y + col] = v.v[0];
+                    if (col + 1 < g.N) y[t * g.ld_y + col + 1] = v.v[1];
+                }
+            }
+        }
+    }
+}
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+}  // namespace
+
+hipError_t ss_launch_pack_adapter(const ss_adapters &s, int index, const u64 *a, const u64 *b, int given, int n, int t, hipStream_t stream)
+{
+    const int padded = (int)padded_rank(s.rank), nr = 2 * t + 1;
+    const size_t down = down_party_bytes(s.K, s.rank), up = up_party_bytes(s.rank, s.N);
+    const unsigned down_items = (unsigned)(down / SS_NLIMB / 16), up_items = (unsigned)(up / 16);
+    hipLaunchKernelGGL(pack_down_kernel, dim3((unsigned)div_up(down_items, BLOCK), nr), dim3(BLOCK), 0, stream, a, s.down + (size_t)index * nr * down, s.K, given,
+                       s.rank, down_items, down);
+    hipLaunchKernelGGL(pack_up_kernel, dim3((unsigned)div_up(up_items, BLOCK), n), dim3(BLOCK), 0, stream, b, s.up + (size_t)index * n * up, given, padded, s.N,
+                       up_items, up);
+    return hipGetLastError();
+}
+
+hipError_t ss_launch_adapters_down(const adapter_plan &plan, const ss_adapters &s, const ss_requests &req, const u64 *x, size_t ld_x, u64 *planes, int n, int t,
+                                   hipStream_t stream)
+{
+    adapter_args g = {};
+    g.start = req.start, g.adapter = req.adapter, g.requests = req.requests, g.tokens = req.tokens;
+    g.adapters = s.adapters, g.K = s.K, g.rank = s.rank;
+    g.down = s.down, g.nr = 2 * t + 1, g.n = n;
+    g.down_party = down_party_bytes(s.K, s.rank), g.down_bytes = g.nr * g.down_party;
+    g.x = x, g.ld_x = ld_x, g.planes = planes, g.plane = (size_t)g.nr * req.tokens * s.rank;
+    g.run = plan.run;
+    const dim3 grid((unsigned)request_tiles(req.tokens, req.requests, plan.down_rows), g.nr * plan.rank_tiles, plan.splits);
+    const bool wide = s.K % 2 == 0 && ld_x % 2 == 0 && aligned16(x);
+    hipLaunchKernelGGL((wide ? down_kernel<true> : down_kernel<false>), grid, dim3(BLOCK), 0, stream, g);
+    return hipGetLastError();
+}
+
+hipError_t ss_launch_adapters_up(const adapter_plan &plan, const ss_adapters &s, const ss_requests &req, const u64 *z, const u64 *base, size_t ld_base, u64 *y,
+                                 size_t ld_y, int n, int t, hipStream_t stream)
+{
+    (void)t;
+    adapter_args g = {};
+    g.start = req.start, g.adapter = req.adapter, g.requests = req.requests, g.tokens = req.tokens;
+    g.adapters = s.adapters, g.rank = s.rank, g.padded = (int)padded_rank(s.rank), g.N = s.N;
+    g.up = s.up, g.n = n;
+    g.up_party = up_party_bytes(s.rank, s.N), g.up_bytes = n * g.up_party;
+    g.z = z, g.base = base, g.ld_base = ld_base, g.y = y, g.ld_y = ld_y;
+    g.col_groups = plan.col_groups;
+    const int steps = (int)div_up(SS_NLIMB * g.padded, 64);
+    const size_t lds = (size_t)plan.up_rows * (15 * g.padded + 64 * steps);
+    const dim3 grid((unsigned)request_tiles(req.tokens, req.requests, plan.up_rows), n * plan.col_groups);
+    const bool wide = s.N % 2 == 0 && ld_y % 2 == 0 && aligned16(y) && (!base || (ld_base % 2 == 0 && aligned16(base)));
+    if (plan.up_rows == 1)
+        hipLaunchKernelGGL((up_kernel<1, false>), grid, dim3(BLOCK), lds, stream, g);
+    else
+        hipLaunchKernelGGL((wide ? up_kernel<16, true> : up_kernel<16, false>), grid, dim3(BLOCK), lds, stream, g);
+    return hipGetLastError();
+}
+
+}  // namespace SS_NS

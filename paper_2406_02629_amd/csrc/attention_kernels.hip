@@ -21,6 +21,7 @@
 #include "digits.hpp"
 #include "diagonals.hpp"
 #include "truncation.hpp"
+#include "power2.hpp"
 
 namespace SS_NS {
 
@@ -691,22 +692,12 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(attn_args g, ss_softmax_
 
 __device__ __forceinline__ long long lift(u64 v) { return v <= (SS_P - 1) / 2 ? (long long)v : (long long)v - (long long)SS_P; }
 
-// floor(2^30 2^-x) for the distance `below` >= 0 of a score (2 f fraction bits) from the row's maximum, x in octaves with 16 fraction
-// bits: 2^-x for x in [0, 1) by a polynomial of degree 5 that takes the value 1 at 0 and is off by 2.2e-7 at most, Horner's scheme
-// in 30 fraction bits, each product cut to them
+// floor(2^30 2^-x) for the distance `below` >= 0 of a score (2 f fraction bits) from the row's maximum, x in octaves with 16 fraction bits
 __device__ __forceinline__ u32 softmax_weight(long long below, const ss_softmax_params &sp)
 {
     const int h = min(2 * sp.f, 24);
     const u64 d = min((u64)below >> (2 * sp.f - h), (u64)1 << 37), u = (d * sp.scale) >> (h + 8);
-    const u32 r = (u32)u << 16;                  // the fraction, 32 bits
-    u32 w = 1077640u;
-    w = 10033292u - __umulhi(w, r);
-    w = 59494488u - __umulhi(w, r);
-    w = 257928559u - __umulhi(w, r);
-    w = 744260865u - __umulhi(w, r);
-    w = 1073741824u - __umulhi(w, r);
-    const u64 octaves = u >> 16;
-    return octaves < 31 ? w >> octaves : 0;
+    return power2(u);
 }
 
 template <int THREADS = BLOCK, typename T, typename F>

@@ -4,6 +4,7 @@
 #include "field.hpp"
 #include "gemm_plan.hpp"
 #include "attention_plan.hpp"
+#include "serving_plan.hpp"
 
 // Everything below lives in a namespace named after the field (ss61 / ss45), so that the two libraries built
 // from these sources never share a C++ symbol or a kernel name.
@@ -263,5 +264,37 @@ hipError_t ss_launch_append(const ss_paged &cache, const u64 *k, size_t ld_k, co
 // room: plan.bytes bytes for what the launches hand on
 hipError_t ss_launch_attention(const attention_plan &plan, const ss_paged &cache, const ss_sequences &seqs, const u64 *q, size_t ld_q, int heads,
                                int causal, const ss_softmax_params &sp, void *room, u64 *out, hipStream_t stream);
+
+// ---- low-rank adapters of many requests (adapter_kernels.hip) ----
+struct ss_adapters {              // laid out as serving_plan.hpp says
+    signed char *down, *up;
+    int adapters, K, rank, N;
+};
+
+// tokens start[b] .. start[b + 1] - 1 are those of request b, which takes adapter[b] (none if there is no such adapter)
+struct ss_requests {
+    const int *start, *adapter;
+    int requests, tokens;
+};
+
+// a [n][K][given], b [n][given][N], given <= s.rank, into place `index`
+hipError_t ss_launch_pack_adapter(const ss_adapters &s, int index, const u64 *a, const u64 *b, int given, int n, int t, hipStream_t stream);
+// x A of the parties 1..2t+1 -> planes [plan.splits][2t+1][tokens][rank], whose sum it is
+hipError_t ss_launch_adapters_down(const adapter_plan &plan, const ss_adapters &s, const ss_requests &req, const u64 *x, size_t ld_x, u64 *planes, int n, int t,
+                                   hipStream_t stream);
+// y = base + z B; base may be y, or nullptr for 0
+hipError_t ss_launch_adapters_up(const adapter_plan &plan, const ss_adapters &s, const ss_requests &req, const u64 *z, const u64 *base, size_t ld_base, u64 *y,
+                                 size_t ld_y, int n, int t, hipStream_t stream);
+
+// ---- sampling (sample_kernels.hip) ----
+struct ss_sampling {
+    const int4 *params;           // of a row: scale, top_k, top_p, min_p
+    const long long *random;
+    const u32 *allowed;           // a bit to a token, or nullptr
+    size_t ld_allowed;
+};
+
+hipError_t ss_launch_sample(const ss_sampling &q, const u64 *logits, size_t ld, int rows, int vocab, int f, const ss_rec_params &rp, void *room, long long *tokens,
+                            int *shown, hipStream_t stream);
 
 }  // namespace SS_NS

@@ -1,0 +1,60 @@
+// How the calls of adapter_kernels.hip and sample_kernels.hip are cut up.  Plain C++, so that the rules can be checked without a GPU.
+// SS_NLIMB: limbs of a field element (8, or 6 over the 45-bit prime).
+#pragma once
+#include <algorithm>
+#include <stddef.h>
+
+namespace SS_NS {
+
+inline size_t div_up(size_t a, size_t b) { return (a + b - 1) / b; }
+
+// ------------------------------------------------------------------ low-rank adapters
+
+// An adapter lies in memory as the digits of its two matrices:
+//   down [2t+1][K / 64][limb][4][rank][16] int8: byte b of quarter q is element k = 64 block + 8 (b / 2) + 2 q + b % 2 of the contraction, so
+//     that four lanes find 8 elements of a row of x in 64 bytes; past K zeros
+//   up [n][N / 32][2][limb R / 16][16][16] int8: column 32 block + 2 c + h is number c of half h, whose 16 bytes of a chunk are consecutive digits
+//     in the order limb, rank (R: the rank in whole eights, zeros behind it); past N zeros
+inline size_t padded_rank(size_t rank) { return (rank + 7) & ~(size_t)7; }
+inline size_t down_party_bytes(int K, int rank) { return div_up(K, 64) * SS_NLIMB * 64 * rank; }
+inline size_t up_party_bytes(int rank, int N) { return div_up(N, 32) * 2 * SS_NLIMB * padded_rank(rank) * 16; }
+
+constexpr size_t MAX_SERVING_GROUPS = ((size_t)1 << 24) - 1;   // workgroups of 256 threads in a launch: less than 2^32 threads
+constexpr int MAX_PLANES = 8;                                  // partial sums of the first product, which the reduction adds
+
+struct adapter_plan {
+    int down_rows, up_rows;       // tokens to a tile
+    int rank_tiles;               // of 16, of the first product
+    int splits, run;              // its contraction: in `splits` runs of `run` blocks of 64
+    int col_groups;               // workgroups that share the columns of a tile of the second product
+    size_t messages, planes, z;   // bytes: of the reduction's messages, of the first product's planes, of its reduced result
+    size_t down_groups, up_groups, bytes;
+};
+
+// most tiles of `rows` tokens that requests can have
+inline size_t request_tiles(size_t tokens, size_t requests, size_t rows) { return rows == 1 ? tokens : std::min(tokens, tokens / rows + requests); }
+
+inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K, int rank, int N)
+{
+    adapter_plan p = {};
+    const size_t nr = 2 * t + 1, k = t + 1, count = (size_t)tokens * rank, blocks = div_up(K, 64);
+    p.down_rows = 16;
+    p.up_rows = tokens <= 2 * (size_t)requests ? 1 : 16;
+    p.rank_tiles = (int)div_up(rank, 16);
+    const size_t tiles = request_tiles(tokens, requests, p.down_rows) * nr * p.rank_tiles;
+    p.splits = (int)std::max<size_t>(1, std::min(std::min<size_t>(MAX_PLANES, div_up(512, tiles)), blocks / 8));
+    p.run = (int)div_up(blocks, p.splits);
+    p.splits = (int)div_up(blocks, p.run);
+    p.down_groups = tiles * p.splits;
+    const size_t up_tiles = request_tiles(tokens, requests, p.up_rows), units = div_up(N, p.up_rows == 1 ? 64 : 32);
+    p.col_groups = (int)std::max<size_t>(1, std::min(div_up(512, up_tiles * n), div_up(units, 4)));
+    p.up_groups = up_tiles * n * p.col_groups;
+    auto whole = [](size_t b) { return (b + 255) & ~(size_t)255; };
+    p.messages = whole((nr * k + k * n + k + n) * count * 8);
+    p.planes = whole((size_t)p.splits * nr * count * 8);
+    p.z = whole((size_t)n * count * 8);
+    p.bytes = p.messages + p.planes + p.z;
+    return p;
+}
+
+}  // namespace SS_NS

@@ -1358,6 +1358,125 @@ int ssnet_paged_attention(ssnet_ctx *ctx, const ssnet_paged_cache *cache, const 
     return e == hipSuccess ? SSNET_OK : fail_hip(ctx, e);
 }
 
+namespace {
+
+static bool adapters_ok(const ssnet_adapters *s, bool pointers)
+{
+    if (!s || s->adapters < 1 || s->adapters > (1 << 20) || s->K < 1 || s->K > SSNET_MAX_K || s->rank < 1 || s->rank > SSNET_MAX_RANK || s->N < 1 ||
+        s->N > (1 << 20))
+        return false;
+    return !pointers || (s->d_down && s->d_up && !((uintptr_t)s->d_down & 15) && !((uintptr_t)s->d_up & 15));
+}
+
+static ss_adapters make_adapters(const ssnet_adapters *s)
+{
+    return {(signed char *)s->d_down, (signed char *)s->d_up, s->adapters, s->K, s->rank, s->N};
+}
+
+// a tensor [n][tokens][width] whose tokens lie ld apart
+static bool tokens_ok(int tokens, int width, size_t ld) { return ld >= (size_t)width && ld <= MAX_COUNT / tokens; }
+
+static size_t tokens_bytes(const ssnet_ctx *ctx, int tokens, int width, size_t ld) { return (((size_t)ctx->n * tokens - 1) * ld + width) * 8; }
+
+// how a call is cut up; false: sizes out of range, or launches of 2^32 threads
+static bool adapters_plan(const ssnet_ctx *ctx, const ssnet_adapters *s, int requests, int tokens, adapter_plan *plan)
+{
+    if (requests < 1 || requests > (1 << 20) || tokens < 1 || tokens > (1 << 24)) return false;
+    *plan = plan_adapters(ctx->n, ctx->t, tokens, requests, s->K, s->rank, s->N);
+    return plan->down_groups <= MAX_SERVING_GROUPS && plan->up_groups <= MAX_SERVING_GROUPS;
+}
+
+}  // namespace
+
+size_t ssnet_adapter_down_bytes(const ssnet_ctx *ctx, int K, int rank)
+{
+    const ssnet_adapters s = {nullptr, nullptr, 1, K, rank, 1};
+    return ctx && adapters_ok(&s, false) ? (2 * ctx->t + 1) * down_party_bytes(K, rank) : 0;
+}
+
+size_t ssnet_adapter_up_bytes(const ssnet_ctx *ctx, int rank, int N)
+{
+    const ssnet_adapters s = {nullptr, nullptr, 1, 1, rank, N};
+    return ctx && adapters_ok(&s, false) ? ctx->n * up_party_bytes(rank, N) : 0;
+}
+
+int ssnet_pack_adapter(ssnet_ctx *ctx, const ssnet_adapters *set, int index, const uint64_t *d_a, const uint64_t *d_b, int rank)
+{
+    if (!ctx || !adapters_ok(set, true) || index < 0 || index >= set->adapters || !d_a || !d_b || rank < 1 || rank > set->rank) return SSNET_EINVAL;
+    timed tm(ctx, SSNET_PROF_PACK_W);
+    hipError_t e = ss_launch_pack_adapter(make_adapters(set), index, d_a, d_b, rank, ctx->n, ctx->t, ctx->stream);
+    return e == hipSuccess ? SSNET_OK : fail_hip(ctx, e);
+}
+
+size_t ssnet_workspace_bytes_adapters(const ssnet_ctx *ctx, const ssnet_adapters *set, int requests, int tokens)
+{
+    adapter_plan plan;
+    return ctx && adapters_ok(set, false) && adapters_plan(ctx, set, requests, tokens, &plan) ? WS_HEADER_BYTES + plan.bytes : 0;
+}
+
+int ssnet_adapters_mod(ssnet_ctx *ctx, const ssnet_adapters *set, const ssnet_requests *requests, const uint64_t *d_x, size_t ld_x, const uint64_t *d_base,
+                       size_t ld_base, uint64_t stream_id, uint64_t *d_y, size_t ld_y)
+{
+    if (!ctx || !adapters_ok(set, true) || !requests || !requests->d_start || !requests->d_adapter || !d_x || !d_y) return SSNET_EINVAL;
+    const int tokens = requests->tokens;
+    adapter_plan plan;
+    if (!adapters_plan(ctx, set, requests->requests, tokens, &plan)) return SSNET_EINVAL;
+    if (!tokens_ok(tokens, set->K, ld_x) || !tokens_ok(tokens, set->N, ld_y) || (d_base && !tokens_ok(tokens, set->N, ld_base))) return SSNET_EINVAL;
+    const size_t out = tokens_bytes(ctx, tokens, set->N, ld_y);
+    if (overlap(d_x, tokens_bytes(ctx, tokens, set->K, ld_x), d_y, out)) return SSNET_EINVAL;
+    if (d_base && overlap(d_base, tokens_bytes(ctx, tokens, set->N, ld_base), d_y, out) && !(d_base == d_y && ld_base == ld_y)) return SSNET_EINVAL;
+    if (scratch_room(ctx) < plan.bytes) return SSNET_EWORKSPACE;
+    const size_t k = ctx->t + 1, nr = 2 * ctx->t + 1, n = ctx->n, count = (size_t)tokens * set->rank;
+    u64 *msg1 = (u64 *)ws_scratch(ctx), *msg2 = msg1 + nr * k * count, *u = msg2 + k * n * count, *wsh = u + k * count;
+    u64 *planes = (u64 *)(ws_scratch(ctx) + plan.messages), *z = (u64 *)(ws_scratch(ctx) + plan.messages + plan.planes);
+    const ss_adapters s = make_adapters(set);
+    const ss_requests req = {requests->d_start, requests->d_adapter, requests->requests, tokens};
+    hipError_t e;
+    {
+        timed tm(ctx, SSNET_PROF_GEMM);
+        e = ss_launch_adapters_down(plan, s, req, d_x, ld_x, planes, ctx->n, ctx->t, ctx->stream);
+    }
+    if (e == hipSuccess) {
+        timed tm(ctx, SSNET_PROF_DEGREE_REDUCE);
+        ss_part_src ps = {};
+        ps.planes = plan.splits;
+        ps.stride = nr * count;
+        ss_tr_params tp = make_tr_params(ctx, stream_id);
+        set_kdiv(ctx, tp, 1);
+        e = ss_launch_degree_reduce_truncate(planes, msg1, msg2, u, wsh, z, nullptr, count, make_dr_params(ctx, stream_id), tp, ps, ctx->stream);
+    }
+    if (e == hipSuccess) {
+        timed tm(ctx, SSNET_PROF_GEMM);
+        e = ss_launch_adapters_up(plan, s, req, z, d_base, ld_base, d_y, ld_y, ctx->n, ctx->t, ctx->stream);
+    }
+    return e == hipSuccess ? SSNET_OK : fail_hip(ctx, e);
+}
+
+static bool sample_ok(int rows, int vocab) { return rows >= 1 && rows <= (1 << 20) && vocab >= 1 && vocab <= SSNET_MAX_VOCAB; }
+
+size_t ssnet_workspace_bytes_sample(const ssnet_ctx *ctx, int rows, int vocab)
+{
+    return ctx && sample_ok(rows, vocab) ? WS_HEADER_BYTES + align256((size_t)rows * vocab * 4) : 0;
+}
+
+int ssnet_sample(ssnet_ctx *ctx, const uint64_t *d_logits, size_t ld, int rows, int vocab, const int *party_ids, int m, const ssnet_sampling *how,
+                 int64_t *d_tokens, int32_t *d_shown)
+{
+    if (!ctx || !d_logits || !how || !how->d_params || !how->d_random || !d_tokens || !d_shown || !sample_ok(rows, vocab)) return SSNET_EINVAL;
+    if (ld < (size_t)vocab || ld > MAX_COUNT / rows || ((uintptr_t)how->d_params & 15)) return SSNET_EINVAL;
+    if (how->d_allowed && (how->ld_allowed < (size_t)(vocab + 31) / 32 || how->ld_allowed > MAX_COUNT / rows)) return SSNET_EINVAL;
+    if (int rc = check_ids(ctx, party_ids, m)) return rc;
+    ss_rec_params rp = {};
+    rp.m = m;
+    for (int i = 0; i < m; i++) rp.plane[i] = party_ids[i] - 1;
+    if (!h_lagrange_int(party_ids, m, rp.ilambda, &rp.dinv)) return SSNET_EINVAL;
+    if (scratch_room(ctx) < ssnet_workspace_bytes_sample(ctx, rows, vocab) - WS_HEADER_BYTES) return SSNET_EWORKSPACE;
+    const ss_sampling q = {(const int4 *)how->d_params, (const long long *)how->d_random, how->d_allowed, how->ld_allowed};
+    timed tm(ctx, SSNET_PROF_RECONSTRUCT);
+    hipError_t e = ss_launch_sample(q, d_logits, ld, rows, vocab, ctx->f, rp, ws_scratch(ctx), (long long *)d_tokens, d_shown, ctx->stream);
+    return e == hipSuccess ? SSNET_OK : fail_hip(ctx, e);
+}
+
 int ssnet_host_lagrange(const ssnet_ctx *ctx, const int *party_ids, int m, uint64_t *out)
 {
     if (!ctx || !party_ids || !out || m < 1 || m > ctx->n) return SSNET_EINVAL;

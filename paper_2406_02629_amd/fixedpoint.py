@@ -54,3 +54,23 @@ def rotary_table(positions: int, frequencies: torch.Tensor, f: int, magnitude: f
     if bool((t.abs() >= 2.0 ** 31).any()):
         raise ValueError("the table does not fit 32 bits")
     return torch.round(t).to(torch.int32).to(device).contiguous()
+
+
+def sampling_parameters(temperature, top_k=0, top_p=1.0, min_p=0.0, rows: int = 1, device=None) -> torch.Tensor:
+    """int32 [rows][4] for SSNet.sample, each argument a number or one for every row: temperature 0.0113 to 1477 (0: the most likely token), top_k
+    (0: all), top_p and min_p between 0 and 1"""
+    def column(v, name, low, high):
+        t = torch.as_tensor(v, dtype=torch.float64)
+        if t.dim() > 1 or (t.dim() == 1 and t.shape[0] != rows):
+            raise ValueError(f"{name} must be a number or one for each of {rows} rows")
+        if not bool(((t >= low) & (t <= high)).all()):
+            raise ValueError(f"{name} must lie between {low} and {high}")
+        return t.expand(rows)
+
+    t = column(temperature, "temperature", 0, 1477)
+    if bool(((t > 0) & (t < 0.0113)).any()):
+        raise ValueError("temperature must be 0 or at least 0.0113")
+    scale = torch.where(t > 0, (2.0 ** 24 / 0.6931471805599453 / t.clamp(min=0.0113)).round(), 0)
+    k = column(top_k, "top_k", 0, 2 ** 31 - 1)
+    p, m = (2.0 ** 30 * column(v, name, 0, 1) for v, name in ((top_p, "top_p"), (min_p, "min_p")))
+    return torch.stack([scale, k, p.round(), m.round()], 1).to(torch.int32).to(device).contiguous()
