@@ -216,15 +216,110 @@ __device__ __forceinline__ u64 fold_items(const v4i (&acc)[4], u64 more)
 #endif
 }
 
-// Step 3.  The contraction is short, so it runs over limbs and rank together: D[s][c] = sum over (j, r) of z_{s-j}[r] B_j[r][c] is diagonal sum s
-// of column c, which makes one MFMA of 16 diagonals by 16 columns for 64 digits of a column, and one accumulator.  A's rows are the
-// digits of z, in LDS with their limbs falling and zeros around them, read from a place that moves up by the rank with every diagonal.
-// One workgroup per (tile of ROWS tokens, part of the columns and party).  Its waves take 32 columns of 16 tokens at a time, or 64 of
-// one.  WIDE: pairs of columns in 16 bytes.
-template <int ROWS, bool WIDE>
-__global__ __launch_bounds__(BLOCK, 2) void up_kernel(adapter_args g)
+// y = base of the tokens of a request without an adapter
+__device__ __forceinline__ void pass_through(const adapter_args &g, const request_tile &r, const u64 *base, u64 *y, int part)
 {
-    extern __shared__ signed char zd[];          // [ROWS][stride]
+    if (base == y) return;
+    for (int t = 0; t < r.count; t++)
+        for (int c = part * BLOCK + threadIdx.x; c < g.N; c += g.col_groups * BLOCK) y[t * g.ld_y + c] = base ? base[t * g.ld_base + c] : 0;
+}
+
+// columns col and col + 1 of a row: both exist, or (!WIDE) at most the first
+template <bool WIDE>
+__device__ __forceinline__ pack_t<2> load_pair(const u64 *row, int col, int N)
+{
+    pack_t<2> v = {{0, 0}};
+    if (WIDE) {
+        if (col < N) v.load(row + col);
+    } else {
+        if (col < N) v.v[0] = row[col];
+        if (col + 1 < N) v.v[1] = row[col + 1];
+    }
+    return v;
+}
+
+template <bool WIDE>
+__device__ __forceinline__ void store_pair(u64 *row, int col, int N, const pack_t<2> &v)
+{
+    if (WIDE) {
+        if (col < N) v.store(row + col);
+    } else {
+        if (col < N) row[col] = v.v[0];
+        if (col + 1 < N) row[col + 1] = v.v[1];
+    }
+}
+
+// Step 3 over limbs and rank together: D[s][c] = sum over (j, r) of z_{s-j}[r] B_j[r][c] is diagonal sum s of column c, which makes one MFMA of 16
+// diagonals by 16 columns for 64 digits of a column, and one accumulator.  A's rows are the digits of z, in LDS with their limbs falling
+// and zeros around them, read from a place that moves up by the rank with every diagonal: limb l of element i of a token lies at (15 - l) R + i.
+__device__ __forceinline__ int diagonals_stride(int R, int steps) { return 15 * R + 64 * steps; }
+
+__device__ __forceinline__ void stage_diagonals(const adapter_args &g, signed char *zd, int rows, int stride, int party, const request_tile &r)
+{
+    const int tid = threadIdx.x;
+    for (int i = tid * 4; i < rows * stride; i += BLOCK * 4) *reinterpret_cast<int *>(zd + i) = 0;
+    __syncthreads();
+    for (int i = tid; i < r.count * g.rank; i += BLOCK) {
+        const int t = i / g.rank, e = i - t * g.rank;
+        const u64 d = balanced_digits(g.z[((size_t)party * g.tokens + r.first) * g.rank + i]);
+#pragma unroll
+        for (int l = 0; l < NL; l++) zd[t * stride + (15 - l) * g.padded + e] = (signed char)(d >> (8 * l));
+    }
+    __syncthreads();
+}
+
+// 64 digits, step m, of the 16 diagonals of a token (8-byte alignment)
+__device__ __forceinline__ v4i diagonals_at(const signed char *zd, int R, int m)
+{
+    const int lane = threadIdx.x & 63;
+    const int2 *p = reinterpret_cast<const int2 *>(zd + (15 - (lane & 15)) * R + (lane >> 4) * 16 + m * 64);
+    const int2 a = p[0], b = p[1];
+    return (v4i){a.x, a.y, b.x, b.y};
+}
+
+// Single tokens.  One workgroup per (token, part of the columns and party); a wave takes 64 columns at a time.
+__global__ __launch_bounds__(BLOCK, 2) void up_single_kernel(adapter_args g)
+{
+    extern __shared__ signed char zd[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int part = blockIdx.y / g.n, party = blockIdx.y - part * g.n;
+    request_tile r;
+    if (!tile_at(g, blockIdx.x, 1, r)) return;
+    const u64 *base = g.base ? g.base + ((size_t)party * g.tokens + r.first) * g.ld_base : nullptr;
+    u64 *y = g.y + ((size_t)party * g.tokens + r.first) * g.ld_y;
+    if (r.adapter < 0) {
+        pass_through(g, r, base, y, part);
+        return;
+    }
+    const int R = g.padded, chunks = NL * R / 16, steps = (chunks + 3) >> 2, halves = 2 * ((g.N + 31) >> 5), q = lane >> 4, c16 = lane & 15;
+    stage_diagonals(g, zd, 1, diagonals_stride(R, steps), party, r);
+    const signed char *b = g.up + r.adapter * g.up_bytes + party * g.up_party + c16 * 16;
+    for (int u = part * 4 + wave; u * 64 < g.N; u += g.col_groups * 4) {
+        v4i acc[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) acc[i] = (v4i){0, 0, 0, 0};
+        const int col = 64 * u + 32 * (q >> 1) + 2 * c16 + (q & 1);
+        const u64 more = base && col < g.N ? base[col] : 0;
+        for (int m = 0; m < steps; m++) {
+            const v4i a = diagonals_at(zd, R, m);
+            const int chunk = 4 * m + q;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const v4i v = *reinterpret_cast<const v4i *>(b + ((size_t)min(4 * u + i, halves - 1) * chunks + min(chunk, chunks - 1)) * 256);
+                acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, chunk < chunks ? v : (v4i){0, 0, 0, 0}, acc[i], 0, 0, 0);
+            }
+        }
+        const u64 o = fold_items(acc, more);
+        if (col < g.N) y[col] = o;
+    }
+}
+
+// Tiles of ROWS tokens of a request whose rank takes M products: the digits of all of them stay in registers, a wave takes 32 columns of B at a
+// time, the next 32 and the base's on their way.
+template <int M, int ROWS, bool WIDE>
+__global__ __launch_bounds__(BLOCK, 2) void up_diagonals_kernel(adapter_args g)
+{
+    extern __shared__ signed char zd[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = blockIdx.y / g.n, party = blockIdx.y - part * g.n;
     request_tile r;
@@ -232,94 +327,124 @@ __global__ __launch_bounds__(BLOCK, 2) void up_kernel(adapter_args g)
     const u64 *base = g.base ? g.base + ((size_t)party * g.tokens + r.first) * g.ld_base : nullptr;
     u64 *y = g.y + ((size_t)party * g.tokens + r.first) * g.ld_y;
     if (r.adapter < 0) {
-        if (base == y) return;
-        for (int t = 0; t < r.count; t++)
-            for (int c = part * BLOCK + tid; c < g.N; c += g.col_groups * BLOCK) y[t * g.ld_y + c] = base ? base[t * g.ld_base + c] : 0;
+        pass_through(g, r, base, y, part);
         return;
     }
-    const int R = g.padded, chunks = NL * R / 16, steps = (chunks + 3) >> 2, stride = 15 * R + 64 * steps;
-    // limb l of element i of a token's z lies at (15 - l) R + i
-    for (int i = tid * 4; i < ROWS * stride; i += BLOCK * 4) *reinterpret_cast<int *>(zd + i) = 0;
-    __syncthreads();
-    for (int i = tid; i < r.count * g.rank; i += BLOCK) {
-        const int t = i / g.rank, e = i - t * g.rank;
-        const u64 d = balanced_digits(g.z[((size_t)party * g.tokens + r.first) * g.rank + i]);
-#pragma unroll
-        for (int l = 0; l < NL; l++) zd[t * stride + (15 - l) * R + e] = (signed char)(d >> (8 * l));
-    }
-    __syncthreads();
-    const int q = lane >> 4, c16 = lane & 15;
-    const signed char *z = zd + (15 - c16) * R + q * 16;
-    auto digits = [&](int t, int m) {            // (8-byte alignment)
-        const int2 *p = reinterpret_cast<const int2 *>(z + t * stride + m * 64);
-        const int2 a = p[0], b = p[1];
-        return (v4i){a.x, a.y, b.x, b.y};
-    };
-    const size_t half = (size_t)chunks * 256;    // bytes of 16 columns
+    const int R = g.padded, chunks = NL * R / 16, stride = diagonals_stride(R, M), q = lane >> 4, c16 = lane & 15;
     const signed char *b = g.up + r.adapter * g.up_bytes + party * g.up_party + c16 * 16;
-    auto columns = [&](size_t at, int m) {
-        const int chunk = 4 * m + q;
-        const v4i v = *reinterpret_cast<const v4i *>(b + at * half + (size_t)min(chunk, chunks - 1) * 256);
-        return chunk < chunks ? v : (v4i){0, 0, 0, 0};
+    const int units = (g.N + 31) >> 5, step = g.col_groups * 4;
+    int u = part * 4 + wave;
+    auto load = [&](int unit, v4i (&w)[2][M], pack_t<2> (&more)[ROWS / 4]) {
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int m = 0; m < M; m++) {
+                const int chunk = 4 * m + q;
+                w[h][m] = *reinterpret_cast<const v4i *>(b + ((size_t)(2 * unit + h) * chunks + min(chunk, chunks - 1)) * 256);
+                if (NL != 8 && chunk >= chunks) w[h][m] = (v4i){0, 0, 0, 0};
+            }
+#pragma unroll
+        for (int t = 0; t < ROWS / 4; t++)
+            more[t] = base ? load_pair<WIDE>(base + (size_t)min(4 * t + q, r.count - 1) * g.ld_base, 32 * unit + 2 * c16, g.N) : pack_t<2>{{0, 0}};
     };
-    if constexpr (ROWS == 1) {
-        const int halves = 2 * ((g.N + 31) >> 5);
-        for (int u = part * 4 + wave; u * 64 < g.N; u += g.col_groups * 4) {
-            v4i acc[4];
+    v4i w[2][M], next[2][M], a[ROWS][M];
+    pack_t<2> more[ROWS / 4], more_next[ROWS / 4];
+    if (u < units) load(u, w, more);
+    stage_diagonals(g, zd, ROWS, stride, party, r);
 #pragma unroll
-            for (int i = 0; i < 4; i++) acc[i] = (v4i){0, 0, 0, 0};
-            const int col = 64 * u + 32 * (q >> 1) + 2 * c16 + (q & 1);
-            const u64 more = base && col < g.N ? base[col] : 0;
-            for (int m = 0; m < steps; m++) {
-                const v4i a = digits(0, m);
+    for (int t = 0; t < ROWS; t++)
 #pragma unroll
-                for (int i = 0; i < 4; i++)
-                    acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, columns((size_t)min(4 * u + i, halves - 1), m), acc[i], 0, 0, 0);
-            }
-            const u64 o = fold_items(acc, more);
-            if (col < g.N) y[col] = o;
-        }
-    } else {
-        for (int u = part * 4 + wave; u * 32 < g.N; u += g.col_groups * 4) {
-            v4i acc[2][ROWS];
+        for (int m = 0; m < M; m++) a[t][m] = diagonals_at(zd + t * stride, R, m);
+    for (; u < units; u += step) {
+        load(min(u + step, units - 1), next, more_next);   // (behind the last, some again)
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < ROWS; t++) acc[0][t] = acc[1][t] = (v4i){0, 0, 0, 0};
-            for (int m = 0; m < steps; m++) {
-                const v4i b0 = columns(2 * (size_t)u, m), b1 = columns(2 * (size_t)u + 1, m);
+        for (int t0 = 0; t0 < ROWS; t0 += 4) {
+            if (t0 >= r.count) break;
+            v4i acc[2][4];
 #pragma unroll
-                for (int t = 0; t < ROWS; t++) {
-                    const v4i a = digits(t, m);
-                    acc[0][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b0, acc[0][t], 0, 0, 0);
-                    acc[1][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b1, acc[1][t], 0, 0, 0);
-                }
-            }
-            const int col = 32 * u + 2 * c16;
-#pragma unroll
-            for (int t0 = 0; t0 < ROWS; t0 += 4) {
-                const int t = t0 + q;
-                const bool live = t < r.count;
-                pack_t<2> v = {{0, 0}};
-                if (base && live) {
-                    if (WIDE) {
-                        if (col < g.N) v.load(base + t * g.ld_base + col);
-                    } else {
-                        if (col < g.N) v.v[0] = base[t * g.ld_base + col];
-                        if (col + 1 < g.N) v.v[1] = base[t * g.ld_base + col + 1];
-                    }
-                }
+            for (int i = 0; i < 4; i++)
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
-                    const v4i four[4] = {acc[h][t0], acc[h][t0 + 1], acc[h][t0 + 2], acc[h][t0 + 3]};
-                    v.v[h] = fold_items(four, v.v[h]);
+                    acc[h][i] = (v4i){0, 0, 0, 0};
+#pragma unroll
+                    for (int m = 0; m < M; m++) acc[h][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[t0 + i][m], w[h][m], acc[h][i], 0, 0, 0);
                 }
-                if (!live) continue;
-                if (WIDE) {
-                    if (col < g.N) v.store(y + t * g.ld_y + col);
-                } else {
-                    if (col < g.N) y[t * g.ld_y + col] = v.v[0];
-                    if (col + 1 < g.N) y[t * g.ld_y + col + 1] = v.v[1];
+            pack_t<2> o;
+#pragma unroll
+            for (int h = 0; h < 2; h++) o.v[h] = fold_items(acc[h], more[t0 / 4].v[h]);
+            if (t0 + q < r.count) store_pair<WIDE>(y + (size_t)(t0 + q) * g.ld_y, 32 * u + 2 * c16, g.N, o);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int m = 0; m < M; m++) w[h][m] = next[h][m];
+#pragma unroll
+        for (int t = 0; t < ROWS / 4; t++) more[t] = more_next[t];
+    }
+}
+
+// Tiles of 16 tokens of a request with a larger rank: diagonal sums apart, as in a dense layer; the digits of z in LDS in MFMA order, a wave takes
+// 32 columns of B at a time.
+template <bool WIDE>
+__global__ __launch_bounds__(BLOCK, 2) void up_tile_kernel(adapter_args g)
+{
+    extern __shared__ v4i zt[];                  // [rank / 64][limb][64 lanes]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int part = blockIdx.y / g.n, party = blockIdx.y - part * g.n;
+    request_tile r;
+    if (!tile_at(g, blockIdx.x, 16, r)) return;
+    const u64 *base = g.base ? g.base + ((size_t)party * g.tokens + r.first) * g.ld_base : nullptr;
+    u64 *y = g.y + ((size_t)party * g.tokens + r.first) * g.ld_y;
+    if (r.adapter < 0) {
+        pass_through(g, r, base, y, part);
+        return;
+    }
+    const int per_limb = g.padded / 16, chunks = NL * per_limb, blocks = (g.rank + 63) >> 6, q = lane >> 4, c16 = lane & 15;
+    const u64 *z = g.z + ((size_t)party * g.tokens + r.first) * g.rank;
+    for (int i = tid; i < 16 * blocks * 16; i += BLOCK) {      // four elements of a row
+        const int row = i & 15, e = (i >> 4) * 4;
+        u64 v[4];
+#pragma unroll
+        for (int c = 0; c < 4; c++) v[c] = balanced_digits(row < r.count && e + c < g.rank ? z[(size_t)row * g.rank + e + c] : 0);
+        u32 *dst = reinterpret_cast<u32 *>(zt + (e >> 6) * TILE + row + 16 * ((e & 63) >> 4)) + ((e & 15) >> 2);
+#pragma unroll
+        for (int l = 0; l < NL; l++) dst[l * 256] = limb_dword(v, l);
+    }
+    __syncthreads();
+    const signed char *b = g.up + r.adapter * g.up_bytes + party * g.up_party + c16 * 16;
+    const int units = (g.N + 31) >> 5;
+    for (int u = part * 4 + wave; u < units; u += g.col_groups * 4) {
+        v4i acc[2][ND];
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int s = 0; s < ND; s++) acc[h][s] = (v4i){0, 0, 0, 0};
+        for (int kb = 0; kb < blocks; kb++) {
+            // (behind the rank the digits of z are 0)
+            const signed char *src = b + ((size_t)(2 * u) * chunks + min(4 * kb + q, per_limb - 1)) * 256;
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                v4i w[NL];
+#pragma unroll
+                for (int j = 0; j < NL; j++) w[j] = *reinterpret_cast<const v4i *>(src + (size_t)(h * chunks + j * per_limb) * 256);
+#pragma unroll
+                for (int i = 0; i < NL; i++) {
+                    const v4i x = zt[kb * TILE + i * 64 + lane];
+#pragma unroll
+                    for (int j = 0; j < NL; j++) acc[h][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, w[j], acc[h][i + j], 0, 0, 0);
                 }
             }
+        }
+        const int col = 32 * u + 2 * c16;
+#pragma unroll
+        for (int c = 0; c < 4; c++) {
+            const int row = 4 * q + c;
+            if (row >= r.count) continue;
+            pack_t<2> o = base ? load_pair<WIDE>(base + (size_t)row * g.ld_base, col, g.N) : pack_t<2>{{0, 0}};
+            o.v[0] = fold_diagonals(acc[0], c, o.v[0]);
+            o.v[1] = fold_diagonals(acc[1], c, o.v[1]);
+            store_pair<WIDE>(y + (size_t)row * g.ld_y, col, g.N, o);
         }
     }
 }
@@ -367,14 +492,22 @@ hipError_t ss_launch_adapters_up(const adapter_plan &plan, const ss_adapters &s,
     g.up_party = up_party_bytes(s.rank, s.N), g.up_bytes = n * g.up_party;
     g.z = z, g.base = base, g.ld_base = ld_base, g.y = y, g.ld_y = ld_y;
     g.col_groups = plan.col_groups;
-    const int steps = (int)div_up(SS_NLIMB * g.padded, 64);
-    const size_t lds = (size_t)plan.up_rows * (15 * g.padded + 64 * steps);
+    const int steps = (int)up_steps(s.rank);
+    const size_t lds = plan.up == UP_TILE ? div_up(s.rank, 64) * TILE * 16 : (size_t)plan.up_rows * (15 * g.padded + 64 * steps);
     const dim3 grid((unsigned)request_tiles(req.tokens, req.requests, plan.up_rows), n * plan.col_groups);
     const bool wide = s.N % 2 == 0 && ld_y % 2 == 0 && aligned16(y) && (!base || (ld_base % 2 == 0 && aligned16(base)));
-    if (plan.up_rows == 1)
-        hipLaunchKernelGGL((up_kernel<1, false>), grid, dim3(BLOCK), lds, stream, g);
+#define SS_UP(M) hipLaunchKernelGGL((wide ? up_diagonals_kernel<M, 8, true> : up_diagonals_kernel<M, 8, false>), grid, dim3(BLOCK), lds, stream, g)
+    if (plan.up == UP_SINGLE)
+        hipLaunchKernelGGL(up_single_kernel, grid, dim3(BLOCK), lds, stream, g);
+    else if (plan.up == UP_TILE)
+        hipLaunchKernelGGL((wide ? up_tile_kernel<true> : up_tile_kernel<false>), grid, dim3(BLOCK), lds, stream, g);
+    else if (steps == 1)
+        SS_UP(1);
+    else if (steps == 2)
+        SS_UP(2);
     else
-        hipLaunchKernelGGL((wide ? up_kernel<16, true> : up_kernel<16, false>), grid, dim3(BLOCK), lds, stream, g);
+        SS_UP((SS_NLIMB / 2));                   // a rank of 17 to 32
+#undef SS_UP
     return hipGetLastError();
 }
 

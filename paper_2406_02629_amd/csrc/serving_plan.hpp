@@ -14,16 +14,21 @@ inline size_t div_up(size_t a, size_t b) { return (a + b - 1) / b; }
 //   down [2t+1][K / 64][limb][4][rank][16] int8: byte b of quarter q is element k = 64 block + 8 (b / 2) + 2 q + b % 2 of the contraction, so
 //     that four lanes find 8 elements of a row of x in 64 bytes; past K zeros
 //   up [n][N / 32][2][limb R / 16][16][16] int8: column 32 block + 2 c + h is number c of half h, whose 16 bytes of a chunk are consecutive digits
-//     in the order limb, rank (R: the rank in whole eights, zeros behind it); past N zeros
-inline size_t padded_rank(size_t rank) { return (rank + 7) & ~(size_t)7; }
+//     in the order limb, rank (R: 8, or the rank in whole sixteens, zeros behind it); past N zeros
+inline size_t padded_rank(size_t rank) { return rank <= 8 ? 8 : (rank + 15) & ~(size_t)15; }
+inline size_t up_steps(size_t rank) { return div_up(SS_NLIMB * padded_rank(rank), 64); }   // products that the digits of a column take
 inline size_t down_party_bytes(int K, int rank) { return div_up(K, 64) * SS_NLIMB * 64 * rank; }
 inline size_t up_party_bytes(int rank, int N) { return div_up(N, 32) * 2 * SS_NLIMB * padded_rank(rank) * 16; }
 
 constexpr size_t MAX_SERVING_GROUPS = ((size_t)1 << 24) - 1;   // workgroups of 256 threads in a launch: less than 2^32 threads
 constexpr int MAX_PLANES = 8;                                  // partial sums of the first product, which the reduction adds
 
+// The kernel of the second product: tokens one by one, in tiles with all digits of their z in registers, or in tiles with the diagonals apart.
+enum up_kind { UP_SINGLE, UP_DIAGONALS, UP_TILE };
+
 struct adapter_plan {
     int down_rows, up_rows;       // tokens to a tile
+    up_kind up;
     int rank_tiles;               // of 16, of the first product
     int splits, run;              // its contraction: in `splits` runs of `run` blocks of 64
     int col_groups;               // workgroups that share the columns of a tile of the second product
@@ -39,7 +44,8 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
     adapter_plan p = {};
     const size_t nr = 2 * t + 1, k = t + 1, count = (size_t)tokens * rank, blocks = div_up(K, 64);
     p.down_rows = 16;
-    p.up_rows = tokens <= 2 * (size_t)requests ? 1 : 16;
+    p.up = tokens <= 2 * (size_t)requests ? UP_SINGLE : rank <= 32 ? UP_DIAGONALS : UP_TILE;
+    p.up_rows = p.up == UP_SINGLE ? 1 : p.up == UP_DIAGONALS ? 8 : 16;
     p.rank_tiles = (int)div_up(rank, 16);
     const size_t tiles = request_tiles(tokens, requests, p.down_rows) * nr * p.rank_tiles;
     p.splits = (int)std::max<size_t>(1, std::min(std::min<size_t>(MAX_PLANES, div_up(512, tiles)), blocks / 8));

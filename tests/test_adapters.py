@@ -101,7 +101,7 @@ def test_refusals_before_any_launch():
     # 2t+1 parties, blocks of 64 elements with 64 bytes a limb and rank; n parties, blocks of 32 columns
     assert lib.ssnet_adapter_down_bytes(ctx, 100, 5) == 5 * 2 * 8 * 64 * 5 and lib.ssnet_adapter_up_bytes(ctx, 5, 33) == 5 * 64 * 8 * 8
     other = SSNet(4, 1, p=P45, device=None)
-    assert other.lib.ssnet_adapter_down_bytes(other._ctx, 64, 16) == 3 * 6 * 64 * 16 and other.lib.ssnet_adapter_up_bytes(other._ctx, 17, 32) == 4 * 32 * 6 * 24
+    assert other.lib.ssnet_adapter_down_bytes(other._ctx, 64, 16) == 3 * 6 * 64 * 16 and other.lib.ssnet_adapter_up_bytes(other._ctx, 17, 32) == 4 * 32 * 6 * 32
     assert lib.ssnet_adapter_down_bytes(ctx, 0, 5) == lib.ssnet_adapter_up_bytes(ctx, 129, 5) == lib.ssnet_adapter_down_bytes(None, 1, 1) == 0
     one, many = (lib.ssnet_workspace_bytes_adapters(ctx, C.byref(sets), 1, k) for k in (1, 600))
     assert binding.WS_HEADER_BYTES < one < many and lib.ssnet_workspace_bytes_adapters(ctx, C.byref(sets), 0, 1) == 0
