@@ -68,7 +68,9 @@ struct adapter_args {
     size_t ld_x, ld_base, ld_y;
     u64 *planes, *y;                // planes [splits][2t+1][tokens][rank]
     const u64 *z;                   // [n][tokens][rank]
-    int nr, n, rank_tiles, run, col_groups;
+    int nr, n, run, col_groups;
+    unsigned tiles;                 // that the requests can have
+    fdiv dTiles;
     size_t plane;                   // 2t+1 shares
 };
 
@@ -110,105 +112,142 @@ __device__ __forceinline__ bool tile_at(const adapter_args &g, int tile, int row
     return false;
 }
 
-// 16 elements of a row for a lane of quarter q, in the order of the laid out A; past the row's end anything (A is zero there)
-template <bool WIDE>
-__device__ __forceinline__ void load_row(const u64 *row, int k0, int K, u64 (&v)[16])
-{
-#pragma unroll
-    for (int j = 0; j < 8; j++) {
-        const int k = k0 + 8 * j;
-        if constexpr (WIDE) {
-            pack_t<2> p;
-            p.load(row + (k < K ? k : 0));
-            v[2 * j] = p.v[0], v[2 * j + 1] = p.v[1];
-        } else {
-            v[2 * j] = row[k < K ? k : 0];
-            v[2 * j + 1] = row[k + 1 < K ? k + 1 : 0];
-        }
-    }
-}
-
-// Step 1: one workgroup per (tile of 16 tokens, 16 columns of A, party and run of the contraction); its four waves take every fourth block of 64
-// elements, and add their sums up in LDS as whole numbers.
-template <bool WIDE>
+// Step 1: one workgroup per (tile of 16 tokens, party and run of the contraction).  Its four waves share the columns of A between CW and the blocks of
+// 64 elements between 4 / CW; a wave takes CT times 16 columns.  Elements become digits where they are loaded: those that several waves need
+// go through LDS, each wave bringing a part.  The next block's elements and digits of A are on their way while those at hand are multiplied.
+template <int CW, int CT, bool WIDE>
 __global__ __launch_bounds__(BLOCK, 2) void down_kernel(adapter_args g)
 {
-    __shared__ int sums[ND][BLOCK];
+    constexpr int KW = 4 / CW, PAIRS = 8 / CW, WORDS = 4 / CW;
+    __shared__ v4i xd[CW > 1 ? 2 : 1][CW > 1 ? KW * TILE : 1];
+    __shared__ int sums[KW > 1 ? CW : 1][KW > 1 ? ND : 1][BLOCK];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int column = blockIdx.y / g.nr, party = blockIdx.y - column * g.nr, split = blockIdx.z;
+    const unsigned slot = xcd_slot(blockIdx.x, gridDim.x), run = fd_div(slot, g.dTiles);
+    const int cw = wave % CW, kw = wave / CW, split = (int)(run / (unsigned)g.nr), party = (int)run - split * g.nr, q = lane >> 4, c16 = lane & 15;
     request_tile r;
-    if (!tile_at(g, blockIdx.x, 16, r)) return;
-    u64 *out = g.planes + split * g.plane + (size_t)party * g.tokens * g.rank;
-    const int token = tid >> 4, c = column * 16 + (tid & 15);
-    const bool live = token < r.count && c < g.rank;
-    const size_t at = (size_t)(r.first + token) * g.rank + c;
+    if (!tile_at(g, (int)(slot - run * g.tiles), 16, r)) return;
+    u64 *out = g.planes + split * g.plane + ((size_t)party * g.tokens + r.first) * g.rank;
     if (r.adapter < 0) {
-        if (live) out[at] = 0;
+        for (int i = tid; i < r.count * g.rank; i += BLOCK) out[i] = 0;
         return;
     }
-#pragma unroll
-    for (int s = 0; s < ND; s++) sums[s][tid] = 0;
-    __syncthreads();
-    const int blocks = (g.K + 63) >> 6, end = min((split + 1) * g.run, blocks);
-    const u64 *row = g.x + ((size_t)party * g.tokens + r.first + min(lane & 15, r.count - 1)) * g.ld_x;
-    const signed char *a = g.down + r.adapter * g.down_bytes + party * g.down_party + ((size_t)(lane >> 4) * g.rank + min(column * 16 + (lane & 15), g.rank - 1)) * 16;
+    if constexpr (KW > 1) {
+        for (int i = tid; i < CW * ND * BLOCK; i += BLOCK) (&sums[0][0][0])[i] = 0;
+    }
+    const int begin = split * g.run, end = min(begin + g.run, (g.K + 63) >> 6), turns = (end - begin + KW - 1) / KW;
+    const u64 *row = g.x + ((size_t)party * g.tokens + r.first + min(c16, r.count - 1)) * g.ld_x;
     const size_t limb = (size_t)g.rank * 64;
-    v4i acc[ND];
+    const signed char *a = g.down + r.adapter * g.down_bytes + party * g.down_party + (size_t)q * g.rank * 16;
+    size_t column[CT];
 #pragma unroll
-    for (int s = 0; s < ND; s++) acc[s] = (v4i){0, 0, 0, 0};
-    for (int kb = split * g.run + wave; kb < end; kb += 4) {
-        v4i w[NL];
+    for (int c = 0; c < CT; c++) column[c] = (size_t)min((cw * CT + c) * 16 + c16, g.rank - 1) * 16;
+    // this wave's part of a lane's 16 elements of block kb; past the row's end anything (A is zero there)
+    auto load_x = [&](int kb, u64 (&v)[2 * PAIRS]) {
 #pragma unroll
-        for (int l = 0; l < NL; l++) w[l] = *reinterpret_cast<const v4i *>(a + (size_t)kb * NL * limb + l * limb);
-        u64 v[16];
-        load_row<WIDE>(row, 64 * kb + 2 * (lane >> 4), g.K, v);
-        u32 d[4][8];
+        for (int j = 0; j < PAIRS; j++) {
+            const int k = 64 * kb + 2 * q + 8 * (cw * PAIRS + j);
+            if constexpr (WIDE) {
+                pack_t<2> p;
+                p.load_streaming(row + (k < g.K ? k : 0));
+                v[2 * j] = p.v[0], v[2 * j + 1] = p.v[1];
+            } else {
+                v[2 * j] = row[k < g.K ? k : 0];
+                v[2 * j + 1] = row[k + 1 < g.K ? k + 1 : 0];
+            }
+        }
+    };
+    auto load_a = [&](int kb, int c, v4i (&w)[NL]) {
 #pragma unroll
-        for (int b = 0; b < 4; b++) {
+        for (int l = 0; l < NL; l++) w[l] = *reinterpret_cast<const v4i *>(a + (size_t)kb * NL * limb + l * limb + column[c]);
+    };
+    v4i acc[CT][ND], w[NL], next[NL];
+    u64 v[2 * PAIRS];
+#pragma unroll
+    for (int c = 0; c < CT; c++)
+#pragma unroll
+        for (int s = 0; s < ND; s++) acc[c][s] = (v4i){0, 0, 0, 0};
+    int kb = begin + kw;
+    load_x(min(kb, end - 1), v);
+    load_a(min(kb, end - 1), 0, w);
+    for (int turn = 0; turn < turns; turn++) {
+        const bool live = kb < end;
+        const int kb_next = kb + KW;
+        u32 d[WORDS][8];
+#pragma unroll
+        for (int b = 0; b < WORDS; b++) {
             const u64 y[4] = {balanced_digits(v[4 * b]), balanced_digits(v[4 * b + 1]), balanced_digits(v[4 * b + 2]), balanced_digits(v[4 * b + 3])};
             limb_dwords(y, d[b]);
         }
+        const v4i *tile = nullptr;
+        if constexpr (CW > 1) {
+            tile = &xd[turn & 1][kw * TILE + lane];
 #pragma unroll
-        for (int i = 0; i < NL; i++) {
-            const v4i x = (v4i){(int)d[0][i], (int)d[1][i], (int)d[2][i], (int)d[3][i]};
+            for (int l = 0; l < NL; l++)
 #pragma unroll
-            for (int j = 0; j < NL; j++) acc[i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, w[j], acc[i + j], 0, 0, 0);
+                for (int b = 0; b < WORDS; b++) reinterpret_cast<u32 *>(&xd[turn & 1][kw * TILE + l * 64 + lane])[cw * WORDS + b] = d[b][l];
         }
+        load_x(min(kb_next, end - 1), v);
+        if constexpr (CW > 1) __syncthreads();
+#pragma unroll
+        for (int c = 0; c < CT; c++) {
+            load_a(min(c + 1 < CT ? kb : kb_next, end - 1), c + 1 < CT ? c + 1 : 0, next);
+            __builtin_amdgcn_sched_barrier(0);       // the loads leave before the products
+            if (live) {
+#pragma unroll
+                for (int i = 0; i < NL; i++) {
+                    v4i x;
+                    if constexpr (CW > 1)
+                        x = tile[i * 64];
+                    else
+                        x = (v4i){(int)d[0][i], (int)d[1][i], (int)d[2][i], (int)d[3][i]};
+#pragma unroll
+                    for (int j = 0; j < NL; j++) acc[c][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, w[j], acc[c][i + j], 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int l = 0; l < NL; l++) w[l] = next[l];
+        }
+        kb = kb_next;
     }
+    if constexpr (KW > 1) {                          // the sums of several waves, as whole numbers
+        __syncthreads();
 #pragma unroll
-    for (int s = 0; s < ND; s++)
+        for (int s = 0; s < ND; s++)
 #pragma unroll
-        for (int q = 0; q < 4; q++) atomicAdd(&sums[s][(4 * (lane >> 4) + q) * 16 + (lane & 15)], acc[s][q]);
-    __syncthreads();
-    if (!live) return;
-    v4i total[ND];
+            for (int i = 0; i < 4; i++) atomicAdd(&sums[cw][s][(4 * q + i) * 16 + c16], acc[0][s][i]);
+        __syncthreads();
+        const int token = tid >> 4;
 #pragma unroll
-    for (int s = 0; s < ND; s++) total[s][0] = sums[s][tid];
-    out[at] = fold_diagonals(total, 0);
+        for (int c = 0; c < CW; c++) {
+            const int col = c * 16 + (tid & 15);
+            if (token >= r.count || col >= g.rank) continue;
+            v4i total[ND];
+#pragma unroll
+            for (int s = 0; s < ND; s++) total[s][0] = sums[c][s][tid];
+            out[token * g.rank + col] = fold_diagonals(total, 0);
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < CT; c++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int token = 4 * q + i, col = (cw * CT + c) * 16 + c16;
+                if (token < r.count && col < g.rank) out[token * g.rank + col] = fold_diagonals(acc[c], i);
+            }
+    }
 }
 
 // Words that four rows of 16 lanes hold of four items, one part of each: afterwards row q has the four parts of item q.
-__device__ __forceinline__ void exchange(long long (&g)[4])
+__device__ __forceinline__ void exchange(int (&v)[4])
 {
-    u32 h[2][4];
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
-        const auto a = __builtin_amdgcn_permlane32_swap((u32)((u64)g[0] >> (32 * i)), (u32)((u64)g[2] >> (32 * i)), false, false);   // parts 0 1 of items 0 and 2, 2 3
-        const auto b = __builtin_amdgcn_permlane32_swap((u32)((u64)g[1] >> (32 * i)), (u32)((u64)g[3] >> (32 * i)), false, false);
-        const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-        h[i][0] = lo[0], h[i][1] = lo[1], h[i][2] = hi[0], h[i][3] = hi[1];
-    }
-#pragma unroll
-    for (int q = 0; q < 4; q++) g[q] = (long long)((u64)h[1][q] << 32 | h[0][q]);
+    const auto a = __builtin_amdgcn_permlane32_swap((u32)v[0], (u32)v[2], false, false);   // parts 0 and 1 of items 0 and 2, parts 2 and 3
+    const auto b = __builtin_amdgcn_permlane32_swap((u32)v[1], (u32)v[3], false, false);
+    const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    v[0] = (int)lo[0], v[1] = (int)lo[1], v[2] = (int)hi[0], v[3] = (int)hi[1];
 }
 
-// four items' diagonal sums 4 q .. 4 q + 3 of a column in row q -> in row q item q's field element plus `more`
-__device__ __forceinline__ u64 fold_items(const v4i (&acc)[4], u64 more)
+__device__ __forceinline__ u64 fold_parts(const long long (&g)[4], u64 more)
 {
-    long long g[4];
-#pragma unroll
-    for (int i = 0; i < 4; i++) g[i] = join4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
-    exchange(g);
 #if defined(SS_FIELD_P45)
     return fold_words((u64)(g[0] + WORD_OFFSET), (u64)(g[1] + WORD_OFFSET), (u64)(g[2] + WORD_OFFSET), more);
 #else
@@ -216,35 +255,80 @@ __device__ __forceinline__ u64 fold_items(const v4i (&acc)[4], u64 more)
 #endif
 }
 
+// Four items' diagonal sums 4 q .. 4 q + 3 of a column in row q -> in row q item q's field element plus `more`.  SHORT: sums below 2^22 (a rank of at
+// most 32: 8 * 32 * 2^14), two of which fit 32 bits.
+template <bool SHORT>
+__device__ __forceinline__ u64 fold_items(const v4i (&acc)[4], u64 more)
+{
+    int lo[4], hi[4];
+    long long g[4];
+    if constexpr (SHORT) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            lo[i] = acc[i][0] + (int)((u32)acc[i][1] << 8);
+            hi[i] = acc[i][2] + (int)((u32)acc[i][3] << 8);
+        }
+        exchange(lo), exchange(hi);
+#pragma unroll
+        for (int q = 0; q < 4; q++) g[q] = mad_i64(hi[q], 1 << 16, (long long)lo[q]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const long long w = join4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+            lo[i] = (int)w, hi[i] = (int)(w >> 32);
+        }
+        exchange(lo), exchange(hi);
+#pragma unroll
+        for (int q = 0; q < 4; q++) g[q] = (long long)((u64)(u32)hi[q] << 32 | (u32)lo[q]);
+    }
+    return fold_parts(g, more);
+}
+
+// y = 0 in the rows of all requests, where there is no base
+__global__ __launch_bounds__(BLOCK) void clear_kernel(adapter_args g)
+{
+    const int first = min(max(fixed_at(g.start, 0), 0), g.tokens), last = min(fixed_at(g.start, g.requests), g.tokens);
+    for (int t = first + (int)blockIdx.x; t < last; t += gridDim.x)
+        for (int c = threadIdx.x; c < g.N; c += BLOCK) g.y[((size_t)blockIdx.y * g.tokens + t) * g.ld_y + c] = 0;
+}
+
 // y = base of the tokens of a request without an adapter
 __device__ __forceinline__ void pass_through(const adapter_args &g, const request_tile &r, const u64 *base, u64 *y, int part)
 {
     if (base == y) return;
     for (int t = 0; t < r.count; t++)
-        for (int c = part * BLOCK + threadIdx.x; c < g.N; c += g.col_groups * BLOCK) y[t * g.ld_y + c] = base ? base[t * g.ld_base + c] : 0;
+        for (int c = part * BLOCK + threadIdx.x; c < g.N; c += g.col_groups * BLOCK) y[t * g.ld_y + c] = base[t * g.ld_base + c];
 }
 
-// columns col and col + 1 of a row: both exist, or (!WIDE) at most the first
-template <bool WIDE>
+// How a tensor is read and written: element by element, two neighbours in 16 bytes, or these past the caches
+enum access { NARROW, PAIRS, STREAM_PAIRS };
+
+// columns col and col + 1 of a row of N (NARROW: at most the first may exist)
+template <access MODE>
 __device__ __forceinline__ pack_t<2> load_pair(const u64 *row, int col, int N)
 {
     pack_t<2> v = {{0, 0}};
-    if (WIDE) {
-        if (col < N) v.load(row + col);
-    } else {
-        if (col < N) v.v[0] = row[col];
-        if (col + 1 < N) v.v[1] = row[col + 1];
+    if (col < N) {
+        if constexpr (MODE == STREAM_PAIRS)
+            v.load_streaming(row + col);
+        else if constexpr (MODE == PAIRS)
+            v.load(row + col);
+        else {
+            v.v[0] = row[col];
+            if (col + 1 < N) v.v[1] = row[col + 1];
+        }
     }
     return v;
 }
 
-template <bool WIDE>
+template <access MODE>
 __device__ __forceinline__ void store_pair(u64 *row, int col, int N, const pack_t<2> &v)
 {
-    if (WIDE) {
-        if (col < N) v.store(row + col);
-    } else {
-        if (col < N) row[col] = v.v[0];
+    if (col >= N) return;
+    if constexpr (MODE != NARROW)
+        v.template send<MODE == STREAM_PAIRS>(row + col);
+    else {
+        row[col] = v.v[0];
         if (col + 1 < N) row[col + 1] = v.v[1];
     }
 }
@@ -285,7 +369,7 @@ __global__ __launch_bounds__(BLOCK, 2) void up_single_kernel(adapter_args g)
     const int part = blockIdx.y / g.n, party = blockIdx.y - part * g.n;
     request_tile r;
     if (!tile_at(g, blockIdx.x, 1, r)) return;
-    const u64 *base = g.base ? g.base + ((size_t)party * g.tokens + r.first) * g.ld_base : nullptr;
+    const u64 *base = g.base + ((size_t)party * g.tokens + r.first) * g.ld_base;
     u64 *y = g.y + ((size_t)party * g.tokens + r.first) * g.ld_y;
     if (r.adapter < 0) {
         pass_through(g, r, base, y, part);
@@ -299,7 +383,7 @@ __global__ __launch_bounds__(BLOCK, 2) void up_single_kernel(adapter_args g)
 #pragma unroll
         for (int i = 0; i < 4; i++) acc[i] = (v4i){0, 0, 0, 0};
         const int col = 64 * u + 32 * (q >> 1) + 2 * c16 + (q & 1);
-        const u64 more = base && col < g.N ? base[col] : 0;
+        const u64 more = col < g.N ? base[col] : 0;
         for (int m = 0; m < steps; m++) {
             const v4i a = diagonals_at(zd, R, m);
             const int chunk = 4 * m + q;
@@ -309,92 +393,104 @@ __global__ __launch_bounds__(BLOCK, 2) void up_single_kernel(adapter_args g)
                 acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, chunk < chunks ? v : (v4i){0, 0, 0, 0}, acc[i], 0, 0, 0);
             }
         }
-        const u64 o = fold_items(acc, more);
+        const u64 o = fold_items<false>(acc, more);
         if (col < g.N) y[col] = o;
     }
 }
 
-// Tiles of ROWS tokens of a request whose rank takes M products: the digits of all of them stay in registers, a wave takes 32 columns of B at a
-// time, the next 32 and the base's on their way.
-template <int M, int ROWS, bool WIDE>
+// Tiles of UP_ROWS tokens of a request whose rank takes M products.  A wave keeps the digits of 128 columns of B in registers and takes the tokens one
+// after the other, each a result of 1 KB in a row; the next token's digits and the base of those after it are on their way.
+constexpr int UP_ROWS = 16;
+template <int M, access MODE>
 __global__ __launch_bounds__(BLOCK, 2) void up_diagonals_kernel(adapter_args g)
 {
     extern __shared__ signed char zd[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = blockIdx.y / g.n, party = blockIdx.y - part * g.n;
     request_tile r;
-    if (!tile_at(g, blockIdx.x, ROWS, r)) return;
-    const u64 *base = g.base ? g.base + ((size_t)party * g.tokens + r.first) * g.ld_base : nullptr;
+    if (!tile_at(g, (int)xcd_slot(blockIdx.x, gridDim.x), UP_ROWS, r)) return;
+    const u64 *base = g.base + ((size_t)party * g.tokens + r.first) * g.ld_base;
     u64 *y = g.y + ((size_t)party * g.tokens + r.first) * g.ld_y;
     if (r.adapter < 0) {
         pass_through(g, r, base, y, part);
         return;
     }
     const int R = g.padded, chunks = NL * R / 16, stride = diagonals_stride(R, M), q = lane >> 4, c16 = lane & 15;
-    const signed char *b = g.up + r.adapter * g.up_bytes + party * g.up_party + c16 * 16;
-    const int units = (g.N + 31) >> 5, step = g.col_groups * 4;
-    int u = part * 4 + wave;
-    auto load = [&](int unit, v4i (&w)[2][M], pack_t<2> (&more)[ROWS / 4]) {
+    const int blocks = (g.N + 31) >> 5, units = (blocks + 3) >> 2, step = g.col_groups * 4;
+    const signed char *b = g.up + r.adapter * g.up_bytes + party * g.up_party;
+    v4i w[2][4][M];
+    auto load_b = [&](int unit) {
 #pragma unroll
-        for (int h = 0; h < 2; h++)
+        for (int i = 0; i < 4; i++)              // (behind the last block of 32 columns, it again)
 #pragma unroll
-            for (int m = 0; m < M; m++) {
-                const int chunk = 4 * m + q;
-                w[h][m] = *reinterpret_cast<const v4i *>(b + ((size_t)(2 * unit + h) * chunks + min(chunk, chunks - 1)) * 256);
-                if (NL != 8 && chunk >= chunks) w[h][m] = (v4i){0, 0, 0, 0};
+            for (int h = 0; h < 2; h++) {
+                const signed char *at = b + (size_t)(2 * min(4 * unit + i, blocks - 1) + h) * chunks * 256;
+#pragma unroll
+                for (int m = 0; m < M; m++)
+                    w[h][i][m] = *reinterpret_cast<const v4i *>(at + min(4 * m + q, chunks - 1) * 256 + c16 * 16);
             }
-#pragma unroll
-        for (int t = 0; t < ROWS / 4; t++)
-            more[t] = base ? load_pair<WIDE>(base + (size_t)min(4 * t + q, r.count - 1) * g.ld_base, 32 * unit + 2 * c16, g.N) : pack_t<2>{{0, 0}};
     };
-    v4i w[2][M], next[2][M], a[ROWS][M];
-    pack_t<2> more[ROWS / 4], more_next[ROWS / 4];
-    if (u < units) load(u, w, more);
-    stage_diagonals(g, zd, ROWS, stride, party, r);
+    constexpr int AHEAD = 4;
+    pack_t<2> more[AHEAD];
+    int unit = part * 4 + wave;
+    auto load_base = [&](int t, int u) { return load_pair<MODE>(base + (size_t)min(t, r.count - 1) * g.ld_base, 128 * u + 32 * q + 2 * c16, g.N); };
+    if (unit < units) {
+        load_b(unit);
 #pragma unroll
-    for (int t = 0; t < ROWS; t++)
+        for (int i = 0; i < AHEAD; i++) more[i] = load_base(i, unit);
+    }
+    stage_diagonals(g, zd, UP_ROWS + 1, stride, party, r);
+    auto digits = [&](int t, v4i (&a)[M]) {
 #pragma unroll
-        for (int m = 0; m < M; m++) a[t][m] = diagonals_at(zd + t * stride, R, m);
-    for (; u < units; u += step) {
-        load(min(u + step, units - 1), next, more_next);   // (behind the last, some again)
-        __builtin_amdgcn_sched_barrier(0);
+        for (int m = 0; m < M; m++) {
+            a[m] = diagonals_at(zd + t * stride, R, m);
+            if (NL != 8 && 4 * m + q >= chunks) a[m] = (v4i){0, 0, 0, 0};   // (of the last product's chunks those that do not exist)
+        }
+    };
+    for (; unit < units; unit += step) {
+        const int col = 128 * unit + 32 * q + 2 * c16;
+        v4i a[2][M];
+        digits(0, a[0]);
+        for (int t0 = 0; t0 < r.count; t0 += AHEAD) {
 #pragma unroll
-        for (int t0 = 0; t0 < ROWS; t0 += 4) {
-            if (t0 >= r.count) break;
-            v4i acc[2][4];
-#pragma unroll
-            for (int i = 0; i < 4; i++)
+            for (int i = 0; i < AHEAD; i++) {
+                const int t = t0 + i;
+                if (t >= r.count) break;
+                digits(t + 1, a[(i + 1) & 1]);           // (there is a place behind the last token)
+                pack_t<2> o;
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
-                    acc[h][i] = (v4i){0, 0, 0, 0};
+                    v4i acc[4];
 #pragma unroll
-                    for (int m = 0; m < M; m++) acc[h][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[t0 + i][m], w[h][m], acc[h][i], 0, 0, 0);
+                    for (int m = 0; m < M; m++)
+#pragma unroll
+                        for (int k = 0; k < 4; k++)
+                            acc[k] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i & 1][m], w[h][k][m], m ? acc[k] : (v4i){0, 0, 0, 0}, 0, 0, 0);
+                    o.v[h] = fold_items<true>(acc, more[i].v[h]);
                 }
-            pack_t<2> o;
-#pragma unroll
-            for (int h = 0; h < 2; h++) o.v[h] = fold_items(acc[h], more[t0 / 4].v[h]);
-            if (t0 + q < r.count) store_pair<WIDE>(y + (size_t)(t0 + q) * g.ld_y, 32 * u + 2 * c16, g.N, o);
+                more[i] = load_base(t + AHEAD, unit);
+                store_pair<MODE>(y + (size_t)t * g.ld_y, col, g.N, o);
+            }
         }
+        if (unit + step < units) {
+            load_b(unit + step);
 #pragma unroll
-        for (int h = 0; h < 2; h++)
-#pragma unroll
-            for (int m = 0; m < M; m++) w[h][m] = next[h][m];
-#pragma unroll
-        for (int t = 0; t < ROWS / 4; t++) more[t] = more_next[t];
+            for (int i = 0; i < AHEAD; i++) more[i] = load_base(i, unit + step);
+        }
     }
 }
 
-// Tiles of 16 tokens of a request with a larger rank: diagonal sums apart, as in a dense layer; the digits of z in LDS in MFMA order, a wave takes
-// 32 columns of B at a time.
-template <bool WIDE>
+// Tiles of 64 tokens of a request with a larger rank: diagonal sums apart, as in a dense layer; the digits of z in LDS in MFMA order, a wave takes
+// 16 tokens and 32 columns of B at a time.  The waves share the columns as above.
+template <access MODE>
 __global__ __launch_bounds__(BLOCK, 2) void up_tile_kernel(adapter_args g)
 {
-    extern __shared__ v4i zt[];                  // [rank / 64][limb][64 lanes]
+    extern __shared__ v4i zt[];                  // [token / 16][rank / 64][limb][64 lanes]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = blockIdx.y / g.n, party = blockIdx.y - part * g.n;
     request_tile r;
-    if (!tile_at(g, blockIdx.x, 16, r)) return;
-    const u64 *base = g.base ? g.base + ((size_t)party * g.tokens + r.first) * g.ld_base : nullptr;
+    if (!tile_at(g, blockIdx.x, 64, r)) return;
+    const u64 *base = g.base + ((size_t)party * g.tokens + r.first) * g.ld_base;
     u64 *y = g.y + ((size_t)party * g.tokens + r.first) * g.ld_y;
     if (r.adapter < 0) {
         pass_through(g, r, base, y, part);
@@ -402,19 +498,21 @@ __global__ __launch_bounds__(BLOCK, 2) void up_tile_kernel(adapter_args g)
     }
     const int per_limb = g.padded / 16, chunks = NL * per_limb, blocks = (g.rank + 63) >> 6, q = lane >> 4, c16 = lane & 15;
     const u64 *z = g.z + ((size_t)party * g.tokens + r.first) * g.rank;
-    for (int i = tid; i < 16 * blocks * 16; i += BLOCK) {      // four elements of a row
-        const int row = i & 15, e = (i >> 4) * 4;
+    const int log = r.count > 32 ? 2 : r.count > 16 ? 1 : 0, first = (wave & ((1 << log) - 1)) * 16;
+    for (int i = tid; i < (16 << log) * blocks * 16; i += BLOCK) {      // four elements of a row
+        const int row = i & ((16 << log) - 1), e = (i >> (4 + log)) * 4;
         u64 v[4];
 #pragma unroll
         for (int c = 0; c < 4; c++) v[c] = balanced_digits(row < r.count && e + c < g.rank ? z[(size_t)row * g.rank + e + c] : 0);
-        u32 *dst = reinterpret_cast<u32 *>(zt + (e >> 6) * TILE + row + 16 * ((e & 63) >> 4)) + ((e & 15) >> 2);
+        u32 *dst = reinterpret_cast<u32 *>(zt + ((row >> 4) * blocks + (e >> 6)) * TILE + (row & 15) + 16 * ((e & 63) >> 4)) + ((e & 15) >> 2);
 #pragma unroll
         for (int l = 0; l < NL; l++) dst[l * 256] = limb_dword(v, l);
     }
     __syncthreads();
     const signed char *b = g.up + r.adapter * g.up_bytes + party * g.up_party + c16 * 16;
     const int units = (g.N + 31) >> 5;
-    for (int u = part * 4 + wave; u < units; u += g.col_groups * 4) {
+    const v4i *mine = zt + (first >> 4) * blocks * TILE + lane;
+    for (int u = part * (4 >> log) + (wave >> log); u < units; u += g.col_groups * (4 >> log)) {
         v4i acc[2][ND];
 #pragma unroll
         for (int h = 0; h < 2; h++)
@@ -430,7 +528,7 @@ __global__ __launch_bounds__(BLOCK, 2) void up_tile_kernel(adapter_args g)
                 for (int j = 0; j < NL; j++) w[j] = *reinterpret_cast<const v4i *>(src + (size_t)(h * chunks + j * per_limb) * 256);
 #pragma unroll
                 for (int i = 0; i < NL; i++) {
-                    const v4i x = zt[kb * TILE + i * 64 + lane];
+                    const v4i x = mine[kb * TILE + i * 64];
 #pragma unroll
                     for (int j = 0; j < NL; j++) acc[h][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, w[j], acc[h][i + j], 0, 0, 0);
                 }
@@ -439,12 +537,12 @@ __global__ __launch_bounds__(BLOCK, 2) void up_tile_kernel(adapter_args g)
         const int col = 32 * u + 2 * c16;
 #pragma unroll
         for (int c = 0; c < 4; c++) {
-            const int row = 4 * q + c;
+            const int row = first + 4 * q + c;
             if (row >= r.count) continue;
-            pack_t<2> o = base ? load_pair<WIDE>(base + (size_t)row * g.ld_base, col, g.N) : pack_t<2>{{0, 0}};
+            pack_t<2> o = load_pair<MODE>(base + (size_t)row * g.ld_base, col, g.N);
             o.v[0] = fold_diagonals(acc[0], c, o.v[0]);
             o.v[1] = fold_diagonals(acc[1], c, o.v[1]);
-            store_pair<WIDE>(y + (size_t)row * g.ld_y, col, g.N, o);
+            store_pair<MODE>(y + (size_t)row * g.ld_y, col, g.N, o);
         }
     }
 }
@@ -475,9 +573,20 @@ hipError_t ss_launch_adapters_down(const adapter_plan &plan, const ss_adapters &
     g.down_party = down_party_bytes(s.K, s.rank), g.down_bytes = g.nr * g.down_party;
     g.x = x, g.ld_x = ld_x, g.planes = planes, g.plane = (size_t)g.nr * req.tokens * s.rank;
     g.run = plan.run;
-    const dim3 grid((unsigned)request_tiles(req.tokens, req.requests, plan.down_rows), g.nr * plan.rank_tiles, plan.splits);
+    g.tiles = (unsigned)request_tiles(req.tokens, req.requests, plan.down_rows);
+    g.dTiles = make_fdiv(g.tiles);
+    const dim3 grid((unsigned)plan.down_groups);
     const bool wide = s.K % 2 == 0 && ld_x % 2 == 0 && aligned16(x);
-    hipLaunchKernelGGL((wide ? down_kernel<true> : down_kernel<false>), grid, dim3(BLOCK), 0, stream, g);
+#define SS_DOWN(CW, CT) hipLaunchKernelGGL((wide ? down_kernel<CW, CT, true> : down_kernel<CW, CT, false>), grid, dim3(BLOCK), 0, stream, g)
+    if (s.rank <= 16)
+        SS_DOWN(1, 1);
+    else if (s.rank <= 32)
+        SS_DOWN(2, 1);
+    else if (s.rank <= 64)
+        SS_DOWN(4, 1);
+    else
+        SS_DOWN(4, 2);
+#undef SS_DOWN
     return hipGetLastError();
 }
 
@@ -493,21 +602,30 @@ hipError_t ss_launch_adapters_up(const adapter_plan &plan, const ss_adapters &s,
     g.z = z, g.base = base, g.ld_base = ld_base, g.y = y, g.ld_y = ld_y;
     g.col_groups = plan.col_groups;
     const int steps = (int)up_steps(s.rank);
-    const size_t lds = plan.up == UP_TILE ? div_up(s.rank, 64) * TILE * 16 : (size_t)plan.up_rows * (15 * g.padded + 64 * steps);
+    const size_t lds = plan.up == UP_TILE ? 4 * div_up(s.rank, 64) * TILE * 16 : (size_t)(plan.up_rows + (plan.up == UP_DIAGONALS ? 1 : 0)) * (15 * g.padded + 64 * steps);
     const dim3 grid((unsigned)request_tiles(req.tokens, req.requests, plan.up_rows), n * plan.col_groups);
-    const bool wide = s.N % 2 == 0 && ld_y % 2 == 0 && aligned16(y) && (!base || (ld_base % 2 == 0 && aligned16(base)));
-#define SS_UP(M) hipLaunchKernelGGL((wide ? up_diagonals_kernel<M, 8, true> : up_diagonals_kernel<M, 8, false>), grid, dim3(BLOCK), lds, stream, g)
+    const bool pairs = s.N % 2 == 0 && ld_y % 2 == 0 && aligned16(y) && (!base || (ld_base % 2 == 0 && aligned16(base)));
+    if (!base) {
+        hipLaunchKernelGGL(clear_kernel, dim3((unsigned)std::min(req.tokens, 4096), n), dim3(BLOCK), 0, stream, g);
+        g.base = y, g.ld_base = ld_y;
+    }
+    const access mode = !pairs ? NARROW : plan.streams ? STREAM_PAIRS : PAIRS;
+#define SS_MODE(KERNEL, ...)                                                                                                              \
+    hipLaunchKernelGGL((mode == NARROW ? KERNEL<__VA_ARGS__ NARROW> : mode == PAIRS ? KERNEL<__VA_ARGS__ PAIRS> : KERNEL<__VA_ARGS__ STREAM_PAIRS>), grid, \
+                       dim3(BLOCK), lds, stream, g)
+#define SS_COMMA ,
     if (plan.up == UP_SINGLE)
         hipLaunchKernelGGL(up_single_kernel, grid, dim3(BLOCK), lds, stream, g);
     else if (plan.up == UP_TILE)
-        hipLaunchKernelGGL((wide ? up_tile_kernel<true> : up_tile_kernel<false>), grid, dim3(BLOCK), lds, stream, g);
+        SS_MODE(up_tile_kernel, );
     else if (steps == 1)
-        SS_UP(1);
+        SS_MODE(up_diagonals_kernel, 1 SS_COMMA);
     else if (steps == 2)
-        SS_UP(2);
+        SS_MODE(up_diagonals_kernel, 2 SS_COMMA);
     else
-        SS_UP((SS_NLIMB / 2));                   // a rank of 17 to 32
-#undef SS_UP
+        SS_MODE(up_diagonals_kernel, SS_NLIMB / 2 SS_COMMA);                   // a rank of 17 to 32
+#undef SS_COMMA
+#undef SS_MODE
     return hipGetLastError();
 }
 

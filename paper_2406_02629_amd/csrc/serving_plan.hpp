@@ -21,6 +21,7 @@ inline size_t down_party_bytes(int K, int rank) { return div_up(K, 64) * SS_NLIM
 inline size_t up_party_bytes(int rank, int N) { return div_up(N, 32) * 2 * SS_NLIMB * padded_rank(rank) * 16; }
 
 constexpr size_t MAX_SERVING_GROUPS = ((size_t)1 << 24) - 1;   // workgroups of 256 threads in a launch: less than 2^32 threads
+constexpr size_t STREAMED_BYTES = (size_t)256 << 20;           // tensors that the caches do not hold
 constexpr int MAX_PLANES = 8;                                  // partial sums of the first product, which the reduction adds
 
 // The kernel of the second product: tokens one by one, in tiles with all digits of their z in registers, or in tiles with the diagonals apart.
@@ -29,8 +30,8 @@ enum up_kind { UP_SINGLE, UP_DIAGONALS, UP_TILE };
 struct adapter_plan {
     int down_rows, up_rows;       // tokens to a tile
     up_kind up;
-    int rank_tiles;               // of 16, of the first product
     int splits, run;              // its contraction: in `splits` runs of `run` blocks of 64
+    bool streams;                 // the second product's tensors go past the caches
     int col_groups;               // workgroups that share the columns of a tile of the second product
     size_t messages, planes, z;   // bytes: of the reduction's messages, of the first product's planes, of its reduced result
     size_t down_groups, up_groups, bytes;
@@ -45,15 +46,15 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
     const size_t nr = 2 * t + 1, k = t + 1, count = (size_t)tokens * rank, blocks = div_up(K, 64);
     p.down_rows = 16;
     p.up = tokens <= 2 * (size_t)requests ? UP_SINGLE : rank <= 32 ? UP_DIAGONALS : UP_TILE;
-    p.up_rows = p.up == UP_SINGLE ? 1 : p.up == UP_DIAGONALS ? 8 : 16;
-    p.rank_tiles = (int)div_up(rank, 16);
-    const size_t tiles = request_tiles(tokens, requests, p.down_rows) * nr * p.rank_tiles;
+    p.up_rows = p.up == UP_SINGLE ? 1 : p.up == UP_DIAGONALS ? 16 : 64;
+    p.streams = (size_t)n * tokens * N * 16 > STREAMED_BYTES;
+    const size_t tiles = request_tiles(tokens, requests, p.down_rows) * nr;
     p.splits = (int)std::max<size_t>(1, std::min(std::min<size_t>(MAX_PLANES, div_up(512, tiles)), blocks / 8));
     p.run = (int)div_up(blocks, p.splits);
     p.splits = (int)div_up(blocks, p.run);
     p.down_groups = tiles * p.splits;
-    const size_t up_tiles = request_tiles(tokens, requests, p.up_rows), units = div_up(N, p.up_rows == 1 ? 64 : 32);
-    p.col_groups = (int)std::max<size_t>(1, std::min(div_up(512, up_tiles * n), div_up(units, 4)));
+    const size_t up_tiles = request_tiles(tokens, requests, p.up_rows), units = div_up(N, p.up == UP_SINGLE ? 64 : p.up == UP_DIAGONALS ? 128 : 32);
+    p.col_groups = (int)std::max<size_t>(1, std::min(div_up(p.up == UP_SINGLE ? 512 : 2048, up_tiles * n), div_up(units, 4)));
     p.up_groups = up_tiles * n * p.col_groups;
     auto whole = [](size_t b) { return (b + 255) & ~(size_t)255; };
     p.messages = whole((nr * k + k * n + k + n) * count * 8);
