@@ -294,7 +294,8 @@ struct ss_sampling {
     size_t ld_allowed;
 };
 
-hipError_t ss_launch_sample(const ss_sampling &q, const u64 *logits, size_t ld, int rows, int vocab, int f, const ss_rec_params &rp, void *room, long long *tokens,
-                            int *shown, hipStream_t stream);
+// room: plan.bytes bytes for what the launches hand on
+hipError_t ss_launch_sample(const sample_plan &plan, const ss_sampling &q, const u64 *logits, size_t ld, int rows, int vocab, int f, const ss_rec_params &rp,
+                            void *room, long long *tokens, int *shown, hipStream_t stream);
 
 }  // namespace SS_NS

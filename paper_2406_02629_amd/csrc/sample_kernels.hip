@@ -1,14 +1,23 @@
 // The next token of every row from shares of its logits: REC, then a draw in whole numbers from the softmax of the row, cut by top-k, top-p and
 // min-p.  The tokens that may be drawn are the first ones in the order of falling logits, equal ones by their number, so a cut is a distance from
-// the row's largest logit and how many of the tokens at that distance are kept; it is found by histograms of distances, digit by digit.
+// the row's largest logit and how many of the tokens at that distance are kept.  A histogram of distances, with how many tokens each bin has and
+// what they weigh, says in which bin a cut lies; the tokens of that bin alone are looked at further.
+//
+// Up to SMALL_VOCAB tokens one workgroup takes a row in one launch.  Longer rows go through four, so that many workgroups share a row:
+//   open     REC, and the largest logit of every 2048
+//   count    the histogram
+//   collect  what the tokens weigh that stay whatever the cut is, for every 512; the tokens of the bins with a cut, in a list
+//   pick     the cut, the weights of the list's tokens that stay, and the draw
 #include "kernels.hpp"
 #include "power2.hpp"
+#include "truncation.hpp"
 
 namespace SS_NS {
 
 namespace {
 
-constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = 2048, BIN_BITS = 11;
+constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = SAMPLE_BINS, CHUNK = SAMPLE_CHUNK;
+constexpr int OPEN_THREADS = 256;
 constexpr int NOT_ALLOWED = -2147483647 - 1;
 
 struct sample_args {
@@ -19,9 +28,18 @@ struct sample_args {
     const long long *random;
     const u32 *allowed;             // a bit to a token, or nullptr
     size_t ld_allowed;
-    int *keys;                      // [rows][vocab]: logits in units of 2^-min(f, 16)
     long long *tokens;
     int *shown;                     // probability of the token, 30 fraction bits
+    // of the rows of this launch, row0 the first
+    int row0, opens, blocks, key_ld;
+    fdiv dOpens, dBlocks;
+    int *keys;                      // [.][key_ld]: logits in units of 2^-min(f, 16)
+    int *tops;                      // [.][opens]
+    u32 *count;                     // [.][BINS]
+    u64 *sum;                       // [.][BINS]
+    u64 *chunks;                    // [.][blocks * THREADS / 64]
+    u32 *listed;                    // [.]
+    u64 *list;                      // [.][SAMPLE_LIST]: distance 2^20 + token
 };
 
 // the opened logit in units of 2^-min(f, 16), the far ones as the last that 32 bits hold
@@ -33,11 +51,30 @@ __device__ __forceinline__ int logit_of(u64 v, int f)
 
 // what a row asks for, and the weight of a distance
 struct row_rule {
-    u32 scale, least;               // smallest weight that is kept
-    int shift;
-    u64 reach;                      // distances from here on have no weight
+    u32 scale, least, few, part;    // least: smallest weight that is kept; few: top_k or 0; part: top_p, 2^30 for none
+    int shift, bin_shift;
+    u32 reach;                      // distances from here on have no weight
     __device__ __forceinline__ u32 weight(u32 distance) const { return power2((u64)distance * scale >> shift); }
+    // what tokens that weigh `of` have to be cut to, see top_p
+    __device__ __forceinline__ u64 need(u64 of) const
+    {
+        const u64 lo = of * part, hi = __umul64hi(of, part), up = (hi << 34 | lo >> 30) + ((lo & ((1u << 30) - 1)) != 0);
+        return up ? up : 1;
+    }
 };
+
+__device__ __forceinline__ row_rule rule_of(const int4 &p, int f)
+{
+    row_rule r;
+    r.scale = (u32)max(p.x, 1 << 14);
+    r.least = (u32)min(max(p.w, 1), 1 << 30);
+    r.few = p.x <= 0 ? 1 : (u32)max(p.y, 0);
+    r.part = (u32)min(max(p.z, 0), 1 << 30);
+    r.shift = min(f, 16) + 8;
+    r.reach = (u32)(((31ull << (16 + r.shift)) + r.scale - 1) / r.scale);   // <= 31 2^26
+    r.bin_shift = max(0, 32 - __clz((int)(r.reach - 1)) - SAMPLE_BIN_BITS);
+    return r;
+}
 
 template <typename T>
 __device__ __forceinline__ T wave_upto(T v)      // sum of the lanes up to one's own
@@ -56,6 +93,13 @@ __device__ __forceinline__ T wave_sum(T v)
 {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+__device__ __forceinline__ int wave_max(int v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v = max(v, __shfl_xor(v, d));
     return v;
 }
 
@@ -78,172 +122,171 @@ __device__ __forceinline__ T block_upto(T v, T *lds, T &all)
     return v + before;
 }
 
-// tokens at a distance below `distance` and at it; of the latter the first `ties` are kept
+struct row_state {
+    u32 count[BINS];                // of the tokens in a bin, then of those at the cut in a chunk
+    u64 sum[BINS];                  // what they weigh, then what stays of a chunk
+    u64 red64[WAVES], found_sum;
+    u32 red32[WAVES], found_count;
+    int bin[3];
+};
+
+// Distances lo .. lo + span - 1 among which a cut lies, and what comes before them
+struct cut_range {
+    u32 lo, span;                   // span 0: no such cut
+    u64 left;                       // tokens (top_k) or weight (top_p) to take from the range
+    u64 before;                     // weight of the tokens in front
+};
+
+struct row_plan {
+    u32 sure;                       // distances below stay
+    cut_range few, part;            // part.left only where few.span is 0: it depends on what few leaves
+};
+
+// From the histogram in s: where the cuts lie.
+__device__ __forceinline__ row_plan plan_row(row_state &s, const row_rule &rule)
+{
+    const int tid = threadIdx.x;
+    const u32 c0 = s.count[2 * tid], c1 = s.count[2 * tid + 1];
+    const u64 s0 = s.sum[2 * tid], s1 = s.sum[2 * tid + 1];
+    u32 all_count;
+    u64 all_sum;
+    const u32 c = block_upto(c0 + c1, s.red32, all_count);
+    const u64 w = block_upto(s0 + s1, s.red64, all_sum);
+    if (tid < 3) s.bin[tid] = BINS;
+    __syncthreads();
+    row_plan p = {rule.reach, {0, 0, 0, 0}, {0, 0, 0, 0}};
+    const u32 width = 1u << rule.bin_shift;
+    u64 least = all_sum, most = all_sum;         // what top_k leaves weighs so much
+    if (rule.few && all_count >= rule.few) {     // (uniform)
+        if (c >= rule.few && c - c0 - c1 < rule.few) {
+            const bool second = c - c1 < rule.few;
+            s.bin[0] = 2 * tid + second;
+            s.found_count = second ? c - c1 : c - c1 - c0;
+            s.found_sum = second ? w - s1 : w - s1 - s0;
+            s.red64[0] = second ? s1 : s0;       // (what the block sums left there is no longer needed)
+        }
+        __syncthreads();
+        p.few = {(u32)s.bin[0] << rule.bin_shift, width, rule.few - s.found_count, s.found_sum};
+        p.sure = p.few.lo;
+        least = s.found_sum;
+        most = s.found_sum + s.red64[0];
+    }
+    if (rule.part < 1u << 30) {
+        const u64 low = rule.need(least), high = rule.need(most);
+        __syncthreads();
+        auto look = [&](u64 need, int which) {   // the first bin up to which the tokens weigh so much
+            if (w >= need && w - s0 - s1 < need) {
+                const bool second = w - s1 < need;
+                s.bin[which] = 2 * tid + second;
+                if (which == 1) s.found_sum = second ? w - s1 : w - s1 - s0;
+            }
+        };
+        look(low, 1), look(high, 2);
+        __syncthreads();
+        p.part = {(u32)s.bin[1] << rule.bin_shift, (u32)(s.bin[2] - s.bin[1] + 1) << rule.bin_shift, high - s.found_sum, s.found_sum};
+        p.sure = p.part.lo;
+    }
+    return p;
+}
+
 struct cut_place {
-    u32 distance;
-    u32 ties;
+    u32 distance, ties;             // tokens below the distance stay, and so many of those at it
     u64 before;                     // weight of the former
 };
 
-struct row_state {
-    u32 count[BINS];
-    u64 sum[BINS];
-    u64 red64[WAVES];
-    u32 red32[WAVES];
-    int bin;
-    u64 before_sum;
-    u32 before_count, at;
-};
-
-// The first distance at which the tokens up to it are `few` (BY_SUM: weigh `need`), or no place if they are less altogether.  total: weight of all
-// tokens, set by the first histogram; need_of(total) gives what is needed.
-template <bool BY_SUM, typename F>
-__device__ __forceinline__ bool find_cut(const int *keys, int vocab, int top, const row_rule &rule, row_state &s, u32 few, F &&need_of, u64 &total, cut_place &cut)
+// The distance in a range at which the tokens up to it are as many as is left to take (BY_SUM: weigh as much).  each(f) calls f(distance, token) for all tokens
+// of the range at least.
+template <bool BY_SUM, typename E>
+__device__ __forceinline__ cut_place find_cut(row_state &s, const row_rule &rule, cut_range r, E &&each)
 {
     const int tid = threadIdx.x;
-    int shift = 0;
-    while ((rule.reach - 1) >> shift >= BINS) shift++;
-    u64 lo = 0, need = 0, before_sum = 0;
-    u32 before_count = 0;
-    for (bool first = true;; first = false) {
-        for (int i = tid; i < BINS; i += THREADS) s.count[i] = 0, s.sum[i] = 0;
-        if (tid == 0) s.bin = BINS;
+    for (;;) {
+        const int shift = max(0, 32 - __clz((int)(r.span - 1)) - SAMPLE_BIN_BITS);
         __syncthreads();
-        for (int j = tid; j < vocab; j += THREADS) {
-            const int key = keys[j];
-            const u32 d = (u32)top - (u32)key;
-            if (key == NOT_ALLOWED || d >= rule.reach || d < lo) continue;
-            const u64 bin = (d - lo) >> shift;
-            if (bin >= BINS) continue;
-            atomicAdd(&s.count[bin], 1u);
-            atomicAdd((unsigned long long *)&s.sum[bin], (unsigned long long)rule.weight(d));
-        }
+        for (int i = tid; i < BINS; i += THREADS) s.count[i] = 0, s.sum[i] = 0;
+        __syncthreads();
+        each([&](u32 d, int) {
+            if (d < r.lo || d - r.lo >= r.span) return;
+            atomicAdd(&s.count[(d - r.lo) >> shift], 1u);
+            atomicAdd((unsigned long long *)&s.sum[(d - r.lo) >> shift], (unsigned long long)rule.weight(d));
+        });
         __syncthreads();
         const u32 c0 = s.count[2 * tid], c1 = s.count[2 * tid + 1];
         const u64 s0 = s.sum[2 * tid], s1 = s.sum[2 * tid + 1];
         u32 all_count;
         u64 all_sum;
-        const u32 c = before_count + block_upto(c0 + c1, s.red32, all_count);
-        const u64 w = before_sum + block_upto(s0 + s1, s.red64, all_sum);
-        if (first) {
-            total = all_sum;
-            need = BY_SUM ? need_of(total) : 0;
-            if (!BY_SUM && all_count < few) return false;
-        }
-        const bool past0 = BY_SUM ? w - s1 >= need : c - c1 >= few, past1 = BY_SUM ? w >= need : c >= few;
-        if (past1) atomicMin(&s.bin, past0 ? 2 * tid : 2 * tid + 1);
-        __syncthreads();
-        if (s.bin >> 1 == tid) {
-            const bool second = s.bin & 1;
-            s.before_count = second ? c - c1 : c - c1 - c0;
-            s.before_sum = second ? w - s1 : w - s1 - s0;
-            s.at = second ? c1 : c0;
+        const u32 c = block_upto(c0 + c1, s.red32, all_count);
+        const u64 w = block_upto(s0 + s1, s.red64, all_sum);
+        const u64 to = BY_SUM ? w : c, before = to - (BY_SUM ? s0 + s1 : c0 + c1);
+        if (to >= r.left && before < r.left) {
+            const bool second = to - (BY_SUM ? s1 : c1) < r.left;
+            s.bin[0] = 2 * tid + second;
+            s.found_count = second ? c - c1 : c - c1 - c0;
+            s.found_sum = second ? w - s1 : w - s1 - s0;
         }
         __syncthreads();
-        before_count = s.before_count;
-        before_sum = s.before_sum;
-        lo += (u64)s.bin << shift;
+        r.left -= BY_SUM ? s.found_sum : s.found_count;
+        r.before += s.found_sum;
+        r.lo += (u32)s.bin[0] << shift;
+        r.span = 1u << shift;
         if (shift == 0) break;
-        shift = max(0, shift - BIN_BITS);
-        __syncthreads();
     }
-    cut.distance = (u32)lo;
-    cut.before = before_sum;
-    if constexpr (BY_SUM) {
-        const u32 w = rule.weight(cut.distance);
-        cut.ties = (u32)((need - before_sum + w - 1) / w);
-    } else {
-        cut.ties = few - before_count;
-    }
-    __syncthreads();
-    return true;
+    const u32 w = rule.weight(r.lo);
+    return {r.lo, (u32)(BY_SUM ? (r.left + w - 1) / w : r.left), r.before};
 }
 
-// One workgroup to a row.
-__global__ __launch_bounds__(THREADS) void sample_kernel(sample_args g, ss_rec_params rp)
+// The cuts of a row, then, with what is sure of every chunk in sure(c), the draw.  each: as in find_cut, of the tokens in the ranges of the plan;
+// key(j): that of token j.
+template <typename E, typename S, typename K>
+__device__ __forceinline__ void draw_token(const sample_args &g, int row, row_state &s, const row_rule &rule, const row_plan &plan, int top, E &&each, S &&sure,
+                                           K &&key)
 {
-    __shared__ row_state s;
-    const int tid = threadIdx.x, row = blockIdx.x;
-    int *keys = g.keys + (size_t)row * g.vocab;
-    const int4 p = g.params[row];
-    int top = NOT_ALLOWED;
-    for (int j = tid; j < g.vocab; j += THREADS) {
-        ss_sacc acc;
-        acc.clear();
-        for (int i = 0; i < rp.m; i++) acc.mac(g.logits[((size_t)rp.plane[i] * g.rows + row) * g.ld + j], rp.ilambda[i]);
-        const u64 v = rp.dinv == 1 ? acc.value() : ss_mul(acc.value(), rp.dinv);
-        const bool allowed = !g.allowed || (g.allowed[row * g.ld_allowed + (j >> 5)] >> (j & 31) & 1);
-        const int key = allowed ? logit_of(v, g.f) : NOT_ALLOWED;
-        keys[j] = key;
-        top = max(top, key);
+    const int tid = threadIdx.x;
+    cut_place cut = {rule.reach, 0, 0};
+    cut_range part = plan.part;
+    if (plan.few.span) {
+        cut = find_cut<false>(s, rule, plan.few, each);
+        if (part.span) part.left = rule.need(cut.before + (u64)cut.ties * rule.weight(cut.distance)) - part.before;
     }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) top = max(top, __shfl_xor(top, d));
-    if ((tid & 63) == 0) s.red32[tid >> 6] = (u32)top;
-    __syncthreads();
-    for (int w = 0; w < WAVES; w++) top = max(top, (int)s.red32[w]);
-    __syncthreads();
-    if (top == NOT_ALLOWED) {
-        if (tid == 0) g.tokens[row] = -1, g.shown[row] = 0;
-        return;
-    }
-    row_rule rule;
-    rule.scale = (u32)max(p.x, 1 << 14);
-    rule.least = (u32)min(max(p.w, 1), 1 << 30);
-    rule.shift = min(g.f, 16) + 8;
-    rule.reach = ((31ull << (16 + rule.shift)) + rule.scale - 1) / rule.scale;   // <= 31 2^26
-    cut_place cut = {(u32)rule.reach, 0, 0};
-    u64 total = 0;
-    const u32 few = p.x <= 0 ? 1 : p.y <= 0 ? 0 : (u32)p.y;
-    bool limited = few && find_cut<false>(keys, g.vocab, top, rule, s, few, [](u64) { return 0ull; }, total, cut);
-    if (p.z < 1 << 30) {
-        const u64 within = limited ? cut.before + (u64)cut.ties * rule.weight(cut.distance) : 0;
-        const u32 part = (u32)max(p.z, 0);
-        find_cut<true>(keys, g.vocab, top, rule, s, 0, [&](u64 all) {
-            const u64 of = limited ? within : all, lo = of * part, hi = __umul64hi(of, part);
-            return max(1ull, (unsigned long long)((hi << 34 | lo >> 30) + ((lo & ((1 << 30) - 1)) != 0)));
-        }, total, cut);
-    }
-    // weights of chunks of 1024 tokens in their own order, tokens at the cut apart
+    if (part.span) cut = find_cut<true>(s, rule, part, each);
     const u32 at_cut = cut.distance < rule.reach ? rule.weight(cut.distance) : 0;
-    const int lane = tid & 63, chunks = (g.vocab + THREADS - 1) / THREADS;
-    for (int c = tid >> 6; c < chunks; c += WAVES) {
-        u64 sum = 0;
-        u32 ties = 0;
-        for (int i = 0; i < THREADS; i += 64) {
-            const int j = c * THREADS + i + lane;
-            if (j >= g.vocab) continue;
-            const int key = keys[j];
-            const u32 d = (u32)top - (u32)key;
-            if (key == NOT_ALLOWED || d > cut.distance) continue;
-            const u32 w = d < rule.reach ? rule.weight(d) : 0;
-            if (w < rule.least) continue;
-            if (d == cut.distance) ties++; else sum += w;
-        }
-        sum = wave_sum(sum), ties = wave_sum(ties);
-        if (lane == 0) s.sum[c] = sum, s.count[c] = ties;
+    const int chunks = (g.vocab + CHUNK - 1) / CHUNK;
+    __syncthreads();
+    for (int c = tid; c < 2 * THREADS; c += THREADS) {
+        s.count[c] = 0;
+        s.sum[c] = c < chunks ? sure(c) : 0;
     }
     __syncthreads();
-    const u32 mine = tid < chunks ? s.count[tid] : 0;
+    each([&](u32 d, int j) {
+        if (d < plan.sure || d > cut.distance) return;
+        const u32 w = rule.weight(d);
+        if (w < rule.least) return;
+        if (d == cut.distance)
+            atomicAdd(&s.count[j / CHUNK], 1u);
+        else
+            atomicAdd((unsigned long long *)&s.sum[j / CHUNK], (unsigned long long)w);
+    });
+    __syncthreads();
+    const u32 t0 = s.count[2 * tid], t1 = s.count[2 * tid + 1];
     u32 all_ties;
     u64 sum;
-    const u32 ties_before = block_upto(mine, s.red32, all_ties) - mine;
-    const u64 weight = (tid < chunks ? s.sum[tid] : 0) + (u64)at_cut * min(mine, cut.ties > ties_before ? cut.ties - ties_before : 0);
-    const u64 upto = block_upto(weight, s.red64, sum);
+    const u32 before0 = block_upto(t0 + t1, s.red32, all_ties) - t0 - t1, before1 = before0 + t0;
+    auto kept = [&](u32 mine, u32 before) { return cut.ties > before ? min(mine, cut.ties - before) : 0; };
+    const u64 w0 = s.sum[2 * tid] + (u64)at_cut * kept(t0, before0), w1 = s.sum[2 * tid + 1] + (u64)at_cut * kept(t1, before1);
+    const u64 upto = block_upto(w0 + w1, s.red64, sum);
     const u64 target = __umul64hi((u64)g.random[row] << 2, sum);
-    if (upto - weight <= target && target < upto) {
-        s.bin = tid;
-        s.before_count = ties_before;
-        s.before_sum = upto - weight;
+    if (upto > target && upto - w0 - w1 <= target) {
+        const bool second = upto - w1 <= target;
+        s.bin[0] = 2 * tid + second;
+        s.found_count = second ? before1 : before0;
+        s.found_sum = second ? upto - w1 : upto - w1 - w0;
     }
     __syncthreads();
-    const int j = s.bin * THREADS + tid;
-    const int key = j < g.vocab ? keys[j] : NOT_ALLOWED;
-    const u32 d = (u32)top - (u32)key, w0 = key != NOT_ALLOWED && d < rule.reach && d <= cut.distance ? rule.weight(d) : 0;
-    const bool tie = w0 >= rule.least && d == cut.distance;
-    const u32 rank = s.before_count + block_upto((u32)tie, s.red32, all_ties);
-    const u64 before = s.before_sum;
-    const u64 w = w0 < rule.least || (tie && rank > cut.ties) ? 0 : w0;
+    const int j = s.bin[0] * CHUNK + tid, k = tid < CHUNK && j < g.vocab ? key(j) : NOT_ALLOWED;
+    const u32 d = (u32)top - (u32)k, v = k != NOT_ALLOWED && d < rule.reach && d <= cut.distance ? rule.weight(d) : 0;
+    const bool tie = v >= rule.least && d == cut.distance;
+    const u32 rank = s.found_count + block_upto((u32)tie, s.red32, all_ties);
+    const u64 before = s.found_sum, w = v < rule.least || (tie && rank > cut.ties) ? 0 : v;
     u64 chunk;
     const u64 to = before + block_upto(w, s.red64, chunk);
     if (to - w <= target && target < to) {
@@ -252,13 +295,275 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(sample_args g, ss_rec_p
     }
 }
 
+__device__ __forceinline__ int key_of(const sample_args &g, const ss_rec_params &rp, int row, int j, u64 opened)
+{
+    const u64 v = rp.dinv == 1 ? opened : ss_mul(opened, rp.dinv);
+    const bool allowed = !g.allowed || (g.allowed[(size_t)row * g.ld_allowed + (j >> 5)] >> (j & 31) & 1);
+    return allowed ? logit_of(v, g.f) : NOT_ALLOWED;
+}
+
+// ------------------------------------------------------------------ small vocabularies
+
+__global__ __launch_bounds__(THREADS) void sample_kernel(sample_args g, ss_rec_params rp)
+{
+    __shared__ row_state s;
+    __shared__ int keys[SMALL_VOCAB];
+    const int tid = threadIdx.x, row = blockIdx.x;
+    const row_rule rule = rule_of(g.params[row], g.f);
+    int top = NOT_ALLOWED;
+    for (int j = tid; j < g.vocab; j += THREADS) {
+        ss_sacc acc;
+        acc.clear();
+        for (int i = 0; i < rp.m; i++) acc.mac(g.logits[((size_t)rp.plane[i] * g.rows + row) * g.ld + j], rp.ilambda[i]);
+        const int key = key_of(g, rp, row, j, acc.value());
+        keys[j] = key;
+        top = max(top, key);
+    }
+    top = wave_max(top);
+    if ((tid & 63) == 0) s.red32[tid >> 6] = (u32)top;
+    for (int i = tid; i < BINS; i += THREADS) s.count[i] = 0, s.sum[i] = 0;
+    __syncthreads();
+    for (int w = 0; w < WAVES; w++) top = max(top, (int)s.red32[w]);
+    __syncthreads();
+    if (top == NOT_ALLOWED) {
+        if (tid == 0) g.tokens[row] = -1, g.shown[row] = 0;
+        return;
+    }
+    auto each = [&](auto &&f) {
+        for (int j = tid; j < g.vocab; j += THREADS) {
+            const u32 d = (u32)top - (u32)keys[j];
+            if (keys[j] != NOT_ALLOWED && d < rule.reach) f(d, j);
+        }
+    };
+    each([&](u32 d, int) {
+        atomicAdd(&s.count[d >> rule.bin_shift], 1u);
+        atomicAdd((unsigned long long *)&s.sum[d >> rule.bin_shift], (unsigned long long)rule.weight(d));
+    });
+    __syncthreads();
+    row_plan plan = plan_row(s, rule);
+    plan.sure = 0;                               // (all tokens are looked at again)
+    draw_token(g, row, s, rule, plan, top, each, [](int) { return 0ull; }, [&](int j) { return keys[j]; });
+}
+
+// ------------------------------------------------------------------ larger ones
+
+// Bound by reading the shares.
+template <bool WIDE, bool STREAM>
+__global__ __launch_bounds__(OPEN_THREADS) void open_kernel(sample_args g, ss_rec_params rp)
+{
+    __shared__ int red[OPEN_THREADS / 64];
+    const int tid = threadIdx.x;
+    const u32 at = fd_div(blockIdx.x, g.dOpens), block = blockIdx.x - at * g.opens;
+    const int row = g.row0 + (int)at;
+    for (u32 i = block * OPEN_THREADS + tid; i < (u32)BINS; i += g.opens * OPEN_THREADS) g.count[(size_t)at * BINS + i] = 0, g.sum[(size_t)at * BINS + i] = 0;
+    if (block == 0 && tid == 0) g.listed[at] = 0;
+    constexpr int PAIRS = SAMPLE_OPEN / OPEN_THREADS / 2;
+    ss_sacc acc[PAIRS][2];
+#pragma unroll
+    for (int i = 0; i < PAIRS; i++) acc[i][0].clear(), acc[i][1].clear();
+    const int j0 = (int)block * SAMPLE_OPEN + tid * 2;
+    for (int q = 0; q < rp.m; q++) {
+        const u64 *x = g.logits + ((size_t)rp.plane[q] * g.rows + row) * g.ld;
+        pack_t<2> v[PAIRS];
+#pragma unroll
+        for (int i = 0; i < PAIRS; i++) {
+            const int j = j0 + i * 2 * OPEN_THREADS;
+            if constexpr (WIDE) {
+                if (j + 1 < g.vocab)
+                    STREAM ? v[i].load_streaming(x + j) : v[i].load(x + j);
+                else if (j < g.vocab)
+                    v[i].v[0] = x[j], v[i].v[1] = 0;
+                else
+                    v[i].v[0] = v[i].v[1] = 0;
+            } else {
+                v[i].v[0] = x[min(j, g.vocab - 1)];
+                v[i].v[1] = x[min(j + 1, g.vocab - 1)];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < PAIRS; i++)
+#pragma unroll
+            for (int c = 0; c < 2; c++) acc[i][c].mac(v[i].v[c], rp.ilambda[q]);
+    }
+    int top = NOT_ALLOWED;
+#pragma unroll
+    for (int i = 0; i < PAIRS; i++) {
+        const int j = j0 + i * 2 * OPEN_THREADS;
+        int2 k = {NOT_ALLOWED, NOT_ALLOWED};
+        if (j < g.vocab) k.x = key_of(g, rp, row, j, acc[i][0].value());
+        if (j + 1 < g.vocab) k.y = key_of(g, rp, row, j + 1, acc[i][1].value());
+        if (j < g.key_ld) *reinterpret_cast<int2 *>(g.keys + (size_t)at * g.key_ld + j) = k;
+        top = max(top, max(k.x, k.y));
+    }
+    top = wave_max(top);
+    if ((tid & 63) == 0) red[tid >> 6] = top;
+    __syncthreads();
+    if (tid == 0) {
+        for (int w = 1; w < OPEN_THREADS / 64; w++) top = max(top, red[w]);
+        g.tops[(size_t)at * g.opens + block] = top;
+    }
+}
+
+// the largest logit of a row
+__device__ __forceinline__ int top_of(const sample_args &g, u32 at, u32 *lds)
+{
+    int top = NOT_ALLOWED;
+    for (int i = threadIdx.x; i < g.opens; i += THREADS) top = max(top, g.tops[(size_t)at * g.opens + i]);
+    top = wave_max(top);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = (u32)top;
+    __syncthreads();
+    for (int w = 0; w < WAVES; w++) top = max(top, (int)lds[w]);
+    __syncthreads();
+    return top;
+}
+
+// Eight keys of a lane: its wave takes the 512 of a chunk.  (Behind the row's end: not allowed.)
+__device__ __forceinline__ void load_keys(const sample_args &g, u32 at, int chunk, int (&k)[8])
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        const int j = chunk * CHUNK + i * 256 + lane * 4;
+        int4 v = {NOT_ALLOWED, NOT_ALLOWED, NOT_ALLOWED, NOT_ALLOWED};
+        if (j < g.key_ld) v = *reinterpret_cast<const int4 *>(g.keys + (size_t)at * g.key_ld + j);
+        k[4 * i] = v.x, k[4 * i + 1] = v.y, k[4 * i + 2] = v.z, k[4 * i + 3] = v.w;
+    }
+}
+
+__global__ __launch_bounds__(THREADS) void count_kernel(sample_args g)
+{
+    __shared__ u32 count[BINS];
+    __shared__ u64 sum[BINS];
+    __shared__ u32 red[WAVES];
+    const int tid = threadIdx.x;
+    const u32 at = fd_div(blockIdx.x, g.dBlocks), block = blockIdx.x - at * g.blocks;
+    const row_rule rule = rule_of(g.params[g.row0 + at], g.f);
+    if (!rule.few && rule.part == 1u << 30) return;
+    int k[8];
+    load_keys(g, at, (int)block * WAVES + (tid >> 6), k);
+    for (int i = tid; i < BINS; i += THREADS) count[i] = 0, sum[i] = 0;
+    const int top = top_of(g, at, red);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const u32 d = (u32)top - (u32)k[i];
+        if (k[i] == NOT_ALLOWED || d >= rule.reach) continue;
+        atomicAdd(&count[d >> rule.bin_shift], 1u);
+        atomicAdd((unsigned long long *)&sum[d >> rule.bin_shift], (unsigned long long)rule.weight(d));
+    }
+    __syncthreads();
+    for (int i = tid; i < BINS; i += THREADS)
+        if (count[i]) {
+            atomicAdd(g.count + (size_t)at * BINS + i, count[i]);
+            atomicAdd((unsigned long long *)(g.sum + (size_t)at * BINS + i), (unsigned long long)sum[i]);
+        }
+}
+
+// the plan of a row from its histogram in memory
+__device__ __forceinline__ row_plan load_plan(const sample_args &g, u32 at, row_state &s, const row_rule &rule)
+{
+    if (!rule.few && rule.part == 1u << 30) return {rule.reach, {0, 0, 0, 0}, {0, 0, 0, 0}};
+    for (int i = threadIdx.x; i < BINS; i += THREADS) s.count[i] = g.count[(size_t)at * BINS + i], s.sum[i] = g.sum[(size_t)at * BINS + i];
+    __syncthreads();
+    return plan_row(s, rule);
+}
+
+__device__ __forceinline__ bool in_ranges(const row_plan &p, u32 d) { return d - p.few.lo < p.few.span || d - p.part.lo < p.part.span; }
+
+__global__ __launch_bounds__(THREADS) void collect_kernel(sample_args g)
+{
+    __shared__ row_state s;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const u32 at = fd_div(blockIdx.x, g.dBlocks), block = blockIdx.x - at * g.blocks;
+    const row_rule rule = rule_of(g.params[g.row0 + at], g.f);
+    const int chunk = (int)block * WAVES + (tid >> 6);
+    int k[8];
+    load_keys(g, at, chunk, k);
+    const int top = top_of(g, at, s.red32);
+    const row_plan plan = load_plan(g, at, s, rule);
+    u64 sum = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const u32 d = (u32)top - (u32)k[i];
+        const bool live = k[i] != NOT_ALLOWED && d < rule.reach;
+        if (live && d < plan.sure) {
+            const u32 w = rule.weight(d);
+            if (w >= rule.least) sum += w;
+        }
+        const bool mine = live && in_ranges(plan, d);
+        const unsigned long long all = __ballot(mine);
+        if (all) {
+            u32 first = 0;
+            if (lane == 0) first = atomicAdd(g.listed + at, (u32)__popcll(all));
+            first = (u32)__shfl((int)first, 0) + (u32)__popcll(all & ((1ull << lane) - 1));
+            if (mine && first < (u32)SAMPLE_LIST) g.list[(size_t)at * SAMPLE_LIST + first] = (u64)d << 20 | (u32)(chunk * CHUNK + (i >> 2) * 256 + lane * 4 + (i & 3));
+        }
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) g.chunks[(size_t)at * g.blocks * WAVES + chunk] = sum;
+}
+
+__global__ __launch_bounds__(THREADS) void pick_kernel(sample_args g)
+{
+    __shared__ row_state s;
+    const int tid = threadIdx.x, row = g.row0 + blockIdx.x;
+    const u32 at = blockIdx.x;
+    const row_rule rule = rule_of(g.params[row], g.f);
+    const int top = top_of(g, at, s.red32);
+    if (top == NOT_ALLOWED) {
+        if (tid == 0) g.tokens[row] = -1, g.shown[row] = 0;
+        return;
+    }
+    const row_plan plan = load_plan(g, at, s, rule);
+    const int *keys = g.keys + (size_t)at * g.key_ld;
+    const u64 *list = g.list + (size_t)at * SAMPLE_LIST;
+    const u32 listed = g.listed[at];
+    auto each = [&](auto &&f) {
+        if (listed <= (u32)SAMPLE_LIST) {
+            for (u32 i = tid; i < listed; i += THREADS) f((u32)(list[i] >> 20), (int)(list[i] & 0xFFFFF));
+            return;
+        }
+        for (int j = tid; j < g.vocab; j += THREADS) {   // many equal logits
+            const u32 d = (u32)top - (u32)keys[j];
+            if (keys[j] != NOT_ALLOWED && d < rule.reach && in_ranges(plan, d)) f(d, j);
+        }
+    };
+    draw_token(g, row, s, rule, plan, top, each, [&](int c) { return g.chunks[(size_t)at * g.blocks * WAVES + c]; }, [&](int j) { return keys[j]; });
+}
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
 }  // namespace
 
-hipError_t ss_launch_sample(const ss_sampling &q, const u64 *logits, size_t ld, int rows, int vocab, int f, const ss_rec_params &rp, void *room, long long *tokens,
-                            int *shown, hipStream_t stream)
+hipError_t ss_launch_sample(const sample_plan &plan, const ss_sampling &q, const u64 *logits, size_t ld, int rows, int vocab, int f, const ss_rec_params &rp,
+                            void *room, long long *tokens, int *shown, hipStream_t stream)
 {
-    const sample_args g = {logits, ld, rows, vocab, f, q.params, q.random, q.allowed, q.ld_allowed, (int *)room, tokens, shown};
-    hipLaunchKernelGGL(sample_kernel, dim3(rows), dim3(THREADS), 0, stream, g, rp);
+    sample_args g = {};
+    g.logits = logits, g.ld = ld, g.rows = rows, g.vocab = vocab, g.f = f;
+    g.params = q.params, g.random = q.random, g.allowed = q.allowed, g.ld_allowed = q.ld_allowed, g.tokens = tokens, g.shown = shown;
+    if (plan.small) {
+        hipLaunchKernelGGL(sample_kernel, dim3(rows), dim3(THREADS), 0, stream, g, rp);
+        return hipGetLastError();
+    }
+    g.opens = plan.opens, g.blocks = plan.blocks, g.key_ld = plan.key_ld;
+    g.dOpens = make_fdiv((u32)plan.opens), g.dBlocks = make_fdiv((u32)plan.blocks);
+    char *at = (char *)room;
+    g.sum = (u64 *)at, at += (size_t)plan.slab * BINS * 8;
+    g.chunks = (u64 *)at, at += (size_t)plan.slab * plan.blocks * WAVES * 8;
+    g.list = (u64 *)at, at += (size_t)plan.slab * SAMPLE_LIST * 8;
+    g.keys = (int *)at, at += (size_t)plan.slab * plan.key_ld * 4;
+    g.count = (u32 *)at, at += (size_t)plan.slab * BINS * 4;
+    g.tops = (int *)at, at += (size_t)plan.slab * plan.opens * 4;
+    g.listed = (u32 *)at;
+    const bool wide = ld % 2 == 0 && aligned16(logits);
+    const bool streams = (size_t)rp.m * rows * vocab * 8 > STREAMED_BYTES;
+    for (g.row0 = 0; g.row0 < rows; g.row0 += plan.slab) {
+        const unsigned now = (unsigned)std::min(plan.slab, rows - g.row0);
+        hipLaunchKernelGGL((!wide ? open_kernel<false, false> : streams ? open_kernel<true, true> : open_kernel<true, false>), dim3(now * plan.opens), dim3(OPEN_THREADS), 0,
+                           stream, g, rp);
+        hipLaunchKernelGGL(count_kernel, dim3(now * plan.blocks), dim3(THREADS), 0, stream, g);
+        hipLaunchKernelGGL(collect_kernel, dim3(now * plan.blocks), dim3(THREADS), 0, stream, g);
+        hipLaunchKernelGGL(pick_kernel, dim3(now), dim3(THREADS), 0, stream, g);
+    }
     return hipGetLastError();
 }
 

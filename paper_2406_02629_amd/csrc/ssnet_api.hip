@@ -1456,7 +1456,7 @@ static bool sample_ok(int rows, int vocab) { return rows >= 1 && rows <= (1 << 2
 
 size_t ssnet_workspace_bytes_sample(const ssnet_ctx *ctx, int rows, int vocab)
 {
-    return ctx && sample_ok(rows, vocab) ? WS_HEADER_BYTES + align256((size_t)rows * vocab * 4) : 0;
+    return ctx && sample_ok(rows, vocab) ? WS_HEADER_BYTES + align256(plan_sample(rows, vocab, SIZE_MAX).bytes) : 0;
 }
 
 int ssnet_sample(ssnet_ctx *ctx, const uint64_t *d_logits, size_t ld, int rows, int vocab, const int *party_ids, int m, const ssnet_sampling *how,
@@ -1470,10 +1470,11 @@ int ssnet_sample(ssnet_ctx *ctx, const uint64_t *d_logits, size_t ld, int rows, 
     rp.m = m;
     for (int i = 0; i < m; i++) rp.plane[i] = party_ids[i] - 1;
     if (!h_lagrange_int(party_ids, m, rp.ilambda, &rp.dinv)) return SSNET_EINVAL;
-    if (scratch_room(ctx) < ssnet_workspace_bytes_sample(ctx, rows, vocab) - WS_HEADER_BYTES) return SSNET_EWORKSPACE;
+    const sample_plan plan = plan_sample(rows, vocab, scratch_room(ctx));
+    if (!plan.slab || !ws_fits(ctx, 0)) return SSNET_EWORKSPACE;
     const ss_sampling q = {(const int4 *)how->d_params, (const long long *)how->d_random, how->d_allowed, how->ld_allowed};
     timed tm(ctx, SSNET_PROF_RECONSTRUCT);
-    hipError_t e = ss_launch_sample(q, d_logits, ld, rows, vocab, ctx->f, rp, ws_scratch(ctx), (long long *)d_tokens, d_shown, ctx->stream);
+    hipError_t e = ss_launch_sample(plan, q, d_logits, ld, rows, vocab, ctx->f, rp, ws_scratch(ctx), (long long *)d_tokens, d_shown, ctx->stream);
     return e == hipSuccess ? SSNET_OK : fail_hip(ctx, e);
 }
 
