@@ -31,13 +31,13 @@ struct sample_args {
     long long *tokens;
     int *shown;                     // probability of the token, 30 fraction bits
     // of the rows of this launch, row0 the first
-    int row0, opens, blocks, key_ld;
-    fdiv dOpens, dBlocks;
+    int row0, opens, groups, chunks, key_ld;
+    fdiv dOpens, dGroups;
     int *keys;                      // [.][key_ld]: logits in units of 2^-min(f, 16)
     int *tops;                      // [.][opens]
     u32 *count;                     // [.][BINS]
     u64 *sum;                       // [.][BINS]
-    u64 *chunks;                    // [.][blocks * THREADS / 64]
+    u64 *sure;                      // [.][chunks]
     u32 *listed;                    // [.]
     u64 *list;                      // [.][SAMPLE_LIST]: distance 2^20 + token
 };
@@ -52,8 +52,21 @@ __device__ __forceinline__ int logit_of(u64 v, int f)
 // what a row asks for, and the weight of a distance
 struct row_rule {
     u32 scale, least, few, part;    // least: smallest weight that is kept; few: top_k or 0; part: top_p, 2^30 for none
-    int shift, bin_shift;
+    int shift, bits;
     u32 reach;                      // distances from here on have no weight
+    __device__ __forceinline__ bool cuts() const { return few || part < 1u << 30; }
+    // Bins of the histogram: distances below 2^(bits + 1) have one each, others share one with those that have the same `bits` + 1 first digits, so
+    // that whatever the temperature is a bin is narrow beside its distance
+    __device__ __forceinline__ u32 bin_of(u32 d) const
+    {
+        const int s = max(0, 31 - bits - __clz((int)d));
+        return ((u32)s << bits) + (d >> s);
+    }
+    __device__ __forceinline__ u32 first_of(u32 bin) const   // the next bin's, less one, is its last
+    {
+        const int s = max(0, (int)(bin >> bits) - 1);
+        return (bin - ((u32)s << bits)) << s;
+    }
     __device__ __forceinline__ u32 weight(u32 distance) const { return power2((u64)distance * scale >> shift); }
     // what tokens that weigh `of` have to be cut to, see top_p
     __device__ __forceinline__ u64 need(u64 of) const
@@ -66,35 +79,46 @@ struct row_rule {
 __device__ __forceinline__ row_rule rule_of(const int4 &p, int f)
 {
     row_rule r;
-    r.scale = (u32)max(p.x, 1 << 14);
+    r.scale = p.x <= 0 ? 0x7FFFFFFFu : (u32)max(p.x, 1 << 14);   // (of the largest logit alone the weight does not depend on it)
     r.least = (u32)min(max(p.w, 1), 1 << 30);
     r.few = p.x <= 0 ? 1 : (u32)max(p.y, 0);
     r.part = (u32)min(max(p.z, 0), 1 << 30);
     r.shift = min(f, 16) + 8;
     r.reach = (u32)(((31ull << (16 + r.shift)) + r.scale - 1) / r.scale);   // <= 31 2^26
-    r.bin_shift = max(0, 32 - __clz((int)(r.reach - 1)) - SAMPLE_BIN_BITS);
+    r.bits = r.reach <= 1u << 22 ? 7 : 6;        // (digits of a distance + 1 - bits) 2^bits bins: up to 22 digits 2048, up to 31 1664
     return r;
 }
 
+// the value of another lane by DPP, 0 where there is none or its row is not in ROWS
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u32 lane_of(u32 v) { return (u32)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 lane_of(u64 v) { return (u64)lane_of<CTRL, ROWS>((u32)(v >> 32)) << 32 | lane_of<CTRL, ROWS>((u32)v); }
+
+__device__ __forceinline__ u32 read_lane(u32 v, int lane) { return (u32)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ u64 read_lane(u64 v, int lane) { return (u64)read_lane((u32)(v >> 32), lane) << 32 | read_lane((u32)v, lane); }
+
 template <typename T>
-__device__ __forceinline__ T wave_upto(T v)      // sum of the lanes up to one's own
+__device__ __forceinline__ T row_upto(T v)       // sum of the 16 lanes of a row up to one's own
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const T x = __shfl_up(v, d);
-        if (lane >= d) v += x;
-    }
+    v += lane_of<0x111, 0xF>(v);                 // row_shr 1, 2, 4, 8
+    v += lane_of<0x112, 0xF>(v);
+    v += lane_of<0x114, 0xF>(v);
+    v += lane_of<0x118, 0xF>(v);
     return v;
 }
 
 template <typename T>
-__device__ __forceinline__ T wave_sum(T v)
+__device__ __forceinline__ T wave_upto(T v)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    v = row_upto(v);
+    v += lane_of<0x142, 0xA>(v);                 // row_bcast 15 to rows 1 and 3, row_bcast 31 to rows 2 and 3
+    v += lane_of<0x143, 0xC>(v);
     return v;
 }
+
+template <typename T>
+__device__ __forceinline__ T wave_sum(T v) { return read_lane(wave_upto(v), 63); }
 
 __device__ __forceinline__ int wave_max(int v)
 {
@@ -107,19 +131,15 @@ __device__ __forceinline__ int wave_max(int v)
 template <typename T>
 __device__ __forceinline__ T block_upto(T v, T *lds, T &all)
 {
-    const int wave = threadIdx.x >> 6;
+    static_assert(WAVES == 16, "a row of lanes adds up the waves");
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     v = wave_upto(v);
     __syncthreads();
     if ((threadIdx.x & 63) == 63) lds[wave] = v;
     __syncthreads();
-    T before = 0;
-    all = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; w++) {
-        if (w < wave) before += lds[w];
-        all += lds[w];
-    }
-    return v + before;
+    const T waves = row_upto(lds[threadIdx.x & 15]);
+    all = read_lane(waves, 15);
+    return wave ? v + read_lane(waves, wave - 1) : v;
 }
 
 struct row_state {
@@ -155,7 +175,6 @@ __device__ __forceinline__ row_plan plan_row(row_state &s, const row_rule &rule)
     if (tid < 3) s.bin[tid] = BINS;
     __syncthreads();
     row_plan p = {rule.reach, {0, 0, 0, 0}, {0, 0, 0, 0}};
-    const u32 width = 1u << rule.bin_shift;
     u64 least = all_sum, most = all_sum;         // what top_k leaves weighs so much
     if (rule.few && all_count >= rule.few) {     // (uniform)
         if (c >= rule.few && c - c0 - c1 < rule.few) {
@@ -166,7 +185,8 @@ __device__ __forceinline__ row_plan plan_row(row_state &s, const row_rule &rule)
             s.red64[0] = second ? s1 : s0;       // (what the block sums left there is no longer needed)
         }
         __syncthreads();
-        p.few = {(u32)s.bin[0] << rule.bin_shift, width, rule.few - s.found_count, s.found_sum};
+        const u32 lo = rule.first_of((u32)s.bin[0]);
+        p.few = {lo, rule.first_of((u32)s.bin[0] + 1) - lo, rule.few - s.found_count, s.found_sum};
         p.sure = p.few.lo;
         least = s.found_sum;
         most = s.found_sum + s.red64[0];
@@ -183,7 +203,8 @@ __device__ __forceinline__ row_plan plan_row(row_state &s, const row_rule &rule)
         };
         look(low, 1), look(high, 2);
         __syncthreads();
-        p.part = {(u32)s.bin[1] << rule.bin_shift, (u32)(s.bin[2] - s.bin[1] + 1) << rule.bin_shift, high - s.found_sum, s.found_sum};
+        const u32 lo = rule.first_of((u32)s.bin[1]);
+        p.part = {lo, rule.first_of((u32)s.bin[2] + 1) - lo, high - s.found_sum, s.found_sum};
         p.sure = p.part.lo;
     }
     return p;
@@ -336,8 +357,8 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(sample_args g, ss_rec_p
         }
     };
     each([&](u32 d, int) {
-        atomicAdd(&s.count[d >> rule.bin_shift], 1u);
-        atomicAdd((unsigned long long *)&s.sum[d >> rule.bin_shift], (unsigned long long)rule.weight(d));
+        atomicAdd(&s.count[rule.bin_of(d)], 1u);
+        atomicAdd((unsigned long long *)&s.sum[rule.bin_of(d)], (unsigned long long)rule.weight(d));
     });
     __syncthreads();
     row_plan plan = plan_row(s, rule);
@@ -357,43 +378,43 @@ __global__ __launch_bounds__(OPEN_THREADS) void open_kernel(sample_args g, ss_re
     const int row = g.row0 + (int)at;
     for (u32 i = block * OPEN_THREADS + tid; i < (u32)BINS; i += g.opens * OPEN_THREADS) g.count[(size_t)at * BINS + i] = 0, g.sum[(size_t)at * BINS + i] = 0;
     if (block == 0 && tid == 0) g.listed[at] = 0;
-    constexpr int PAIRS = SAMPLE_OPEN / OPEN_THREADS / 2;
-    ss_sacc acc[PAIRS][2];
+    // eight tokens to a thread: neighbours two by two (WIDE), or one by one
+    constexpr int PER = SAMPLE_OPEN / OPEN_THREADS;
+    ss_sacc acc[PER];
 #pragma unroll
-    for (int i = 0; i < PAIRS; i++) acc[i][0].clear(), acc[i][1].clear();
-    const int j0 = (int)block * SAMPLE_OPEN + tid * 2;
+    for (int i = 0; i < PER; i++) acc[i].clear();
+    const int j0 = (int)block * SAMPLE_OPEN + (WIDE ? 2 * tid : tid);
+    auto place = [&](int i) { return WIDE ? j0 + (i >> 1) * 2 * OPEN_THREADS + (i & 1) : j0 + i * OPEN_THREADS; };
     for (int q = 0; q < rp.m; q++) {
         const u64 *x = g.logits + ((size_t)rp.plane[q] * g.rows + row) * g.ld;
-        pack_t<2> v[PAIRS];
+        u64 v[PER];
+        if constexpr (WIDE) {
 #pragma unroll
-        for (int i = 0; i < PAIRS; i++) {
-            const int j = j0 + i * 2 * OPEN_THREADS;
-            if constexpr (WIDE) {
+            for (int i = 0; i < PER; i += 2) {
+                const int j = place(i);
+                pack_t<2> p = {{0, 0}};
                 if (j + 1 < g.vocab)
-                    STREAM ? v[i].load_streaming(x + j) : v[i].load(x + j);
+                    STREAM ? p.load_streaming(x + j) : p.load(x + j);
                 else if (j < g.vocab)
-                    v[i].v[0] = x[j], v[i].v[1] = 0;
-                else
-                    v[i].v[0] = v[i].v[1] = 0;
-            } else {
-                v[i].v[0] = x[min(j, g.vocab - 1)];
-                v[i].v[1] = x[min(j + 1, g.vocab - 1)];
+                    p.v[0] = x[j];
+                v[i] = p.v[0], v[i + 1] = p.v[1];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER; i++) {
+                const u64 *from = x + min(place(i), g.vocab - 1);
+                v[i] = STREAM ? __builtin_nontemporal_load(from) : *from;
             }
         }
 #pragma unroll
-        for (int i = 0; i < PAIRS; i++)
-#pragma unroll
-            for (int c = 0; c < 2; c++) acc[i][c].mac(v[i].v[c], rp.ilambda[q]);
+        for (int i = 0; i < PER; i++) acc[i].mac(v[i], rp.ilambda[q]);
     }
-    int top = NOT_ALLOWED;
+    int top = NOT_ALLOWED, *keys = g.keys + (size_t)at * g.key_ld;
 #pragma unroll
-    for (int i = 0; i < PAIRS; i++) {
-        const int j = j0 + i * 2 * OPEN_THREADS;
-        int2 k = {NOT_ALLOWED, NOT_ALLOWED};
-        if (j < g.vocab) k.x = key_of(g, rp, row, j, acc[i][0].value());
-        if (j + 1 < g.vocab) k.y = key_of(g, rp, row, j + 1, acc[i][1].value());
-        if (j < g.key_ld) *reinterpret_cast<int2 *>(g.keys + (size_t)at * g.key_ld + j) = k;
-        top = max(top, max(k.x, k.y));
+    for (int i = 0; i < PER; i++) {
+        const int j = place(i), k = j < g.vocab ? key_of(g, rp, row, j, acc[i].value()) : NOT_ALLOWED;
+        if (j < g.key_ld) keys[j] = k;
+        top = max(top, k);
     }
     top = wave_max(top);
     if ((tid & 63) == 0) red[tid >> 6] = top;
@@ -436,19 +457,25 @@ __global__ __launch_bounds__(THREADS) void count_kernel(sample_args g)
     __shared__ u64 sum[BINS];
     __shared__ u32 red[WAVES];
     const int tid = threadIdx.x;
-    const u32 at = fd_div(blockIdx.x, g.dBlocks), block = blockIdx.x - at * g.blocks;
+    const u32 at = fd_div(blockIdx.x, g.dGroups), group = blockIdx.x - at * g.groups;
     const row_rule rule = rule_of(g.params[g.row0 + at], g.f);
-    if (!rule.few && rule.part == 1u << 30) return;
-    int k[8];
-    load_keys(g, at, (int)block * WAVES + (tid >> 6), k);
+    if (!rule.cuts()) return;
+    int chunk = (int)group * WAVES + (tid >> 6), k[8];
+    load_keys(g, at, chunk, k);
     for (int i = tid; i < BINS; i += THREADS) count[i] = 0, sum[i] = 0;
     const int top = top_of(g, at, red);
+    while (chunk < g.chunks) {
+        int next[8];
+        load_keys(g, at, chunk += g.groups * WAVES, next);
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const u32 d = (u32)top - (u32)k[i];
-        if (k[i] == NOT_ALLOWED || d >= rule.reach) continue;
-        atomicAdd(&count[d >> rule.bin_shift], 1u);
-        atomicAdd((unsigned long long *)&sum[d >> rule.bin_shift], (unsigned long long)rule.weight(d));
+        for (int i = 0; i < 8; i++) {
+            const u32 d = (u32)top - (u32)k[i];
+            if (k[i] != NOT_ALLOWED && d < rule.reach) {
+                atomicAdd(&count[rule.bin_of(d)], 1u);
+                atomicAdd((unsigned long long *)&sum[rule.bin_of(d)], (unsigned long long)rule.weight(d));
+            }
+            k[i] = next[i];
+        }
     }
     __syncthreads();
     for (int i = tid; i < BINS; i += THREADS)
@@ -461,7 +488,7 @@ __global__ __launch_bounds__(THREADS) void count_kernel(sample_args g)
 // the plan of a row from its histogram in memory
 __device__ __forceinline__ row_plan load_plan(const sample_args &g, u32 at, row_state &s, const row_rule &rule)
 {
-    if (!rule.few && rule.part == 1u << 30) return {rule.reach, {0, 0, 0, 0}, {0, 0, 0, 0}};
+    if (!rule.cuts()) return {rule.reach, {0, 0, 0, 0}, {0, 0, 0, 0}};
     for (int i = threadIdx.x; i < BINS; i += THREADS) s.count[i] = g.count[(size_t)at * BINS + i], s.sum[i] = g.sum[(size_t)at * BINS + i];
     __syncthreads();
     return plan_row(s, rule);
@@ -469,17 +496,10 @@ __device__ __forceinline__ row_plan load_plan(const sample_args &g, u32 at, row_
 
 __device__ __forceinline__ bool in_ranges(const row_plan &p, u32 d) { return d - p.few.lo < p.few.span || d - p.part.lo < p.part.span; }
 
-__global__ __launch_bounds__(THREADS) void collect_kernel(sample_args g)
+// What a wave does with a chunk once the plan is known: what is sure of it, its tokens near the cuts to the list
+__device__ __forceinline__ void collect_chunk(const sample_args &g, u32 at, int chunk, const int (&k)[8], int top, const row_rule &rule, const row_plan &plan)
 {
-    __shared__ row_state s;
-    const int tid = threadIdx.x, lane = tid & 63;
-    const u32 at = fd_div(blockIdx.x, g.dBlocks), block = blockIdx.x - at * g.blocks;
-    const row_rule rule = rule_of(g.params[g.row0 + at], g.f);
-    const int chunk = (int)block * WAVES + (tid >> 6);
-    int k[8];
-    load_keys(g, at, chunk, k);
-    const int top = top_of(g, at, s.red32);
-    const row_plan plan = load_plan(g, at, s, rule);
+    const int lane = threadIdx.x & 63;
     u64 sum = 0;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
@@ -499,18 +519,37 @@ __global__ __launch_bounds__(THREADS) void collect_kernel(sample_args g)
         }
     }
     sum = wave_sum(sum);
-    if (lane == 0) g.chunks[(size_t)at * g.blocks * WAVES + chunk] = sum;
+    if (lane == 0) g.sure[(size_t)at * g.chunks + chunk] = sum;
+}
+
+__global__ __launch_bounds__(THREADS) void collect_kernel(sample_args g)
+{
+    __shared__ row_state s;
+    const u32 at = fd_div(blockIdx.x, g.dGroups), group = blockIdx.x - at * g.groups;
+    const row_rule rule = rule_of(g.params[g.row0 + at], g.f);
+    int chunk = (int)group * WAVES + (threadIdx.x >> 6), k[8];
+    load_keys(g, at, chunk, k);
+    const int top = top_of(g, at, s.red32);
+    const row_plan plan = load_plan(g, at, s, rule);
+    while (chunk < g.chunks) {
+        int next[8];
+        load_keys(g, at, chunk + g.groups * WAVES, next);
+        collect_chunk(g, at, chunk, k, top, rule, plan);
+        chunk += g.groups * WAVES;
+#pragma unroll
+        for (int i = 0; i < 8; i++) k[i] = next[i];
+    }
 }
 
 __global__ __launch_bounds__(THREADS) void pick_kernel(sample_args g)
 {
     __shared__ row_state s;
-    const int tid = threadIdx.x, row = g.row0 + blockIdx.x;
+    const int row = g.row0 + blockIdx.x;
     const u32 at = blockIdx.x;
     const row_rule rule = rule_of(g.params[row], g.f);
     const int top = top_of(g, at, s.red32);
     if (top == NOT_ALLOWED) {
-        if (tid == 0) g.tokens[row] = -1, g.shown[row] = 0;
+        if (threadIdx.x == 0) g.tokens[row] = -1, g.shown[row] = 0;
         return;
     }
     const row_plan plan = load_plan(g, at, s, rule);
@@ -519,15 +558,15 @@ __global__ __launch_bounds__(THREADS) void pick_kernel(sample_args g)
     const u32 listed = g.listed[at];
     auto each = [&](auto &&f) {
         if (listed <= (u32)SAMPLE_LIST) {
-            for (u32 i = tid; i < listed; i += THREADS) f((u32)(list[i] >> 20), (int)(list[i] & 0xFFFFF));
+            for (u32 i = threadIdx.x; i < listed; i += THREADS) f((u32)(list[i] >> 20), (int)(list[i] & 0xFFFFF));
             return;
         }
-        for (int j = tid; j < g.vocab; j += THREADS) {   // many equal logits
+        for (int j = threadIdx.x; j < g.vocab; j += THREADS) {   // many equal logits
             const u32 d = (u32)top - (u32)keys[j];
             if (keys[j] != NOT_ALLOWED && d < rule.reach && in_ranges(plan, d)) f(d, j);
         }
     };
-    draw_token(g, row, s, rule, plan, top, each, [&](int c) { return g.chunks[(size_t)at * g.blocks * WAVES + c]; }, [&](int j) { return keys[j]; });
+    draw_token(g, row, s, rule, plan, top, each, [&](int c) { return g.sure[(size_t)at * g.chunks + c]; }, [&](int j) { return keys[j]; });
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -544,11 +583,11 @@ hipError_t ss_launch_sample(const sample_plan &plan, const ss_sampling &q, const
         hipLaunchKernelGGL(sample_kernel, dim3(rows), dim3(THREADS), 0, stream, g, rp);
         return hipGetLastError();
     }
-    g.opens = plan.opens, g.blocks = plan.blocks, g.key_ld = plan.key_ld;
-    g.dOpens = make_fdiv((u32)plan.opens), g.dBlocks = make_fdiv((u32)plan.blocks);
+    g.opens = plan.opens, g.groups = plan.groups, g.chunks = plan.chunks, g.key_ld = plan.key_ld;
+    g.dOpens = make_fdiv((u32)plan.opens), g.dGroups = make_fdiv((u32)plan.groups);
     char *at = (char *)room;
     g.sum = (u64 *)at, at += (size_t)plan.slab * BINS * 8;
-    g.chunks = (u64 *)at, at += (size_t)plan.slab * plan.blocks * WAVES * 8;
+    g.sure = (u64 *)at, at += (size_t)plan.slab * ((plan.chunks + 1) & ~1) * 8;
     g.list = (u64 *)at, at += (size_t)plan.slab * SAMPLE_LIST * 8;
     g.keys = (int *)at, at += (size_t)plan.slab * plan.key_ld * 4;
     g.count = (u32 *)at, at += (size_t)plan.slab * BINS * 4;
@@ -558,10 +597,10 @@ hipError_t ss_launch_sample(const sample_plan &plan, const ss_sampling &q, const
     const bool streams = (size_t)rp.m * rows * vocab * 8 > STREAMED_BYTES;
     for (g.row0 = 0; g.row0 < rows; g.row0 += plan.slab) {
         const unsigned now = (unsigned)std::min(plan.slab, rows - g.row0);
-        hipLaunchKernelGGL((!wide ? open_kernel<false, false> : streams ? open_kernel<true, true> : open_kernel<true, false>), dim3(now * plan.opens), dim3(OPEN_THREADS), 0,
+        hipLaunchKernelGGL((wide ? streams ? open_kernel<true, true> : open_kernel<true, false> : streams ? open_kernel<false, true> : open_kernel<false, false>), dim3(now * plan.opens), dim3(OPEN_THREADS), 0,
                            stream, g, rp);
-        hipLaunchKernelGGL(count_kernel, dim3(now * plan.blocks), dim3(THREADS), 0, stream, g);
-        hipLaunchKernelGGL(collect_kernel, dim3(now * plan.blocks), dim3(THREADS), 0, stream, g);
+        hipLaunchKernelGGL(count_kernel, dim3(now * plan.groups), dim3(THREADS), 0, stream, g);
+        hipLaunchKernelGGL(collect_kernel, dim3(now * plan.groups), dim3(THREADS), 0, stream, g);
         hipLaunchKernelGGL(pick_kernel, dim3(now), dim3(THREADS), 0, stream, g);
     }
     return hipGetLastError();

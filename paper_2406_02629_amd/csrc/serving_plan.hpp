@@ -70,14 +70,14 @@ constexpr int SMALL_VOCAB = 8192;             // tokens whose logits one workgro
 constexpr int SAMPLE_BIN_BITS = 11, SAMPLE_BINS = 1 << SAMPLE_BIN_BITS;
 constexpr int SAMPLE_OPEN = 2048;             // tokens to a workgroup that opens
 constexpr int SAMPLE_CHUNK = 512;             // to a wave that counts or collects: 2^20 tokens are 2048 chunks
-constexpr int SAMPLE_BLOCK = 16 * SAMPLE_CHUNK;
 constexpr int SAMPLE_LIST = 4096;             // tokens near a cut that are listed (more are found among all)
 constexpr size_t SAMPLE_ROOM = (size_t)512 << 20;
 
 struct sample_plan {
-    bool small;
+    bool small;                   // one launch
     int slab;                     // rows at a time, 0: the room is too small
-    int opens, blocks, key_ld;    // workgroups of a row that open, that count; its keys with what fills the last 16 bytes
+    int opens, groups;            // workgroups of a row that open, that count
+    int chunks, key_ld;           // of a row; its keys with what fills the last 16 bytes
     size_t bytes;
 };
 
@@ -88,9 +88,10 @@ inline sample_plan plan_sample(int rows, int vocab, size_t room)
     p.slab = rows;
     if (p.small) return p;
     p.opens = (int)div_up(vocab, SAMPLE_OPEN);
-    p.blocks = (int)div_up(vocab, SAMPLE_BLOCK);
+    p.chunks = (int)div_up(vocab, SAMPLE_CHUNK);
+    p.groups = (int)std::min(div_up(p.chunks, 16), div_up(512, rows));
     p.key_ld = (vocab + 3) & ~3;
-    const size_t row = (size_t)SAMPLE_BINS * 12 + (size_t)p.blocks * 16 * 8 + (size_t)SAMPLE_LIST * 8 + (size_t)p.key_ld * 4 + (size_t)p.opens * 4 + 4;
+    const size_t row = (size_t)SAMPLE_BINS * 12 + (size_t)((p.chunks + 1) & ~1) * 8 + (size_t)SAMPLE_LIST * 8 + (size_t)p.key_ld * 4 + (size_t)p.opens * 4 + 4;
     const size_t most = std::max<size_t>(1, std::min(room, SAMPLE_ROOM) / row);
     p.slab = (int)std::min<size_t>(std::min<size_t>(rows, most), MAX_SERVING_GROUPS / p.opens / 4);
     p.bytes = p.slab * row;
