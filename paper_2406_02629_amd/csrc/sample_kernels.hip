@@ -4,7 +4,7 @@
 // what they weigh, says in which bin a cut lies; the tokens of that bin alone are looked at further.
 //
 // Up to SMALL_VOCAB tokens one workgroup takes a row in one launch.  Longer rows go through four, so that many workgroups share a row:
-//   open     REC, and the largest logit of every 2048
+//   open     REC, and the largest logit of every 1024
 //   count    the histogram
 //   collect  what the tokens weigh that stay whatever the cut is, for every 512; the tokens of the bins with a cut, in a list
 //   pick     the cut, the weights of the list's tokens that stay, and the draw
@@ -378,9 +378,9 @@ __global__ __launch_bounds__(OPEN_THREADS) void open_kernel(sample_args g, ss_re
     const int row = g.row0 + (int)at;
     for (u32 i = block * OPEN_THREADS + tid; i < (u32)BINS; i += g.opens * OPEN_THREADS) g.count[(size_t)at * BINS + i] = 0, g.sum[(size_t)at * BINS + i] = 0;
     if (block == 0 && tid == 0) g.listed[at] = 0;
-    // eight tokens to a thread: neighbours two by two (WIDE), or one by one
+    // four tokens to a thread: neighbours two by two (WIDE), or one by one
     constexpr int PER = SAMPLE_OPEN / OPEN_THREADS;
-    ss_sacc acc[PER];
+    ss_sacc2 acc[PER];
 #pragma unroll
     for (int i = 0; i < PER; i++) acc[i].clear();
     const int j0 = (int)block * SAMPLE_OPEN + (WIDE ? 2 * tid : tid);
@@ -407,7 +407,10 @@ __global__ __launch_bounds__(OPEN_THREADS) void open_kernel(sample_args g, ss_re
             }
         }
 #pragma unroll
-        for (int i = 0; i < PER; i++) acc[i].mac(v[i], rp.ilambda[q]);
+        for (int i = 0; i < PER; i++) {
+            SS_SPLIT31(v[i], w0, w1);
+            acc[i].mac(w0, w1, rp.ilambda[q]);
+        }
     }
     int top = NOT_ALLOWED, *keys = g.keys + (size_t)at * g.key_ld;
 #pragma unroll

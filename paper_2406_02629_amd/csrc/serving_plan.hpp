@@ -68,7 +68,7 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
 
 constexpr int SMALL_VOCAB = 8192;             // tokens whose logits one workgroup holds
 constexpr int SAMPLE_BIN_BITS = 11, SAMPLE_BINS = 1 << SAMPLE_BIN_BITS;
-constexpr int SAMPLE_OPEN = 2048;             // tokens to a workgroup that opens
+constexpr int SAMPLE_OPEN = 1024;             // tokens to a workgroup that opens
 constexpr int SAMPLE_CHUNK = 512;             // to a wave that counts or collects: 2^20 tokens are 2048 chunks
 constexpr int SAMPLE_LIST = 4096;             // tokens near a cut that are listed (more are found among all)
 constexpr size_t SAMPLE_ROOM = (size_t)512 << 20;
