@@ -8,6 +8,7 @@
 #include "digits.hpp"
 #include "diagonals.hpp"
 #include "truncation.hpp"
+#include "lanes.hpp"
 
 namespace SS_NS {
 
@@ -60,7 +61,7 @@ __global__ __launch_bounds__(BLOCK) void pack_up_kernel(const u64 *b, signed cha
 
 struct adapter_args {
     const int *start, *adapter;     // [requests + 1], [requests]
-    int requests, tokens, adapters;
+    int requests, tokens, adapters, grouped;
     int K, rank, padded, N;
     const signed char *down, *up;
     size_t down_party, up_party, down_bytes, up_bytes;   // of a party, of an adapter
@@ -74,42 +75,73 @@ struct adapter_args {
     size_t plane;                   // 2t+1 shares
 };
 
-// the tokens of a tile, all of one request
-struct request_tile {
-    int first, count, adapter;      // adapter: -1 if the request has none
+// the tokens of a tile, all with one adapter
+struct row_tile {
+    int count, adapter;             // adapter: -1 if they have none
 };
 
-// tile number -> its tokens; every lane of the wave calls.  False: no such tile.
-__device__ __forceinline__ bool tile_at(const adapter_args &g, int tile, int rows, request_tile &r)
+// Tile number -> its tokens, `most` at most, to rows in LDS (everyone's after the next barrier); all waves call.  False: no such tile.
+// Tiles follow one another request by request, or (grouped) tile i is that of token i, which has the tokens behind it with the same adapter too, whichever requests
+// they belong to, if the number of those in front of it is a multiple of `most`, and is none otherwise: requests of single tokens read an adapter that they
+// share once.
+__device__ __forceinline__ bool find_rows(const adapter_args &g, int tile, int most, int *rows, row_tile &r)
 {
     const int lane = threadIdx.x & 63;
-    int base = 0;
-    for (int b0 = 0; b0 < g.requests; b0 += 64) {
-        const int b = b0 + lane;
-        int first = 0, count = 0;
-        if (b < g.requests) {
-            first = min(max(g.start[b], 0), g.tokens);
-            count = max(0, min(g.start[b + 1], g.tokens) - first);
+    auto request = [&](int b, int &first, int &count, int &adapter) {
+        first = count = 0, adapter = -1;
+        if (b >= g.requests) return;
+        first = min(max(g.start[b], 0), g.tokens);
+        count = max(0, min(g.start[b + 1], g.tokens) - first);
+        adapter = g.adapter[b];
+        if (adapter < 0 || adapter >= g.adapters) adapter = -1;
+    };
+    auto keep = [&](int first, int count, int adapter) {
+        r = {__builtin_amdgcn_readfirstlane(min(most, count)), __builtin_amdgcn_readfirstlane(adapter)};
+        if ((int)threadIdx.x < r.count) rows[threadIdx.x] = first + threadIdx.x;
+        return true;
+    };
+    int first, count, adapter;
+    if (!g.grouped) {
+        int base = 0;
+        for (int b0 = 0; b0 < g.requests; b0 += 64) {
+            request(b0 + lane, first, count, adapter);
+            const int mine = (count + most - 1) / most, upto = (int)wave_upto((u32)mine);
+            const unsigned long long past = __ballot(base + upto > tile);
+            if (past) {
+                const int l = __ffsll((long long)past) - 1, at = (tile - base - __builtin_amdgcn_readlane(upto - mine, l)) * most;
+                return keep(__builtin_amdgcn_readlane(first, l) + at, __builtin_amdgcn_readlane(count, l) - at, __builtin_amdgcn_readlane(adapter, l));
+            }
+            base += __builtin_amdgcn_readlane(upto, 63);
         }
-        const int mine = (count + rows - 1) / rows;
-        int upto = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int v = __shfl_up(upto, d);
-            if (lane >= d) upto += v;
-        }
-        const unsigned long long past = __ballot(base + upto > tile);
-        if (past) {
-            const int l = __ffsll((long long)past) - 1, at = (tile - base - __shfl(upto - mine, l)) * rows;
-            r.first = __builtin_amdgcn_readfirstlane(__shfl(first, l) + at);
-            r.count = __builtin_amdgcn_readfirstlane(min(rows, __shfl(count, l) - at));
-            const int adapter = fixed_at(g.adapter, (size_t)__builtin_amdgcn_readfirstlane(b0 + l));
-            r.adapter = adapter < 0 || adapter >= g.adapters ? -1 : adapter;
-            return true;
-        }
-        base += __shfl(upto, 63);
+        return false;
     }
-    return false;
+    int owner = -1, wanted = -1, place = 0;
+    for (int b0 = 0; b0 < g.requests && owner < 0; b0 += 64) {
+        request(b0 + lane, first, count, adapter);
+        const unsigned long long mine = __ballot(tile >= first && tile < first + count);
+        if (!mine) continue;
+        const int l = __ffsll((long long)mine) - 1;
+        owner = b0 + l, wanted = __builtin_amdgcn_readlane(adapter, l), place = tile - __builtin_amdgcn_readlane(first, l);
+    }
+    if (owner < 0) return false;
+    if (wanted < 0) return keep(tile, 1, -1);
+    int behind = 0;                              // tokens listed so far
+    for (int b0 = 0; b0 < g.requests; b0 += 64) {
+        request(b0 + lane, first, count, adapter);
+        if (adapter != wanted) count = 0;
+        const bool before = b0 + lane < owner;
+        place += (int)wave_sum((u32)(before ? count : 0));
+        if (b0 + 64 <= owner) continue;
+        if (before) count = 0;
+        if (b0 + lane == owner) count -= tile - first, first = tile;
+        if (b0 <= owner && place % most) return false;
+        const int upto = (int)wave_upto((u32)count), at = behind + upto - count;
+        for (int i = 0; i < count && at + i < most; i++) rows[at + i] = first + i;
+        behind += __builtin_amdgcn_readlane(upto, 63);
+        if (behind >= most) break;
+    }
+    r = {min(behind, most), wanted};
+    return true;
 }
 
 // Step 1: one workgroup per (tile of 16 tokens, party and run of the contraction).  Its four waves share the columns of A between CW and the blocks of
@@ -121,21 +153,23 @@ __global__ __launch_bounds__(BLOCK, 2) void down_kernel(adapter_args g)
     constexpr int KW = 4 / CW, PAIRS = 8 / CW, WORDS = 4 / CW;
     __shared__ v4i xd[CW > 1 ? 2 : 1][CW > 1 ? KW * TILE : 1];
     __shared__ int sums[KW > 1 ? CW : 1][KW > 1 ? ND : 1][BLOCK];
+    __shared__ int rows[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const unsigned slot = xcd_slot(blockIdx.x, gridDim.x), run = fd_div(slot, g.dTiles);
+    const unsigned slot = g.grouped ? blockIdx.x : xcd_slot(blockIdx.x, gridDim.x), run = fd_div(slot, g.dTiles);
     const int cw = wave % CW, kw = wave / CW, split = (int)(run / (unsigned)g.nr), party = (int)run - split * g.nr, q = lane >> 4, c16 = lane & 15;
-    request_tile r;
-    if (!tile_at(g, (int)(slot - run * g.tiles), 16, r)) return;
-    u64 *out = g.planes + split * g.plane + ((size_t)party * g.tokens + r.first) * g.rank;
+    row_tile r;
+    if (!find_rows(g, (int)(slot - run * g.tiles), 16, rows, r)) return;
+    u64 *out = g.planes + split * g.plane + (size_t)party * g.tokens * g.rank;
+    __syncthreads();
     if (r.adapter < 0) {
-        for (int i = tid; i < r.count * g.rank; i += BLOCK) out[i] = 0;
+        for (int i = tid; i < r.count * g.rank; i += BLOCK) out[(size_t)rows[i / g.rank] * g.rank + i % g.rank] = 0;
         return;
     }
     if constexpr (KW > 1) {
         for (int i = tid; i < CW * ND * BLOCK; i += BLOCK) (&sums[0][0][0])[i] = 0;
     }
     const int begin = split * g.run, end = min(begin + g.run, (g.K + 63) >> 6), turns = (end - begin + KW - 1) / KW;
-    const u64 *row = g.x + ((size_t)party * g.tokens + r.first + min(c16, r.count - 1)) * g.ld_x;
+    const u64 *row = g.x + ((size_t)party * g.tokens + rows[min(c16, r.count - 1)]) * g.ld_x;
     const size_t limb = (size_t)g.rank * 64;
     const signed char *a = g.down + r.adapter * g.down_bytes + party * g.down_party + (size_t)q * g.rank * 16;
     size_t column[CT];
@@ -224,7 +258,7 @@ __global__ __launch_bounds__(BLOCK, 2) void down_kernel(adapter_args g)
             v4i total[ND];
 #pragma unroll
             for (int s = 0; s < ND; s++) total[s][0] = sums[c][s][tid];
-            out[token * g.rank + col] = fold_diagonals(total, 0);
+            out[(size_t)rows[token] * g.rank + col] = fold_diagonals(total, 0);
         }
     } else {
 #pragma unroll
@@ -232,7 +266,7 @@ __global__ __launch_bounds__(BLOCK, 2) void down_kernel(adapter_args g)
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 const int token = 4 * q + i, col = (cw * CT + c) * 16 + c16;
-                if (token < r.count && col < g.rank) out[token * g.rank + col] = fold_diagonals(acc[c], i);
+                if (token < r.count && col < g.rank) out[(size_t)rows[token] * g.rank + col] = fold_diagonals(acc[c], i);
             }
     }
 }
@@ -246,42 +280,25 @@ __device__ __forceinline__ void exchange(int (&v)[4])
     v[0] = (int)lo[0], v[1] = (int)lo[1], v[2] = (int)hi[0], v[3] = (int)hi[1];
 }
 
-__device__ __forceinline__ u64 fold_parts(const long long (&g)[4], u64 more)
+// Four items' diagonal sums 4 q .. 4 q + 3 of a column in row q -> in row q item q's field element plus `more`.  The sums lie below 2^22 (a rank of at
+// most 32: 8 * 32 * 2^14), so that two of them fit 32 bits.
+__device__ __forceinline__ u64 fold_items(const v4i (&acc)[4], u64 more)
 {
+    int lo[4], hi[4];
+    long long g[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        lo[i] = acc[i][0] + (int)((u32)acc[i][1] << 8);
+        hi[i] = acc[i][2] + (int)((u32)acc[i][3] << 8);
+    }
+    exchange(lo), exchange(hi);
+#pragma unroll
+    for (int q = 0; q < 4; q++) g[q] = mad_i64(hi[q], 1 << 16, (long long)lo[q]);
 #if defined(SS_FIELD_P45)
     return fold_words((u64)(g[0] + WORD_OFFSET), (u64)(g[1] + WORD_OFFSET), (u64)(g[2] + WORD_OFFSET), more);
 #else
     return fold_words(g[0], g[1], g[2], g[3], more);
 #endif
-}
-
-// Four items' diagonal sums 4 q .. 4 q + 3 of a column in row q -> in row q item q's field element plus `more`.  SHORT: sums below 2^22 (a rank of at
-// most 32: 8 * 32 * 2^14), two of which fit 32 bits.
-template <bool SHORT>
-__device__ __forceinline__ u64 fold_items(const v4i (&acc)[4], u64 more)
-{
-    int lo[4], hi[4];
-    long long g[4];
-    if constexpr (SHORT) {
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            lo[i] = acc[i][0] + (int)((u32)acc[i][1] << 8);
-            hi[i] = acc[i][2] + (int)((u32)acc[i][3] << 8);
-        }
-        exchange(lo), exchange(hi);
-#pragma unroll
-        for (int q = 0; q < 4; q++) g[q] = mad_i64(hi[q], 1 << 16, (long long)lo[q]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const long long w = join4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
-            lo[i] = (int)w, hi[i] = (int)(w >> 32);
-        }
-        exchange(lo), exchange(hi);
-#pragma unroll
-        for (int q = 0; q < 4; q++) g[q] = (long long)((u64)(u32)hi[q] << 32 | (u32)lo[q]);
-    }
-    return fold_parts(g, more);
 }
 
 // y = 0 in the rows of all requests, where there is no base
@@ -292,12 +309,12 @@ __global__ __launch_bounds__(BLOCK) void clear_kernel(adapter_args g)
         for (int c = threadIdx.x; c < g.N; c += BLOCK) g.y[((size_t)blockIdx.y * g.tokens + t) * g.ld_y + c] = 0;
 }
 
-// y = base of the tokens of a request without an adapter
-__device__ __forceinline__ void pass_through(const adapter_args &g, const request_tile &r, const u64 *base, u64 *y, int part)
+// y = base of tokens without an adapter; rows: in LDS, behind a barrier
+__device__ __forceinline__ void pass_through(const adapter_args &g, const row_tile &r, const int *rows, const u64 *base, u64 *y, int part)
 {
     if (base == y) return;
     for (int t = 0; t < r.count; t++)
-        for (int c = part * BLOCK + threadIdx.x; c < g.N; c += g.col_groups * BLOCK) y[t * g.ld_y + c] = base[t * g.ld_base + c];
+        for (int c = part * BLOCK + threadIdx.x; c < g.N; c += g.col_groups * BLOCK) y[rows[t] * g.ld_y + c] = base[rows[t] * g.ld_base + c];
 }
 
 // How a tensor is read and written: element by element, two neighbours in 16 bytes, or these past the caches
@@ -338,14 +355,14 @@ __device__ __forceinline__ void store_pair(u64 *row, int col, int N, const pack_
 // and zeros around them, read from a place that moves up by the rank with every diagonal: limb l of element i of a token lies at (15 - l) R + i.
 __device__ __forceinline__ int diagonals_stride(int R, int steps) { return 15 * R + 64 * steps; }
 
-__device__ __forceinline__ void stage_diagonals(const adapter_args &g, signed char *zd, int rows, int stride, int party, const request_tile &r)
+__device__ __forceinline__ void stage_diagonals(const adapter_args &g, signed char *zd, int places, int stride, int party, const row_tile &r, const int *rows)
 {
     const int tid = threadIdx.x;
-    for (int i = tid * 4; i < rows * stride; i += BLOCK * 4) *reinterpret_cast<int *>(zd + i) = 0;
+    for (int i = tid * 4; i < places * stride; i += BLOCK * 4) *reinterpret_cast<int *>(zd + i) = 0;
     __syncthreads();
     for (int i = tid; i < r.count * g.rank; i += BLOCK) {
         const int t = i / g.rank, e = i - t * g.rank;
-        const u64 d = balanced_digits(g.z[((size_t)party * g.tokens + r.first) * g.rank + i]);
+        const u64 d = balanced_digits(g.z[((size_t)party * g.tokens + rows[t]) * g.rank + e]);
 #pragma unroll
         for (int l = 0; l < NL; l++) zd[t * stride + (15 - l) * g.padded + e] = (signed char)(d >> (8 * l));
     }
@@ -361,60 +378,26 @@ __device__ __forceinline__ v4i diagonals_at(const signed char *zd, int R, int m)
     return (v4i){a.x, a.y, b.x, b.y};
 }
 
-// Single tokens.  One workgroup per (token, part of the columns and party); a wave takes 64 columns at a time.
-__global__ __launch_bounds__(BLOCK, 2) void up_single_kernel(adapter_args g)
-{
-    extern __shared__ signed char zd[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int part = blockIdx.y / g.n, party = blockIdx.y - part * g.n;
-    request_tile r;
-    if (!tile_at(g, blockIdx.x, 1, r)) return;
-    const u64 *base = g.base + ((size_t)party * g.tokens + r.first) * g.ld_base;
-    u64 *y = g.y + ((size_t)party * g.tokens + r.first) * g.ld_y;
-    if (r.adapter < 0) {
-        pass_through(g, r, base, y, part);
-        return;
-    }
-    const int R = g.padded, chunks = NL * R / 16, steps = (chunks + 3) >> 2, halves = 2 * ((g.N + 31) >> 5), q = lane >> 4, c16 = lane & 15;
-    stage_diagonals(g, zd, 1, diagonals_stride(R, steps), party, r);
-    const signed char *b = g.up + r.adapter * g.up_bytes + party * g.up_party + c16 * 16;
-    for (int u = part * 4 + wave; u * 64 < g.N; u += g.col_groups * 4) {
-        v4i acc[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) acc[i] = (v4i){0, 0, 0, 0};
-        const int col = 64 * u + 32 * (q >> 1) + 2 * c16 + (q & 1);
-        const u64 more = col < g.N ? base[col] : 0;
-        for (int m = 0; m < steps; m++) {
-            const v4i a = diagonals_at(zd, R, m);
-            const int chunk = 4 * m + q;
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const v4i v = *reinterpret_cast<const v4i *>(b + ((size_t)min(4 * u + i, halves - 1) * chunks + min(chunk, chunks - 1)) * 256);
-                acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, chunk < chunks ? v : (v4i){0, 0, 0, 0}, acc[i], 0, 0, 0);
-            }
-        }
-        const u64 o = fold_items<false>(acc, more);
-        if (col < g.N) y[col] = o;
-    }
-}
-
 // Tiles of UP_ROWS tokens of a request whose rank takes M products.  A wave keeps the digits of 128 columns of B in registers and takes the tokens one
 // after the other, each a result of 1 KB in a row; the next token's digits and the base of those after it are on their way.
-constexpr int UP_ROWS = 16;
 template <int M, access MODE>
 __global__ __launch_bounds__(BLOCK, 2) void up_diagonals_kernel(adapter_args g)
 {
     extern __shared__ signed char zd[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = blockIdx.y / g.n, party = blockIdx.y - part * g.n;
-    request_tile r;
-    if (!tile_at(g, (int)xcd_slot(blockIdx.x, gridDim.x), UP_ROWS, r)) return;
-    const u64 *base = g.base + ((size_t)party * g.tokens + r.first) * g.ld_base;
-    u64 *y = g.y + ((size_t)party * g.tokens + r.first) * g.ld_y;
+    __shared__ int rows[UP_ROWS];
+    row_tile r;
+    // (of grouped tiles those that there are stand in front: they are spread over the XCDs)
+    if (!find_rows(g, g.grouped ? (int)blockIdx.x : (int)xcd_slot(blockIdx.x, gridDim.x), UP_ROWS, rows, r)) return;
+    const u64 *base = g.base + (size_t)party * g.tokens * g.ld_base;
+    u64 *y = g.y + (size_t)party * g.tokens * g.ld_y;
+    __syncthreads();
     if (r.adapter < 0) {
-        pass_through(g, r, base, y, part);
+        pass_through(g, r, rows, base, y, part);
         return;
     }
+    const int own_row = rows[min(lane & (UP_ROWS - 1), r.count - 1)];   // of the token with the lane's number
     const int R = g.padded, chunks = NL * R / 16, stride = diagonals_stride(R, M), q = lane >> 4, c16 = lane & 15;
     const int blocks = (g.N + 31) >> 5, units = (blocks + 3) >> 2, step = g.col_groups * 4;
     const signed char *b = g.up + r.adapter * g.up_bytes + party * g.up_party;
@@ -433,13 +416,13 @@ __global__ __launch_bounds__(BLOCK, 2) void up_diagonals_kernel(adapter_args g)
     constexpr int AHEAD = 4;
     pack_t<2> more[AHEAD];
     int unit = part * 4 + wave;
-    auto load_base = [&](int t, int u) { return load_pair<MODE>(base + (size_t)min(t, r.count - 1) * g.ld_base, 128 * u + 32 * q + 2 * c16, g.N); };
+    auto load_base = [&](int t, int u) { return load_pair<MODE>(base + (size_t)__builtin_amdgcn_readlane(own_row, min(t, r.count - 1)) * g.ld_base, 128 * u + 32 * q + 2 * c16, g.N); };
     if (unit < units) {
         load_b(unit);
 #pragma unroll
         for (int i = 0; i < AHEAD; i++) more[i] = load_base(i, unit);
     }
-    stage_diagonals(g, zd, UP_ROWS + 1, stride, party, r);
+    stage_diagonals(g, zd, UP_ROWS + 1, stride, party, r, rows);
     auto digits = [&](int t, v4i (&a)[M]) {
 #pragma unroll
         for (int m = 0; m < M; m++) {
@@ -466,10 +449,10 @@ __global__ __launch_bounds__(BLOCK, 2) void up_diagonals_kernel(adapter_args g)
 #pragma unroll
                         for (int k = 0; k < 4; k++)
                             acc[k] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i & 1][m], w[h][k][m], m ? acc[k] : (v4i){0, 0, 0, 0}, 0, 0, 0);
-                    o.v[h] = fold_items<true>(acc, more[i].v[h]);
+                    o.v[h] = fold_items(acc, more[i].v[h]);
                 }
                 more[i] = load_base(t + AHEAD, unit);
-                store_pair<MODE>(y + (size_t)t * g.ld_y, col, g.N, o);
+                store_pair<MODE>(y + (size_t)__builtin_amdgcn_readlane(own_row, t) * g.ld_y, col, g.N, o);
             }
         }
         if (unit + step < units) {
@@ -488,22 +471,29 @@ __global__ __launch_bounds__(BLOCK, 2) void up_tile_kernel(adapter_args g)
     extern __shared__ v4i zt[];                  // [token / 16][rank / 64][limb][64 lanes]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = blockIdx.y / g.n, party = blockIdx.y - part * g.n;
-    request_tile r;
-    if (!tile_at(g, blockIdx.x, 64, r)) return;
-    const u64 *base = g.base + ((size_t)party * g.tokens + r.first) * g.ld_base;
-    u64 *y = g.y + ((size_t)party * g.tokens + r.first) * g.ld_y;
+    int *rows = reinterpret_cast<int *>(zt);     // (until the digits are written)
+    row_tile r;
+    if (!find_rows(g, blockIdx.x, 64, rows, r)) return;
+    const u64 *base = g.base + (size_t)party * g.tokens * g.ld_base;
+    u64 *y = g.y + (size_t)party * g.tokens * g.ld_y;
+    __syncthreads();
     if (r.adapter < 0) {
-        pass_through(g, r, base, y, part);
+        pass_through(g, r, rows, base, y, part);
         return;
     }
     const int per_limb = g.padded / 16, chunks = NL * per_limb, blocks = (g.rank + 63) >> 6, q = lane >> 4, c16 = lane & 15;
-    const u64 *z = g.z + ((size_t)party * g.tokens + r.first) * g.rank;
-    const int log = r.count > 32 ? 2 : r.count > 16 ? 1 : 0, first = (wave & ((1 << log) - 1)) * 16;
-    for (int i = tid; i < (16 << log) * blocks * 16; i += BLOCK) {      // four elements of a row
-        const int row = i & ((16 << log) - 1), e = (i >> (4 + log)) * 4;
+    const u64 *z = g.z + (size_t)party * g.tokens * g.rank;
+    const int log = r.count > 32 ? 2 : r.count > 16 ? 1 : 0, first = (wave & ((1 << log) - 1)) * 16;   // 2^log waves to the tokens, the others to the columns
+    const int row = tid & ((16 << log) - 1), own_row = rows[min(row, r.count - 1)];   // a thread stages parts of one row
+    int to[4];
+#pragma unroll
+    for (int c = 0; c < 4; c++) to[c] = rows[min(first + 4 * q + c, r.count - 1)];
+    __syncthreads();
+    for (int i = tid; i < (16 << log) * blocks * 16; i += BLOCK) {      // four elements of it
+        const int e = (i >> (4 + log)) * 4;
         u64 v[4];
 #pragma unroll
-        for (int c = 0; c < 4; c++) v[c] = balanced_digits(row < r.count && e + c < g.rank ? z[(size_t)row * g.rank + e + c] : 0);
+        for (int c = 0; c < 4; c++) v[c] = balanced_digits(row < r.count && e + c < g.rank ? z[(size_t)own_row * g.rank + e + c] : 0);
         u32 *dst = reinterpret_cast<u32 *>(zt + ((row >> 4) * blocks + (e >> 6)) * TILE + (row & 15) + 16 * ((e & 63) >> 4)) + ((e & 15) >> 2);
 #pragma unroll
         for (int l = 0; l < NL; l++) dst[l * 256] = limb_dword(v, l);
@@ -537,12 +527,11 @@ __global__ __launch_bounds__(BLOCK, 2) void up_tile_kernel(adapter_args g)
         const int col = 32 * u + 2 * c16;
 #pragma unroll
         for (int c = 0; c < 4; c++) {
-            const int row = first + 4 * q + c;
-            if (row >= r.count) continue;
-            pack_t<2> o = load_pair<MODE>(base + (size_t)row * g.ld_base, col, g.N);
+            if (first + 4 * q + c >= r.count) continue;
+            pack_t<2> o = load_pair<MODE>(base + (size_t)to[c] * g.ld_base, col, g.N);
             o.v[0] = fold_diagonals(acc[0], c, o.v[0]);
             o.v[1] = fold_diagonals(acc[1], c, o.v[1]);
-            store_pair<MODE>(y + (size_t)row * g.ld_y, col, g.N, o);
+            store_pair<MODE>(y + (size_t)to[c] * g.ld_y, col, g.N, o);
         }
     }
 }
@@ -567,13 +556,13 @@ hipError_t ss_launch_adapters_down(const adapter_plan &plan, const ss_adapters &
                                    hipStream_t stream)
 {
     adapter_args g = {};
-    g.start = req.start, g.adapter = req.adapter, g.requests = req.requests, g.tokens = req.tokens;
+    g.start = req.start, g.adapter = req.adapter, g.requests = req.requests, g.tokens = req.tokens, g.grouped = plan.grouped;
     g.adapters = s.adapters, g.K = s.K, g.rank = s.rank;
     g.down = s.down, g.nr = 2 * t + 1, g.n = n;
     g.down_party = down_party_bytes(s.K, s.rank), g.down_bytes = g.nr * g.down_party;
     g.x = x, g.ld_x = ld_x, g.planes = planes, g.plane = (size_t)g.nr * req.tokens * s.rank;
     g.run = plan.run;
-    g.tiles = (unsigned)request_tiles(req.tokens, req.requests, plan.down_rows);
+    g.tiles = (unsigned)plan.down_tiles;
     g.dTiles = make_fdiv(g.tiles);
     const dim3 grid((unsigned)plan.down_groups);
     const bool wide = s.K % 2 == 0 && ld_x % 2 == 0 && aligned16(x);
@@ -595,15 +584,15 @@ hipError_t ss_launch_adapters_up(const adapter_plan &plan, const ss_adapters &s,
 {
     (void)t;
     adapter_args g = {};
-    g.start = req.start, g.adapter = req.adapter, g.requests = req.requests, g.tokens = req.tokens;
+    g.start = req.start, g.adapter = req.adapter, g.requests = req.requests, g.tokens = req.tokens, g.grouped = plan.grouped;
     g.adapters = s.adapters, g.rank = s.rank, g.padded = (int)padded_rank(s.rank), g.N = s.N;
     g.up = s.up, g.n = n;
     g.up_party = up_party_bytes(s.rank, s.N), g.up_bytes = n * g.up_party;
     g.z = z, g.base = base, g.ld_base = ld_base, g.y = y, g.ld_y = ld_y;
     g.col_groups = plan.col_groups;
     const int steps = (int)up_steps(s.rank);
-    const size_t lds = plan.up == UP_TILE ? 4 * div_up(s.rank, 64) * TILE * 16 : (size_t)(plan.up_rows + (plan.up == UP_DIAGONALS ? 1 : 0)) * (15 * g.padded + 64 * steps);
-    const dim3 grid((unsigned)request_tiles(req.tokens, req.requests, plan.up_rows), n * plan.col_groups);
+    const size_t lds = plan.diagonals ? (UP_ROWS + 1) * (15 * g.padded + 64 * steps) : 4 * div_up(s.rank, 64) * TILE * 16;
+    const dim3 grid((unsigned)plan.up_tiles, n * plan.col_groups);
     const bool pairs = s.N % 2 == 0 && ld_y % 2 == 0 && aligned16(y) && (!base || (ld_base % 2 == 0 && aligned16(base)));
     if (!base) {
         hipLaunchKernelGGL(clear_kernel, dim3((unsigned)std::min(req.tokens, 4096), n), dim3(BLOCK), 0, stream, g);
@@ -614,9 +603,7 @@ hipError_t ss_launch_adapters_up(const adapter_plan &plan, const ss_adapters &s,
     hipLaunchKernelGGL((mode == NARROW ? KERNEL<__VA_ARGS__ NARROW> : mode == PAIRS ? KERNEL<__VA_ARGS__ PAIRS> : KERNEL<__VA_ARGS__ STREAM_PAIRS>), grid, \
                        dim3(BLOCK), lds, stream, g)
 #define SS_COMMA ,
-    if (plan.up == UP_SINGLE)
-        hipLaunchKernelGGL(up_single_kernel, grid, dim3(BLOCK), lds, stream, g);
-    else if (plan.up == UP_TILE)
+    if (!plan.diagonals)
         SS_MODE(up_tile_kernel, );
     else if (steps == 1)
         SS_MODE(up_diagonals_kernel, 1 SS_COMMA);

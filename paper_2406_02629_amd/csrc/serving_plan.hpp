@@ -22,40 +22,45 @@ inline size_t up_party_bytes(int rank, int N) { return div_up(N, 32) * 2 * SS_NL
 
 constexpr size_t MAX_SERVING_GROUPS = ((size_t)1 << 24) - 1;   // workgroups of 256 threads in a launch: less than 2^32 threads
 constexpr size_t STREAMED_BYTES = (size_t)256 << 20;           // tensors that the caches do not hold
-constexpr int MAX_PLANES = 8;                                  // partial sums of the first product, which the reduction adds
+constexpr int MAX_PLANES = 4;                                  // partial sums of the first product, which the reduction adds
 
-// The kernel of the second product: tokens one by one, in tiles with all digits of their z in registers, or in tiles with the diagonals apart.
-enum up_kind { UP_SINGLE, UP_DIAGONALS, UP_TILE };
+constexpr int DOWN_ROWS = 16, UP_ROWS = 16, UP_TILE_ROWS = 64;   // tokens to a tile of the first product, of the second by either kernel
 
 struct adapter_plan {
-    int down_rows, up_rows;       // tokens to a tile
-    up_kind up;
-    int splits, run;              // its contraction: in `splits` runs of `run` blocks of 64
+    bool grouped;                 // tiles of tokens that share an adapter, whichever requests they belong to
+    bool diagonals;               // the second product over limbs and rank together
+    int splits, run;              // contraction of the first product: in `splits` runs of `run` blocks of 64
     bool streams;                 // the second product's tensors go past the caches
     int col_groups;               // workgroups that share the columns of a tile of the second product
     size_t messages, planes, z;   // bytes: of the reduction's messages, of the first product's planes, of its reduced result
+    size_t down_tiles, up_tiles;  // most that there can be
     size_t down_groups, up_groups, bytes;
 };
 
 // most tiles of `rows` tokens that requests can have
-inline size_t request_tiles(size_t tokens, size_t requests, size_t rows) { return rows == 1 ? tokens : std::min(tokens, tokens / rows + requests); }
+inline size_t request_tiles(size_t tokens, size_t requests, size_t rows, bool grouped)
+{
+    return grouped ? tokens : std::min(tokens, tokens / rows + requests);
+}
 
 inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K, int rank, int N)
 {
     adapter_plan p = {};
     const size_t nr = 2 * t + 1, k = t + 1, count = (size_t)tokens * rank, blocks = div_up(K, 64);
-    p.down_rows = 16;
-    p.up = tokens <= 2 * (size_t)requests ? UP_SINGLE : rank <= 32 ? UP_DIAGONALS : UP_TILE;
-    p.up_rows = p.up == UP_SINGLE ? 1 : p.up == UP_DIAGONALS ? 16 : 64;
-    p.streams = (size_t)n * tokens * N * 16 > STREAMED_BYTES;
-    const size_t tiles = request_tiles(tokens, requests, p.down_rows) * nr;
+    // every workgroup goes through the requests, and those of tokens that are in another's tile for nothing
+    p.grouped = requests > 1 && requests <= 1024 && tokens <= 2 * (size_t)requests;
+    p.diagonals = rank <= 32;
+    p.down_tiles = request_tiles(tokens, requests, DOWN_ROWS, p.grouped);
+    const size_t tiles = p.down_tiles * nr;
     p.splits = (int)std::max<size_t>(1, std::min(std::min<size_t>(MAX_PLANES, div_up(512, tiles)), blocks / 8));
     p.run = (int)div_up(blocks, p.splits);
     p.splits = (int)div_up(blocks, p.run);
     p.down_groups = tiles * p.splits;
-    const size_t up_tiles = request_tiles(tokens, requests, p.up_rows), units = div_up(N, p.up == UP_SINGLE ? 64 : p.up == UP_DIAGONALS ? 128 : 32);
-    p.col_groups = (int)std::max<size_t>(1, std::min(div_up(p.up == UP_SINGLE ? 512 : 2048, up_tiles * n), div_up(units, 4)));
-    p.up_groups = up_tiles * n * p.col_groups;
+    p.up_tiles = request_tiles(tokens, requests, p.diagonals ? UP_ROWS : UP_TILE_ROWS, p.grouped);
+    const size_t units = div_up(N, p.diagonals ? 128 : 32);
+    p.col_groups = (int)std::max<size_t>(1, std::min(div_up(2048, p.up_tiles * n), div_up(units, 4)));
+    p.up_groups = p.up_tiles * n * p.col_groups;
+    p.streams = (size_t)n * tokens * N * 16 > STREAMED_BYTES;
     auto whole = [](size_t b) { return (b + 255) & ~(size_t)255; };
     p.messages = whole((nr * k + k * n + k + n) * count * 8);
     p.planes = whole((size_t)p.splits * nr * count * 8);

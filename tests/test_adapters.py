@@ -171,6 +171,12 @@ SHAPES = [
     (190, 66, 128, [7, 30, 1], [0, 1, 2]),
     (64, 1030, 16, [21], [1]),                                  # wide
     (3001, 18, 7, [9], [0]),                                    # long
+    # single tokens that share adapters: more of one than a tile has, requests beyond a wave's lanes, of no tokens and of several among them
+    (64, 130, 12, [1] * 90, [0] * 90),
+    (70, 40, 20, [1, 0, 2, 1] * 40, [(7 * i) % 5 - 1 for i in range(160)]),
+    (96, 200, 70, [1, 1, 0, 3, 1, 1] * 11, [i % 3 for i in range(66)]),
+    (64, 36, 4, [0] * 63 + [1, 1, 5, 1] + [0] * 61 + [1, 4] + [1] * 9, [0] * 128 + [1, 0, 1, 2, 0, 0, 3, 0, 0, 0, 0]),
+    (64, 33, 8, [1] * 1030, [i % 4 for i in range(1030)]),
 ]
 
 
