@@ -101,6 +101,11 @@ __device__ __forceinline__ bool find_rows(const adapter_args &g, int tile, int m
         return true;
     };
     int first, count, adapter;
+    if (g.requests == 1) {                       // without a search
+        first = min(max(fixed_at(g.start, 0), 0), g.tokens), count = min(fixed_at(g.start, 1), g.tokens) - first - tile * most;
+        adapter = fixed_at(g.adapter, 0);
+        return count > 0 && keep(first + tile * most, count, adapter < 0 || adapter >= g.adapters ? -1 : adapter);
+    }
     if (!g.grouped) {
         int base = 0;
         for (int b0 = 0; b0 < g.requests; b0 += 64) {
@@ -502,28 +507,35 @@ __global__ __launch_bounds__(BLOCK, 2) void up_tile_kernel(adapter_args g)
     const signed char *b = g.up + r.adapter * g.up_bytes + party * g.up_party + c16 * 16;
     const int units = (g.N + 31) >> 5;
     const v4i *mine = zt + (first >> 4) * blocks * TILE + lane;
-    for (int u = part * (4 >> log) + (wave >> log); u < units; u += g.col_groups * (4 >> log)) {
+    int u = part * (4 >> log) + (wave >> log);
+    const int step = g.col_groups * (4 >> log);
+    // 16 columns (half h of 32) by 64 ranks; behind the rank the digits of z are 0
+    auto load = [&](int unit, int kb, int h, v4i (&w)[NL]) {
+        const signed char *src = b + ((size_t)(2 * unit + h) * chunks + min(4 * kb + q, per_limb - 1)) * 256;
+#pragma unroll
+        for (int j = 0; j < NL; j++) w[j] = *reinterpret_cast<const v4i *>(src + (size_t)j * per_limb * 256);
+    };
+    v4i w[2][NL];
+    if (u < units) load(u, 0, 0, w[0]);
+    for (; u < units; u += step) {
         v4i acc[2][ND];
 #pragma unroll
         for (int h = 0; h < 2; h++)
 #pragma unroll
             for (int s = 0; s < ND; s++) acc[h][s] = (v4i){0, 0, 0, 0};
-        for (int kb = 0; kb < blocks; kb++) {
-            // (behind the rank the digits of z are 0)
-            const signed char *src = b + ((size_t)(2 * u) * chunks + min(4 * kb + q, per_limb - 1)) * 256;
+        for (int kb = 0; kb < blocks; kb++)
 #pragma unroll
             for (int h = 0; h < 2; h++) {
-                v4i w[NL];
-#pragma unroll
-                for (int j = 0; j < NL; j++) w[j] = *reinterpret_cast<const v4i *>(src + (size_t)(h * chunks + j * per_limb) * 256);
+                // the next 16 columns on their way (behind the last, some again)
+                load(h == 0 || kb + 1 < blocks ? u : min(u + step, units - 1), h == 0 ? kb : kb + 1 < blocks ? kb + 1 : 0, 1 - h, w[1 - h]);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < NL; i++) {
                     const v4i x = mine[kb * TILE + i * 64];
 #pragma unroll
-                    for (int j = 0; j < NL; j++) acc[h][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, w[j], acc[h][i + j], 0, 0, 0);
+                    for (int j = 0; j < NL; j++) acc[h][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, w[h][j], acc[h][i + j], 0, 0, 0);
                 }
             }
-        }
         const int col = 32 * u + 2 * c16;
 #pragma unroll
         for (int c = 0; c < 4; c++) {

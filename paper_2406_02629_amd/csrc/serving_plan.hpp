@@ -52,7 +52,7 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
     p.diagonals = rank <= 32;
     p.down_tiles = request_tiles(tokens, requests, DOWN_ROWS, p.grouped);
     const size_t tiles = p.down_tiles * nr;
-    p.splits = (int)std::max<size_t>(1, std::min(std::min<size_t>(MAX_PLANES, div_up(512, tiles)), blocks / 8));
+    p.splits = (int)std::max<size_t>(1, std::min(std::min<size_t>(MAX_PLANES, div_up(1024, tiles)), blocks / 6));
     p.run = (int)div_up(blocks, p.splits);
     p.splits = (int)div_up(blocks, p.run);
     p.down_groups = tiles * p.splits;
