@@ -5,7 +5,8 @@ in a paged cache:
     queries, keys (turned on the way) and values into the cache -> attention over the cache -> degree reduction, truncation -> dense
     layer of the heads -> degree reduction, truncation
 
-Everything runs on the shares; the result is a degree-t sharing at scale 2^f.  `Sequences` is the caller's side of the paged cache: which
+With adapters, either dense layer adds each sequence's own low-rank change to its product, in front of the reduction.  Everything runs on the
+shares; the result is a degree-t sharing at scale 2^f.  `Sequences` is the caller's side of the paged cache: which
 pages belong to which sequence.
 """
 from __future__ import annotations
@@ -15,7 +16,7 @@ from typing import Dict, List, Optional
 import torch
 
 from . import fixedpoint as fx
-from .binding import PagedCache, SSNet
+from .binding import Adapters, PagedCache, SSNet
 
 
 class Sequences:
@@ -81,12 +82,15 @@ class Attention:
     owner, shared and packed once.  table: fixedpoint.rotary_table.  weight_bits: f, or 2 f for long contexts (the weights of `length`
     keys are about 1 / length); default: what the longest context that table and cache have room for needs.  stream_base: the first
     stream id of its calls, each of which takes STREAMS of them; the two in front of it share the weights.  Default: whatever ids the context has free
-    (SSNet.take_streams); ids that another layer has are refused."""
+    (SSNet.take_streams); ids that another layer has are refused.  adapters_qkv, adapters_out: sets of low-rank adapters of the two dense layers (any
+factor of theirs in B), of which forward gives each sequence one; a pass with adapters takes STREAMS + ADAPTER_STREAMS ids."""
 
     STREAMS = 8      # stream ids that a forward pass uses
+    ADAPTER_STREAMS = 2
 
     def __init__(self, ss: SSNet, w_qkv: torch.Tensor, w_out: torch.Tensor, heads: int, kv_heads: int, table: torch.Tensor, pages: int,
-                 page_size: int = 64, layout: str = "half", weight_bits: Optional[int] = None, stream_base: Optional[int] = None):
+                 page_size: int = 64, layout: str = "half", weight_bits: Optional[int] = None, stream_base: Optional[int] = None,
+                 adapters_qkv: Optional[Adapters] = None, adapters_out: Optional[Adapters] = None):
         self.ss, self.heads, self.kv, self.table, self.layout = ss, heads, kv_heads, table, layout
         self.dim = w_out.shape[0] // heads
         self.width = w_out.shape[1]
@@ -97,6 +101,10 @@ class Attention:
             raise ValueError("weight_bits must be f or 2 f: the result is brought back to scale by truncations by 2^f")
         if w_qkv.shape != (self.width, (heads + 2 * kv_heads) * self.dim):
             raise ValueError("w_qkv must be [width][(heads + 2 kv_heads) head_dim]")
+        for name, held, shape in (("adapters_qkv", adapters_qkv, w_qkv.shape), ("adapters_out", adapters_out, w_out.shape)):
+            if held is not None and (held.K, held.N) != tuple(shape):
+                raise ValueError(f"{name} must be of a layer {tuple(shape)}")
+        self.adapters_qkv, self.adapters_out = adapters_qkv, adapters_out
         self.stream = stream_base        # of the next call, where the caller has a say
         weights = ss.take_streams(2, None if stream_base is None else stream_base - 2)
 
@@ -107,9 +115,10 @@ class Attention:
         self.cache = PagedCache(ss, pages, page_size, kv_heads, self.dim)
         self.sequences = Sequences(self.cache)
 
-    def forward(self, x: torch.Tensor, counts: Dict[int, int]) -> torch.Tensor:
-        """x: shares [n][tokens][width] at scale 2^f of the new tokens, counts as in Sequences.extend -> shares [n][tokens][width].  A call
-        that is refused or fails leaves the sequences as they were."""
+    def forward(self, x: torch.Tensor, counts: Dict[int, int], adapters: Optional[Dict[int, int]] = None) -> torch.Tensor:
+        """x: shares [n][tokens][width] at scale 2^f of the new tokens, counts as in Sequences.extend -> shares [n][tokens][width].  adapters: the place in the
+        layer's sets that a sequence's adapter has; those that are not in it have none.  A call that is refused or fails leaves the sequences as they
+        were."""
         ss, heads, kv, dim = self.ss, self.heads, self.kv, self.dim
         n, tokens, _ = x.shape
         if sum(counts.values()) != tokens:
@@ -117,10 +126,20 @@ class Attention:
         batch, after = self.sequences.place(counts, x.device)
         if batch["max_ctx"] > self.table.shape[0]:
             raise ValueError(f"the table has {self.table.shape[0]} positions, a sequence would have {batch['max_ctx']}")
-        stream = ss.take_streams(self.STREAMS, self.stream)
+        index = None
+        if adapters is not None:
+            if self.adapters_qkv is None and self.adapters_out is None:
+                raise ValueError("the layer has no adapters")
+            index = torch.tensor([adapters.get(s, -1) for s in counts], dtype=torch.int32, device=x.device)
+        streams = self.STREAMS + (self.ADAPTER_STREAMS if adapters is not None else 0)
+        stream = ss.take_streams(streams, self.stream)
         if self.stream is not None:
-            self.stream += self.STREAMS
-        qkv = ss.linear_mod_packed(x, self.w_qkv, (heads + 2 * kv) * dim)
+            self.stream += streams
+
+        def adapted(held, x, y, own):
+            return y if held is None or index is None else ss.adapters_mod(held, x, batch["seq_start"], index, own, base=y, out=y)
+
+        qkv = adapted(self.adapters_qkv, x, ss.linear_mod_packed(x, self.w_qkv, (heads + 2 * kv) * dim), stream + self.STREAMS)
         qkv = ss.degree_reduce_truncate(qkv, stream_id=stream).view(n, tokens, heads + 2 * kv, dim)
         q = ss.rotary_truncate(qkv[:, :, :heads], self.table, batch["pos"], stream + 1, layout=self.layout)
         ss.cache_append(self.cache, qkv[:, :, heads:heads + kv], qkv[:, :, heads + kv:], batch["slots"], stream + 2, table=self.table,
@@ -130,7 +149,8 @@ class Attention:
         o = ss.degree_reduce_truncate(o, stream_id=stream + 4)
         if self.bits == 2 * ss.f:
             o = ss.truncate(o, stream_id=stream + 5)
-        y = ss.linear_mod_packed(o.view(n, tokens, heads * dim), self.w_out, self.width)
+        o = o.view(n, tokens, heads * dim)
+        y = adapted(self.adapters_out, o, ss.linear_mod_packed(o, self.w_out, self.width), stream + self.STREAMS + 1)
         y = ss.degree_reduce_truncate(y, stream_id=stream + 6)
         self.sequences.keep(after)
         return y
