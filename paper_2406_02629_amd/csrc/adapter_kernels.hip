@@ -523,6 +523,10 @@ __global__ __launch_bounds__(BLOCK, 2) void up_tile_kernel(adapter_args g)
         for (int h = 0; h < 2; h++)
 #pragma unroll
             for (int s = 0; s < ND; s++) acc[h][s] = (v4i){0, 0, 0, 0};
+        const int col = 32 * u + 2 * c16;
+        pack_t<2> more[4];
+#pragma unroll
+        for (int c = 0; c < 4; c++) more[c] = load_pair<MODE>(base + (size_t)to[c] * g.ld_base, col, g.N);
         for (int kb = 0; kb < blocks; kb++)
 #pragma unroll
             for (int h = 0; h < 2; h++) {
@@ -536,13 +540,12 @@ __global__ __launch_bounds__(BLOCK, 2) void up_tile_kernel(adapter_args g)
                     for (int j = 0; j < NL; j++) acc[h][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, w[h][j], acc[h][i + j], 0, 0, 0);
                 }
             }
-        const int col = 32 * u + 2 * c16;
 #pragma unroll
         for (int c = 0; c < 4; c++) {
             if (first + 4 * q + c >= r.count) continue;
-            pack_t<2> o = load_pair<MODE>(base + (size_t)to[c] * g.ld_base, col, g.N);
-            o.v[0] = fold_diagonals(acc[0], c, o.v[0]);
-            o.v[1] = fold_diagonals(acc[1], c, o.v[1]);
+            pack_t<2> o;
+            o.v[0] = fold_diagonals(acc[0], c, more[c].v[0]);
+            o.v[1] = fold_diagonals(acc[1], c, more[c].v[1]);
             store_pair<MODE>(y + (size_t)to[c] * g.ld_y, col, g.N, o);
         }
     }

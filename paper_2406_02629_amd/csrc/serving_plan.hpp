@@ -22,7 +22,7 @@ inline size_t up_party_bytes(int rank, int N) { return div_up(N, 32) * 2 * SS_NL
 
 constexpr size_t MAX_SERVING_GROUPS = ((size_t)1 << 24) - 1;   // workgroups of 256 threads in a launch: less than 2^32 threads
 constexpr size_t STREAMED_BYTES = (size_t)256 << 20;           // tensors that the caches do not hold
-constexpr int MAX_PLANES = 4;                                  // partial sums of the first product, which the reduction adds
+constexpr int MAX_PLANES = 8;                                  // partial sums of the first product, which the reduction adds
 
 constexpr int DOWN_ROWS = 16, UP_ROWS = 16, UP_TILE_ROWS = 64;   // tokens to a tile of the first product, of the second by either kernel
 
@@ -52,7 +52,12 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
     p.diagonals = rank <= 32;
     p.down_tiles = request_tiles(tokens, requests, DOWN_ROWS, p.grouped);
     const size_t tiles = p.down_tiles * nr;
-    p.splits = (int)std::max<size_t>(1, std::min(std::min<size_t>(MAX_PLANES, div_up(1024, tiles)), blocks / 6));
+    // a block of 64 elements takes a CU so long, a workgroup half a microsecond beside its blocks, the reduction 0.3 for each plane
+    const double block = rank <= 16 ? 0.25 : rank <= 32 ? 0.5 : rank <= 64 ? 1.0 : 2.0;
+    auto cost = [&](size_t s) { return div_up(tiles * s, 256) * (block * div_up(blocks, s) + 0.5) + 0.3 * s; };
+    p.splits = 1;
+    for (size_t s = 2; s <= MAX_PLANES && s * 6 <= blocks; s++)
+        if (cost(s) < cost(p.splits)) p.splits = (int)s;
     p.run = (int)div_up(blocks, p.splits);
     p.splits = (int)div_up(blocks, p.run);
     p.down_groups = tiles * p.splits;
