@@ -62,8 +62,15 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
     p.splits = (int)div_up(blocks, p.run);
     p.down_groups = tiles * p.splits;
     p.up_tiles = request_tiles(tokens, requests, p.diagonals ? UP_ROWS : UP_TILE_ROWS, p.grouped);
-    const size_t units = div_up(N, p.diagonals ? 128 : 32);
-    p.col_groups = (int)std::max<size_t>(1, std::min(div_up(2048, p.up_tiles * n), div_up(units, 4)));
+    const size_t units = div_up(N, p.diagonals ? 128 : 32), per_tile = p.diagonals ? div_up(units, 4) : units;
+    // Workgroups with the diagonals apart stage their tile's digits for some 10 us and take 3 for 32 columns; two of them fit a CU.  What fills the chip once
+    // is best while each of them has few columns (us, 37 to 333 tokens, 2560 columns, rank 64, 45-bit prime, by workgroups to a tile: 8 46.8, 16 30.4, 20 42.1,
+    // 40 41.0; 100 to 401 tokens, 1024 columns, rank 128: 4 52.8, 8 43.3, 16 53.4); long ones are as good in several rounds (2048 tokens,
+    // 4096 columns, rank 64, n = 5: 4 336, 8 298, 20 306, 64 362).
+    const double full = n * ((double)tokens / UP_TILE_ROWS + requests * 0.5);   // tiles, about
+    size_t wanted = (size_t)(512 / full);
+    if (p.diagonals || wanted < 1 || units > 16 * wanted) wanted = div_up(2048, p.up_tiles * n);
+    p.col_groups = (int)std::max<size_t>(1, std::min(wanted, per_tile));
     p.up_groups = p.up_tiles * n * p.col_groups;
     p.streams = (size_t)n * tokens * N * 16 > STREAMED_BYTES;
     auto whole = [](size_t b) { return (b + 255) & ~(size_t)255; };
