@@ -48,7 +48,7 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
     adapter_plan p = {};
     const size_t nr = 2 * t + 1, k = t + 1, count = (size_t)tokens * rank, blocks = div_up(K, 64);
     // every workgroup goes through the requests, and those of tokens that are in another's tile for nothing
-    p.grouped = requests > 1 && requests <= 1024 && tokens <= 2 * (size_t)requests;
+    p.grouped = requests > 1 && requests <= 1024 && tokens <= 2 * requests;
     p.diagonals = rank <= 32;
     p.down_tiles = request_tiles(tokens, requests, DOWN_ROWS, p.grouped);
     const size_t tiles = p.down_tiles * nr;
