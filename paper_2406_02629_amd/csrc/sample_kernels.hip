@@ -474,6 +474,8 @@ __device__ __forceinline__ void collect_chunk(const sample_args &g, u32 at, int 
 {
     const int lane = threadIdx.x & 63;
     u64 sum = 0;
+    unsigned long long near[8];                  // lanes whose token is near a cut
+    u32 listed = 0;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
         const u32 d = (u32)top - (u32)k[i];
@@ -482,13 +484,19 @@ __device__ __forceinline__ void collect_chunk(const sample_args &g, u32 at, int 
             const u32 w = rule.weight(d);
             if (w >= rule.least) sum += w;
         }
-        const bool mine = live && in_ranges(plan, d);
-        const unsigned long long all = __ballot(mine);
-        if (all) {
-            u32 first = 0;
-            if (lane == 0) first = atomicAdd(g.listed + at, (u32)__popcll(all));
-            first = (u32)__shfl((int)first, 0) + (u32)__popcll(all & ((1ull << lane) - 1));
-            if (mine && first < (u32)SAMPLE_LIST) g.list[(size_t)at * SAMPLE_LIST + first] = (u64)d << 20 | (u32)(chunk * CHUNK + (i >> 2) * 256 + lane * 4 + (i & 3));
+        near[i] = __ballot(live && in_ranges(plan, d));
+        listed += (u32)__popcll(near[i]);
+    }
+    if (listed) {                                // (one place in the list for all of them: the wave waits for it once)
+        u32 first = 0;
+        if (lane == 0) first = atomicAdd(g.listed + at, listed);
+        first = (u32)__builtin_amdgcn_readfirstlane((int)first);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const u32 place = first + (u32)__popcll(near[i] & ((1ull << lane) - 1));
+            if ((near[i] >> lane & 1) && place < (u32)SAMPLE_LIST)
+                g.list[(size_t)at * SAMPLE_LIST + place] = (u64)((u32)top - (u32)k[i]) << 20 | (u32)(chunk * CHUNK + (i >> 2) * 256 + lane * 4 + (i & 3));
+            first += (u32)__popcll(near[i]);
         }
     }
     sum = wave_sum(sum);
