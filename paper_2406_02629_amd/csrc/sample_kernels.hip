@@ -21,6 +21,18 @@ constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = SAMPLE_BINS, CHUNK = 
 constexpr int OPEN_THREADS = 256;
 constexpr int NOT_ALLOWED = -2147483647 - 1;
 
+// Distances lo .. lo + span - 1 among which a cut lies, and what comes before them
+struct cut_range {
+    u32 lo, span;                   // span 0: no such cut
+    u64 left;                       // tokens (top_k) or weight (top_p) to take from the range
+    u64 before;                     // weight of the tokens in front
+};
+
+struct row_plan {
+    u32 sure;                       // distances below stay
+    cut_range few, part;            // part.left only where few.span is 0: it depends on what few leaves
+};
+
 struct sample_args {
     const u64 *logits;              // [n][rows][ld]
     size_t ld;
@@ -40,6 +52,7 @@ struct sample_args {
     u64 *sum;                       // [.][BINS]
     u64 *sure;                      // [.][chunks]
     u32 *listed;                    // [.]
+    row_plan *plans;                // [.]
     u64 *list;                      // [.][SAMPLE_LIST]: distance 2^20 + token
 };
 
@@ -118,18 +131,6 @@ struct row_state {
     u64 red64[WAVES], found_sum;
     u32 red32[WAVES], found_count;
     int bin[3];
-};
-
-// Distances lo .. lo + span - 1 among which a cut lies, and what comes before them
-struct cut_range {
-    u32 lo, span;                   // span 0: no such cut
-    u64 left;                       // tokens (top_k) or weight (top_p) to take from the range
-    u64 before;                     // weight of the tokens in front
-};
-
-struct row_plan {
-    u32 sure;                       // distances below stay
-    cut_range few, part;            // part.left only where few.span is 0: it depends on what few leaves
 };
 
 // From the histogram in s: where the cuts lie.
@@ -512,6 +513,7 @@ __global__ __launch_bounds__(THREADS) void collect_kernel(sample_args g)
     load_keys(g, at, chunk, k);
     const int top = top_of(g, at, s.red32);
     const row_plan plan = load_plan(g, at, s, rule);
+    if (group == 0 && threadIdx.x == 0) g.plans[at] = plan;
     while (chunk < g.chunks) {
         int next[8];
         load_keys(g, at, chunk + g.groups * WAVES, next);
@@ -533,7 +535,7 @@ __global__ __launch_bounds__(THREADS) void pick_kernel(sample_args g)
         if (threadIdx.x == 0) g.tokens[row] = -1, g.shown[row] = 0;
         return;
     }
-    const row_plan plan = load_plan(g, at, s, rule);
+    const row_plan plan = g.plans[at];
     const int *keys = g.keys + (size_t)at * g.key_ld;
     const u64 *list = g.list + (size_t)at * SAMPLE_LIST;
     const u32 listed = g.listed[at];
@@ -570,10 +572,12 @@ hipError_t ss_launch_sample(const sample_plan &plan, const ss_sampling &q, const
     g.sum = (u64 *)at, at += (size_t)plan.slab * BINS * 8;
     g.sure = (u64 *)at, at += (size_t)plan.slab * ((plan.chunks + 1) & ~1) * 8;
     g.list = (u64 *)at, at += (size_t)plan.slab * SAMPLE_LIST * 8;
+    g.plans = (row_plan *)at, at += (size_t)plan.slab * SAMPLE_PLAN;
     g.keys = (int *)at, at += (size_t)plan.slab * plan.key_ld * 4;
     g.count = (u32 *)at, at += (size_t)plan.slab * BINS * 4;
     g.tops = (int *)at, at += (size_t)plan.slab * plan.opens * 4;
     g.listed = (u32 *)at;
+    static_assert(sizeof(row_plan) <= SAMPLE_PLAN && alignof(row_plan) <= 16, "a row's plan has its room");
     const bool wide = ld % 2 == 0 && aligned16(logits);
     const bool streams = (size_t)rp.m * rows * vocab * 8 > STREAMED_BYTES;
     for (g.row0 = 0; g.row0 < rows; g.row0 += plan.slab) {

@@ -47,7 +47,10 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
 {
     adapter_plan p = {};
     const size_t nr = 2 * t + 1, k = t + 1, count = (size_t)tokens * rank, blocks = div_up(K, 64);
-    // every workgroup goes through the requests, and those of tokens that are in another's tile for nothing
+    // Tokens by their adapters, although every workgroup goes through the requests then, and those of tokens that are in another's tile for nothing (first and
+    // second product, us, so / request by request: 128 requests of a token with 27 adapters between them, n = 3, 23 + 61 / 35 + 103, with an adapter each
+    // 44 + 140 / 43 + 139; 64 with 8, n = 5, 24 + 23 / 28 + 30; 400 with 8 72 + 94 / 124 + 89; 8 with 8 10.0 + 7.9 / 9.2 + 7.7.  Of two tokens each, 64 with 27,
+    // n = 3, 23 + 75 / 30 + 66; of four each, 32 with 4, n = 5, 48 + 66 / 23 + 26).
     p.grouped = requests > 1 && requests <= 1024 && tokens <= 2 * requests;
     p.diagonals = rank <= 32;
     p.down_tiles = request_tiles(tokens, requests, DOWN_ROWS, p.grouped);
@@ -88,6 +91,7 @@ constexpr int SAMPLE_BIN_BITS = 11, SAMPLE_BINS = 1 << SAMPLE_BIN_BITS;
 constexpr int SAMPLE_OPEN = 1024;             // tokens to a workgroup that opens
 constexpr int SAMPLE_CHUNK = 512;             // to a wave that counts or collects: 2^20 tokens are 2048 chunks
 constexpr int SAMPLE_LIST = 4096;             // tokens near a cut that are listed (more are found among all)
+constexpr int SAMPLE_PLAN = 64;                // bytes for where the cuts of a row lie
 constexpr size_t SAMPLE_ROOM = (size_t)512 << 20;
 
 struct sample_plan {
@@ -108,7 +112,7 @@ inline sample_plan plan_sample(int rows, int vocab, size_t room)
     p.chunks = (int)div_up(vocab, SAMPLE_CHUNK);
     p.groups = (int)std::min(div_up(p.chunks, 16), div_up(512, rows));
     p.key_ld = (vocab + 3) & ~3;
-    const size_t row = (size_t)SAMPLE_BINS * 12 + (size_t)((p.chunks + 1) & ~1) * 8 + (size_t)SAMPLE_LIST * 8 + (size_t)p.key_ld * 4 + (size_t)p.opens * 4 + 4;
+    const size_t row = (size_t)SAMPLE_BINS * 12 + (size_t)((p.chunks + 1) & ~1) * 8 + (size_t)SAMPLE_LIST * 8 + (size_t)p.key_ld * 4 + (size_t)p.opens * 4 + SAMPLE_PLAN + 4;
     const size_t most = std::max<size_t>(1, std::min(room, SAMPLE_ROOM) / row);
     p.slab = (int)std::min<size_t>(std::min<size_t>(rows, most), MAX_SERVING_GROUPS / p.opens / 4);
     p.bytes = p.slab * row;
