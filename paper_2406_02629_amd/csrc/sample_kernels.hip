@@ -3,7 +3,8 @@
 // the row's largest logit and how many of the tokens at that distance are kept.  A histogram of distances, with how many tokens each bin has and
 // what they weigh, says in which bin a cut lies; the tokens of that bin alone are looked at further.
 //
-// Up to SMALL_VOCAB tokens one workgroup takes a row in one launch.  Longer rows go through four, so that many workgroups share a row:
+// Up to SMALL_VOCAB tokens, and up to MEDIUM_VOCAB where there are about as many rows as CUs, one workgroup takes a row in one launch.  Other rows go
+// through four, so that many workgroups share a row:
 //   open     REC, and the largest logit of every 1024
 //   count    the histogram
 //   collect  what the tokens weigh that stay whatever the cut is, for every 512; the tokens of the bins with a cut, in a list
@@ -294,22 +295,43 @@ __device__ __forceinline__ int key_of(const sample_args &g, const ss_rec_params 
     return allowed ? logit_of(v, g.f) : NOT_ALLOWED;
 }
 
-// ------------------------------------------------------------------ small vocabularies
+// ------------------------------------------------------------------ a workgroup to a row
 
+// The row's logits stay in LDS.  Bound by the row's way through one CU: its shares, two atomics of LDS to a token, and three to five times over the keys.  256 rows
+// of 2048 16 us, of 8192 25, of 32000 63 (131 MB; four launches 75).
+
+template <int MOST>
 __global__ __launch_bounds__(THREADS) void sample_kernel(sample_args g, ss_rec_params rp)
 {
     __shared__ row_state s;
-    __shared__ int keys[SMALL_VOCAB];
+    __shared__ int keys[MOST];
+    constexpr int FLIGHT = 4;                    // loads of a share on their way
     const int tid = threadIdx.x, row = blockIdx.x;
     const row_rule rule = rule_of(g.params[row], g.f);
     int top = NOT_ALLOWED;
-    for (int j = tid; j < g.vocab; j += THREADS) {
-        ss_sacc acc;
-        acc.clear();
-        for (int i = 0; i < rp.m; i++) acc.mac(g.logits[((size_t)rp.plane[i] * g.rows + row) * g.ld + j], rp.ilambda[i]);
-        const int key = key_of(g, rp, row, j, acc.value());
-        keys[j] = key;
-        top = max(top, key);
+    for (int j0 = tid; j0 < g.vocab; j0 += FLIGHT * THREADS) {
+        ss_sacc2 acc[FLIGHT];
+#pragma unroll
+        for (int i = 0; i < FLIGHT; i++) acc[i].clear();
+        for (int q = 0; q < rp.m; q++) {
+            const u64 *x = g.logits + ((size_t)rp.plane[q] * g.rows + row) * g.ld;
+            u64 v[FLIGHT];
+#pragma unroll
+            for (int i = 0; i < FLIGHT; i++) v[i] = x[min(j0 + i * THREADS, g.vocab - 1)];
+#pragma unroll
+            for (int i = 0; i < FLIGHT; i++) {
+                SS_SPLIT31(v[i], w0, w1);
+                acc[i].mac(w0, w1, rp.ilambda[q]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < FLIGHT; i++) {
+            const int j = j0 + i * THREADS;
+            if (j >= g.vocab) continue;
+            const int key = key_of(g, rp, row, j, acc[i].value());
+            keys[j] = key;
+            top = max(top, key);
+        }
     }
     top = wave_max(top);
     if ((tid & 63) == 0) s.red32[tid >> 6] = (u32)top;
@@ -563,7 +585,7 @@ hipError_t ss_launch_sample(const sample_plan &plan, const ss_sampling &q, const
     g.logits = logits, g.ld = ld, g.rows = rows, g.vocab = vocab, g.f = f;
     g.params = q.params, g.random = q.random, g.allowed = q.allowed, g.ld_allowed = q.ld_allowed, g.tokens = tokens, g.shown = shown;
     if (plan.small) {
-        hipLaunchKernelGGL(sample_kernel, dim3(rows), dim3(THREADS), 0, stream, g, rp);
+        hipLaunchKernelGGL((vocab <= SMALL_VOCAB ? sample_kernel<SMALL_VOCAB> : sample_kernel<MEDIUM_VOCAB>), dim3(rows), dim3(THREADS), 0, stream, g, rp);
         return hipGetLastError();
     }
     g.opens = plan.opens, g.groups = plan.groups, g.chunks = plan.chunks, g.key_ld = plan.key_ld;

@@ -86,7 +86,8 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
 
 // ------------------------------------------------------------------ sampling
 
-constexpr int SMALL_VOCAB = 8192;             // tokens whose logits one workgroup holds
+constexpr int SMALL_VOCAB = 8192;             // tokens whose logits one workgroup holds,
+constexpr int MEDIUM_VOCAB = 32768;           // alone on its CU
 constexpr int SAMPLE_BIN_BITS = 11, SAMPLE_BINS = 1 << SAMPLE_BIN_BITS;
 constexpr int SAMPLE_OPEN = 1024;             // tokens to a workgroup that opens
 constexpr int SAMPLE_CHUNK = 512;             // to a wave that counts or collects: 2^20 tokens are 2048 chunks
@@ -95,7 +96,7 @@ constexpr int SAMPLE_PLAN = 64;                // bytes for where the cuts of a 
 constexpr size_t SAMPLE_ROOM = (size_t)512 << 20;
 
 struct sample_plan {
-    bool small;                   // one launch
+    bool small;                   // one launch, a workgroup to a row
     int slab;                     // rows at a time, 0: the room is too small
     int opens, groups;            // workgroups of a row that open, that count
     int chunks, key_ld;           // of a row; its keys with what fills the last 16 bytes
@@ -105,7 +106,10 @@ struct sample_plan {
 inline sample_plan plan_sample(int rows, int vocab, size_t room)
 {
     sample_plan p = {};
-    p.small = vocab <= SMALL_VOCAB;
+    // One launch or four, us: 1 row of 4096 tokens 13.5 / 25.2, of 8192 17.6 / 26.7, 256 rows of 2048 16.1 / 32.5, of 8192 24.6 / 38.4, 1000 68 / 102.  Beyond, a
+    // workgroup has a CU to itself and a row of 32000 takes it 58 us: 1 row of 16384 25.0 / 24.9, of 32000 38.2 / 25.0; 32 rows 32.3 / 30.0 and 57.6 / 32.1; 128
+    // 34.1 / 36.8 and 58.6 / 49.6; 256 of 32000 62.6 / 75.1, 300 106 / 88.
+    p.small = vocab <= SMALL_VOCAB || (vocab <= MEDIUM_VOCAB && div_up(rows, 256) * (10.0 + vocab / 640.0) < 22.0 + rows * (vocab / 150000.0));
     p.slab = rows;
     if (p.small) return p;
     p.opens = (int)div_up(vocab, SAMPLE_OPEN);

@@ -86,7 +86,7 @@ def test_rows_that_are_sampled_together_fit_the_room(rules):
     for rows in (1, 7, 256, 5000, 1 << 20):
         for vocab in (1, 8192, 8193, 32000, 200003, 1 << 20):
             p = lib.sample(rows, vocab, (1 << 64) - 1)
-            assert 1 <= p.slab <= rows and p.small == (vocab <= 8192)
+            assert 1 <= p.slab <= rows and p.small >= (vocab <= 8192) and p.small <= (vocab <= 32768)
             if p.small:
                 assert p.slab == rows and p.bytes == 0
                 continue
@@ -133,3 +133,26 @@ def test_logits_of_more_than_4_gb_in_several_runs():
     equal = [r for r in range(rows) if r not in picked]
     want = np.array([int(random[r]) * 44 >> 62 for r in equal])
     assert np.array_equal(tokens[equal].cpu().numpy(), want)
+
+
+@gpu
+@pytest.mark.parametrize("rows,vocab,small", [(256, 32768, True), (250, 9000, True), (256, 32769, False), (3, 8193, False)])
+def test_rows_in_one_launch_and_in_four(rules, rows, vocab, small):
+    """either side of the rules, every kind of cut among the rows that are looked at"""
+    assert rules[P61].sample(rows, vocab, (1 << 64) - 1).small == small
+    f = 13
+    rng = np.random.default_rng(vocab)
+    ss = SSNet(3, 1, f=f, seed=3)
+    picked = sorted({0, 1, rows // 2, rows - 2, rows - 1})      # each once: of three rows 0, 1, 2
+    values = np.rint(rng.standard_normal((len(picked), vocab)) * 3 * 2 ** f).astype(np.int64)
+    values[-1] >>= 13                           # few different ones
+    shares = dev(orc.share((values % P61).astype(np.uint64), 3, 1, P61, 5, 6))
+    logits = torch.zeros((3, rows, vocab), dtype=torch.int64, device="cuda")
+    for i, r in enumerate(picked):
+        logits[:, r] = shares[:, i]
+    random = torch.from_numpy(rng.integers(0, 1 << 62, rows)).cuda()
+    for params in ((0.8, 50, 0.9, 0.0), (1.0, 0, 1.0, 0.0), (0.0, 0, 1.0, 0.0), (1.3, 0, 0.97, 0.01), (0.5, 700, 1.0, 0.0)):
+        how = fx.sampling_parameters(*params, rows=rows, device="cuda")
+        tokens, shown = ss.sample(logits, [1, 2], how, random)
+        for i, r in enumerate(picked):
+            assert (int(tokens[r]), int(shown[r])) == draw(kept_weights(values[i], f, how[0].tolist()), int(random[r])), (params, r)
