@@ -589,7 +589,8 @@ int ssnet_adapters_mod(ssnet_ctx *ctx, const ssnet_adapters *set, const ssnet_re
  * S = the sum of what stays.  d_tokens: the first token, by number, up to and
  * with which the weights sum to more than floor(random * S / 2^62); d_shown: its
  * probability floor((2^30 w + S / 2) / S).  A row that allows nothing: -1, 0.
- * vocab <= SSNET_MAX_VOCAB.  Needs ssnet_workspace_bytes_sample. */
+ * vocab <= SSNET_MAX_VOCAB.  Needs ssnet_workspace_bytes_sample (that of more rows
+ * will do too). */
 #define SSNET_MAX_VOCAB (1 << 20)
 typedef struct ssnet_sampling {
     const int32_t *d_params;

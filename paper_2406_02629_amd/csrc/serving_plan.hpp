@@ -21,7 +21,9 @@ inline size_t down_party_bytes(int K, int rank) { return div_up(K, 64) * SS_NLIM
 inline size_t up_party_bytes(int rank, int N) { return div_up(N, 32) * 2 * SS_NLIMB * padded_rank(rank) * 16; }
 
 constexpr size_t MAX_SERVING_GROUPS = ((size_t)1 << 24) - 1;   // workgroups of 256 threads in a launch: less than 2^32 threads
-constexpr size_t STREAMED_BYTES = (size_t)256 << 20;           // tensors that the caches do not hold
+// Tensors that the caches do not hold: read and written past them (second product, us, past / by way of them: 2048 tokens by 4096 columns, n = 5, 671 MB, rank 16
+// 156 / 158, rank 64 300 / 310; n = 3, 403 MB, 86.8 / 93.6; 134 MB 62.2 / 60.8, 49 MB 23.8 / 22.8)
+constexpr size_t STREAMED_BYTES = (size_t)256 << 20;
 constexpr int MAX_PLANES = 8;                                  // partial sums of the first product, which the reduction adds
 
 constexpr int DOWN_ROWS = 16, UP_ROWS = 16, UP_TILE_ROWS = 64;   // tokens to a tile of the first product, of the second by either kernel
@@ -52,10 +54,14 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
     // 44 + 140 / 43 + 139; 64 with 8, n = 5, 24 + 23 / 28 + 30; 400 with 8 72 + 94 / 124 + 89; 8 with 8 10.0 + 7.9 / 9.2 + 7.7.  Of two tokens each, 64 with 27,
     // n = 3, 23 + 75 / 30 + 66; of four each, 32 with 4, n = 5, 48 + 66 / 23 + 26).
     p.grouped = requests > 1 && requests <= 1024 && tokens <= 2 * requests;
+    // Limbs and rank together, or diagonals apart (second product, us: 2048 tokens by 4096 columns, n = 5, rank 8 135 / 265, 16 157 / 274, 32 241 / 278; 1000
+    // by 1024, n = 3, rank 32 22.8 / 23.7; over the 45-bit prime 37 to 333 by 2560 35.6 / 28.0).  Beyond rank 32 two sums no longer fit 32 bits.
     p.diagonals = rank <= 32;
     p.down_tiles = request_tiles(tokens, requests, DOWN_ROWS, p.grouped);
     const size_t tiles = p.down_tiles * nr;
-    // a block of 64 elements takes a CU so long, a workgroup half a microsecond beside its blocks, the reduction 0.3 for each plane
+    // A block of 64 elements takes a CU so long, a workgroup half a microsecond beside its blocks, the reduction 0.3 for each plane.  First product, us, by runs:
+    // 64 tokens of 4096, rank 16, n = 5, 1 19, 2 13, 4 9.9, 6 9.6, 8 10.7 (reduction 4.0 to 6.2); 128 tokens, rank 32, 1 30, 2 23, 4 27; 2048 tokens, rank
+    // 16, 1 112, 2 101, 3 102; 37 to 333 tokens, rank 64, 45-bit prime, 1 19, 2 12.5, 4 11.8; 668 tokens, rank 128, 1 133, 2 114, 3 124, 4 110, 5 99.
     const double block = rank <= 16 ? 0.25 : rank <= 32 ? 0.5 : rank <= 64 ? 1.0 : 2.0;
     auto cost = [&](size_t s) { return div_up(tiles * s, 256) * (block * div_up(blocks, s) + 0.5) + 0.3 * s; };
     p.splits = 1;
@@ -78,7 +84,8 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
     p.streams = (size_t)n * tokens * N * 16 > STREAMED_BYTES;
     auto whole = [](size_t b) { return (b + 255) & ~(size_t)255; };
     p.messages = whole((nr * k + k * n + k + n) * count * 8);
-    p.planes = whole((size_t)p.splits * nr * count * 8);
+    // (room for as many as any number of tokens asks for, so that the room of a larger call holds a smaller one)
+    p.planes = whole(std::max<size_t>(1, std::min<size_t>(MAX_PLANES, blocks / 6)) * nr * count * 8);
     p.z = whole((size_t)n * count * 8);
     p.bytes = p.messages + p.planes + p.z;
     return p;
@@ -89,7 +96,8 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
 constexpr int SMALL_VOCAB = 8192;             // tokens whose logits one workgroup holds,
 constexpr int MEDIUM_VOCAB = 32768;           // alone on its CU
 constexpr int SAMPLE_BIN_BITS = 11, SAMPLE_BINS = 1 << SAMPLE_BIN_BITS;
-constexpr int SAMPLE_OPEN = 1024;             // tokens to a workgroup that opens
+constexpr int SAMPLE_OPEN = 1024;             // tokens to a workgroup that opens (us at 512, 1024, 2048: 1 row of 32000 3.5, 4.2, 5.5;
+                                              // 256 of them 31.8, 32.7, 37.6; 64 of 200003 64.6, 60.2, 63.7)
 constexpr int SAMPLE_CHUNK = 512;             // to a wave that counts or collects: 2^20 tokens are 2048 chunks
 constexpr int SAMPLE_LIST = 4096;             // tokens near a cut that are listed (more are found among all)
 constexpr int SAMPLE_PLAN = 64;                // bytes for where the cuts of a row lie
@@ -111,16 +119,20 @@ inline sample_plan plan_sample(int rows, int vocab, size_t room)
     // 34.1 / 36.8 and 58.6 / 49.6; 256 of 32000 62.6 / 75.1, 300 106 / 88.
     p.small = vocab <= SMALL_VOCAB || (vocab <= MEDIUM_VOCAB && div_up(rows, 256) * (10.0 + vocab / 640.0) < 22.0 + rows * (vocab / 150000.0));
     p.slab = rows;
-    if (p.small) return p;
+    if (vocab <= SMALL_VOCAB) return p;
     p.opens = (int)div_up(vocab, SAMPLE_OPEN);
     p.chunks = (int)div_up(vocab, SAMPLE_CHUNK);
     p.groups = (int)std::min(div_up(p.chunks, 16), div_up(512, rows));
     p.key_ld = (vocab + 3) & ~3;
-    const size_t row = (size_t)SAMPLE_BINS * 12 + (size_t)((p.chunks + 1) & ~1) * 8 + (size_t)SAMPLE_LIST * 8 + (size_t)p.key_ld * 4 + (size_t)p.opens * 4 + SAMPLE_PLAN + 4;
+    const size_t row = (size_t)SAMPLE_BINS * 12 + (size_t)((p.chunks + 1) & ~1) * 8 + (size_t)SAMPLE_LIST * 8 + (size_t)p.key_ld * 4 + (size_t)p.opens * 4 +
+                       SAMPLE_PLAN + 4;
     const size_t most = std::max<size_t>(1, std::min(room, SAMPLE_ROOM) / row);
     p.slab = (int)std::min<size_t>(std::min<size_t>(rows, most), MAX_SERVING_GROUPS / p.opens / 4);
     p.bytes = p.slab * row;
-    if (p.bytes > room) p.slab = 0;
+    if (p.small)                                  // (which needs no room; less rows may)
+        p.slab = rows;
+    else if (p.bytes > room)
+        p.slab = 0;
     return p;
 }
 

@@ -88,13 +88,31 @@ def test_rows_that_are_sampled_together_fit_the_room(rules):
             p = lib.sample(rows, vocab, (1 << 64) - 1)
             assert 1 <= p.slab <= rows and p.small >= (vocab <= 8192) and p.small <= (vocab <= 32768)
             if p.small:
-                assert p.slab == rows and p.bytes == 0
+                assert p.slab == rows and (p.bytes == 0) == (vocab <= 8192) and lib.sample(rows, vocab, 0).slab == rows
                 continue
             assert p.opens * 1024 >= vocab > (p.opens - 1) * 1024 and p.chunks * 512 >= vocab > (p.chunks - 1) * 512 and p.chunks <= 2048
             assert vocab <= p.key_ld < vocab + 4 and p.key_ld % 4 == 0 and 16 * p.groups <= p.chunks + 15
             assert p.slab * p.opens < 1 << 24 and p.bytes <= max(512 << 20, p.bytes // p.slab)
             one = p.bytes // p.slab
             assert lib.sample(rows, vocab, one - 1).slab == 0 and lib.sample(rows, vocab, one).slab == 1
+
+
+def test_the_room_of_a_larger_call_holds_smaller_ones(rules):
+    rng = np.random.default_rng(3)
+    for lib in rules.values():
+        for _ in range(300):
+            n, t = [(3, 1), (5, 2), (8, 3)][rng.integers(3)]
+            K, rank, N, most = int(2 ** rng.uniform(0, 13.99)), int(rng.integers(1, 129)), int(2 ** rng.uniform(0, 14)), int(2 ** rng.uniform(0, 12))
+            room = lib.adapters(n, t, most, 16, K, rank, N).bytes
+            for tokens in rng.integers(1, most + 1, 8).tolist() + [1, most]:
+                for requests in (1, 5, 16, 2000):
+                    assert lib.adapters(n, t, tokens, requests, K, rank, N).bytes <= room
+        for vocab in (100, 8193, 16384, 32000, 32768, 32769, 128000, 1 << 20):
+            for most in (2, 128, 256, 300, 1000):
+                room = lib.sample(most, vocab, (1 << 64) - 1).bytes
+                for rows in {1, most - 1, most // 2, min(256, most), min(200, most), most}:
+                    p = lib.sample(rows, vocab, room)
+                    assert p.bytes <= room and p.slab == rows or most * vocab > 1 << 26
 
 
 @gpu
