@@ -80,7 +80,7 @@ struct row_tile {
     int count, adapter;             // adapter: -1 if they have none
 };
 
-// Tile number -> its tokens, `most` at most, to rows in LDS (everyone's after the next barrier); all waves call.  False: no such tile.
+// Tile number -> its tokens, `most` at most, to rows in LDS (the wave's own, or everyone's after the next barrier).  False: no such tile.
 // Tiles follow one another request by request, or (grouped) tile i is that of token i, which has the tokens behind it with the same adapter too, whichever requests
 // they belong to, if the number of those in front of it is a multiple of `most`, and is none otherwise: requests of single tokens read an adapter that they
 // share once.
@@ -97,7 +97,7 @@ __device__ __forceinline__ bool find_rows(const adapter_args &g, int tile, int m
     };
     auto keep = [&](int first, int count, int adapter) {
         r = {__builtin_amdgcn_readfirstlane(min(most, count)), __builtin_amdgcn_readfirstlane(adapter)};
-        if ((int)threadIdx.x < r.count) rows[threadIdx.x] = first + threadIdx.x;
+        if (lane < r.count) rows[lane] = first + lane;
         return true;
     };
     int first, count, adapter;
@@ -150,27 +150,32 @@ __device__ __forceinline__ bool find_rows(const adapter_args &g, int tile, int m
 }
 
 // Step 1: one workgroup per (tile of 16 tokens, party and run of the contraction).  Its four waves share the columns of A between CW and the blocks of
-// 64 elements between 4 / CW; a wave takes CT times 16 columns.  Elements become digits where they are loaded: those that several waves need
+// 64 elements between 4 / CW; a wave takes CT times 16 columns.  APART: four tiles, a wave has one to itself.  Elements become digits where they are loaded: those that several waves need
 // go through LDS, each wave bringing a part.  The next block's elements and digits of A are on their way while those at hand are multiplied.
 // Bound by products and the making of digits, which loads overlap only in part, and by how evenly the workgroups fill 256 CUs.  2048 tokens of 4096, rank 16,
-// n = 5: 103 us (336 MB, 53 at a copy's rate; 86 G operations, 25; without the loads 51, without those of x 61, of A 87).  1001 tokens of 4096, rank 128, n = 3:
+// n = 5: 89 us (336 MB, 53 at a copy's rate; 86 G operations, 25; four waves to a tile 103, of which without the loads 51, without those of x 61, of A 87).  1001 tokens of 4096, rank 128, n = 3:
 // 99 us, 2.0 of 3.5 POP/s.  8 tokens with an adapter each, K = 4096, rank 16, n = 5: 9.6 us, 22 MB (eight waves to a workgroup 10.0 to 12).
-template <int CW, int CT, bool WIDE>
+template <int CW, int CT, bool WIDE, bool APART = false>
 __global__ __launch_bounds__(BLOCK, 2) void down_kernel(adapter_args g)
 {
-    constexpr int KW = 4 / CW, PAIRS = 8 / CW, WORDS = 4 / CW;
+    constexpr int KW = APART ? 1 : 4 / CW, PAIRS = 8 / CW, WORDS = 4 / CW;
+    static_assert(!APART || CW == 1, "a wave with its own tile has all the columns");
     __shared__ v4i xd[CW > 1 ? 2 : 1][CW > 1 ? KW * TILE : 1];
     __shared__ int sums[KW > 1 ? CW : 1][KW > 1 ? ND : 1][BLOCK];
-    __shared__ int rows[16];
+    __shared__ int tile_rows[APART ? 4 : 1][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const unsigned slot = g.grouped ? blockIdx.x : xcd_slot(blockIdx.x, gridDim.x), run = fd_div(slot, g.dTiles);
-    const int cw = wave % CW, kw = wave / CW, split = (int)(run / (unsigned)g.nr), party = (int)run - split * g.nr, q = lane >> 4, c16 = lane & 15;
+    const int cw = wave % CW, kw = APART ? 0 : wave / CW, split = (int)(run / (unsigned)g.nr), party = (int)run - split * g.nr, q = lane >> 4, c16 = lane & 15;
+    int *rows = tile_rows[APART ? wave : 0];
     row_tile r;
-    if (!find_rows(g, (int)(slot - run * g.tiles), 16, rows, r)) return;
+    if (!find_rows(g, (int)(slot - run * g.tiles) * (APART ? 4 : 1) + (APART ? wave : 0), 16, rows, r)) return;
     u64 *out = g.planes + split * g.plane + (size_t)party * g.tokens * g.rank;
-    __syncthreads();
+    if constexpr (APART)
+        __builtin_amdgcn_wave_barrier();
+    else
+        __syncthreads();
     if (r.adapter < 0) {
-        for (int i = tid; i < r.count * g.rank; i += BLOCK) out[(size_t)rows[i / g.rank] * g.rank + i % g.rank] = 0;
+        for (int i = APART ? lane : tid; i < r.count * g.rank; i += APART ? 64 : BLOCK) out[(size_t)rows[i / g.rank] * g.rank + i % g.rank] = 0;
         return;
     }
     if constexpr (KW > 1) {
@@ -587,12 +592,14 @@ hipError_t ss_launch_adapters_down(const adapter_plan &plan, const ss_adapters &
     g.down_party = down_party_bytes(s.K, s.rank), g.down_bytes = g.nr * g.down_party;
     g.x = x, g.ld_x = ld_x, g.planes = planes, g.plane = (size_t)g.nr * req.tokens * s.rank;
     g.run = plan.run;
-    g.tiles = (unsigned)plan.down_tiles;
+    g.tiles = (unsigned)(plan.apart ? div_up(plan.down_tiles, 4) : plan.down_tiles);
     g.dTiles = make_fdiv(g.tiles);
     const dim3 grid((unsigned)plan.down_groups);
     const bool wide = s.K % 2 == 0 && ld_x % 2 == 0 && aligned16(x);
 #define SS_DOWN(CW, CT) hipLaunchKernelGGL((wide ? down_kernel<CW, CT, true> : down_kernel<CW, CT, false>), grid, dim3(BLOCK), 0, stream, g)
-    if (s.rank <= 16)
+    if (plan.apart)
+        hipLaunchKernelGGL((wide ? down_kernel<1, 1, true, true> : down_kernel<1, 1, false, true>), grid, dim3(BLOCK), 0, stream, g);
+    else if (s.rank <= 16)
         SS_DOWN(1, 1);
     else if (s.rank <= 32)
         SS_DOWN(2, 1);

@@ -30,6 +30,7 @@ constexpr int DOWN_ROWS = 16, UP_ROWS = 16, UP_TILE_ROWS = 64;   // tokens to a 
 
 struct adapter_plan {
     bool grouped;                 // tiles of tokens that share an adapter, whichever requests they belong to
+    bool apart;                   // every wave of the first product has a tile of its own
     bool diagonals;               // the second product over limbs and rank together
     int splits, run;              // contraction of the first product: in `splits` runs of `run` blocks of 64
     bool streams;                 // the second product's tensors go past the caches
@@ -61,15 +62,21 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
     const size_t tiles = p.down_tiles * nr;
     // A block of 64 elements takes a CU so long, a workgroup half a microsecond beside its blocks, the reduction 0.3 for each plane.  First product, us, by runs:
     // 64 tokens of 4096, rank 16, n = 5, 1 19, 2 13, 4 9.9, 6 9.6, 8 10.7 (reduction 4.0 to 6.2); 128 tokens, rank 32, 1 30, 2 23, 4 27; 2048 tokens, rank
-    // 16, 1 112, 2 101, 3 102; 37 to 333 tokens, rank 64, 45-bit prime, 1 19, 2 12.5, 4 11.8; 668 tokens, rank 128, 1 133, 2 114, 3 124, 4 110, 5 99.
+    // 16, 1 112, 2 101, 3 103; 37 to 333 tokens, rank 64, 45-bit prime, 1 19, 2 12.5, 4 11.8; 668 tokens, rank 128, 1 133, 2 114, 3 124, 4 110, 5 99.
     const double block = rank <= 16 ? 0.25 : rank <= 32 ? 0.5 : rank <= 64 ? 1.0 : 2.0;
-    auto cost = [&](size_t s) { return div_up(tiles * s, 256) * (block * div_up(blocks, s) + 0.5) + 0.3 * s; };
+    auto cost = [&](size_t s, int own) { return div_up(div_up(p.down_tiles, own) * nr * s, 256) * (own * block * div_up(blocks, s) + 0.5) + 0.3 * s; };
     p.splits = 1;
     for (size_t s = 2; s <= MAX_PLANES && s * 6 <= blocks; s++)
-        if (cost(s) < cost(p.splits)) p.splits = (int)s;
+        if (cost(s, 1) < cost(p.splits, 1)) p.splits = (int)s;
+    // Where there are many tiles each wave has its own, goes through all the blocks of its run, and adds its sums to nobody's (us, so / four waves to a tile: 2048
+    // tokens of 4096, n = 5, 3 runs 89 / 103, 2 117, 4 110; 1000 47 / 53; 16384 of 64 25 / 71; 8192 of 256 33 / 44; 5000 of 512, n = 3, 22 / 25; 512 of
+    // 4096, whose cost is more, 36 / 28).
+    const double together = cost(p.splits, 1);
+    for (size_t s = 1; rank <= 16 && !p.grouped && s <= MAX_PLANES && (s == 1 || s * 6 <= blocks); s++)
+        if (cost(s, 4) < (p.apart ? cost(p.splits, 4) : together)) p.splits = (int)s, p.apart = true;
     p.run = (int)div_up(blocks, p.splits);
     p.splits = (int)div_up(blocks, p.run);
-    p.down_groups = tiles * p.splits;
+    p.down_groups = (p.apart ? div_up(p.down_tiles, 4) * nr : tiles) * p.splits;
     p.up_tiles = request_tiles(tokens, requests, p.diagonals ? UP_ROWS : UP_TILE_ROWS, p.grouped);
     const size_t units = div_up(N, p.diagonals ? 128 : 32), per_tile = p.diagonals ? div_up(units, 4) : units;
     // Workgroups with the diagonals apart stage their tile's digits for some 10 us and take 3 for 32 columns; two of them fit a CU.  What fills the chip once

@@ -177,6 +177,9 @@ SHAPES = [
     (96, 200, 70, [1, 1, 0, 3, 1, 1] * 11, [i % 3 for i in range(66)]),
     (64, 36, 4, [0] * 63 + [1, 1, 5, 1] + [0] * 61 + [1, 4] + [1] * 9, [0] * 128 + [1, 0, 1, 2, 0, 0, 3, 0, 0, 0, 0]),
     (64, 33, 8, [1] * 1030, [i % 4 for i in range(1030)]),
+    # so many tiles that each wave of the first product has its own
+    (64, 34, 5, [2100, 0, 3, 900, 17], [1, 0, -1, 2, 0]),
+    (63, 30, 16, [3001], [2]),
 ]
 
 

@@ -20,7 +20,7 @@ sz = C.c_size_t
 
 
 class AdapterPlan(C.Structure):
-    _fields_ = [("grouped", C.c_bool), ("diagonals", C.c_bool), ("splits", C.c_int), ("run", C.c_int), ("streams", C.c_bool), ("col_groups", C.c_int)] + \
+    _fields_ = [("grouped", C.c_bool), ("apart", C.c_bool), ("diagonals", C.c_bool), ("splits", C.c_int), ("run", C.c_int), ("streams", C.c_bool), ("col_groups", C.c_int)] + \
                [(k, sz) for k in ("messages", "planes", "z", "down_tiles", "up_tiles", "down_groups", "up_groups", "bytes")]
 
 
@@ -54,10 +54,10 @@ def test_shapes_of_the_tests_take_every_kernel(rules):
         for K, N, rank, counts, _ in SHAPES:
             plan = rules[p].adapters(n, t, sum(counts), len(counts), K, rank, N)
             width = 1 if rank <= 16 else 2 if rank <= 32 else 4 if rank <= 64 else 8      # columns of A among the waves, see ss_launch_adapters_down
-            seen |= {(p, "down", width), (p, "grouped", plan.grouped, plan.diagonals), (p, "runs", plan.splits > 1), (p, "steps", -(-rank // 8) if rank <= 8 else -(-rank // 16), plan.diagonals),
+            seen |= {(p, "down", width), (p, "apart", plan.apart, K % 2 == 0), (p, "grouped", plan.grouped, plan.diagonals), (p, "runs", plan.splits > 1), (p, "steps", -(-rank // 8) if rank <= 8 else -(-rank // 16), plan.diagonals),
                      (p, "parts", plan.col_groups > 1)}
     for p in (P61, P45):
-        assert {(p, "down", w) for w in (1, 2, 4, 8)} | {(p, "grouped", a, b) for a in (False, True) for b in (False, True)} <= seen
+        assert {(p, "down", w) for w in (1, 2, 4, 8)} | {(p, "apart", a, w) for a in (False, True) for w in (False, True)} | {(p, "grouped", a, b) for a in (False, True) for b in (False, True)} <= seen
         assert {(p, "runs", False), (p, "runs", True), (p, "parts", False), (p, "parts", True), (p, "steps", 1, True), (p, "steps", 2, True)} <= seen
 
 
@@ -73,7 +73,7 @@ def test_a_plan_covers_its_call(rules):
             assert 1 <= p.splits <= 8 and (p.splits - 1) * p.run < blocks <= p.splits * p.run and p.run * 64 <= 16384
             assert p.col_groups >= 1 and n * p.col_groups < 65536 and p.grouped <= (requests <= 1024)
             assert p.bytes == p.messages + p.planes + p.z and p.planes >= p.splits * (2 * t + 1) * tokens * rank * 8 and p.z >= n * tokens * rank * 8
-            assert p.down_groups == p.down_tiles * (2 * t + 1) * p.splits and p.up_groups == p.up_tiles * n * p.col_groups
+            assert p.down_groups == (-(-p.down_tiles // 4) if p.apart else p.down_tiles) * (2 * t + 1) * p.splits and p.apart <= (rank <= 16) and p.up_groups == p.up_tiles * n * p.col_groups
         for _ in range(300):
             counts = rng.integers(0, 70, rng.integers(1, 30))
             if counts.sum():
