@@ -150,11 +150,13 @@ __device__ __forceinline__ bool find_rows(const adapter_args &g, int tile, int m
 }
 
 // Step 1: one workgroup per (tile of 16 tokens, party and run of the contraction).  Its four waves share the columns of A between CW and the blocks of
-// 64 elements between 4 / CW; a wave takes CT times 16 columns.  APART: four tiles, a wave has one to itself.  Elements become digits where they are loaded: those that several waves need
-// go through LDS, each wave bringing a part.  The next block's elements and digits of A are on their way while those at hand are multiplied.
+// 64 elements between 4 / CW; a wave takes CT times 16 columns.  APART: four tiles, a wave has one to itself.  Elements become digits where they are
+// loaded: those that several waves need go through LDS, each wave bringing a part.  The next block's elements and digits of A are on their way while those at
+// hand are multiplied.
 // Bound by products and the making of digits, which loads overlap only in part, and by how evenly the workgroups fill 256 CUs.  2048 tokens of 4096, rank 16,
-// n = 5: 89 us (336 MB, 53 at a copy's rate; 86 G operations, 25; four waves to a tile 103, of which without the loads 51, without those of x 61, of A 87).  1001 tokens of 4096, rank 128, n = 3:
-// 99 us, 2.0 of 3.5 POP/s.  8 tokens with an adapter each, K = 4096, rank 16, n = 5: 9.6 us, 22 MB (eight waves to a workgroup 10.0 to 12).
+// n = 5: 89 us (336 MB, 53 at a copy's rate; 86 G operations, 25; four waves to a tile 103, of which without the loads 51, without those of x 61, of A
+// 87).  1001 tokens of 4096, rank 128, n = 3: 99 us, 2.0 of 3.5 POP/s.  8 tokens with an adapter each, K = 4096, rank 16, n = 5: 9.6 us, 22 MB (eight waves to
+// a workgroup 10.0 to 12).
 template <int CW, int CT, bool WIDE, bool APART = false>
 __global__ __launch_bounds__(BLOCK, 2) void down_kernel(adapter_args g)
 {

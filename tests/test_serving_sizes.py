@@ -154,17 +154,17 @@ def test_logits_of_more_than_4_gb_in_several_runs():
 
 
 @gpu
-@pytest.mark.parametrize("rows,vocab,small", [(256, 32768, True), (250, 9000, True), (256, 32769, False), (3, 8193, False)])
-def test_rows_in_one_launch_and_in_four(rules, rows, vocab, small):
+@pytest.mark.parametrize("p,rows,vocab,small", [(P61, 256, 32768, True), (P61, 250, 9000, True), (P45, 200, 16001, True), (P61, 256, 32769, False), (P61, 3, 8193, False)])
+def test_rows_in_one_launch_and_in_four(rules, p, rows, vocab, small):
     """either side of the rules, every kind of cut among the rows that are looked at"""
-    assert rules[P61].sample(rows, vocab, (1 << 64) - 1).small == small
-    f = 13
+    assert rules[p].sample(rows, vocab, (1 << 64) - 1).small == small
+    f = 13 if p == P61 else 12
     rng = np.random.default_rng(vocab)
-    ss = SSNet(3, 1, f=f, seed=3)
+    ss = SSNet(3, 1, f=f, seed=3, p=p)
     picked = sorted({0, 1, rows // 2, rows - 2, rows - 1})      # each once: of three rows 0, 1, 2
     values = np.rint(rng.standard_normal((len(picked), vocab)) * 3 * 2 ** f).astype(np.int64)
     values[-1] >>= 13                           # few different ones
-    shares = dev(orc.share((values % P61).astype(np.uint64), 3, 1, P61, 5, 6))
+    shares = dev(orc.share((values % p).astype(np.uint64), 3, 1, p, 5, 6))
     logits = torch.zeros((3, rows, vocab), dtype=torch.int64, device="cuda")
     for i, r in enumerate(picked):
         logits[:, r] = shares[:, i]
