@@ -159,3 +159,23 @@ def test_logits_past_the_caches_in_pairs(p):
         tokens, shown = ss.sample(logits, list(range(1, m + 1)), how, random)
         for i, r in enumerate(picked):
             assert (int(tokens[r]), int(shown[r])) == draw(kept_weights(values[i], f, how[0].tolist()), int(random[r])), (params, r)
+
+
+def test_the_room_of_more_rows_serves_fewer(rules):
+    """Where rows go in several runs as well: a smaller call is never refused, stays in its room, and goes in one run where its rows fit what a run may take."""
+    run = 512 << 20
+    several = 0
+    for lib in rules.values():
+        for vocab in (100, 8193, 16384, 32000, 32768, 32769, 128000, 1 << 20):
+            for most in (2, 128, 256, 300, 1000, 5000):
+                room = lib.sample(most, vocab, (1 << 64) - 1).bytes
+                for rows in {1, 2, most // 7, most // 2, min(200, most), min(256, most), most - 1, most} - {0}:
+                    p = lib.sample(rows, vocab, room)
+                    assert p.slab >= 1 and (p.small or p.bytes <= room)
+                    if p.small:
+                        assert p.slab == rows
+                        continue
+                    row = p.bytes // p.slab
+                    assert row * p.slab == p.bytes and p.slab == min(rows, run // row, ((1 << 24) - 1) // p.opens // 4)
+                    several += p.slab < rows
+    assert several
