@@ -117,8 +117,8 @@ factor of theirs in B), of which forward gives each sequence one; a pass with ad
 
     def forward(self, x: torch.Tensor, counts: Dict[int, int], adapters: Optional[Dict[int, int]] = None) -> torch.Tensor:
         """x: shares [n][tokens][width] at scale 2^f of the new tokens, counts as in Sequences.extend -> shares [n][tokens][width].  adapters: the place in the
-        layer's sets that a sequence's adapter has; those that are not in it have none.  A call that is refused or fails leaves the sequences as they
-        were."""
+        layer's sets that a sequence's adapter has (a set that ends before it changes nothing); sequences that are not in it, or at -1, have none.  A call
+        that is refused or fails leaves the sequences as they were."""
         ss, heads, kv, dim = self.ss, self.heads, self.kv, self.dim
         n, tokens, _ = x.shape
         if sum(counts.values()) != tokens:
@@ -130,7 +130,10 @@ factor of theirs in B), of which forward gives each sequence one; a pass with ad
         if adapters is not None:
             if self.adapters_qkv is None and self.adapters_out is None:
                 raise ValueError("the layer has no adapters")
-            index = torch.tensor([adapters.get(s, -1) for s in counts], dtype=torch.int32, device=x.device)
+            places, held = [adapters.get(s, -1) for s in counts], max(a.adapters for a in (self.adapters_qkv, self.adapters_out) if a is not None)
+            if not all(-1 <= i < held for i in places):
+                raise ValueError(f"a sequence's adapter must be a place of the layer's sets, 0 to {held - 1}, or -1: {places}")
+            index = torch.tensor(places, dtype=torch.int32, device=x.device)
         streams = self.STREAMS + (self.ADAPTER_STREAMS if adapters is not None else 0)
         stream = ss.take_streams(streams, self.stream)
         if self.stream is not None:
