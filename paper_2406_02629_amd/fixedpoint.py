@@ -72,5 +72,7 @@ def sampling_parameters(temperature, top_k=0, top_p=1.0, min_p=0.0, rows: int = 
         raise ValueError("temperature must be 0 or at least 0.0113")
     scale = torch.where(t > 0, (2.0 ** 24 / 0.6931471805599453 / t.clamp(min=0.0113)).round(), 0)
     k = column(top_k, "top_k", 0, 2 ** 31 - 1)
+    if bool((k != k.round()).any()):
+        raise ValueError("top_k must be a whole number")
     p, m = (2.0 ** 30 * column(v, name, 0, 1) for v, name in ((top_p, "top_p"), (min_p, "min_p")))
     return torch.stack([scale, k, p.round(), m.round()], 1).to(torch.int32).to(device).contiguous()
