@@ -538,7 +538,9 @@ int ssnet_paged_attention(ssnet_ctx *ctx, const ssnet_paged_cache *cache, const 
  *   ssnet_adapters_mod: `tokens` tokens belong to `requests` requests, those of
  *     request b are d_start[b] .. d_start[b+1] - 1 (d_start[0] = 0,
  *     d_start[requests] = tokens, none or more each) and take adapter d_adapter[b];
- *     a number outside the set is none.  Per token:
+ *     a number outside the set is none.  Tokens in front of d_start[0] or behind
+ *     d_start[requests], in a batch that is larger, belong to no request: their y
+ *     stays as it is, and step 2 takes zeros for them.  Per token:
  *       1. parties i = 1..2t+1: Z_i = x_i A_i mod p (degree 2t, 2f fraction bits);
  *       2. degree reduction and truncation of Z, messages and draws as in
  *          ssnet_degree_reduce_truncate with count = tokens * rank -> z;

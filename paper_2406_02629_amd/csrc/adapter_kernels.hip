@@ -70,7 +70,7 @@ struct adapter_args {
     u64 *planes, *y;                // planes [splits][2t+1][tokens][rank]
     const u64 *z;                   // [n][tokens][rank]
     int nr, n, run, col_groups;
-    unsigned tiles;                 // that the requests can have
+    unsigned tiles;                 // that there can be
     fdiv dTiles;
     size_t plane;                   // 2t+1 shares
 };
@@ -84,6 +84,8 @@ struct row_tile {
 // Tiles follow one another request by request, or (grouped) tile i is that of token i, which has the tokens behind it with the same adapter too, whichever requests
 // they belong to, if the number of those in front of it is a multiple of `most`, and is none otherwise: requests of single tokens read an adapter that they
 // share once.
+// OUTSIDE: tokens that no request has (in front of the first, behind the last) have tiles too, without an adapter, behind the others.
+template <bool OUTSIDE>
 __device__ __forceinline__ bool find_rows(const adapter_args &g, int tile, int most, int *rows, row_tile &r)
 {
     const int lane = threadIdx.x & 63;
@@ -100,11 +102,20 @@ __device__ __forceinline__ bool find_rows(const adapter_args &g, int tile, int m
         if (lane < r.count) rows[lane] = first + lane;
         return true;
     };
+    auto outside = [&](int number) {
+        const int begin = min(max(fixed_at(g.start, 0), 0), g.tokens), inside = max(0, min(fixed_at(g.start, g.requests), g.tokens) - begin);
+        const int at = number * most, left = g.tokens - inside - at;
+        if (!OUTSIDE || left <= 0) return false;
+        r = {min(most, left), -1};
+        if (lane < r.count) rows[lane] = at + lane < begin ? at + lane : at + lane + inside;
+        return true;
+    };
     int first, count, adapter;
     if (g.requests == 1) {                       // without a search
-        first = min(max(fixed_at(g.start, 0), 0), g.tokens), count = min(fixed_at(g.start, 1), g.tokens) - first - tile * most;
+        first = min(max(fixed_at(g.start, 0), 0), g.tokens), count = min(fixed_at(g.start, 1), g.tokens) - first;
         adapter = fixed_at(g.adapter, 0);
-        return count > 0 && keep(first + tile * most, count, adapter < 0 || adapter >= g.adapters ? -1 : adapter);
+        if (tile * most >= count) return outside(tile - (max(count, 0) + most - 1) / most);
+        return keep(first + tile * most, count - tile * most, adapter < 0 || adapter >= g.adapters ? -1 : adapter);
     }
     if (!g.grouped) {
         int base = 0;
@@ -118,7 +129,7 @@ __device__ __forceinline__ bool find_rows(const adapter_args &g, int tile, int m
             }
             base += __builtin_amdgcn_readlane(upto, 63);
         }
-        return false;
+        return outside(tile - base);
     }
     int owner = -1, wanted = -1, place = 0;
     for (int b0 = 0; b0 < g.requests && owner < 0; b0 += 64) {
@@ -128,7 +139,7 @@ __device__ __forceinline__ bool find_rows(const adapter_args &g, int tile, int m
         const int l = __ffsll((long long)mine) - 1;
         owner = b0 + l, wanted = __builtin_amdgcn_readlane(adapter, l), place = tile - __builtin_amdgcn_readlane(first, l);
     }
-    if (owner < 0) return false;
+    if (owner < 0 && !OUTSIDE) return false;
     if (wanted < 0) return keep(tile, 1, -1);
     int behind = 0;                              // tokens listed so far
     for (int b0 = 0; b0 < g.requests; b0 += 64) {
@@ -170,13 +181,13 @@ __global__ __launch_bounds__(BLOCK, 2) void down_kernel(adapter_args g)
     const int cw = wave % CW, kw = APART ? 0 : wave / CW, split = (int)(run / (unsigned)g.nr), party = (int)run - split * g.nr, q = lane >> 4, c16 = lane & 15;
     int *rows = tile_rows[APART ? wave : 0];
     row_tile r;
-    if (!find_rows(g, (int)(slot - run * g.tiles) * (APART ? 4 : 1) + (APART ? wave : 0), 16, rows, r)) return;
+    if (!find_rows<true>(g, (int)(slot - run * g.tiles) * (APART ? 4 : 1) + (APART ? wave : 0), 16, rows, r)) return;
     u64 *out = g.planes + split * g.plane + (size_t)party * g.tokens * g.rank;
     if constexpr (APART)
         __builtin_amdgcn_wave_barrier();
     else
         __syncthreads();
-    if (r.adapter < 0) {
+    if (r.adapter < 0) {                             // (zeros: the reduction sends what is left here, also for tokens of no request)
         for (int i = APART ? lane : tid; i < r.count * g.rank; i += APART ? 64 : BLOCK) out[(size_t)rows[i / g.rank] * g.rank + i % g.rank] = 0;
         return;
     }
@@ -407,7 +418,7 @@ __global__ __launch_bounds__(BLOCK, 2) void up_diagonals_kernel(adapter_args g)
     __shared__ int rows[UP_ROWS];
     row_tile r;
     // (of grouped tiles those that there are stand in front: they are spread over the XCDs)
-    if (!find_rows(g, g.grouped ? (int)blockIdx.x : (int)xcd_slot(blockIdx.x, gridDim.x), UP_ROWS, rows, r)) return;
+    if (!find_rows<false>(g, g.grouped ? (int)blockIdx.x : (int)xcd_slot(blockIdx.x, gridDim.x), UP_ROWS, rows, r)) return;
     const u64 *base = g.base + (size_t)party * g.tokens * g.ld_base;
     u64 *y = g.y + (size_t)party * g.tokens * g.ld_y;
     __syncthreads();
@@ -495,7 +506,7 @@ __global__ __launch_bounds__(BLOCK, 2) void up_tile_kernel(adapter_args g)
     const int part = blockIdx.y / g.n, party = blockIdx.y - part * g.n;
     int *rows = reinterpret_cast<int *>(zt);     // (until the digits are written)
     row_tile r;
-    if (!find_rows(g, blockIdx.x, 64, rows, r)) return;
+    if (!find_rows<false>(g, blockIdx.x, 64, rows, r)) return;
     const u64 *base = g.base + (size_t)party * g.tokens * g.ld_base;
     u64 *y = g.y + (size_t)party * g.tokens * g.ld_y;
     __syncthreads();

@@ -59,7 +59,6 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
     // by 1024, n = 3, rank 32 22.8 / 23.7; over the 45-bit prime 37 to 333 by 2560 35.6 / 28.0).  Beyond rank 32 two sums no longer fit 32 bits.
     p.diagonals = rank <= 32;
     p.down_tiles = request_tiles(tokens, requests, DOWN_ROWS, p.grouped);
-    const size_t tiles = p.down_tiles * nr;
     // A block of 64 elements takes a CU so long, a workgroup half a microsecond beside its blocks, the reduction 0.3 for each plane.  First product, us, by runs:
     // 64 tokens of 4096, rank 16, n = 5, 1 19, 2 13, 4 9.9, 6 9.6, 8 10.7 (reduction 4.0 to 6.2); 128 tokens, rank 32, 1 30, 2 23, 4 27; 2048 tokens, rank
     // 16, 1 112, 2 101, 3 103; 37 to 333 tokens, rank 64, 45-bit prime, 1 19, 2 12.5, 4 11.8; 668 tokens, rank 128, 1 133, 2 114, 3 124, 4 110, 5 99.
@@ -74,9 +73,10 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
     const double together = cost(p.splits, 1);
     for (size_t s = 1; rank <= 16 && !p.grouped && s <= MAX_PLANES && (s == 1 || s * 6 <= blocks); s++)
         if (cost(s, 4) < (p.apart ? cost(p.splits, 4) : together)) p.splits = (int)s, p.apart = true;
+    p.down_tiles = request_tiles(tokens, requests + 1, DOWN_ROWS, p.grouped);   // with those of tokens that no request has
     p.run = (int)div_up(blocks, p.splits);
     p.splits = (int)div_up(blocks, p.run);
-    p.down_groups = (p.apart ? div_up(p.down_tiles, 4) * nr : tiles) * p.splits;
+    p.down_groups = div_up(p.down_tiles, p.apart ? 4 : 1) * nr * p.splits;
     p.up_tiles = request_tiles(tokens, requests, p.diagonals ? UP_ROWS : UP_TILE_ROWS, p.grouped);
     const size_t units = div_up(N, p.diagonals ? 128 : 32), per_tile = p.diagonals ? div_up(units, 4) : units;
     // Workgroups with the diagonals apart stage their tile's digits for some 10 us and take 3 for 32 columns; two of them fit a CU.  What fills the chip once

@@ -179,3 +179,22 @@ def test_the_room_of_more_rows_serves_fewer(rules):
                     assert row * p.slab == p.bytes and p.slab == min(rows, run // row, ((1 << 24) - 1) // p.opens // 4)
                     several += p.slab < rows
     assert several
+
+
+def test_tokens_of_no_request_have_tiles(rules):
+    """of the first product, whose planes the reduction sends: tiles of 16 of each request's tokens and of the others together"""
+    rng = np.random.default_rng(5)
+    spare = set()
+    for lib in rules.values():
+        for _ in range(2000):
+            requests = int(2 ** rng.uniform(0, 7))
+            counts = rng.integers(0, rng.integers(2, 80), requests)
+            others = int(rng.integers(0, 50))
+            tokens = int(counts.sum()) + others
+            if not tokens:
+                continue
+            plan = lib.adapters(3, 1, tokens, requests, 256, 16, 64)
+            need = tokens if plan.grouped else int((-(-counts // 16)).sum()) + -(-others // 16)
+            assert need <= plan.down_tiles <= tokens
+            spare.add(plan.down_tiles - need)
+    assert 0 in spare
