@@ -183,9 +183,10 @@ __global__ __launch_bounds__(BLOCK, 2) void down_kernel(adapter_args g)
     row_tile r;
     if (!find_rows<true>(g, (int)(slot - run * g.tiles) * (APART ? 4 : 1) + (APART ? wave : 0), 16, rows, r)) return;
     u64 *out = g.planes + split * g.plane + (size_t)party * g.tokens * g.rank;
-    if constexpr (APART)
+    if constexpr (APART) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (other lanes' rows: the barrier alone orders no memory; LDS is in order, so no instruction)
         __builtin_amdgcn_wave_barrier();
-    else
+    } else
         __syncthreads();
     if (r.adapter < 0) {                             // (zeros: the reduction sends what is left here, also for tokens of no request)
         for (int i = APART ? lane : tid; i < r.count * g.rank; i += APART ? 64 : BLOCK) out[(size_t)rows[i / g.rank] * g.rank + i % g.rank] = 0;
