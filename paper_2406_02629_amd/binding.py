@@ -257,6 +257,8 @@ class Adapters:
 
     def load(self, index: int, a: torch.Tensor, b: torch.Tensor):
         """shares a [n][K][r], b [n][r][N], r up to the set's rank, into place `index`"""
+        if not 0 <= index < self.adapters:
+            raise SSNetError(EINVAL, "ssnet_pack_adapter")
         _device_tensor(a, torch.int64, "a"), _device_tensor(b, torch.int64, "b")
         r = a.shape[2] if a.dim() == 3 else 0
         if a.shape != (self.n, self.K, r) or b.shape != (self.n, r, self.N) or not 1 <= r <= self.rank:
