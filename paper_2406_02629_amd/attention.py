@@ -82,8 +82,9 @@ class Attention:
     owner, shared and packed once.  table: fixedpoint.rotary_table.  weight_bits: f, or 2 f for long contexts (the weights of `length`
     keys are about 1 / length); default: what the longest context that table and cache have room for needs.  stream_base: the first
     stream id of its calls, each of which takes STREAMS of them; the two in front of it share the weights.  Default: whatever ids the context has free
-    (SSNet.take_streams); ids that another layer has are refused.  adapters_qkv, adapters_out: sets of low-rank adapters of the two dense layers (any
-factor of theirs in B), of which forward gives each sequence one; a pass with adapters takes STREAMS + ADAPTER_STREAMS ids."""
+    (SSNet.take_streams); ids that another layer has are refused.  adapters_qkv, adapters_out: sets of low-rank adapters of the two
+    dense layers (any factor of theirs in B), of which forward gives each sequence one; a pass with adapters takes STREAMS +
+    ADAPTER_STREAMS ids."""
 
     STREAMS = 8      # stream ids that a forward pass uses
     ADAPTER_STREAMS = 2

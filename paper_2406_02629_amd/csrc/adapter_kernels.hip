@@ -40,7 +40,9 @@ __global__ __launch_bounds__(BLOCK) void pack_down_kernel(const u64 *a, signed c
             (v4i){(int)limb_dword(y[0], l), (int)limb_dword(y[1], l), (int)limb_dword(y[2], l), (int)limb_dword(y[3], l)};
 }
 
-// 16 digits of a column of B to a thread (up).  b [n][given][N]; padded: the rank in whole eights
+// 16 digits of a column of B to a thread (up).  b [n][given][N]; padded: the rank in whole eights.  Every element is read and split once for each limb, which
+// happens when an adapter is loaded, not when it is used (4096 by 4096, n = 5, both matrices: rank 16 10.7 us, rank 64 26; 960 by 2560, rank 64,
+// n = 3, 45-bit prime 10.7).
 __global__ __launch_bounds__(BLOCK) void pack_up_kernel(const u64 *b, signed char *up, int given, int padded, int N, unsigned items, size_t party_bytes)
 {
     const unsigned i = blockIdx.x * BLOCK + threadIdx.x;
@@ -328,7 +330,8 @@ __device__ __forceinline__ u64 fold_items(const v4i (&acc)[4], u64 more)
 #endif
 }
 
-// y = 0 in the rows of all requests, where there is no base
+// y = 0 in the rows of all requests, where there is no base, which the second product then adds to: y is written twice and read once (2048 tokens of 4096 by 4096,
+// rank 16, n = 5, whole calls: 285 us, with a base 245)
 __global__ __launch_bounds__(BLOCK) void clear_kernel(adapter_args g)
 {
     const int first = min(max(fixed_at(g.start, 0), 0), g.tokens), last = min(fixed_at(g.start, g.requests), g.tokens);

@@ -297,8 +297,9 @@ __device__ __forceinline__ int key_of(const sample_args &g, const ss_rec_params 
 
 // ------------------------------------------------------------------ a workgroup to a row
 
-// The row's logits stay in LDS.  Bound by the row's way through one CU: its shares, two atomics of LDS to a token, and three to five times over the keys.  256 rows
-// of 2048 16 us, of 8192 25, of 32000 63 (m = 2: 131 MB).
+// The row's logits stay in LDS.  Bound by the row's way through one CU: its shares, two atomics of LDS to a token for the histogram, one for the draw to the
+// word of its chunk, which all 64 lanes of a wave have in common, and three to five times over the keys.  256 rows of 2048 16 us, of 8192 25, of 32000 63
+// (m = 2: 131 MB).
 template <int MOST>
 __global__ __launch_bounds__(THREADS) void sample_kernel(sample_args g, ss_rec_params rp)
 {

@@ -53,10 +53,13 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
     // Tokens by their adapters, although every workgroup goes through the requests then, and those of tokens that are in another's tile for nothing (first and
     // second product, us, so / request by request: 128 requests of a token with 27 adapters between them, n = 3, 23 + 61 / 35 + 103, with an adapter each
     // 44 + 140 / 43 + 139; 64 with 8, n = 5, 24 + 23 / 28 + 30; 400 with 8 72 + 94 / 124 + 89; 8 with 8 10.0 + 7.9 / 9.2 + 7.7.  Of two tokens each, 64 with 27,
-    // n = 3, 23 + 75 / 30 + 66; of four each, 32 with 4, n = 5, 48 + 66 / 23 + 26).
+    // n = 3, 23 + 75 / 30 + 66; of four each, 32 with 4, n = 5, 48 + 66 / 23 + 26).  It goes by the whole call, so that one long request leaves single tokens with a
+    // tile each (8 adapters, rank 16, n = 5, whole calls: 512 tokens 81, 64 single ones 53, together in a call 113).  Beyond 1024 requests the searches cost what the
+    // fewer reads save (single tokens with 8 adapters, whole calls: 1024 519, 1025 526).
     p.grouped = requests > 1 && requests <= 1024 && tokens <= 2 * requests;
     // Limbs and rank together, or diagonals apart (second product, us: 2048 tokens by 4096 columns, n = 5, rank 8 135 / 265, 16 157 / 274, 32 241 / 278; 1000
-    // by 1024, n = 3, rank 32 22.8 / 23.7; over the 45-bit prime 37 to 333 by 2560 35.6 / 28.0).  Beyond rank 32 two sums no longer fit 32 bits.
+    // by 1024, n = 3, rank 32 22.8 / 23.7).  Beyond rank 32 two sums no longer fit 32 bits.  The rule does not tell the primes apart, though over the 45-bit
+    // one the form that it takes for ranks 17 to 32 is the slower where it was measured (37 to 333 tokens by 2560, rank 32, 35.6 / 28.0).
     p.diagonals = rank <= 32;
     p.down_tiles = request_tiles(tokens, requests, DOWN_ROWS, p.grouped);
     // A block of 64 elements takes a CU so long, a workgroup half a microsecond beside its blocks, the reduction 0.3 for each plane.  First product, us, by runs:
@@ -91,7 +94,8 @@ inline adapter_plan plan_adapters(int n, int t, int tokens, int requests, int K,
     p.streams = (size_t)n * tokens * N * 16 > STREAMED_BYTES;
     auto whole = [](size_t b) { return (b + 255) & ~(size_t)255; };
     p.messages = whole((nr * k + k * n + k + n) * count * 8);
-    // (room for as many as any number of tokens asks for, so that the room of a larger call holds a smaller one)
+    // (room for as many as any number of tokens asks for, so that the room of a larger call holds a smaller one; a call that takes one run leaves up to seven
+    // parts of eight unused)
     p.planes = whole(std::max<size_t>(1, std::min<size_t>(MAX_PLANES, blocks / 6)) * nr * count * 8);
     p.z = whole((size_t)n * count * 8);
     p.bytes = p.messages + p.planes + p.z;
@@ -106,7 +110,8 @@ constexpr int SAMPLE_BIN_BITS = 11, SAMPLE_BINS = 1 << SAMPLE_BIN_BITS;
 constexpr int SAMPLE_OPEN = 1024;             // tokens to a workgroup that opens (us at 512, 1024, 2048: 1 row of 32000 3.5, 4.2, 5.5;
                                               // 256 of them 31.8, 32.7, 37.6; 64 of 200003 64.6, 60.2, 63.7)
 constexpr int SAMPLE_CHUNK = 512;             // to a wave that counts or collects: 2^20 tokens are 2048 chunks
-constexpr int SAMPLE_LIST = 4096;             // tokens near a cut that are listed (more are found among all)
+constexpr int SAMPLE_LIST = 4096;             // tokens near a cut that are listed (more are found among all, by one workgroup: 1 row of 2^20 tokens, normal logits of
+                                              // deviation 2.5, top_p 0.99 746 us, top_k 50, whose list has room, 32; 2^18 tokens, top_p 0.99 33)
 constexpr int SAMPLE_PLAN = 64;                // bytes for where the cuts of a row lie
 constexpr size_t SAMPLE_ROOM = (size_t)512 << 20;
 
